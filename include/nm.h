@@ -76,7 +76,8 @@ enum {
                                   either way; reported segment indices are always primary cell indices */
 };
 
-enum { NM_DT_I32 = 0, NM_DT_F32 = 1 };
+/* Types of a tensor.  The calls on int8 codes take I32 and F32; those of a decode step (the last section) say which of the others. */
+enum { NM_DT_I32 = 0, NM_DT_F32 = 1, NM_DT_BF16 = 2, NM_DT_F16 = 3, NM_DT_I8 = 4 };
 
 #define NM_MAX_SEGMENTS 4096 /* per table */
 #define NM_MAX_TABLES 16     /* per nm_tables object */
@@ -464,6 +465,106 @@ typedef struct {
 
 int32_t nm_cnn_workspace(const nm_cnn_op* ops, int32_t n_ops, size_t* bytes);
 int32_t nm_cnn_run(const nm_cnn_op* ops, int32_t n_ops, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * One step of a decoder over a paged key-value cache.
+ *
+ * The cache is a pool of num_pages pages of page_size slots (a power of two); a slot holds the key, and in the value cache the
+ * value, of one token for all key heads.  Slot number = page * page_size + place in the page.  A request owns the pages that its row of
+ * the block table names, in the order of its positions; position p of request b lies in slot
+ * block_table[b][p / page_size] * page_size + p % page_size.  Element c of head h of a slot is at
+ * page * page_stride + place * slot_stride + h * head_stride + c (strides in elements, alike for keys and values), so a page may be
+ * laid out by tokens or by heads.  All of a step's numbers (lengths, slots, tables) are device memory, so that a step can
+ * be captured once and replayed while they change.
+ *
+ * Unlike the calls above, these three compute the functions themselves, not tables of them: a softmax that is split over the cache's
+ * length and joined relies on exp(a + b) = exp(a) exp(b), which a piecewise-linear exp does not have.  nm_gemv_w4 takes tables.
+ * Sums and statistics are binary32 (integer products exact int32); outputs are rounded once, to nearest even; int8 codes
+ * as above.  Results do not depend on timing (no atomics) and agree with the formulas to rounding; they are not specified bit for bit.
+ * --------------------------------------------------------------------------------------------- */
+
+/*
+ * nm_page_plan: block tables, slots and positions of a step from the requests' lengths.  Request b holds cached[b] tokens and adds
+ * fresh[b] (0: idle).  With up(n) = ceil(n / page_size), it needs up(cached + fresh) - up(cached) new pages where fresh > 0; they come
+ * from free_pages, from number *free_begin on, in the order of the requests, and are entered into its row behind the
+ * up(cached) entries that are there.  Then, everything int32:
+ *   lens[b] = cached[b] + fresh[b];  row_start[0 .. B] = prefix sums of fresh;  *free_end = *free_begin + pages taken;
+ *   for token t, the i-th new one of request b:  requests[t] = b, positions[t] = cached[b] + i, slots[t] = its slot;
+ *   rows behind the last token:  requests -1, positions 0, slots -1.
+ * A token whose table or list entry is no page (outside [0, num_pages)) has slot -1.
+ * status[0]: 0, or a sum of NM_PLAN_*; status[1]: new tokens, [2]: new pages needed, [3]: largest of cached + fresh (0 for B = 0); each at
+ * most 2^31 - 1.  With any flag set nothing is assigned: the table is left as it is, slots and requests are -1, positions and
+ * row_start 0, lens = cached, *free_end = *free_begin.  (The calls below leave rows without a slot out.)
+ * cached, fresh: device [B].  free_pages: device [n_free].  block_table: device [B] rows of max_pages entries, table_stride
+ * apart.  slots, positions, requests: [max_tokens].  lens, row_start, positions, requests may be NULL.  No output may be an input
+ * (one workgroup writes while another still reads): *free_end and lens need memory of their own.
+ * Limits: B <= NM_PLAN_MAX_REQUESTS; num_pages * page_size < 2^31; page_size <= 65536.
+ */
+#define NM_PLAN_MAX_REQUESTS 4096
+enum { NM_PLAN_NO_PAGES = 1,      /* the free list is too short */
+       NM_PLAN_TABLE_FULL = 2,    /* a request needs more than max_pages entries */
+       NM_PLAN_NO_ROWS = 4,       /* more than max_tokens new tokens */
+       NM_PLAN_BAD_LENGTH = 8 };  /* a negative length, or *free_begin negative */
+typedef struct {
+    int32_t B, page_size, num_pages, max_pages, n_free, max_tokens;
+    const int32_t* cached;
+    const int32_t* fresh;
+    const int32_t* free_pages;
+    const int32_t* free_begin;
+    int32_t* free_end;
+    int32_t* block_table;
+    int64_t table_stride;
+    int32_t* lens;
+    int32_t* row_start;
+    int32_t* slots;
+    int32_t* positions;
+    int32_t* requests;
+    int32_t* status; /* [4] */
+} nm_plan_desc;
+
+int32_t nm_page_plan(const nm_plan_desc* desc, void* stream);
+
+/*
+ * nm_qk_norm_rope: what lies between a step's QKV projection and its attention, in one pass.  For each of T tokens, hq heads of
+ * queries and hk of keys, d elements each:
+ *   y = x / sqrt(mean(x^2) + eps) * gamma     with NM_QK_NORM (gamma NULL: 1), else y = x
+ *   the first rot elements are turned by the angles a_i = position * inv_freq[i], i < rot / 2 (products exact to 2^-53):
+ *   (y_p, y_q) -> (y_p cos a_i - y_q sin a_i, y_q cos a_i + y_p sin a_i),  p, q = i, i + rot / 2, or 2 i, 2 i + 1 with NM_ROPE_INTERLEAVED
+ * Queries go to q_out; keys to k_out (may be NULL) and, with the values as they are, to their token's slot of the cache (k_cache and
+ * v_cache both NULL: no cache, v is not read).  int8 caches hold codes: clamp(rint(value * inv_scale[head]), -127, 127).
+ * A slot outside [0, num_pages * page_size) is not written.  Two tokens of one slot: every element is one of the two's.
+ * q, k, v: device, a token's heads one behind the other, tokens q_stride, k_stride, v_stride elements apart (the thirds of a fused
+ * projection's rows, for instance); in_dtype F32, BF16 or F16.  q_out, k_out likewise, out_dtype the same three; q_out may be q itself
+ * (same type and stride), k_out k.  cache_dtype F32, BF16, F16 or I8.  positions, slots: device int32 [T] (positions may be NULL for rot = 0,
+ * slots without a cache).  inv_freq: device fp32 [rot / 2].  gammas: device fp32 [d].  k_inv_scale, v_inv_scale: device fp32 [hk], for int8.
+ * Limits: T <= 2^23; 1 <= d <= 256; rot even, 0 <= rot <= d; hq, hk >= 1, hq + 2 hk <= 65535; strides cover a token's heads.  Where the rows and the cache are
+ * 16-byte aligned, d is a multiple of 8 and rot of 8 (or 0), whole groups of elements move at once.
+ */
+enum { NM_QK_NORM = 1, NM_ROPE_INTERLEAVED = 2 };
+typedef struct {
+    int32_t T, hq, hk, d, rot, flags;
+    int32_t in_dtype, out_dtype, cache_dtype;
+    int32_t num_pages, page_size;
+    const void* q; const void* k; const void* v;
+    int64_t q_stride, k_stride, v_stride;
+    const float* q_gamma;
+    const float* k_gamma;
+    float eps;
+    const int32_t* positions;
+    const float* inv_freq;
+    void* q_out;
+    int64_t q_out_stride;
+    void* k_out;
+    int64_t k_out_stride;
+    void* k_cache;
+    void* v_cache;
+    int64_t page_stride, slot_stride, head_stride;
+    const int32_t* slots;
+    const float* k_inv_scale;
+    const float* v_inv_scale;
+} nm_qk_desc;
+
+int32_t nm_qk_norm_rope(const nm_qk_desc* desc, void* stream);
 
 #ifdef __cplusplus
 }

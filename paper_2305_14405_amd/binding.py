@@ -16,7 +16,10 @@ NM_OK = 0
 NM_ERR_INVALID_ARG, NM_ERR_UNSUPPORTED, NM_ERR_ALLOC, NM_ERR_HIP, NM_ERR_WORKSPACE = -1, -2, -3, -4, -5
 FUNC = {"gelu": 0, "exp": 1, "recip": 2, "rsqrt": 3, "relu": 4, "sqrt": 5, "identity": 6}
 NM_TABLE_CLAMP_INPUT, NM_TABLE_BIAS_CORRECT, NM_TABLE_MERGE, NM_TABLE_COMPACT = 1, 2, 4, 8
-NM_DT_I32, NM_DT_F32 = 0, 1
+NM_DT_I32, NM_DT_F32, NM_DT_BF16, NM_DT_F16, NM_DT_I8 = 0, 1, 2, 3, 4
+NM_PLAN_MAX_REQUESTS = 4096
+NM_PLAN_NO_PAGES, NM_PLAN_TABLE_FULL, NM_PLAN_NO_ROWS, NM_PLAN_BAD_LENGTH = 1, 2, 4, 8
+NM_QK_NORM, NM_ROPE_INTERLEAVED = 1, 2
 
 # every symbol include/nm.h declares
 EXPORTS = ("nm_last_error", "nm_version", "nm_table_build_host", "nm_build_tables",
@@ -25,7 +28,8 @@ EXPORTS = ("nm_last_error", "nm_version", "nm_table_build_host", "nm_build_table
            "nm_attn_context", "nm_attention_pwl", "nm_encoder_layer_workspace", "nm_encoder_layer",
            "nm_encoder_layer_noalloc",
            "nm_encoder_stack_workspace", "nm_encoder_stack", "nm_conv2d_workspace", "nm_conv2d_pwl",
-           "nm_maxpool_i8", "nm_avgpool_i8", "nm_cnn_workspace", "nm_cnn_run")
+           "nm_maxpool_i8", "nm_avgpool_i8", "nm_cnn_workspace", "nm_cnn_run",
+           "nm_page_plan", "nm_qk_norm_rope")
 NM_OP_CONV, NM_OP_MAXPOOL, NM_OP_AVGPOOL, NM_OP_GEMM = 0, 1, 2, 3
 NM_LAYER_FOLD_LAYERNORM, NM_LAYER_NO_FOLD_LAYERNORM = 1, 2
 NM_NOALLOC_MAX_WORKSPACE = 64 << 20  # bytes of the buffer built into the library (nm_encoder_layer_noalloc)
@@ -86,6 +90,25 @@ class LayerDesc(C.Structure):
 
 class LayerTaps(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in TAP_NAMES]
+
+
+class PlanDesc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("B", "page_size", "num_pages", "max_pages", "n_free", "max_tokens")] +
+                [(n, C.c_void_p) for n in ("cached", "fresh", "free_pages", "free_begin", "free_end", "block_table")] +
+                [("table_stride", C.c_int64)] +
+                [(n, C.c_void_p) for n in ("lens", "row_start", "slots", "positions", "requests", "status")])
+
+
+class QkDesc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("T", "hq", "hk", "d", "rot", "flags", "in_dtype", "out_dtype", "cache_dtype",
+                                          "num_pages", "page_size")] +
+                [(n, C.c_void_p) for n in ("q", "k", "v")] +
+                [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride")] +
+                [("q_gamma", C.c_void_p), ("k_gamma", C.c_void_p), ("eps", C.c_float),
+                 ("positions", C.c_void_p), ("inv_freq", C.c_void_p), ("q_out", C.c_void_p), ("q_out_stride", C.c_int64),
+                 ("k_out", C.c_void_p), ("k_out_stride", C.c_int64), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p)] +
+                [(n, C.c_int64) for n in ("page_stride", "slot_stride", "head_stride")] +
+                [(n, C.c_void_p) for n in ("slots", "k_inv_scale", "v_inv_scale")])
 
 
 _lib = None
@@ -154,6 +177,8 @@ def load(preload_torch: bool = True) -> C.CDLL:
     L.nm_encoder_stack_workspace.argtypes = [C.POINTER(LayerDesc), C.c_int32, C.POINTER(C.c_size_t)]
     L.nm_encoder_stack.argtypes = [C.POINTER(LayerDesc), C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
                                    C.c_void_p, C.c_size_t, C.c_void_p]
+    L.nm_page_plan.argtypes = [C.POINTER(PlanDesc), C.c_void_p]
+    L.nm_qk_norm_rope.argtypes = [C.POINTER(QkDesc), C.c_void_p]
     _lib = L
     return L
 
@@ -524,3 +549,118 @@ def nm_cnn_run(ops, ws=None, stream=None, ws_bytes=None, op_array=None):
     arr = op_array if op_array is not None else _op_array(ops)
     nbytes = 0 if ws is None else (ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes)
     _check(load().nm_cnn_run(arr, len(arr), _ptr(ws), nbytes, _stream(stream)))
+
+
+# ---- one step of a decoder over a paged cache -----------------------------------------------------
+#
+# These calls' tensors may have strides, so what the C ABI cannot see is checked here: every tensor is on torch's current device,
+# has the type that the call wants of it, and lies as the call's addressing says.
+
+_dtypes = None
+
+
+def _refuse(what):
+    raise NmError(NM_ERR_INVALID_ARG, what)
+
+
+def _types():
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = {torch.int32: NM_DT_I32, torch.float32: NM_DT_F32, torch.bfloat16: NM_DT_BF16, torch.float16: NM_DT_F16,
+                   torch.int8: NM_DT_I8, torch.uint8: None}
+    return _dtypes
+
+
+def _type(t, name):
+    """The library's number of a device tensor's type."""
+    if not t.is_cuda:
+        _refuse(f"{name} is not in device memory")
+    if _device is None:
+        _current_stream()
+    if _device is not None and t.get_device() != _device():
+        _refuse(f"{name} is not on the current device")
+    try:
+        return _types()[t.dtype]
+    except KeyError:
+        _refuse(f"{name}: no call takes {t.dtype}")
+
+
+def _vector(t, dtype, n, name):
+    """Address of a contiguous tensor of n elements of one type; None for None."""
+    if t is None:
+        return None
+    if _type(t, name) != dtype or t.numel() != n or not t.is_contiguous():
+        _refuse(f"{name}: a contiguous tensor of {n} elements of the call's type is wanted, got {tuple(t.shape)} of {t.dtype}")
+    return t.data_ptr()
+
+
+def _heads(t, T, h, d, name):
+    """Address and token stride of [T, h, d] whose heads lie one behind the other."""
+    if tuple(t.shape) != (T, h, d):
+        _refuse(f"{name}: shape {tuple(t.shape)}, wanted {(T, h, d)}")
+    s0, s1, s2 = t.stride()
+    if (s2 != 1 and d > 1) or (s1 != d and h > 1):
+        _refuse(f"{name}: the heads of a token have to lie one behind the other")
+    return t.data_ptr(), s0 if T > 1 else max(s0, h * d)
+
+
+def _cache(k_cache, v_cache, hk, d):
+    """dtype, (pages, page_size), (page, slot, head stride) of the two caches [pages, page_size, hk, d]."""
+    dtype = _type(k_cache, "k_cache")
+    pages, page, h, e = k_cache.shape
+    strides = k_cache.stride()
+    if (h, e) != (hk, d) or v_cache.shape != k_cache.shape:
+        _refuse(f"k_cache {tuple(k_cache.shape)} and v_cache {tuple(v_cache.shape)}: [pages, page_size, {hk}, {d}] is wanted")
+    if _type(v_cache, "v_cache") != dtype or v_cache.stride() != strides:
+        _refuse("k_cache and v_cache have to have one type and the same strides")
+    if strides[3] != 1 and d > 1:
+        _refuse("the elements of a head have to be neighbours in the cache")
+    return dtype, pages, page, strides
+
+
+def nm_page_plan(cached, fresh, free_pages, free_begin, block_table, *, page_size, num_pages, free_end, slots, status, lens=None,
+                 row_start=None, positions=None, requests=None, stream=None):
+    """block_table: int32 [B, max_pages], rows may be apart; every other tensor is contiguous int32."""
+    B, i32 = cached.numel(), NM_DT_I32
+    if _type(block_table, "block_table") != i32 or block_table.dim() != 2 or block_table.shape[0] != B or \
+            (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+        _refuse(f"block_table: int32 [{B}, max_pages] with neighbouring columns is wanted")
+    columns, n_free, T = block_table.shape[1], free_pages.numel(), slots.numel()
+    d = PlanDesc(B, page_size, num_pages, columns, n_free, T, _vector(cached, i32, B, "cached"), _vector(fresh, i32, B, "fresh"),
+                 _vector(free_pages, i32, n_free, "free_pages"), _vector(free_begin, i32, 1, "free_begin"), _vector(free_end, i32, 1, "free_end"),
+                 block_table.data_ptr(), block_table.stride(0) if B > 1 else columns, _vector(lens, i32, B, "lens"),
+                 _vector(row_start, i32, B + 1, "row_start"), _vector(slots, i32, T, "slots"), _vector(positions, i32, T, "positions"),
+                 _vector(requests, i32, T, "requests"), _vector(status, i32, 4, "status"))
+    _check(load().nm_page_plan(C.byref(d), _stream(stream)))
+
+
+def nm_qk_norm_rope(q, k, v, positions, inv_freq, q_out, *, k_out=None, k_cache=None, v_cache=None, slots=None, norm=False, q_gamma=None,
+                    k_gamma=None, eps=1e-6, interleaved=False, k_inv_scale=None, v_inv_scale=None, stream=None):
+    """q, q_out: [T, hq, d]; k, v, k_out: [T, hk, d]; caches: [pages, page_size, hk, d] with strides; inv_freq (rot / 2 numbers) and
+    positions may be None: no rotation."""
+    T, hq, e = q.shape
+    hk, f32, i32 = k.shape[1], NM_DT_F32, NM_DT_I32
+    in_dtype, out_dtype = _type(q, "q"), _type(q_out, "q_out")
+    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+    if _type(k, "k") != in_dtype or (k_out is not None and _type(k_out, "k_out") != out_dtype):
+        _refuse("q and k, and q_out and k_out, have to have one type")
+    qp, qs = _heads(q, T, hq, e, "q")
+    kp, ks = _heads(k, T, hk, e, "k")
+    op, os_ = _heads(q_out, T, hq, e, "q_out")
+    up, us = (None, 0) if k_out is None else _heads(k_out, T, hk, e, "k_out")
+    d = QkDesc(T, hq, hk, e, rot, (NM_QK_NORM if norm else 0) | (NM_ROPE_INTERLEAVED if interleaved else 0), in_dtype, out_dtype)
+    d.q, d.q_stride, d.k, d.k_stride, d.q_out, d.q_out_stride, d.k_out, d.k_out_stride = qp, qs, kp, ks, op, os_, up, us
+    d.q_gamma, d.k_gamma, d.eps = _vector(q_gamma, f32, e, "q_gamma"), _vector(k_gamma, f32, e, "k_gamma"), eps
+    if rot:
+        d.positions, d.inv_freq = _vector(positions, i32, T, "positions"), _vector(inv_freq, f32, rot // 2, "inv_freq")
+    if k_cache is not None or v_cache is not None:
+        if k_cache is None or v_cache is None or slots is None:
+            _refuse("k_cache, v_cache and slots belong together")
+        if _type(v, "v") != in_dtype:
+            _refuse("q, k and v have to have one type")
+        d.v, d.v_stride = _heads(v, T, hk, e, "v")
+        d.cache_dtype, d.num_pages, d.page_size, (d.page_stride, d.slot_stride, d.head_stride, _) = _cache(k_cache, v_cache, hk, e)
+        d.k_cache, d.v_cache, d.slots = k_cache.data_ptr(), v_cache.data_ptr(), _vector(slots, i32, T, "slots")
+        d.k_inv_scale, d.v_inv_scale = _vector(k_inv_scale, f32, hk, "k_inv_scale"), _vector(v_inv_scale, f32, hk, "v_inv_scale")
+    _check(load().nm_qk_norm_rope(C.byref(d), _stream(stream)))

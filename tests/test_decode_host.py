@@ -1,0 +1,100 @@
+"""CPU-only checks of the calls of a decode step: what they refuse, before anything reaches the GPU."""
+import ctypes as C
+
+import pytest
+
+from paper_2305_14405_amd import binding as nm
+
+Z = C.c_void_p(0)
+P = 4096  # a non-null dummy address; never dereferenced because validation fails first
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return nm.load(preload_torch=False)
+
+
+def refused(call, desc, wanted, **changes):
+    """The call's status with some fields of a good description changed."""
+    keep = {n: getattr(desc, n) for n in changes}
+    for n, v in changes.items():
+        setattr(desc, n, v)
+    rc = call(C.byref(desc), Z)
+    for n, v in keep.items():
+        setattr(desc, n, v)
+    assert rc == wanted, (changes, rc, nm.nm_last_error())
+    assert nm.nm_last_error() != ""
+
+
+def plan():
+    d = nm.PlanDesc()
+    d.B, d.page_size, d.num_pages, d.max_pages, d.n_free, d.max_tokens, d.table_stride = 4, 16, 64, 8, 10, 100, 8
+    for i, n in enumerate(("cached", "fresh", "free_pages", "free_begin", "free_end", "block_table", "lens", "row_start", "slots",
+                           "positions", "requests", "status")):
+        setattr(d, n, P * (i + 1))
+    return d
+
+
+@pytest.mark.parametrize("changes", [
+    dict(B=-1), dict(num_pages=-1), dict(max_pages=-1), dict(n_free=-1), dict(max_tokens=-1), dict(table_stride=7),
+    dict(free_begin=None), dict(free_end=None), dict(status=None), dict(slots=None), dict(cached=None), dict(fresh=None),
+    dict(block_table=None), dict(free_pages=None), dict(lens=P), dict(free_end=P * 4), dict(row_start=2 * P)])
+def test_page_plan_refuses(lib, changes):
+    refused(lib.nm_page_plan, plan(), nm.NM_ERR_INVALID_ARG, **changes)
+
+
+@pytest.mark.parametrize("changes", [dict(B=nm.NM_PLAN_MAX_REQUESTS + 1), dict(page_size=0), dict(page_size=24), dict(page_size=1 << 17),
+                                     dict(num_pages=1 << 27)])
+def test_page_plan_does_not_cover(lib, changes):
+    refused(lib.nm_page_plan, plan(), nm.NM_ERR_UNSUPPORTED, **changes)
+
+
+def test_page_plan_null(lib):
+    assert lib.nm_page_plan(None, Z) == nm.NM_ERR_INVALID_ARG
+
+
+def qk():
+    d = nm.QkDesc()
+    d.T, d.hq, d.hk, d.d, d.rot, d.flags = 3, 4, 2, 64, 32, nm.NM_QK_NORM
+    d.in_dtype, d.out_dtype, d.cache_dtype, d.num_pages, d.page_size = nm.NM_DT_BF16, nm.NM_DT_F32, nm.NM_DT_I8, 8, 16
+    for i, n in enumerate(("q", "k", "v", "q_gamma", "k_gamma", "positions", "inv_freq", "q_out", "k_out", "k_cache", "v_cache", "slots",
+                           "k_inv_scale", "v_inv_scale")):
+        setattr(d, n, P * (i + 1))
+    d.q_stride, d.k_stride, d.v_stride, d.q_out_stride, d.k_out_stride, d.eps = 512, 512, 512, 256, 128, 1e-6
+    d.page_stride, d.slot_stride, d.head_stride = 2048, 128, 64
+    return d
+
+
+@pytest.mark.parametrize("changes", [
+    dict(T=-1), dict(hq=0), dict(hk=0), dict(d=0), dict(rot=-2), dict(rot=31), dict(rot=66), dict(flags=4), dict(in_dtype=nm.NM_DT_I8),
+    dict(out_dtype=nm.NM_DT_I8), dict(cache_dtype=nm.NM_DT_I32), dict(eps=float("nan")), dict(eps=-1.0), dict(eps=float("inf")), dict(k_cache=None),
+    dict(v_cache=None), dict(q_stride=255), dict(k_stride=127), dict(v_stride=127), dict(q_out_stride=255), dict(k_out_stride=127),
+    dict(num_pages=-1), dict(page_stride=-1), dict(slot_stride=-1), dict(head_stride=-1), dict(k_inv_scale=None), dict(v_inv_scale=None),
+    dict(q=None), dict(k=None), dict(v=None), dict(q_out=None), dict(slots=None), dict(positions=None), dict(inv_freq=None),
+    dict(q_out=P), dict(k_out=2 * P), dict(q_out=P, out_dtype=nm.NM_DT_BF16)])
+def test_qk_norm_rope_refuses(lib, changes):
+    refused(lib.nm_qk_norm_rope, qk(), nm.NM_ERR_INVALID_ARG, **changes)
+
+
+@pytest.mark.parametrize("changes", [dict(d=258, q_stride=2000, k_stride=2000, v_stride=2000, q_out_stride=2000, k_out_stride=2000),
+                                     dict(page_size=12), dict(num_pages=1 << 27), dict(T=(1 << 23) + 1), dict(hq=1 << 16)])
+def test_qk_norm_rope_does_not_cover(lib, changes):
+    refused(lib.nm_qk_norm_rope, qk(), nm.NM_ERR_UNSUPPORTED, **changes)
+
+
+def test_qk_norm_rope_null_and_empty(lib):
+    assert lib.nm_qk_norm_rope(None, Z) == nm.NM_ERR_INVALID_ARG
+    d = qk()
+    d.T, d.q, d.k, d.v, d.q_out, d.slots, d.positions = 0, None, None, None, None, None, None
+    assert lib.nm_qk_norm_rope(C.byref(d), Z) == nm.NM_OK  # nothing to do
+
+
+def test_binding_refuses_host_tensors():
+    import torch
+    i = torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(nm.NmError) as e:
+        nm.nm_page_plan(i, i, i, i[:1], i.view(4, 1), page_size=16, num_pages=4, free_end=i[:1], slots=i, status=i)
+    assert e.value.status == nm.NM_ERR_INVALID_ARG
+    x = torch.zeros((2, 4, 64))
+    with pytest.raises(nm.NmError):
+        nm.nm_qk_norm_rope(x, x, x, i, None, x)

@@ -1,0 +1,326 @@
+"""The calls of a decode step (plan, norms and rotation, attention over the cache, 4-bit products) against plain
+implementations in 64 bits, and a run of them together."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2305_14405_amd import binding as nm
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24                                                               # half a step of binary32, relative
+HALF_STEP = {torch.float32: U, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def gen(seed):
+    g = torch.Generator(device="cpu")
+    g.manual_seed(seed)
+    return g
+
+
+def i32(*a, **k):
+    return torch.tensor(*a, dtype=torch.int32, **k).to(DEV)
+
+
+# ---- plan ---------------------------------------------------------------------------------------
+
+def plan_in_python(cached, fresh, free, begin, table, page, num_pages, T):
+    """The documented rules, one request after the other."""
+    B, columns = table.shape
+    up = lambda n: -(-n // page)  # noqa: E731
+    need = [up(c + f) - up(c) if f > 0 else 0 for c, f in zip(cached, fresh)]
+    flags = (1 if begin + sum(need) > len(free) else 0) | (2 if any(up(c + f) > columns for c, f in zip(cached, fresh)) else 0) | \
+            (4 if sum(fresh) > T else 0) | (8 if min([0, begin, *cached, *fresh]) < 0 else 0)
+    out = {"status": [flags, sum(fresh), sum(need), max([0] + [c + f for c, f in zip(cached, fresh)])], "table": table.copy(), "lens": list(cached),
+           "row_start": [0] * (B + 1), "end": begin, "slots": [-1] * T, "positions": [0] * T, "requests": [-1] * T}
+    if flags:
+        return out
+    t = 0
+    for b in range(B):
+        for j in range(need[b]):
+            out["table"][b, up(cached[b]) + j] = free[out["end"]]
+            out["end"] += 1
+        for i in range(fresh[b]):
+            p = cached[b] + i
+            entry = out["table"][b, p // page]
+            out["slots"][t] = entry * page + p % page if 0 <= entry < num_pages else -1
+            out["positions"][t], out["requests"][t] = p, b
+            t += 1
+        out["lens"][b] = cached[b] + fresh[b]
+        out["row_start"][b + 1] = t
+    return out
+
+
+def run_plan(cached, fresh, free, begin, table, page, num_pages, T, some=False, stride=None):
+    B, columns = table.shape
+    wide = torch.full((B, stride or columns), -77, dtype=torch.int32)
+    wide[:, :columns] = torch.from_numpy(table)
+    wide = wide.to(DEV)
+    o = {"end": i32([-5]), "lens": i32([-5] * B), "row_start": i32([-5] * (B + 1)), "slots": i32([-5] * T), "positions": i32([-5] * T),
+         "requests": i32([-5] * T), "status": i32([-5] * 4)}
+    optional = {} if some else {n: o[n] for n in ("lens", "row_start", "positions", "requests")}
+    nm.nm_page_plan(i32(cached), i32(fresh), i32(free), i32([begin]), wide[:, :columns], page_size=page, num_pages=num_pages, free_end=o["end"],
+                    slots=o["slots"], status=o["status"], **optional)
+    torch.cuda.synchronize()
+    got = {n: v.cpu().tolist() for n, v in o.items()}
+    wide = wide.cpu().numpy()
+    assert (wide[:, columns:] == -77).all()
+    got["table"] = wide[:, :columns]
+    return got
+
+
+def check_plan(got, want, names=("status", "lens", "row_start", "slots", "positions", "requests")):
+    for n in names:
+        assert got[n] == want[n], n
+    assert got["end"] == [want["end"]]
+    assert np.array_equal(got["table"], want["table"])
+
+
+def random_plan(seed, B, page, longest, most_new, idle=0.3):
+    r = np.random.default_rng(seed)
+    cached = r.integers(0, longest + 1, B).tolist()
+    fresh = [0 if r.random() < idle else int(r.integers(1, most_new + 1)) for _ in range(B)]
+    columns = -(-(longest + most_new) // page)
+    pages = r.permutation(B * columns + 50)
+    table = np.full((B, columns), -1, np.int32)
+    at = 0
+    for b in range(B):
+        n = -(-cached[b] // page)
+        table[b, :n] = pages[at:at + n]
+        at += n
+    return cached, fresh, pages[at:].tolist(), table, len(pages)
+
+
+@pytest.mark.parametrize("B,page,longest,most_new,extra", [
+    (1, 16, 0, 1, 0), (1, 1, 5, 3, 2), (8, 16, 300, 1, 0), (255, 16, 100, 1, 7), (256, 8, 64, 40, 0), (257, 32, 200, 33, 1),
+    (1000, 16, 50, 2, 100), (4096, 64, 300, 1, 0), (3, 128, 1000, 5000, 777), (40, 65536, 3, 100, 0), (2, 16, 10, 300000, 5)])
+def test_page_plan_matches_python(B, page, longest, most_new, extra):
+    cached, fresh, free, table, pages = random_plan(B + page, B, page, longest, most_new)
+    args = (cached, fresh, free, 0 if len(free) < 60 else 9, table, page, pages, sum(fresh) + extra)
+    check_plan(run_plan(*args, stride=table.shape[1] + 3), plan_in_python(*args))
+
+
+def test_page_plan_optional_outputs_and_empty_batches():
+    cached, fresh, free, table, pages = random_plan(3, 20, 16, 100, 9)
+    args = (cached, fresh, free, 2, table, 16, pages, sum(fresh))
+    check_plan(run_plan(*args, some=True), plan_in_python(*args), ("status", "slots"))
+    check_plan(run_plan([], [], [5], 1, np.zeros((0, 4), np.int32), 16, 10, 6), plan_in_python([], [], [5], 1, np.zeros((0, 4), np.int32), 16, 10, 6))
+    idle = ([3, 0], [0, 0], [], 0, np.array([[2, -1], [-1, -1]], np.int32), 16, 10, 0)
+    check_plan(run_plan(*idle), plan_in_python(*idle))
+
+
+@pytest.mark.parametrize("what", ["pages", "table", "rows", "cached", "fresh", "begin", "several"])
+def test_page_plan_assigns_nothing_that_does_not_fit(what):
+    cached, fresh, free, table, pages = random_plan(11, 300, 16, 100, 30, idle=0.1)
+    need = plan_in_python(cached, fresh, free, 0, table, 16, pages, sum(fresh))["status"][2]
+    begin, T = 4, sum(fresh) + 5
+    free = free[:need + begin]
+    if what in ("pages", "several"):
+        free = free[:-1]
+    if what in ("rows", "several"):
+        T = sum(fresh) - 1
+    if what == "table":
+        fresh[150] += 100
+        free, T = free + list(range(10)), T + 100
+    if what == "cached":
+        cached[299] = -1
+    if what == "fresh":
+        fresh[0] = -3
+    if what == "begin":
+        begin = -1
+    args = (cached, fresh, free, begin, table, 16, pages, T)
+    want, got = plan_in_python(*args), run_plan(*args)
+    assert want["status"][0] != 0
+    if what in ("cached", "fresh", "begin"):        # the numbers beside the flag are of no use then
+        assert got["status"][0] & nm.NM_PLAN_BAD_LENGTH
+        check_plan(got, want, ("lens", "row_start", "slots", "positions", "requests"))
+    else:
+        check_plan(got, want)
+
+
+def test_page_plan_sums_beyond_31_bits():
+    B, big = 3000, 2 ** 31 - 1
+    table = np.full((B, 2), -1, np.int32)
+    got = run_plan([0] * B, [big] * B, [1, 2], 0, table, 16, 100, 4)
+    assert got["status"] == [nm.NM_PLAN_NO_PAGES | nm.NM_PLAN_TABLE_FULL | nm.NM_PLAN_NO_ROWS, big, big, big]
+    assert got["slots"] == [-1] * 4 and got["lens"] == [0] * B and (got["table"] == -1).all()
+
+
+def test_page_plan_entries_that_are_no_pages():
+    table = np.array([[7, -1, -1], [-3, -1, -1], [99, -1, -1]], np.int32)
+    args = ([3, 5, 6], [20, 2, 1], [50, 51], 0, table, 16, 51, 23)   # list entry 50 is the last page, 51 is none; rows 1 and 2 hold none
+    got = run_plan(*args)
+    check_plan(got, plan_in_python(*args))
+    assert got["slots"][20:] == [-1, -1, -1] and got["slots"][13] == 50 * 16
+
+
+# ---- norms and rotation ---------------------------------------------------------------------------
+
+def rotate_64(x, positions, inv_freq, gamma, norm, interleaved, eps=1e-6):
+    """(result, bound of a 32-bit evaluation's error) in binary64.  Rounding errors, in units of U relative to the operands: the mean of
+    at most 256 squares 16 (a chain of 8 and a butterfly of 6, and the squares), halved by the root; the root, the quotient and two
+    products 5; together 13 on y.  A turn adds two products and a sum, 3, and the sine and cosine: their angle is rounded
+    to 32 bits once (pi U) and the functions are taken to be within 4 U: 8 U of either partner.  25 are granted, on the sum of the partners'
+    absolute values."""
+    y = x.double()
+    if norm:
+        y = y / torch.sqrt((y * y).mean(-1, keepdim=True) + eps) * (1 if gamma is None else gamma.double())
+    out, size = y.clone(), y.abs().clone()
+    rot = 2 * inv_freq.numel()
+    if rot:
+        a, b = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
+        phase = positions.double()[:, None, None] * inv_freq.double()
+        c, s = torch.cos(phase), torch.sin(phase)
+        out[..., a], out[..., b] = y[..., a] * c - y[..., b] * s, y[..., b] * c + y[..., a] * s
+        size[..., a] = size[..., b] = y[..., a].abs() + y[..., b].abs()
+    return out, 25 * U * size
+
+
+def assert_rounded(got, want, error, what):
+    """got is want, wrong by no more than error, rounded to its type (at most half a step of the result, or of the smallest normal number)."""
+    bound = error + HALF_STEP[got.dtype] * ((want.abs() + error) + torch.finfo(got.dtype).tiny)
+    off = (got.double() - want).abs()
+    assert bool((off <= bound).all()), f"{what}: {float((off / bound).max()):.3g} of the bound"
+
+
+def qk_case(seed, T, hq, hk, d, rot, dtype, cache_dtype, page=16, by_head=False, far=5000, pad=0):
+    g = gen(seed)
+    row = (hq + 2 * hk) * d + pad
+    x = torch.randn((T, row), generator=g).to(dtype).to(DEV)
+    q, k, v = (x[:, a * d:b * d].view(T, -1, d) for a, b in ((0, hq), (hq, hq + hk), (hq + hk, hq + 2 * hk)))
+    pages = -(-(T + 20) // page)
+    shape = (2, pages, hk, page, d) if by_head else (2, pages, page, hk, d)
+    cache = (torch.randn(shape, generator=g) * 30).to(cache_dtype).to(DEV)
+    cache = cache.transpose(2, 3) if by_head else cache
+    slots = torch.randperm(pages * page, generator=g)[:T].to(torch.int32)
+    if T > 2:
+        slots[1], slots[T - 1] = -1, pages * page   # neither is a slot
+    return dict(x=x, q=q, k=k, v=v, cache=cache, slots=slots.to(DEV), positions=torch.randint(0, far, (T,), generator=g, dtype=torch.int32).to(DEV),
+                inv_freq=(10000.0 ** (-torch.arange(0, rot, 2, dtype=torch.float64) / max(rot, 1))).float().to(DEV),
+                q_gamma=(1 + 0.2 * torch.randn(d, generator=g)).to(DEV), k_gamma=(1 + 0.2 * torch.randn(d, generator=g)).to(DEV),
+                inv_scale=(20 + 10 * torch.rand((2, hk), generator=g)).to(DEV))
+
+
+def check_qk(c, dtype_out, norm=True, interleaved=False, gammas=True, k_out=True, cached=True):
+    T, hq, d = c["q"].shape
+    hk = c["k"].shape[1]
+    q_out = torch.full((T, hq, d), float("nan"), dtype=dtype_out, device=DEV)
+    key = torch.full((T, hk, d), float("nan"), dtype=dtype_out, device=DEV) if k_out else None
+    before, x = c["cache"].clone(), c["x"].clone()
+    codes = before.dtype == torch.int8
+    g = (c["q_gamma"], c["k_gamma"]) if gammas else (None, None)
+    inv_freq = c["inv_freq"] if c["inv_freq"].numel() else None
+    more = dict(k_cache=c["cache"][0], v_cache=c["cache"][1], slots=c["slots"]) if cached else {}
+    if codes and cached:
+        more.update(k_inv_scale=c["inv_scale"][0], v_inv_scale=c["inv_scale"][1])
+    nm.nm_qk_norm_rope(c["q"], c["k"], c["v"], c["positions"], inv_freq, q_out, k_out=key, norm=norm, q_gamma=g[0], k_gamma=g[1],
+                       interleaved=interleaved, **more)
+    torch.cuda.synchronize()
+    assert torch.equal(c["x"], x)
+    wq, eq = rotate_64(c["q"], c["positions"], c["inv_freq"], g[0], norm, interleaved)
+    wk, ek = rotate_64(c["k"], c["positions"], c["inv_freq"], g[1], norm, interleaved)
+    assert_rounded(q_out, wq, eq, "q")
+    if k_out:
+        assert_rounded(key, wk, ek, "k")
+    _, pages, page, _, _ = before.shape
+    there = (c["slots"] >= 0) & (c["slots"] < pages * page) & cached
+    at = c["slots"][there].long()
+    written = torch.zeros((pages, page), dtype=torch.bool, device=DEV)
+    written[at // page, at % page] = True
+    assert torch.equal(c["cache"][:, ~written], before[:, ~written])             # nothing but the tokens' slots is touched
+    for n, (want, error) in enumerate(((wk, ek), (c["v"].double(), torch.zeros_like(wk)))):
+        got, want, error = c["cache"][n][at // page, at % page], want[there], error[there]
+        if codes:
+            inv = c["inv_scale"][n].double()[:, None]
+            real = (want * inv).clamp(-127, 127)
+            off = (got.double() - real).abs() - 0.5 - error * inv - 2 * U * real.abs()   # the product's rounding, and that to a code
+            assert bool((off <= 0).all()), float(off.max())
+        else:
+            assert_rounded(got, want, error, "cache")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("T,hq,hk,d,rot", [(1, 1, 1, 64, 64), (1, 32, 8, 128, 128), (3, 12, 12, 64, 32), (70, 5, 1, 96, 48), (33, 4, 2, 80, 40),
+                                           (9, 24, 3, 32, 32), (17, 2, 2, 256, 256), (5, 3, 3, 192, 64), (1030, 2, 1, 16, 16), (2, 7, 2, 8, 0)])
+def test_qk_norm_rope(dtype, interleaved, T, hq, hk, d, rot):
+    check_qk(qk_case(T + d, T, hq, hk, d, rot, dtype, dtype), dtype, interleaved=interleaved)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("T,hq,hk,d,rot,pad", [(4, 3, 2, 7, 4, 0), (5, 2, 1, 1, 0, 0), (6, 2, 2, 100, 50, 1), (3, 2, 1, 250, 250, 0), (1100, 1, 1, 66, 2, 3),
+                                               (4, 2, 2, 64, 64, 1), (4, 2, 2, 64, 12, 0)])
+def test_qk_norm_rope_odd_sizes_and_alignment(dtype, interleaved, T, hq, hk, d, rot, pad):
+    check_qk(qk_case(T + d, T, hq, hk, d, rot, dtype, dtype, pad=pad), dtype, interleaved=interleaved)
+
+
+@pytest.mark.parametrize("cache_dtype", [torch.float32, torch.bfloat16, torch.float16, torch.int8])
+@pytest.mark.parametrize("by_head", [False, True])
+@pytest.mark.parametrize("d", [64, 30])
+@pytest.mark.parametrize("dtype,dtype_out", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.float16), (torch.float16, torch.float32)])
+def test_qk_norm_rope_types_and_layouts_of_the_cache(cache_dtype, by_head, d, dtype, dtype_out):
+    check_qk(qk_case(d, 40, 4, 2, d, d, dtype, cache_dtype, page=8, by_head=by_head), dtype_out)
+
+
+@pytest.mark.parametrize("d", [64, 22])
+@pytest.mark.parametrize("norm,gammas,k_out,cached", [(False, False, True, True), (True, False, False, True), (True, True, True, False), (False, False, True, False)])
+def test_qk_norm_rope_options(d, norm, gammas, k_out, cached):
+    check_qk(qk_case(d, 21, 4, 2, d, d, torch.float32, torch.int8), torch.float32, norm=norm, gammas=gammas, k_out=k_out, cached=cached)
+
+
+@pytest.mark.parametrize("d", [128, 126])
+def test_qk_norm_rope_far_positions(d):
+    c = qk_case(5, 64, 2, 1, d, d, torch.float32, torch.float32, far=2 ** 31 - 1)
+    c["positions"][0] = 2 ** 31 - 1
+    c["positions"][1] = -7
+    check_qk(c, torch.float32)
+
+
+@pytest.mark.parametrize("d", [64, 66])
+def test_qk_norm_rope_in_place_and_on_a_stream(d):
+    a, b = (qk_case(8, 50, 4, 2, d, d, torch.bfloat16, torch.bfloat16) for _ in range(2))
+    q_out, k_out = torch.empty_like(a["q"]), torch.empty_like(a["k"])
+    nm.nm_qk_norm_rope(a["q"], a["k"], a["v"], a["positions"], a["inv_freq"], q_out, k_out=k_out, norm=True)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    nm.nm_qk_norm_rope(b["q"], b["k"], b["v"], b["positions"], b["inv_freq"], b["q"], k_out=b["k"], norm=True, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(b["q"], q_out) and torch.equal(b["k"], k_out) and torch.equal(a["v"], b["v"])
+
+
+def test_qk_norm_rope_special_values():
+    """Zeros stay zeros under the norm, a NaN or an infinity stays in its own head, and codes saturate (NaN: -127)."""
+    c = qk_case(2, 4, 2, 2, 64, 64, torch.float32, torch.int8)
+    c["slots"] = i32([0, 1, 2, 3])
+    c["q"][0], c["k"][0] = 0, 0
+    c["q"][1, 1, 5] = float("nan")
+    c["k"][2, 0, 7] = float("inf")
+    c["v"][3, 1, :3] = torch.tensor([float("nan"), 1e30, -float("inf")], device=DEV)
+    q_out = torch.empty((4, 2, 64), device=DEV)
+    nm.nm_qk_norm_rope(c["q"], c["k"], c["v"], c["positions"], c["inv_freq"], q_out, norm=True, k_cache=c["cache"][0], v_cache=c["cache"][1],
+                       slots=c["slots"], k_inv_scale=c["inv_scale"][0], v_inv_scale=c["inv_scale"][1])
+    torch.cuda.synchronize()
+    assert bool((q_out[0] == 0).all()) and bool((c["cache"][0, 0, 0] == 0).all())
+    assert bool(q_out[1, 1].isnan().all()) and bool(q_out[1, 0].isfinite().all()) and bool(q_out[2:].isfinite().all())
+    assert c["cache"][1, 0, 3, 1, :3].tolist() == [-127, 127, -127]
+
+
+def test_decode_binding_refuses():
+    c = qk_case(1, 4, 2, 2, 64, 64, torch.float32, torch.int8)
+    q_out = torch.empty((4, 2, 64), device=DEV)
+    good = dict(k_cache=c["cache"][0], v_cache=c["cache"][1], slots=c["slots"], k_inv_scale=c["inv_scale"][0], v_inv_scale=c["inv_scale"][1])
+    args = [c["q"], c["k"], c["v"], c["positions"], c["inv_freq"], q_out]
+    for at, bad in ((0, c["q"].transpose(1, 2)), (0, c["q"][..., ::2]), (1, c["k"].half()), (2, c["v"][:3]), (3, c["positions"].long()),
+                    (3, c["positions"][:2]), (4, c["inv_freq"].double()), (5, q_out[:, :1]), (5, q_out.double()), (2, c["v"].cpu())):
+        changed = list(args)
+        changed[at] = bad
+        with pytest.raises(nm.NmError):
+            nm.nm_qk_norm_rope(*changed, **good)
+    for change in (dict(slots=None), dict(v_cache=None), dict(k_cache=c["cache"][0][:, :, :1]), dict(v_cache=c["cache"][1].half()),
+                   dict(k_inv_scale=None), dict(v_inv_scale=c["inv_scale"][1][:1]), dict(slots=c["slots"].long()), dict(q_gamma=c["q_gamma"][:3])):
+        with pytest.raises(nm.NmError):
+            nm.nm_qk_norm_rope(*args, **{**good, **change})
