@@ -566,6 +566,50 @@ typedef struct {
 
 int32_t nm_qk_norm_rope(const nm_qk_desc* desc, void* stream);
 
+/*
+ * nm_paged_attention: attention of one new token of every request over the request's cache.  With n = lens[b], the query heads
+ * h of a group sharing key head g = h / (hq / hk), and the positions j in [max(0, n - window), n) (window 0: [0, n)):
+ *   s_j = scale * q[b,h] . k_j        k_j, v_j: key and value of position j for head g, int8 codes times k_scale[g], v_scale[g]
+ *   out[b,h] = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),  m = max_j s_j;   lse[b,h] = m + log sum_j exp(s_j - m)
+ * No position (n <= 0): out 0, lse -inf.  A length beyond max_pages * page_size counts as that; a position whose table entry
+ * is no page (outside [0, num_pages)) takes no part.  Slots behind a request's length are never read: what they hold does not matter.
+ * q: device [B, hq, d], requests q_stride elements apart, q_dtype F32, BF16 or F16.  Cache: as above, cache_dtype BF16, F16 or I8
+ * (then k_scale, v_scale: device fp32 [hk]).  block_table: device int32, rows of max_pages entries table_stride apart.  lens:
+ * device int32 [B].  out: device [B, hq, d], requests out_stride apart, out_dtype F32, BF16, F16 or I8 (codes with
+ * out_inv_scale: what nm_gemm_pwl reads).  lse: device fp32 [B, hq] or NULL.
+ * q is split into as many terms of the matrix instructions' type as hold it, the weights into two (fp32 results: three), so nothing
+ * but the outputs is rounded to fewer than 16 bits.
+ * Workspace: query nm_paged_attention_workspace (it looks at the shape and the types only, never at device memory; 0: none); 256-byte
+ * aligned, contents are scratch, calls that overlap in time need one each.  A cache is split over its length by max_pages (the
+ * lengths are on the device), so a table much wider than the lengths costs launches of empty workgroups.
+ * Limits: hq % hk == 0; d a multiple of 16 up to 256; cache addresses and strides multiples of 16 bytes; page_size a power of
+ * two up to 65536; num_pages * page_size < 2^31; B * hk * groups of 16 query heads * pieces of the length < 2^24.
+ */
+typedef struct {
+    int32_t B, hq, hk, d;
+    int32_t q_dtype, cache_dtype, out_dtype;
+    int32_t page_size, num_pages, max_pages;
+    const void* q;
+    int64_t q_stride;
+    const void* k_cache;
+    const void* v_cache;
+    int64_t page_stride, slot_stride, head_stride;
+    const float* k_scale;
+    const float* v_scale;
+    const int32_t* block_table;
+    int64_t table_stride;
+    const int32_t* lens;
+    float scale;
+    int32_t window;
+    void* out;
+    int64_t out_stride;
+    float out_inv_scale;
+    float* lse;
+} nm_paged_desc;
+
+int32_t nm_paged_attention_workspace(const nm_paged_desc* desc, size_t* bytes);
+int32_t nm_paged_attention(const nm_paged_desc* desc, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

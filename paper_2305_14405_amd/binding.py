@@ -29,7 +29,7 @@ EXPORTS = ("nm_last_error", "nm_version", "nm_table_build_host", "nm_build_table
            "nm_encoder_layer_noalloc",
            "nm_encoder_stack_workspace", "nm_encoder_stack", "nm_conv2d_workspace", "nm_conv2d_pwl",
            "nm_maxpool_i8", "nm_avgpool_i8", "nm_cnn_workspace", "nm_cnn_run",
-           "nm_page_plan", "nm_qk_norm_rope")
+           "nm_page_plan", "nm_qk_norm_rope", "nm_paged_attention_workspace", "nm_paged_attention")
 NM_OP_CONV, NM_OP_MAXPOOL, NM_OP_AVGPOOL, NM_OP_GEMM = 0, 1, 2, 3
 NM_LAYER_FOLD_LAYERNORM, NM_LAYER_NO_FOLD_LAYERNORM = 1, 2
 NM_NOALLOC_MAX_WORKSPACE = 64 << 20  # bytes of the buffer built into the library (nm_encoder_layer_noalloc)
@@ -111,6 +111,15 @@ class QkDesc(C.Structure):
                 [(n, C.c_void_p) for n in ("slots", "k_inv_scale", "v_inv_scale")])
 
 
+class PagedDesc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("B", "hq", "hk", "d", "q_dtype", "cache_dtype", "out_dtype", "page_size", "num_pages", "max_pages")] +
+                [("q", C.c_void_p), ("q_stride", C.c_int64), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p)] +
+                [(n, C.c_int64) for n in ("page_stride", "slot_stride", "head_stride")] +
+                [("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("block_table", C.c_void_p), ("table_stride", C.c_int64),
+                 ("lens", C.c_void_p), ("scale", C.c_float), ("window", C.c_int32), ("out", C.c_void_p), ("out_stride", C.c_int64),
+                 ("out_inv_scale", C.c_float), ("lse", C.c_void_p)])
+
+
 _lib = None
 
 
@@ -179,6 +188,8 @@ def load(preload_torch: bool = True) -> C.CDLL:
                                    C.c_void_p, C.c_size_t, C.c_void_p]
     L.nm_page_plan.argtypes = [C.POINTER(PlanDesc), C.c_void_p]
     L.nm_qk_norm_rope.argtypes = [C.POINTER(QkDesc), C.c_void_p]
+    L.nm_paged_attention_workspace.argtypes = [C.POINTER(PagedDesc), C.POINTER(C.c_size_t)]
+    L.nm_paged_attention.argtypes = [C.POINTER(PagedDesc), C.c_void_p, C.c_size_t, C.c_void_p]
     _lib = L
     return L
 
@@ -664,3 +675,37 @@ def nm_qk_norm_rope(q, k, v, positions, inv_freq, q_out, *, k_out=None, k_cache=
         d.k_cache, d.v_cache, d.slots = k_cache.data_ptr(), v_cache.data_ptr(), _vector(slots, i32, T, "slots")
         d.k_inv_scale, d.v_inv_scale = _vector(k_inv_scale, f32, hk, "k_inv_scale"), _vector(v_inv_scale, f32, hk, "v_inv_scale")
     _check(load().nm_qk_norm_rope(C.byref(d), _stream(stream)))
+
+
+def make_paged_desc(q, k_cache, v_cache, block_table, lens, out, *, scale, window=0, k_scale=None, v_scale=None, out_inv_scale=1.0,
+                    lse=None) -> PagedDesc:
+    """q, out: [B, hq, d]; caches: [pages, page_size, hk, d] with strides; block_table: int32 [B, max_pages].  The description
+    refers to the tensors' memory: keep them."""
+    B, hq, e = q.shape
+    hk, f32 = k_cache.shape[2], NM_DT_F32
+    dtype, pages, page, strides = _cache(k_cache, v_cache, hk, e)
+    if _type(block_table, "block_table") != NM_DT_I32 or block_table.dim() != 2 or block_table.shape[0] != B or \
+            (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+        _refuse(f"block_table: int32 [{B}, max_pages] with neighbouring columns is wanted")
+    columns = block_table.shape[1]
+    qp, qs = _heads(q, B, hq, e, "q")
+    op, os_ = _heads(out, B, hq, e, "out")
+    return PagedDesc(B, hq, hk, e, _type(q, "q"), dtype, _type(out, "out"), page, pages, columns, qp, qs, k_cache.data_ptr(), v_cache.data_ptr(),
+                     strides[0], strides[1], strides[2], _vector(k_scale, f32, hk, "k_scale"), _vector(v_scale, f32, hk, "v_scale"),
+                     block_table.data_ptr(), block_table.stride(0) if B > 1 else columns, _vector(lens, NM_DT_I32, B, "lens"), scale, window,
+                     op, os_, out_inv_scale, _vector(lse, f32, B * hq, "lse"))
+
+
+def nm_paged_attention_workspace(*tensors, **more) -> int:
+    """Bytes; takes what nm_paged_attention takes, or a description."""
+    desc = tensors[0] if isinstance(tensors[0], PagedDesc) else make_paged_desc(*tensors, **more)
+    n = C.c_size_t()
+    _check(load().nm_paged_attention_workspace(C.byref(desc), C.byref(n)))
+    return n.value
+
+
+def nm_paged_attention(*tensors, ws=None, stream=None, ws_bytes=None, **more):
+    """make_paged_desc's arguments, or a description."""
+    desc = tensors[0] if isinstance(tensors[0], PagedDesc) else make_paged_desc(*tensors, **more)
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+    _check(load().nm_paged_attention(C.byref(desc), _ptr(ws), nbytes, _stream(stream)))

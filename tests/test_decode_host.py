@@ -89,6 +89,50 @@ def test_qk_norm_rope_null_and_empty(lib):
     assert lib.nm_qk_norm_rope(C.byref(d), Z) == nm.NM_OK  # nothing to do
 
 
+def paged():
+    d = nm.PagedDesc()
+    d.B, d.hq, d.hk, d.d, d.q_dtype, d.cache_dtype, d.out_dtype = 2, 8, 2, 64, nm.NM_DT_F32, nm.NM_DT_I8, nm.NM_DT_BF16
+    d.page_size, d.num_pages, d.max_pages, d.q_stride, d.out_stride, d.table_stride = 16, 100, 40, 512, 512, 40
+    for i, n in enumerate(("q", "k_cache", "v_cache", "k_scale", "v_scale", "block_table", "lens", "out", "lse")):
+        setattr(d, n, P * (i + 1))
+    d.page_stride, d.slot_stride, d.head_stride, d.scale, d.out_inv_scale = 2048, 128, 64, 0.125, 1.0
+    return d
+
+
+def attend(lib):
+    return lambda desc, stream: lib.nm_paged_attention(desc, C.c_void_p(P), 1 << 40, stream)
+
+
+@pytest.mark.parametrize("changes", [
+    dict(B=-1), dict(hq=0), dict(hk=0), dict(hq=9), dict(d=0), dict(max_pages=-1), dict(num_pages=-1), dict(window=-1), dict(q_dtype=nm.NM_DT_I8),
+    dict(cache_dtype=nm.NM_DT_F32), dict(out_dtype=nm.NM_DT_I32), dict(q_stride=511), dict(out_stride=511), dict(table_stride=39), dict(page_stride=-16),
+    dict(slot_stride=-16), dict(head_stride=-16), dict(scale=float("nan")), dict(scale=float("inf")), dict(q=None), dict(lens=None), dict(out=None),
+    dict(block_table=None), dict(k_cache=None), dict(v_cache=None), dict(k_scale=None), dict(v_scale=None)])
+def test_paged_attention_refuses(lib, changes):
+    refused(attend(lib), paged(), nm.NM_ERR_INVALID_ARG, **changes)
+
+
+@pytest.mark.parametrize("changes", [
+    dict(d=72), dict(d=272, q_stride=4000, out_stride=4000), dict(page_size=3), dict(num_pages=1 << 27), dict(max_pages=1 << 26, table_stride=1 << 26),
+    dict(k_cache=P + 8), dict(v_cache=P + 4), dict(page_stride=2056), dict(slot_stride=136), dict(head_stride=72), dict(B=1 << 23, hq=2)])
+def test_paged_attention_does_not_cover(lib, changes):
+    refused(attend(lib), paged(), nm.NM_ERR_UNSUPPORTED, **changes)
+
+
+def test_paged_attention_workspace(lib):
+    n, d = C.c_size_t(), paged()
+    assert lib.nm_paged_attention_workspace(None, C.byref(n)) == nm.NM_ERR_INVALID_ARG
+    assert lib.nm_paged_attention_workspace(C.byref(d), None) == nm.NM_ERR_INVALID_ARG
+    assert lib.nm_paged_attention_workspace(C.byref(d), C.byref(n)) == nm.NM_OK and n.value > 0
+    for ws, size in ((None, n.value), (P, n.value - 1), (P + 128, n.value)):
+        assert lib.nm_paged_attention(C.byref(d), C.c_void_p(ws), size, Z) == nm.NM_ERR_WORKSPACE
+        assert "workspace" in nm.nm_last_error()
+    d.max_pages = d.table_stride = 1
+    assert lib.nm_paged_attention_workspace(C.byref(d), C.byref(n)) == nm.NM_OK and n.value == 0   # one piece needs none
+    d.B, d.q, d.out, d.lens = 0, None, None, None
+    assert lib.nm_paged_attention(C.byref(d), None, 0, Z) == nm.NM_OK
+
+
 def test_binding_refuses_host_tensors():
     import torch
     i = torch.zeros(4, dtype=torch.int32)
@@ -98,3 +142,5 @@ def test_binding_refuses_host_tensors():
     x = torch.zeros((2, 4, 64))
     with pytest.raises(nm.NmError):
         nm.nm_qk_norm_rope(x, x, x, i, None, x)
+    with pytest.raises(nm.NmError):
+        nm.nm_paged_attention(x, x.view(2, 1, 4, 64), x.view(2, 1, 4, 64), i.view(2, 2), i[:2], x, scale=1.0)

@@ -324,3 +324,185 @@ def test_decode_binding_refuses():
                    dict(k_inv_scale=None), dict(v_inv_scale=c["inv_scale"][1][:1]), dict(slots=c["slots"].long()), dict(q_gamma=c["q_gamma"][:3])):
         with pytest.raises(nm.NmError):
             nm.nm_qk_norm_rope(*args, **{**good, **change})
+
+
+# ---- attention over the cache -----------------------------------------------------------------------
+
+def paged_case(seed, lens, hq, hk, d, q_dtype, cache_dtype, page=16, by_head=False, columns=None, extra_pages=5, size=1.0):
+    """A pool whose free slots, and pages that no request owns, hold NaN (codes: -128): what is behind a length does not matter."""
+    g = gen(seed)
+    B = len(lens)
+    held = [-(-max(n, 0) // page) for n in lens]
+    columns = max(held + [1]) if columns is None else columns
+    pages = sum(held) + extra_pages
+    shape = (2, pages, hk, page, d) if by_head else (2, pages, page, hk, d)
+    cache = torch.randn(shape, generator=g)
+    cache = (cache * 32).round().clamp(-127, 127).to(torch.int8) if cache_dtype == torch.int8 else (cache * size).to(cache_dtype)
+    cache = cache.transpose(2, 3) if by_head else cache
+    order = torch.randperm(pages, generator=g).tolist()
+    table = torch.full((B, columns), -1, dtype=torch.int32)
+    used, at = torch.zeros((pages, page), dtype=torch.bool), 0
+    for b, n in enumerate(lens):
+        for i in range(held[b]):
+            table[b, i] = order[at]
+            used[order[at], :max(0, min(page, n - i * page))] = True
+            at += 1
+    cache[:, ~used] = -128 if cache_dtype == torch.int8 else float("nan")
+    scales = 0.02 * (1 + torch.rand((2, hk), generator=g)) if cache_dtype == torch.int8 else None
+    cache = cache.to(DEV) if not by_head else cache.transpose(2, 3).contiguous().to(DEV).transpose(2, 3)
+    return dict(q=(torch.randn((B, hq, d), generator=g) * size).to(q_dtype).to(DEV), cache=cache, table=table.to(DEV), lens=i32(lens),
+                scales=None if scales is None else scales.to(DEV))
+
+
+def attend(c, out_dtype, scale, window=0, lse=True, ws=None, stream=None, out=None, out_inv_scale=1.0):
+    B, hq, d = c["q"].shape
+    out = torch.full((B, hq, d), 77, dtype=out_dtype, device=DEV) if out is None else out
+    lse = torch.full((B, hq), 77.0, device=DEV) if lse else None
+    args = (c["q"], c["cache"][0], c["cache"][1], c["table"], c["lens"], out)
+    s = (None, None) if c["scales"] is None else c["scales"]
+    more = dict(scale=scale, window=window, k_scale=s[0], v_scale=s[1], lse=lse, out_inv_scale=out_inv_scale)
+    size = nm.nm_paged_attention_workspace(*args, **more)
+    if ws is None and size:
+        ws = torch.full((size,), 0xff, dtype=torch.uint8, device=DEV)     # NaN, so that nothing unwritten is read
+    nm.nm_paged_attention(*args, ws=ws, stream=stream, **more)
+    return out, lse
+
+
+def attention_64(c, scale, window=0):
+    """(out, lse, bound of out's error, bound of lse's) in binary64, request by request.  A score is a sum of d products in
+    binary32: at most (d + 4) U of the absolute products (the matrix instruction adds 32 at a time; 4: the factor, and the scales); its
+    difference from the maximum, the exponential (2 steps of the result) and the sums add |s| 4 U, 4 U and, chain of n / 128 additions
+    a wavefront, then of pieces and wavefronts, (n / 128 + 64) U; weights in two terms of 8 bits each: 2^-16.  Everything
+    is relative to the weighted mean of |v|, twice (numerator and sum)."""
+    B, hq, d = c["q"].shape
+    _, pages, page, hk, _ = c["cache"].shape
+    out = torch.zeros((B, hq, d), dtype=torch.float64, device=DEV)
+    lse = torch.full((B, hq), -math.inf, dtype=torch.float64, device=DEV)
+    e_out, e_lse = torch.zeros_like(out), torch.zeros_like(lse)
+    top = c["table"].shape[1] * page
+    for b, n in enumerate(c["lens"].tolist()):
+        n = min(max(n, 0), top)
+        where = torch.arange(max(0, n - window) if window else 0, n, device=DEV)
+        entry = c["table"][b].long()[where // page]
+        good = (entry >= 0) & (entry < pages)
+        where, entry = where[good], entry[good]
+        if not where.numel():
+            continue
+        k, v = (c["cache"][i][entry, where % page].double() for i in (0, 1))
+        if c["scales"] is not None:
+            k, v = k * c["scales"][0].double()[:, None], v * c["scales"][1].double()[:, None]
+        k, v = (x.repeat_interleave(hq // hk, 1).transpose(0, 1) for x in (k, v))         # [hq, n, d]
+        q = c["q"][b].double()
+        s = (k * q[:, None]).sum(-1) * scale
+        size = (k.abs() * q.abs()[:, None]).sum(-1) * abs(scale)
+        w = torch.softmax(s, -1)
+        out[b], lse[b] = (w[:, :, None] * v).sum(1), torch.logsumexp(s, -1)
+        span = (s - s.amax(-1, keepdim=True)).abs()
+        err = ((d + 4) * size + 4 * span + n / 128 + 72) * U
+        mean = (w * err).sum(-1) + err[torch.arange(hq), s.argmax(-1)]
+        e_out[b] = ((w * (err + 2.0 ** -16))[:, :, None] * v.abs()).sum(1) + (mean + 2.0 ** -16)[:, None] * (w[:, :, None] * v.abs()).sum(1)
+        e_lse[b] = mean + 4 * U * lse[b].abs()
+    return out, lse, e_out, e_lse
+
+
+def check_attention(c, out_dtype, scale=None, window=0):
+    scale = c["q"].shape[2] ** -0.5 if scale is None else scale
+    out, lse = attend(c, out_dtype, scale, window)
+    torch.cuda.synchronize()
+    want, wl, e_out, e_lse = attention_64(c, scale, window)
+    assert_rounded(out, want, e_out, "out")
+    empty = wl == -math.inf
+    assert bool((lse[empty] == -math.inf).all()) and bool((out[empty] == 0).all())
+    assert bool(((lse.double() - wl)[~empty].abs() <= e_lse[~empty]).all())
+    return out, lse
+
+
+LENGTHS = [0, 1, 15, 16, 17, 31, 32, 33, 64, 127, 128, 129, 300, 1000]
+
+
+@pytest.mark.parametrize("q_dtype,cache_dtype,out_dtype", [
+    (torch.bfloat16, torch.bfloat16, torch.bfloat16), (torch.float16, torch.float16, torch.float16), (torch.float32, torch.int8, torch.float32),
+    (torch.float32, torch.bfloat16, torch.float32), (torch.bfloat16, torch.int8, torch.bfloat16), (torch.float16, torch.bfloat16, torch.float16),
+    (torch.bfloat16, torch.float16, torch.float32), (torch.float32, torch.float16, torch.bfloat16), (torch.float16, torch.int8, torch.float16)])
+@pytest.mark.parametrize("hq,hk,d", [(4, 4, 64), (8, 2, 128), (5, 1, 32), (24, 1, 96), (6, 3, 16), (16, 1, 256), (34, 2, 80)])
+def test_paged_attention(q_dtype, cache_dtype, out_dtype, hq, hk, d):
+    check_attention(paged_case(hq + d, LENGTHS, hq, hk, d, q_dtype, cache_dtype, by_head=bool(d & 32)), out_dtype)
+
+
+@pytest.mark.parametrize("page", [1, 2, 8, 32, 64, 256, 4096])
+@pytest.mark.parametrize("cache_dtype", [torch.bfloat16, torch.int8])
+def test_paged_attention_page_sizes(page, cache_dtype):
+    check_attention(paged_case(page, [100, 0, 513, 1, 260], 8, 2, 64, torch.bfloat16, cache_dtype, page=page), torch.bfloat16)
+
+
+@pytest.mark.parametrize("window", [1, 16, 31, 100, 128, 500, 5000])
+def test_paged_attention_window(window):
+    check_attention(paged_case(window, [0, 1, 90, 128, 700, 1500], 6, 2, 64, torch.float16, torch.float16), torch.float16, window=window)
+
+
+@pytest.mark.parametrize("lens,hk,columns", [([70000], 2, None), ([40000, 3, 0, 17000], 1, None), ([5, 200], 4, 3000), ([129] * 70, 8, 100)])
+def test_paged_attention_long_and_split(lens, hk, columns):
+    check_attention(paged_case(len(lens), lens, hk * 4, hk, 128, torch.bfloat16, torch.bfloat16, page=64, columns=columns), torch.bfloat16)
+
+
+def test_paged_attention_bad_tables_and_lengths():
+    """Entries that are no pages take no part, lengths beyond the table count as the table's, negative ones as none."""
+    c = paged_case(3, [100, 200, 64, 33, 50], 4, 2, 64, torch.bfloat16, torch.bfloat16, columns=13)
+    c["table"][0, 2], c["table"][0, 6], c["table"][2, :] = -5, 10 ** 6, 2 ** 31 - 1
+    c["table"][1, 3] = c["cache"].shape[1]
+    c["lens"][3], c["lens"][1] = -4, 5000
+    c["cache"] = torch.nan_to_num(c["cache"], nan=0.25)
+    out, lse = check_attention(c, torch.bfloat16)
+    assert bool((out[2:4] == 0).all()) and bool((lse[2:4] == -math.inf).all())
+
+
+def test_paged_attention_large_scores_and_sizes():
+    """Scores of thousands (one weight is 1), queries near the types' ends, and a row whose own values are infinite or NaN."""
+    c = paged_case(9, [300, 300, 300, 300], 4, 2, 64, torch.float32, torch.float16, size=30.0)
+    check_attention(c, torch.float32, scale=1.0)
+    c["q"] *= 1e30
+    check_attention(c, torch.float32, scale=1e-30)
+    c["q"] *= 1e-55
+    check_attention(c, torch.float32, scale=1e25)
+    c["cache"][0, c["table"][1, 3], 5, 0, 1] = float("inf")
+    c["cache"][1, c["table"][2, 3], 5, 1, 7] = float("nan")
+    out, _ = attend(c, torch.float32, 1e25)
+    torch.cuda.synchronize()
+    assert bool(out[0].isfinite().all()) and bool(out[3].isfinite().all()) and bool(out[1, 2:].isfinite().all())
+    assert bool(out[2, 2:, 7].isnan().all()) and bool(out[2, :2].isfinite().all()) and bool(out[2, 2:, :7].isfinite().all())
+
+
+def test_paged_attention_codes_strides_and_stream():
+    """int8 results are the codes of the fp32 ones; requests may be strided; another stream gives the same; no lse."""
+    c = paged_case(4, [77, 500, 1200], 8, 2, 64, torch.bfloat16, torch.int8)
+    f, _ = attend(c, torch.float32, 0.125)
+    codes, _ = attend(c, torch.int8, 0.125, out_inv_scale=50.0)
+    torch.cuda.synchronize()
+    assert int((codes.double() - (f.double() * 50).clamp(-127, 127)).abs().gt(0.5 + 127 * 2.0 ** -15).sum()) == 0
+    wide = torch.full((3, 12, 64), 5.0, dtype=torch.bfloat16, device=DEV)
+    qw = torch.zeros((3, 24, 64), dtype=torch.bfloat16, device=DEV)
+    qw[:, 8:16] = c["q"]
+    want, _ = attend(c, torch.bfloat16, 0.125)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    attend({**c, "q": qw[:, 8:16]}, torch.bfloat16, 0.125, lse=False, stream=s, out=wide[:, 2:10])
+    torch.cuda.synchronize()
+    assert torch.equal(wide[:, 2:10], want) and bool((wide[:, :2] == 5).all()) and bool((wide[:, 10:] == 5).all())
+
+
+def test_paged_attention_offsets_beyond_32_bits():
+    """A cache of more than 2^32 bytes (and elements): the last pages of the pool."""
+    pages, page, d = (1 << 32) // (16 * 64) + 40, 16, 64
+    cache = torch.zeros((2, pages, page, 1, d), dtype=torch.int8, device=DEV)
+    g = gen(1)
+    own = [pages - 1, 3, pages - 2, pages // 2 + 7]
+    for p in own:
+        cache[:, p] = torch.randint(-127, 128, (2, page, 1, d), generator=g, dtype=torch.int8).to(DEV)
+    c = dict(q=torch.randn((1, 4, d), generator=g).to(torch.bfloat16).to(DEV), cache=cache, table=i32([own]), lens=i32([61]), scales=torch.full((2, 1), 0.02, device=DEV))
+    check_attention(c, torch.bfloat16)
+    k, v = (torch.randn((1, 1, d), generator=g).to(DEV) for _ in range(2))
+    q_out = torch.empty((1, 1, d), device=DEV)
+    nm.nm_qk_norm_rope(k, k, v, None, None, q_out, k_cache=cache[0], v_cache=cache[1], slots=i32([(pages - 1) * page + 3]),
+                       k_inv_scale=torch.full((1,), 40.0, device=DEV), v_inv_scale=torch.full((1,), 40.0, device=DEV))
+    torch.cuda.synchronize()
+    assert torch.equal(cache[1, pages - 1, 3], (v[0] * 40).round().clamp(-127, 127).to(torch.int8))
