@@ -610,6 +610,35 @@ typedef struct {
 int32_t nm_paged_attention_workspace(const nm_paged_desc* desc, size_t* bytes);
 int32_t nm_paged_attention(const nm_paged_desc* desc, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * nm_gemv_w4: product of a few rows with 4-bit weights, the projections of a step.
+ *   acc[m,n] = sum over groups g of scales[n,g] * sum_{k in g} x[m,k] * w[n,k]      (int8 x: the inner sums are exact int32)
+ *   v = fma(acc, alpha, bias_n);  v = PWL_table(v) if table_idx >= 0;  out[m,n] = v, or its int8 code with out_inv_scale
+ * x: device [M, K], rows x_stride elements apart, x_dtype I8, BF16 or F16.  W: device [N, K / 2], contiguous: byte i of a row holds
+ * w[n, 2 i] in its low and w[n, 2 i + 1] in its high four bits, two's complement (-8 .. 7).  scales: device [N, K / group], contiguous,
+ * scale_dtype F32, BF16 or F16.  bias: device fp32 [N] or NULL.  out: device [M, N], rows out_stride apart, out_dtype F32, BF16, F16
+ * or I8.  Any M: rows are taken 64 at a time, and the weights read again for each 64 (nm_gemm_pwl is the call for many rows).
+ * Limits: group 32, 64 or a multiple of 128; K a multiple of group, at most 65536; x and W 16-byte aligned, x_stride a multiple of 16
+ * bytes; M <= 2^20, N < 2^26.
+ */
+typedef struct {
+    int32_t M, N, K, group;
+    int32_t x_dtype, scale_dtype, out_dtype;
+    const void* x;
+    int64_t x_stride;
+    const uint8_t* W;
+    const void* scales;
+    float alpha;
+    const float* bias;
+    const nm_tables* tables;
+    int32_t table_idx; /* -1 = no nonlinearity */
+    void* out;
+    int64_t out_stride;
+    float out_inv_scale;
+} nm_w4_desc;
+
+int32_t nm_gemv_w4(const nm_w4_desc* desc, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,7 +29,8 @@ EXPORTS = ("nm_last_error", "nm_version", "nm_table_build_host", "nm_build_table
            "nm_encoder_layer_noalloc",
            "nm_encoder_stack_workspace", "nm_encoder_stack", "nm_conv2d_workspace", "nm_conv2d_pwl",
            "nm_maxpool_i8", "nm_avgpool_i8", "nm_cnn_workspace", "nm_cnn_run",
-           "nm_page_plan", "nm_qk_norm_rope", "nm_paged_attention_workspace", "nm_paged_attention")
+           "nm_page_plan", "nm_qk_norm_rope", "nm_paged_attention_workspace", "nm_paged_attention",
+           "nm_gemv_w4")
 NM_OP_CONV, NM_OP_MAXPOOL, NM_OP_AVGPOOL, NM_OP_GEMM = 0, 1, 2, 3
 NM_LAYER_FOLD_LAYERNORM, NM_LAYER_NO_FOLD_LAYERNORM = 1, 2
 NM_NOALLOC_MAX_WORKSPACE = 64 << 20  # bytes of the buffer built into the library (nm_encoder_layer_noalloc)
@@ -120,6 +121,13 @@ class PagedDesc(C.Structure):
                  ("out_inv_scale", C.c_float), ("lse", C.c_void_p)])
 
 
+class W4Desc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("M", "N", "K", "group", "x_dtype", "scale_dtype", "out_dtype")] +
+                [("x", C.c_void_p), ("x_stride", C.c_int64), ("W", C.c_void_p), ("scales", C.c_void_p), ("alpha", C.c_float),
+                 ("bias", C.c_void_p), ("tables", C.c_void_p), ("table_idx", C.c_int32), ("out", C.c_void_p), ("out_stride", C.c_int64),
+                 ("out_inv_scale", C.c_float)])
+
+
 _lib = None
 
 
@@ -190,6 +198,7 @@ def load(preload_torch: bool = True) -> C.CDLL:
     L.nm_qk_norm_rope.argtypes = [C.POINTER(QkDesc), C.c_void_p]
     L.nm_paged_attention_workspace.argtypes = [C.POINTER(PagedDesc), C.POINTER(C.c_size_t)]
     L.nm_paged_attention.argtypes = [C.POINTER(PagedDesc), C.c_void_p, C.c_size_t, C.c_void_p]
+    L.nm_gemv_w4.argtypes = [C.POINTER(W4Desc), C.c_void_p]
     _lib = L
     return L
 
@@ -709,3 +718,18 @@ def nm_paged_attention(*tensors, ws=None, stream=None, ws_bytes=None, **more):
     desc = tensors[0] if isinstance(tensors[0], PagedDesc) else make_paged_desc(*tensors, **more)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
     _check(load().nm_paged_attention(C.byref(desc), _ptr(ws), nbytes, _stream(stream)))
+
+
+def nm_gemv_w4(x, W, scales, out, *, group, alpha=1.0, bias=None, tables: Tables | None = None, table_idx=-1, out_inv_scale=1.0, stream=None):
+    """x: [M, K], out: [M, N], rows may be apart; W: uint8 [N, K / 2]; scales: [N, K / group], both contiguous."""
+    (M, K), N = x.shape, W.shape[0]
+    if _type(W, "W") is not None or tuple(W.shape) != (N, K // 2) or not W.is_contiguous() or K % 2:
+        _refuse(f"W: contiguous uint8 [N, {K // 2}] is wanted, got {tuple(W.shape)} of {W.dtype}")
+    if group < 1 or K % group or tuple(scales.shape) != (N, K // group) or not scales.is_contiguous():
+        _refuse(f"scales: contiguous [{N}, {K} / group] is wanted, got {tuple(scales.shape)}, group {group}")
+    if tuple(out.shape) != (M, N) or (out.stride(1) != 1 and N > 1) or (x.stride(1) != 1 and K > 1):
+        _refuse(f"x and out: rows of neighbouring elements are wanted, out of shape {(M, N)}, got {tuple(out.shape)}")
+    d = W4Desc(M, N, K, group, _type(x, "x"), _type(scales, "scales"), _type(out, "out"), x.data_ptr(), x.stride(0) if M > 1 else K, W.data_ptr(),
+               scales.data_ptr(), alpha, _vector(bias, NM_DT_F32, N, "bias"), tables.handle if tables is not None else None, table_idx,
+               out.data_ptr(), out.stride(0) if M > 1 else N, out_inv_scale)
+    _check(load().nm_gemv_w4(C.byref(d), _stream(stream)))

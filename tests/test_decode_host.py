@@ -133,6 +133,35 @@ def test_paged_attention_workspace(lib):
     assert lib.nm_paged_attention(C.byref(d), None, 0, Z) == nm.NM_OK
 
 
+def w4():
+    d = nm.W4Desc()
+    d.M, d.N, d.K, d.group, d.x_dtype, d.scale_dtype, d.out_dtype = 3, 20, 256, 64, nm.NM_DT_BF16, nm.NM_DT_F32, nm.NM_DT_I8
+    d.x, d.W, d.scales, d.bias, d.out = P, 2 * P, 3 * P, 4 * P, 5 * P
+    d.x_stride, d.out_stride, d.alpha, d.table_idx, d.out_inv_scale = 256, 20, 1.0, -1, 1.0
+    return d
+
+
+@pytest.mark.parametrize("changes", [
+    dict(M=-1), dict(N=0), dict(K=0), dict(group=0), dict(group=-64), dict(x_dtype=nm.NM_DT_F32), dict(scale_dtype=nm.NM_DT_I8), dict(out_dtype=nm.NM_DT_I32),
+    dict(K=288), dict(group=128, K=192), dict(x_stride=255), dict(out_stride=19), dict(alpha=float("nan")), dict(alpha=float("inf")), dict(table_idx=0),
+    dict(x=None), dict(W=None), dict(scales=None), dict(out=None)])
+def test_gemv_w4_refuses(lib, changes):
+    refused(lib.nm_gemv_w4, w4(), nm.NM_ERR_INVALID_ARG, **changes)
+
+
+@pytest.mark.parametrize("changes", [dict(group=16), dict(group=96, K=192), dict(K=65536 + 64, x_stride=1 << 17), dict(M=(1 << 20) + 1), dict(N=1 << 26, out_stride=1 << 26),
+                                     dict(x=P + 8), dict(W=P + 8), dict(x_stride=260)])
+def test_gemv_w4_does_not_cover(lib, changes):
+    refused(lib.nm_gemv_w4, w4(), nm.NM_ERR_UNSUPPORTED, **changes)
+
+
+def test_gemv_w4_null_and_empty(lib):
+    assert lib.nm_gemv_w4(None, Z) == nm.NM_ERR_INVALID_ARG
+    d = w4()
+    d.M, d.x, d.out = 0, None, None
+    assert lib.nm_gemv_w4(C.byref(d), Z) == nm.NM_OK
+
+
 def test_binding_refuses_host_tensors():
     import torch
     i = torch.zeros(4, dtype=torch.int32)

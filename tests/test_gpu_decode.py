@@ -506,3 +506,116 @@ def test_paged_attention_offsets_beyond_32_bits():
                        k_inv_scale=torch.full((1,), 40.0, device=DEV), v_inv_scale=torch.full((1,), 40.0, device=DEV))
     torch.cuda.synchronize()
     assert torch.equal(cache[1, pages - 1, 3], (v[0] * 40).round().clamp(-127, 127).to(torch.int8))
+
+
+# ---- products with 4-bit weights ----------------------------------------------------------------------
+
+def w4_case(seed, M, N, K, group, x_dtype, scale_dtype, pad=0):
+    g = gen(seed)
+    x = torch.randn((M, K + pad), generator=g)
+    x = (x * 32).round().clamp(-128, 127).to(torch.int8) if x_dtype == torch.int8 else x.to(x_dtype)
+    w = torch.randint(-8, 8, (N, K), generator=g)
+    packed = ((w[:, 0::2] & 15) | ((w[:, 1::2] & 15) << 4)).to(torch.uint8)
+    scales = (0.02 * (0.5 + torch.rand((N, K // group), generator=g))).to(scale_dtype)
+    return dict(x=x.to(DEV)[:, :K], w=w.to(DEV), W=packed.to(DEV), scales=scales.to(DEV), group=group,
+                bias=torch.randn(N, generator=g).to(DEV), alpha=0.03 if x_dtype == torch.int8 else 0.7)
+
+
+def product_64(c, bias=True):
+    """(result, bound of the 32-bit evaluation's error).  int8: sums within 128 weights are exact, then at most K / 1024 + 8 additions and 3 more
+    roundings: (K / 1024 + 11) U of sum |x w| s.  bf16, fp16: within 128 weights eight matrix instructions of weights (at most 31) and
+    offsets (24) add, each a tree of five levels and the accumulator, 48 roundings, 96 where they truncate: 96 U of sum |x| 55 s more."""
+    s = c["scales"].double().repeat_interleave(c["group"], 1)
+    w, x, a = c["w"].double() * s, c["x"].double(), c["alpha"]
+    K = x.shape[1]
+    y = x @ w.t().contiguous() * a + (c["bias"].double() if bias else 0)
+    e = (K / 1024 + 11) * U * (x.abs() @ w.abs().t().contiguous()) * abs(a) + 2 * U * (y.abs() + (c["bias"].double().abs() if bias else 0))
+    if c["x"].dtype != torch.int8:
+        e = e + 96 * 55 * U * (x.abs() @ s.t().contiguous()) * abs(a)
+    return y, e
+
+
+def check_w4(c, out_dtype, bias=True):
+    M, N = c["x"].shape[0], c["W"].shape[0]
+    wide = torch.full((M, N + 3), 55.0, dtype=out_dtype, device=DEV)
+    nm.nm_gemv_w4(c["x"], c["W"], c["scales"], wide[:, :N], group=c["group"], alpha=c["alpha"], bias=c["bias"] if bias else None)
+    torch.cuda.synchronize()
+    want, error = product_64(c, bias)
+    assert_rounded(wide[:, :N], want, error, "product")
+    assert bool((wide[:, N:] == 55).all())
+    return wide[:, :N]
+
+
+@pytest.mark.parametrize("x_dtype,scale_dtype,out_dtype", [(torch.int8, torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16, torch.bfloat16),
+                                                           (torch.float16, torch.float16, torch.float16), (torch.bfloat16, torch.float32, torch.float32),
+                                                           (torch.int8, torch.float16, torch.bfloat16)])
+@pytest.mark.parametrize("M,N,K,group", [(1, 1, 32, 32), (1, 16, 128, 128), (2, 17, 160, 32), (3, 100, 192, 64), (7, 33, 1024, 256), (1, 768, 768, 128),
+                                         (16, 40, 4096, 64), (17, 50, 2048, 512), (33, 31, 1120, 32), (64, 130, 896, 128), (65, 20, 384, 384),
+                                         (1, 5, 65536, 128), (200, 9, 320, 64)])
+def test_gemv_w4(x_dtype, scale_dtype, out_dtype, M, N, K, group):
+    check_w4(w4_case(M + K, M, N, K, group, x_dtype, scale_dtype), out_dtype, bias=N % 2 == 0)
+
+
+@pytest.mark.parametrize("x_dtype", [torch.int8, torch.bfloat16, torch.float16])
+def test_gemv_w4_every_weight_in_every_place(x_dtype):
+    """Rows of x with a single one read one weight each: exact, so every place of a word and every one of the 16 weights is seen."""
+    K = 256
+    c = w4_case(3, 64, 48, K, 32, x_dtype, torch.float32)
+    c["scales"].fill_(1.0)
+    got = torch.empty((64, 48), device=DEV)
+    for first in range(0, K, 64):
+        x = torch.zeros((64, K), dtype=x_dtype, device=DEV)
+        x[torch.arange(64), first + torch.arange(64)] = 1
+        nm.nm_gemv_w4(x, c["W"], c["scales"], got, group=32)
+        torch.cuda.synchronize()
+        assert torch.equal(got, c["w"][:, first:first + 64].t().float())
+
+
+def test_gemv_w4_strides_stream_and_codes():
+    c = w4_case(5, 9, 70, 512, 64, torch.int8, torch.float32, pad=16)
+    y = check_w4(c, torch.float32)
+    codes = torch.empty((9, 70), dtype=torch.int8, device=DEV)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    nm.nm_gemv_w4(c["x"], c["W"], c["scales"], codes, group=64, alpha=c["alpha"], bias=c["bias"], out_inv_scale=20.0, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(codes, (y * 20.0).clamp(-127, 127).round().to(torch.int8))
+
+
+@pytest.mark.parametrize("spec", [("gelu", -8.0, 8.0, 64, 0), ("relu", -8.0, 8.0, 2, 0), ("gelu", -4.0, 4.0, 1000, nm.NM_TABLE_CLAMP_INPUT),
+                                  ("exp", -8.0, 0.0, 64, nm.NM_TABLE_MERGE | nm.NM_TABLE_COMPACT, 0.0, 0.05)])
+def test_gemv_w4_table(spec):
+    """The table of the result: the same values as nm_pwl_apply of the product without it."""
+    c = w4_case(8, 5, 90, 256, 128, torch.int8, torch.float32)
+    tables = nm.nm_build_tables([spec])
+    y, z, want = (torch.empty((5, 90), device=DEV) for _ in range(3))
+    args = dict(group=128, alpha=c["alpha"], bias=c["bias"])
+    nm.nm_gemv_w4(c["x"], c["W"], c["scales"], y, **args)
+    nm.nm_gemv_w4(c["x"], c["W"], c["scales"], z, tables=tables, table_idx=0, **args)
+    nm.nm_pwl_apply(y, 1.0, tables, 0, 1.0, out_f32=want)
+    torch.cuda.synchronize()
+    assert torch.equal(z, want)
+
+
+def test_gemv_w4_infinities_stay_in_their_rows():
+    c = w4_case(6, 20, 33, 256, 64, torch.bfloat16, torch.float32)
+    want, _ = product_64(c)
+    clean = check_w4(c, torch.float32).clone()
+    c["x"][4, 100], c["x"][17, 3] = float("inf"), float("nan")
+    got = torch.empty((20, 33), device=DEV)
+    nm.nm_gemv_w4(c["x"], c["W"], c["scales"], got, group=64, alpha=c["alpha"], bias=c["bias"])
+    torch.cuda.synchronize()
+    rest = [m for m in range(20) if m not in (4, 17)]
+    assert torch.equal(got[rest], clean[rest]) and not bool(got[[4, 17]].isfinite().any())
+
+
+def test_gemv_w4_binding_refuses():
+    c = w4_case(1, 2, 16, 128, 64, torch.bfloat16, torch.float32)
+    out = torch.empty((2, 16), device=DEV)
+    good = [c["x"], c["W"], c["scales"], out]
+    for at, bad, group in ((0, c["x"].double(), 64), (0, c["x"].cpu(), 64), (1, c["W"].to(torch.int8), 64), (1, c["W"][:, :32], 64), (2, c["scales"][:, :1], 64),
+                           (2, c["scales"].t().contiguous().t(), 64), (3, out[:, :15], 64), (3, out.t(), 64), (0, c["x"], 48), (0, c["x"], 0), (0, c["x"], 32)):
+        changed = list(good)
+        changed[at] = bad
+        with pytest.raises(nm.NmError):
+            nm.nm_gemv_w4(*changed, group=group)
