@@ -1,356 +1,562 @@
 // Attention of one new token per request over a paged cache (nm_paged_attention).
 //
-// Bound by memory: every key and value is read once, with 4 * (query heads of its group) operations an element.  A workgroup has one
-// request's key head, up to 16 query heads of its group, and a piece of the length; its four wavefronts walk that piece's tiles of 32
-// positions in turn, each with a running maximum, sum and output of its own, and are joined at the end through LDS; pieces are joined
-// by a second kernel.  One tile's keys and values are on their way into registers while the one before is computed.
+// Bound by memory: every key and value is read once, with 4 * (query heads of its group) operations an element.  A row of work is one
+// request's key head with up to 16 query heads of its group; its length is counted in units of 128 positions.  A fixed number of
+// workgroups share all rows' units evenly, each a contiguous run of them, whatever the lengths are: a run may begin and end inside a
+// row, and only those two pieces of it need joining by a second kernel; rows inside a run are written at once.  (Where no row can be long,
+// a workgroup takes a row and there is no second kernel.)  The four wavefronts of a workgroup walk a unit's four tiles of 32
+// positions, each with a running maximum, sum and output of its own, and are joined through LDS at the end of the row's piece.
+// The next tile's keys and values are on their way into registers while one is computed.
 //   Scores: keys are the rows of the 16x16x32 matrix instruction, query heads its columns, so a lane has eight positions of one head:
 // its maximum and sum are in-lane steps and two across lanes.  Those registers are already the second product's operand: the contraction
 // index of a matrix instruction may be permuted, so "row 4 j + i of the first, then of the second 16 keys" is what lane group j contributes, and
 // the values are fetched from LDS in that order by the transposing read.  Output: columns are heads again, so the rescaling factor
 // is in the lane that needs it.
 //   Precision: scores and sums fp32; exp(s - m) goes into the second product as two terms of 16 bits (2^-17 of itself, below what a 16-bit result
-// shows; three terms where the result is fp32), queries that are no 16-bit numbers of the cache's type as three terms of theirs, scaled by a power of two
-// so that nothing overflows.  The matrix cores have 20 times the time this needs.
+// shows; three terms where the result is fp32), queries that are no 16-bit numbers of the matrix instructions' type as three terms of it, scaled by a
+// power of two so that nothing overflows.  int8 codes are exact in either 16-bit type.
+#include <algorithm>
+
 #include "nm_decode.h"
 
 namespace nm {
 
 typedef bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef f16 v8h __attribute__((ext_vector_type(8)));
+typedef f16 v2h __attribute__((ext_vector_type(2)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
 constexpr int kPagedWaves = 4, kPagedThreads = 64 * kPagedWaves;
 constexpr int kTile = 32;                       // positions a wavefront takes at once
-constexpr int kRound = kTile * kPagedWaves;     // and a workgroup
+constexpr int kUnit = kTile * kPagedWaves;      // and a workgroup
+// Workgroups of the kernel for heads of up to dp elements that a CU has registers for (a wavefront on each SIMD each).
+constexpr int workgroups_of(int dp) { return dp <= 64 ? 3 : dp <= 128 ? 2 : 1; }
 
 struct PagedArgs {
     nm_paged_desc d;
     int shift;            // log2 of page_size
     int group;            // query heads of a key head
     int groups;           // of up to 16 of them
-    int piece;            // positions of a piece of the length
-    int pieces;           // of the longest there can be
-    float* part_o;        // [B, hq, pieces, d] not yet divided by the sum; null where there is one piece
-    float2* part_ml;      // [B, hq, pieces]: maximum (of scores in units of log 2) and sum
+    int share;            // rows that read the same lines of the cache: a team of so many workgroups of one XCD takes them side by side
+    int workers;          // teams that share the units; 0: one team to a set of rows
+    int extra;            // units that starting and ending a row costs
+    float* part_o;        // [share, workers, 2, 16, d]: a run's first and last piece, not yet divided by the sum
+    float2* part_ml;      // [share, workers, 2, 16]: maximum (of scores in units of log 2) and sum
+    int4* joined;         // [share, workers]: the row that begins in a run and ends in another: request, first query head, the run's slot for
+                          // it, and how many runs have some of it (0: there is no such row)
 };
 
-template <typename C> struct Mfma;
-template <> struct Mfma<bf16> {
-    typedef bf16 T;
+// Number of a piece's first query head in part_o and part_ml.
+__device__ __forceinline__ long part_of(const PagedArgs& a, int member, long worker, int slot) { return (((long)member * a.workers + worker) * 2 + slot) * 16; }
+
+// The positions of request b that take part are [low, n).
+struct Span { int low, n; };
+__device__ __forceinline__ Span span_of(const PagedArgs& a, int b)
+{
+    const int n = (int)min((long)max(a.d.lens[b], 0), (long)a.d.max_pages << a.shift);
+    return Span{a.d.window ? max(n - a.d.window, 0) : 0, n};
+}
+__device__ __forceinline__ int units_of(const PagedArgs& a, int b)
+{
+    const Span s = span_of(a, b);
+    return (s.n - s.low + kUnit - 1) / kUnit;
+}
+
+// What one of a request's rows counts for when the work is shared: starting and ending a row costs a workgroup about as much as a.extra units.
+__device__ __forceinline__ int cost_of(const PagedArgs& a, int b) { return units_of(a, b) + a.extra; }
+
+// How a total cost is divided: worker w has [begin(w), begin(w + 1)), the first `more` workers one more than `each`.
+struct Shares {
+    long each, more;
+    __device__ __forceinline__ Shares(long all, long workers) : each(all / workers), more(all % workers) {}
+    __device__ __forceinline__ Shares(long e, long m, int) : each(e), more(m) {}
+    __device__ __forceinline__ long begin(long w) const { return each * w + min(w, more); }
+    __device__ __forceinline__ long owner(long x) const
+    {
+        const long longer = (each + 1) * more;
+        return x < longer ? x / (each + 1) : more + (x - longer) / each;
+    }
+};
+
+// The cost of one of a request's rows, summed over the requests in front of each thread's run of them, and over all.  s: LDS of one number a wavefront.
+struct Scan { long before, mine, all; int b0, b1; };
+__device__ __forceinline__ Scan scan_units(const PagedArgs& a, long* s)
+{
+    const int per = (a.d.B + kPagedThreads - 1) / kPagedThreads, tid = threadIdx.x;
+    Scan r;
+    r.b0 = min(tid * per, a.d.B);
+    r.b1 = min(r.b0 + per, a.d.B);
+    r.mine = 0;
+    for (int b = r.b0; b < r.b1; ++b) r.mine += cost_of(a, b);
+    long in = r.mine;
+    for (int step = 1; step < 64; step <<= 1) {
+        const long t = __shfl_up(in, step);
+        if ((tid & 63) >= step) in += t;
+    }
+    if ((tid & 63) == 63) s[tid >> 6] = in;
+    __syncthreads();
+    r.before = in - r.mine;
+    r.all = 0;
+    for (int w = 0; w < kPagedWaves; ++w) {
+        if (w < tid >> 6) r.before += s[w];
+        r.all += s[w];
+    }
+    return r;
+}
+
+// What a workgroup has of a row: positions [k0, k1) of request b for key head g and query heads h0 .. h0 + heads - 1; slot: where its part goes,
+// -1 where it is the whole row.  b: -1 for none.
+struct Piece { int b, g, h0, heads, k0, k1, slot; };
+
+template <typename T> struct Mma;
+template <> struct Mma<bf16> {
     static __device__ __forceinline__ v4f mma(v8s a, v8s b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0); }
 };
-template <> struct Mfma<f16> {
-    typedef f16 T;
+template <> struct Mma<f16> {
     static __device__ __forceinline__ v4f mma(v8s a, v8s b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0); }
 };
-template <> struct Mfma<int8_t> : Mfma<bf16> {};   // codes are exact in bf16
 
 // 16 bytes of a cache row as elements of the matrix instructions' type, to LDS.
-template <typename C>
+template <typename C, typename T>
 __device__ __forceinline__ void put(short* to, v4u w)
 {
-    *reinterpret_cast<v4u*>(to) = w;
-}
-template <>
-__device__ __forceinline__ void put<int8_t>(short* to, v4u w)
-{
+    if constexpr (sizeof(C) == 2) {
+        *reinterpret_cast<v4u*>(to) = w;
+    } else {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        v4u o;
+        for (int half = 0; half < 2; ++half) {
+            v4u o;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const unsigned x = w[half * 2 + i / 2] >> (i % 2 * 16);
-            const unsigned a = __float_as_uint((float)(int8_t)x), b = __float_as_uint((float)(int8_t)(x >> 8));
-            o[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);   // the upper halves: small integers have no bits below
+            for (int i = 0; i < 4; ++i) {
+                const unsigned x = w[half * 2 + i / 2];
+                if constexpr (std::is_same<T, f16>::value) {
+                    // 1024 + (code + 128) is exact under fp16's exponent of 1024, and so is the difference
+                    const unsigned u = __builtin_amdgcn_perm(0x64646464u, x ^ 0x80808080u, i % 2 ? 0x04030402u : 0x04010400u);
+                    o[i] = __builtin_bit_cast(unsigned, (v2h)(__builtin_bit_cast(v2h, u) - v2h{(f16)1152.0f, (f16)1152.0f}));
+                } else {
+                    const unsigned y = x >> (i % 2 * 16);
+                    const unsigned a = __float_as_uint((float)(int8_t)y), b = __float_as_uint((float)(int8_t)(y >> 8));
+                    o[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);   // the upper halves: small integers have no bits below
+                }
+            }
+            *reinterpret_cast<v4u*>(to + half * 8) = o;
         }
-        *reinterpret_cast<v4u*>(to + half * 8) = o;
     }
 }
 
-// C: type of the cache; DP: d rounded up to 64, 128 or 256; kTerms: of the weights (2 or 3); of a query (1 or 3).
-template <typename C, int DP, int kQ, int kP>
-__global__ __launch_bounds__(kPagedThreads) void paged_attention_kernel(PagedArgs a)
+// Lane number I of a lane's row: of 16 lanes where there are eight loads or more, else of four.
+template <int kLoads, int I>
+__device__ __forceinline__ unsigned row_lane(unsigned v)
 {
-    typedef typename Mfma<C>::T T;
+    return __builtin_amdgcn_update_dpp(0, v, kLoads >= 8 ? 0x150 + I : I * 0x55, 0xf, 0xf, false);
+}
+template <int kLoads, int... I>
+__device__ __forceinline__ void fetch_rows(const char* base, unsigned place, v4u (&to)[kLoads], std::integer_sequence<int, I...>)
+{
+    ((to[I] = *reinterpret_cast<const v4u*>(base + (unsigned long)row_lane<kLoads, I>(place) * 16)), ...);
+}
+
+// C: type of the cache; T: of the matrix instructions; DP: d rounded up to 64, 128 or 256; kQ: terms of a query (1 or 3); kP: of the weights
+// (2 or 3).
+template <typename C, typename T, int DP, int kQ, int kP>
+__global__ __launch_bounds__(kPagedThreads, workgroups_of(DP)) void paged_attention_kernel(PagedArgs a)
+{
     constexpr int kRowPieces = DP * (int)sizeof(C) / 16;      // 16-byte pieces of a row: lanes to a row
+    constexpr int kPer16 = 16 / (int)sizeof(C);               // elements of one
     constexpr int kRowsAtOnce = 64 / kRowPieces, kLoads = kTile / kRowsAtOnce;
     constexpr int kStride = DP + 8;                           // elements between rows in LDS
     constexpr int kSteps = DP / 32, kBlocks = DP / 16;
-    constexpr float kLift = std::is_same<C, f16>::value ? 10.0f : 0.0f;   // fp16 weights are held times 2^10, where small ones have more bits
+    constexpr float kLift = std::is_same<T, f16>::value ? 10.0f : 0.0f;   // fp16 weights are held times 2^10, where small ones have more bits
     __shared__ __attribute__((aligned(16))) union {
         short tile[kPagedWaves][kTile * kStride];
         float o[kPagedWaves][16][DP];
     } s;
     __shared__ __attribute__((aligned(16))) short s_q[kQ][16 * kStride];
     __shared__ float s_qscale[16], s_m[kPagedWaves][16], s_l[kPagedWaves][16];
+    __shared__ long s_scan[kPagedWaves], s_before;
+    __shared__ int s_b;
 
     const nm_paged_desc& d = a.d;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int id = blockIdx.x;
-    const int sub = id % a.groups; id /= a.groups;
-    const int g = id % d.hk; id /= d.hk;
-    const int b = id % d.B, piece = id / d.B;
+    const int column = lane & 15, j = lane >> 4;              // head (and row of an operand), lane group
+    const int row_piece = lane % kRowPieces, row_first = lane / kRowPieces;
+    const bool in_row = row_piece * kPer16 < d.d;
+    // Position in a tile of a group of lanes' i-th row: the lanes of a row have the places of their rows between them, and two groups that
+    // share a line of 128 bytes (rows of 64) have neighbouring rows at a time.
+    constexpr bool kPairs = kRowPieces == 4;
+    auto position_of = [](int group, int i) { return kPairs ? (group >> 1) * 2 * kLoads + 2 * i + (group & 1) : group * kLoads + i; };
+    const int my_position = position_of(row_first, lane % kLoads);
+    short* tile = s.tile[wave];
+    const int rows = d.hk * a.groups / a.share;               // sets of rows of a request
+    // workgroup i runs on XCD i mod 8: a team's members are neighbours there
+    const int member = blockIdx.x / 8 % a.share, worker = blockIdx.x / 8 / a.share * 8 + blockIdx.x % 8;
 
-    const long most = (long)d.max_pages << a.shift;
-    const int n = (int)min((long)max(d.lens[b], 0), most);
-    const int low = d.window ? max(n - d.window, 0) : 0;
-    const int k0 = low + piece * a.piece, k1 = min(k0 + a.piece, n);   // piece * a.piece < pieces * a.piece < 2^31
-    const int h0 = g * a.group + sub * 16, heads = min(a.group - sub * 16, 16);
-    if (k0 >= k1 && !(piece == 0 && !a.part_ml)) return;               // nothing here, and the joining kernel knows it
+    // this workgroup's units [u, u1); before: the units of the requests in front of b
+    int b;
+    long u, u1, first, before, each = 0, longer = 0;
+    int4 joined = make_int4(0, 0, 0, 0);
+    if (a.workers) {
+        const Scan scan = scan_units(a, s_scan);
+        const long all = scan.all * rows;
+        const Shares shares(all, a.workers);
+        first = u = shares.begin(worker);
+        u1 = shares.begin(worker + 1);
+        if (worker >= a.workers || u >= u1) {
+            if (worker < a.workers && tid == 0) a.joined[member * a.workers + worker] = make_int4(0, 0, 0, 0);
+            return;
+        }
+        each = shares.each;
+        longer = shares.more;
+        if (scan.before * rows <= u && u < (scan.before + scan.mine) * rows) {
+            int at = scan.b0;
+            long front = scan.before;
+            for (long n; front * rows + (n = cost_of(a, at)) * rows <= u; front += n) ++at;
+            s_b = at;
+            s_before = front * rows;
+        }
+        __syncthreads();
+        b = __builtin_amdgcn_readfirstlane(s_b);
+        before = s_before;
+    } else {
+        b = worker / rows;
+        if (b >= d.B) return;
+        before = 0;
+        u = first = worker % rows;                            // a row of no positions is written too
+        u1 = u + 1;
+    }
 
-    // queries: 16 rows (zeros behind the group's), 16 lanes each
-    {
-        const int row = tid >> 4, c0 = tid & 15;
-        float x[DP / 16], top = 0.0f;
+    // The next piece of a row in this workgroup's run.
+    auto advance = [&]() -> Piece {
+        while (u < u1) {
+            const Span span = span_of(a, b);
+            const int units = (span.n - span.low + kUnit - 1) / kUnit, cost = a.workers ? units + a.extra : 1;
+            if (u >= before + (long)cost * rows) {            // the next request
+                before += (long)cost * rows;
+                ++b;
+                continue;
+            }
+            const int r = (int)((u - before) / cost);
+            const long begin = before + (long)r * cost, end = min(u1, begin + cost);
+            // a row's cost comes first, then its units
+            const int from = a.workers ? max((int)(u - begin) - a.extra, 0) : 0, to = a.workers ? max((int)(end - begin) - a.extra, 0) : units;
+            const bool starts = u == begin;
+            u = end;
+            if (units ? to == 0 : !starts) continue;          // another workgroup has what there is of it
+            Piece n;
+            n.b = b;
+            // requests begin with different heads, so that workgroups in step with one another do not read the same part of every page
+            const int row = (r + b) % rows * a.share + member;
+            n.g = row / a.groups;
+            n.h0 = n.g * a.group + row % a.groups * 16;
+            n.heads = min((n.g + 1) * a.group - n.h0, 16);
+            n.k0 = span.low + from * kUnit;
+            n.k1 = (int)min((long)span.low + (long)to * kUnit, (long)span.n);
+            n.slot = from == 0 && to == units ? -1 : begin > first;
+            if (from == 0 && to < units) joined = make_int4(b, n.h0, n.slot, (int)(Shares(each, longer, 0).owner(begin + a.extra + units - 1) - worker) + 1);
+            return n;
+        }
+        return Piece{-1, 0, 0, 0, 0, 0, -1};
+    };
+    // A tile's places: a lane has one position's distance into the cache in 16 bytes, 0 where it takes no part.  Loads are not
+    // conditional (a branch around one would wait for those before it): a lane of no part reads the first page, and zeros are put
+    // in the place of what it read.
+    auto entry_of = [&](const Piece& n, int t0) {
+        const int* table = d.max_pages && n.b >= 0 ? d.block_table + n.b * d.table_stride : reinterpret_cast<const int*>(g_zero_line);
+        return table[n.k1 > 0 && n.b >= 0 ? min(t0 + my_position, n.k1 - 1) >> a.shift : 0];
+    };
+    auto place_of = [&](const Piece& n, int t0, int entry, unsigned long& valid) -> unsigned {
+        const int k = t0 + my_position;
+        const bool ok = k < n.k1 && entry >= 0 && entry < d.num_pages;
+        valid = __ballot(ok);
+        return ok ? (unsigned)(((long)entry * d.page_stride + (long)(k & (d.page_size - 1)) * d.slot_stride) / kPer16) : 0u;
+    };
+    const int lane_bytes = in_row ? row_piece * 16 : 0;
+    auto fetch = [&](const void* cache, const Piece& n, unsigned place, v4u (&to)[kLoads]) {
+        const char* base = d.num_pages ? static_cast<const char*>(cache) + (long)n.g * d.head_stride * sizeof(C) + lane_bytes : reinterpret_cast<const char*>(g_zero_line);
+        fetch_rows<kLoads>(base, place, to, std::make_integer_sequence<int, kLoads>{});
+        __builtin_amdgcn_sched_barrier(0);                    // the order of the loads is what is waited for
+    };
+    auto stage = [&](const v4u (&from)[kLoads], unsigned long valid) {
+        constexpr int kStep = (kPairs ? 2 : 1) * kStride;
+        short* to = tile + position_of(row_first, 0) * kStride + row_piece * kPer16;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) put<C, T>(to + i * kStep, from[i]);
+        if (valid != ~0ul || d.d != DP) {
+#pragma unroll 1
+            for (int i = 0; i < kLoads; ++i)
+                if (!in_row || !(valid >> (lane - row_piece + i) & 1)) {
+#pragma unroll
+                    for (int e = 0; e < kPer16; e += 8) *reinterpret_cast<v4u*>(to + i * kStep + e) = v4u{};
+                }
+        }
+    };
+    // whether the lane's score number i, of position i / 4 * 16 + j * 4 + i % 4, takes part
+    auto scored = [&](int i, unsigned long valid) {
+        const int at = i / 4 * 16 + j * 4 + i % 4;
+        const int group = kPairs ? at / (2 * kLoads) * 2 + (at & 1) : at / kLoads, nth = kPairs ? at % (2 * kLoads) / 2 : at % kLoads;
+        return valid >> (group * kRowPieces + nth) & 1;
+    };
+
+    // Queries of a piece: 16 rows (zeros behind the group's), 16 lanes each.
+    const int qrow = tid >> 4, qc = tid & 15;
+    float x[DP / 16];
+    auto fetch_queries = [&](const Piece& n) {
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) {
-            const int c = c0 + 16 * i;
-            const long at = b * d.q_stride + (long)(h0 + row) * d.d + c;
-            const bool there = row < heads && c < d.d;
+            const int c = qc + 16 * i;
+            const long at = n.b * d.q_stride + (long)(n.h0 + qrow) * d.d + c;
+            const bool there = n.b >= 0 && qrow < n.heads && c < d.d;
             x[i] = !there ? 0.0f : d.q_dtype == NM_DT_F32 ? static_cast<const float*>(d.q)[at] : d.q_dtype == NM_DT_BF16 ? (float)static_cast<const bf16*>(d.q)[at]
                                                                                                                         : (float)static_cast<const f16*>(d.q)[at];
-            top = fmaxf(top, fabsf(x[i]));
         }
-        float down = 1.0f, up = 1.0f;
+    };
+
+    // What the first tile of a piece needs is requested while the piece before is under way.
+    Piece now = advance();
+    if (now.b < 0) {
+        if (a.workers && tid == 0) a.joined[member * a.workers + worker] = joined;
+        return;
+    }
+    int t0 = now.k0 + wave * kTile;
+    int entry = entry_of(now, t0), entry2 = entry_of(now, t0 + kUnit);
+    fetch_queries(now);
+    v4u kr[kLoads], vr[kLoads];
+    unsigned long valid;
+    {
+        const unsigned place = place_of(now, t0, entry, valid);
+        fetch(d.k_cache, now, place, kr);
+        fetch(d.v_cache, now, place, vr);
+    }
+    while (true) {
+        const Piece then = advance();
+        const int then_t0 = then.k0 + wave * kTile;
+        const int then_entry = entry_of(then, then_t0), then_entry2 = entry_of(then, then_t0 + kUnit);
+        entry = entry2;
+        const int b = now.b, g = now.g, h0 = now.h0, heads = now.heads, k1 = now.k1;
+
+        // the sign of the scale goes with the queries
+        const float by = d.scale * 1.44269504088896340736f * (sizeof(C) == 1 ? d.k_scale[g] : 1.0f);
+        float top_q = 0.0f, down = 1.0f, up = 1.0f;
         if (kQ > 1) {
-            top = __int_as_float(group_reduce<16>(__float_as_int(top), MaxF32{}));
-            const int e = (int)(__float_as_uint(top) >> 23) - 127;     // top in [2^e, 2^(e + 1)): the row goes below 2
-            const int by = max(-126, min(e, 126));
-            down = __uint_as_float((unsigned)(127 - by) << 23);
-            up = __uint_as_float((unsigned)(127 + by) << 23);
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i) top_q = fmaxf(top_q, fabsf(x[i]));
+            top_q = __int_as_float(group_reduce<16>(__float_as_int(top_q), MaxF32{}));
+            const int e = max(-126, min((int)(__float_as_uint(top_q) >> 23) - 127, 126));   // the row goes below 4
+            down = __uint_as_float((unsigned)(127 - e) << 23);
+            up = __uint_as_float((unsigned)(127 + e) << 23);
         }
+        __syncthreads();                                      // the piece before is done with LDS
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) {
-            float rest = x[i] * down;
+            float rest = copysignf(down, by) * x[i];
 #pragma unroll
             for (int q = 0; q < kQ; ++q) {
                 const T t = (T)rest;
                 rest -= (float)t;
-                s_q[q][row * kStride + c0 + 16 * i] = __builtin_bit_cast(short, t);
+                s_q[q][qrow * kStride + qc + 16 * i] = __builtin_bit_cast(short, t);
             }
         }
-        if (c0 == 0) s_qscale[row] = up;
-    }
-    __syncthreads();
+        if (qc == 0) s_qscale[qrow] = up;
+        __syncthreads();
+        // never 0, so that it takes a masked score, minus infinity, for what it is
+        const float factor = fmaxf(fabsf(by) * s_qscale[column], 1.17549435e-38f);
 
-    const int column = lane & 15, j = lane >> 4;              // head (and row of an operand), lane group
-    const float factor = d.scale * 1.44269504088896340736f * s_qscale[column] * (sizeof(C) == 1 ? d.k_scale[g] : 1.0f);
-    const int row_piece = lane % kRowPieces, row_first = lane / kRowPieces;
-    const bool in_row = row_piece * (16 / (int)sizeof(C)) < d.d;
-    const C* kbase = static_cast<const C*>(d.k_cache) + (long)g * d.head_stride + row_piece * (16 / (int)sizeof(C));
-    const C* vbase = static_cast<const C*>(d.v_cache) + (long)g * d.head_stride + row_piece * (16 / (int)sizeof(C));
-    const int* table = d.block_table + b * d.table_stride;
-    short* tile = s.tile[wave];
-
-    // a tile's place: lane l < 32 has position l's offset in the cache (elements), or none
-    auto entry_of = [&](int t0) { const int k = t0 + (lane & 31); return k < k1 ? table[k >> a.shift] : -1; };
-    auto offset_of = [&](int t0, int entry, unsigned& valid) -> long {
-        const int k = t0 + (lane & 31);
-        const bool ok = entry >= 0 && entry < d.num_pages;
-        valid = (unsigned)__ballot(ok);
-        return ok ? (long)entry * d.page_stride + (long)(k & (d.page_size - 1)) * d.slot_stride : 0;
-    };
-    auto fetch = [&](const C* base, long offset, unsigned valid, v4u (&to)[kLoads]) {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int row = i * kRowsAtOnce + row_first;
-            const long at = __shfl(offset, row);
-            to[i] = v4u{};
-            if ((valid >> row & 1) && in_row) to[i] = *reinterpret_cast<const v4u*>(base + at);
+        if (t0 >= k1) {                                       // no tile for this wavefront
+            const unsigned place = place_of(then, then_t0, then_entry, valid);
+            fetch(d.k_cache, then, place, kr);
+            fetch(d.v_cache, then, place, vr);
         }
-    };
-    auto stage = [&](const v4u (&from)[kLoads]) {
+        v4f o[kBlocks];
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) put<C>(tile + (i * kRowsAtOnce + row_first) * kStride + row_piece * (16 / (int)sizeof(C)), from[i]);
-    };
+        for (int i = 0; i < kBlocks; ++i) o[i] = v4f{0, 0, 0, 0};
+        float m = -INFINITY, l = 0.0f;
+        for (; t0 < k1; t0 += kUnit) {
+            unsigned long next_valid;
+            const bool more = t0 + kUnit < k1;
+            const Piece& of = more ? now : then;
+            const unsigned next = place_of(of, more ? t0 + kUnit : then_t0, more ? entry : then_entry, next_valid);
+            entry = entry_of(now, t0 + 2 * kUnit);
+            // scores
+            stage(kr, valid);
+            fetch(d.k_cache, of, next, kr);
+            v4f sc[2];
+#pragma unroll
+            for (int blk = 0; blk < 2; ++blk) {
+                sc[blk] = v4f{0, 0, 0, 0};
+#pragma unroll
+                for (int step = 0; step < kSteps; ++step) {
+                    const v8s ka = *reinterpret_cast<const v8s*>(tile + (blk * 16 + column) * kStride + step * 32 + j * 8);
+#pragma unroll
+                    for (int q = kQ - 1; q >= 0; --q) {
+                        const v8s qb = *reinterpret_cast<const v8s*>(s_q[q] + column * kStride + step * 32 + j * 8);
+                        sc[blk] = Mma<T>::mma(ka, qb, sc[blk]);
+                    }
+                }
+            }
+            if (valid != ~0ul) {
+                asm volatile("");                             // a branch: few tiles need it
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sc[i / 4][i % 4] = scored(i, valid) ? sc[i / 4][i % 4] : -INFINITY;
+            }
+            float top = sc[0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[i / 4][i % 4]);
+            top = __int_as_float(butterfly_step<32>(butterfly_step<16>(__float_as_int(top), MaxF32{}), MaxF32{}));
+            top = fmaxf(m, top == -INFINITY ? top : top * factor);
+            const float base = top == -INFINITY ? 0.0f : top;
+            const float shrink = __builtin_amdgcn_exp2f(m - base);
+            m = top;
+            l *= shrink;
+            const float lifted = kLift - base;
+            v8s p[kP];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i / 4][i % 4], factor, lifted));
+                l += e;
+#pragma unroll
+                for (int q = 0; q < kP; ++q) {
+                    const T t = (T)e;
+                    e = __builtin_fmaf((float)t, -1.0f, e);
+                    p[q][i] = __builtin_bit_cast(short, t);
+                }
+            }
+            // values
+            stage(vr, valid);
+            fetch(d.v_cache, of, next, vr);
+            if (__any(shrink != 1.0f)) {
+#pragma unroll
+                for (int blk = 0; blk < kBlocks; ++blk)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[blk][i] *= shrink;
+            }
+#pragma unroll
+            for (int blk = 0; blk < kBlocks; ++blk) {
+                const short* at = tile + (j * 4 + column / 4) * kStride + blk * 16 + column % 4 * 4;
+                const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at));
+                const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at + 16 * kStride));
+                const v8s va = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+                for (int q = kP - 1; q >= 0; --q) o[blk] = Mma<T>::mma(va, p[q], o[blk]);
+            }
+            valid = next_valid;
+        }
+        fetch_queries(then);
+        l = __int_as_float(butterfly_step<32>(butterfly_step<16>(__float_as_int(l), AddF32{}), AddF32{}));
 
-    v4f o[kBlocks];
+        // the four wavefronts' results as one
+        if (j == 0) { s_m[wave][column] = m; s_l[wave][column] = l; }
+        __syncthreads();                                      // also: no tile is read any more
+        float top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kBlocks; ++i) o[i] = v4f{0, 0, 0, 0};
-    float m = -INFINITY, l = 0.0f;
-
-    int t0 = k0 + wave * kTile;
-    v4u kr[kLoads], vr[kLoads];
-    unsigned valid = 0;
-    int entry = entry_of(t0);
-    {
-        const long offset = offset_of(t0, entry, valid);
-        fetch(kbase, offset, valid, kr);
-        fetch(vbase, offset, valid, vr);
-    }
-    entry = entry_of(t0 + kRound);
-    for (; t0 < k1; t0 += kRound) {
-        unsigned next_valid;
-        const long next = offset_of(t0 + kRound, entry, next_valid);
-        entry = entry_of(t0 + 2 * kRound);
-        // scores
-        stage(kr);
-        fetch(kbase, next, next_valid, kr);
-        v4f sc[2];
+        for (int w = 0; w < kPagedWaves; ++w) top = fmaxf(top, s_m[w][column]);
+        const float base = top == -INFINITY ? 0.0f : top;
+        const float mine = __builtin_amdgcn_exp2f(m - base - kLift);
 #pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
-            sc[blk] = v4f{0, 0, 0, 0};
+        for (int blk = 0; blk < kBlocks; ++blk)
 #pragma unroll
-            for (int step = 0; step < kSteps; ++step) {
-                const v8s ka = *reinterpret_cast<const v8s*>(tile + (blk * 16 + column) * kStride + step * 32 + j * 8);
+            for (int i = 0; i < 4; ++i) s.o[wave][column][blk * 16 + j * 4 + i] = o[blk][i] * mine;
+        __syncthreads();
+        const float vscale = sizeof(C) == 1 ? d.v_scale[g] : 1.0f;
+        const int row = tid >> 4;
+        if (row < heads) {
+            float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-                for (int q = kQ - 1; q >= 0; --q) {
-                    const v8s qb = *reinterpret_cast<const v8s*>(s_q[q] + column * kStride + step * 32 + j * 8);
-                    sc[blk] = Mfma<C>::mma(ka, qb, sc[blk]);
+            for (int w = 0; w < kPagedWaves; ++w) top = fmaxf(top, s_m[w][row]);
+            const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int w = 0; w < kPagedWaves; ++w) sum += s_l[w][row] * __builtin_amdgcn_exp2f(s_m[w][row] - base - kLift);
+            if ((tid & 15) == 0) {
+                if (now.slot >= 0) a.part_ml[part_of(a, member, worker, now.slot) + row] = make_float2(top, sum);
+                else if (d.lse) d.lse[(long)b * d.hq + h0 + row] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
+            }
+            const float by = (sum == 0.0f ? 0.0f : 1.0f / sum) * vscale;
+            for (int c = (tid & 15) * 4; c < d.d; c += 64) {
+                v4f x{0, 0, 0, 0};
+#pragma unroll
+                for (int w = 0; w < kPagedWaves; ++w) x += *reinterpret_cast<const v4f*>(&s.o[w][row][c]);
+                if (now.slot >= 0) {
+                    *reinterpret_cast<v4f*>(a.part_o + (part_of(a, member, worker, now.slot) + row) * d.d + c) = x;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) store1(d.out, d.out_dtype, b * d.out_stride + (long)(h0 + row) * d.d + c + i, x[i] * by, d.out_inv_scale);
                 }
             }
         }
-        float top = m;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float x = sc[i / 4][i % 4] * factor;
-            sc[i / 4][i % 4] = (valid >> (i / 4 * 16 + j * 4 + i % 4) & 1) ? x : -INFINITY;
-            top = fmaxf(top, sc[i / 4][i % 4]);
+        if (then.b < 0) {
+            if (a.workers && tid == 0) a.joined[member * a.workers + worker] = joined;
+            break;
         }
-        top = __int_as_float(butterfly_step<32>(butterfly_step<16>(__float_as_int(top), MaxF32{}), MaxF32{}));
-        const float base = top == -INFINITY ? 0.0f : top;
-        const float shrink = __builtin_amdgcn_exp2f(m - base);
-        m = top;
-        l *= shrink;
-        v8s p[kP];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float e = __builtin_amdgcn_exp2f(sc[i / 4][i % 4] - (base - kLift));
-            l += e;
-#pragma unroll
-            for (int q = 0; q < kP; ++q) {
-                const T t = (T)e;
-                e -= (float)t;
-                p[q][i] = __builtin_bit_cast(short, t);
-            }
-        }
-        // values
-        stage(vr);
-        fetch(vbase, next, next_valid, vr);
-#pragma unroll
-        for (int blk = 0; blk < kBlocks; ++blk) {
-            const short* at = tile + (j * 4 + column / 4) * kStride + blk * 16 + column % 4 * 4;
-            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at));
-            const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at + 16 * kStride));
-            const v8s va = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[blk][i] *= shrink;
-#pragma unroll
-            for (int q = kP - 1; q >= 0; --q) o[blk] = Mfma<C>::mma(va, p[q], o[blk]);
-        }
-        valid = next_valid;
-    }
-    l = __int_as_float(butterfly_step<32>(butterfly_step<16>(__float_as_int(l), AddF32{}), AddF32{}));
-
-    // the four wavefronts' results as one
-    if (j == 0) { s_m[wave][column] = m; s_l[wave][column] = l; }
-    __syncthreads();                                          // also: no tile is read any more
-    float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kPagedWaves; ++w) top = fmaxf(top, s_m[w][column]);
-    const float base = top == -INFINITY ? 0.0f : top;
-    const float mine = __builtin_amdgcn_exp2f(m - base - kLift);
-#pragma unroll
-    for (int blk = 0; blk < kBlocks; ++blk)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s.o[wave][column][blk * 16 + j * 4 + i] = o[blk][i] * mine;
-    __syncthreads();
-    const float vscale = sizeof(C) == 1 ? d.v_scale[g] : 1.0f;
-    for (int row = tid >> 4; row < heads; row += kPagedThreads / 16) {
-        float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kPagedWaves; ++w) top = fmaxf(top, s_m[w][row]);
-        const float base = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-        for (int w = 0; w < kPagedWaves; ++w) sum += s_l[w][row] * __builtin_amdgcn_exp2f(s_m[w][row] - base - kLift);
-        const long bh = (long)b * d.hq + h0 + row;
-        const long part = bh * a.pieces + piece;
-        if ((tid & 15) == 0) {
-            if (a.part_ml) a.part_ml[part] = make_float2(top, sum);
-            else if (d.lse) d.lse[bh] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
-        }
-        const float by = (sum == 0.0f ? 0.0f : 1.0f / sum) * vscale;
-        for (int c = (tid & 15) * 4; c < d.d; c += 64) {
-            v4f x{0, 0, 0, 0};
-#pragma unroll
-            for (int w = 0; w < kPagedWaves; ++w) x += *reinterpret_cast<const v4f*>(&s.o[w][row][c]);
-            if (a.part_ml) {
-                *reinterpret_cast<v4f*>(a.part_o + part * d.d + c) = x;
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) store1(d.out, d.out_dtype, b * d.out_stride + (long)(h0 + row) * d.d + c + i, x[i] * by, d.out_inv_scale);
-            }
-        }
+        now = then;
+        t0 = then_t0;
+        entry2 = then_entry2;
     }
 }
 
-// The pieces of one query head as one: a workgroup to a head; 16 lanes read a piece's output, four elements at a time.
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a)
+// The rows that several runs have a piece of: a workgroup to a run and query head of its last row.  Lanes of four elements read every
+// so-manieth piece's output and join them as they come; their results are joined through LDS.
+__global__ __launch_bounds__(kPagedThreads) void paged_join_kernel(PagedArgs a)
 {
-    __shared__ float s_o[16][256];
-    __shared__ float s_top[4], s_sum[4];
+    __shared__ __attribute__((aligned(16))) float s_o[kPagedThreads * 4];
+    __shared__ float s_m[kPagedThreads / 4], s_l[kPagedThreads / 4];
     const nm_paged_desc& d = a.d;
-    const int bh = blockIdx.x, b = bh / d.hq, h = bh % d.hq, tid = threadIdx.x;
-    const int n = (int)min((long)max(d.lens[b], 0), (long)d.max_pages << a.shift);
-    const int span = d.window ? min(n, d.window) : n;
-    const int used = (span + a.piece - 1) / a.piece;
-    const float2* ml = a.part_ml + (long)bh * a.pieces;
-    float top = -INFINITY, sum = 0.0f;
-    for (int i = tid; i < used; i += 256) top = fmaxf(top, ml[i].x);
-    top = __int_as_float(group_reduce<64>(__float_as_int(top), MaxF32{}));
-    if ((tid & 63) == 0) s_top[tid >> 6] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
-    const float base = top == -INFINITY ? 0.0f : top;
-    for (int i = tid; i < used; i += 256) sum += ml[i].y * __builtin_amdgcn_exp2f(ml[i].x - base);
-    sum = group_sum<64>(sum);
-    if ((tid & 63) == 0) s_sum[tid >> 6] = sum;
-    __syncthreads();
-    sum = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+    const int tid = threadIdx.x, member = blockIdx.x / a.workers, w0 = blockIdx.x % a.workers, nth = blockIdx.y;
+    const int4 row = a.joined[blockIdx.x];
+    const int used = row.w, h = row.y + nth, g = row.y / a.group;
+    if (!used || h >= (g + 1) * a.group) return;
+    const long bh = (long)row.x * d.hq + h;
 
-    const int row = tid >> 4;
-    for (int c = (tid & 15) * 4; c < d.d; c += 64) {
-        v4f x{0, 0, 0, 0};
-        for (int i = row; i < used; i += 16) {
-            const float by = __builtin_amdgcn_exp2f(ml[i].x - base);
-            const v4f y = *reinterpret_cast<const v4f*>(a.part_o + ((long)bh * a.pieces + i) * d.d + c);
+    const int lanes = d.d / 4, at_once = kPagedThreads / lanes, mine = tid / lanes, c = tid % lanes * 4;
+    float m = -INFINITY, l = 0.0f;
+    v4f x{0, 0, 0, 0};
+    if (mine < at_once) {
+#pragma unroll 4
+        for (int i = mine; i < used; i += at_once) {
+            const long part = part_of(a, member, w0 + i, i == 0 ? row.z : 0) + nth;
+            const float2 ml = a.part_ml[part];
+            const v4f y = *reinterpret_cast<const v4f*>(a.part_o + part * d.d + c);
+            const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.0f : top;
+            const float shrink = __builtin_amdgcn_exp2f(m - base), by = __builtin_amdgcn_exp2f(ml.x - base);
+            l = l * shrink + ml.y * by;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(y[e], by, x[e]);
+            for (int e = 0; e < 4; ++e) x[e] = x[e] * shrink + y[e] * by;
+            m = top;
         }
-        *reinterpret_cast<v4f*>(&s_o[row][c]) = x;
+        *reinterpret_cast<v4f*>(&s_o[mine * d.d + c]) = x;
+        if (c == 0) { s_m[mine] = m; s_l[mine] = l; }
     }
     __syncthreads();
-    const float vscale = d.cache_dtype == NM_DT_I8 ? d.v_scale[h / a.group] : 1.0f;
-    const float by = (sum == 0.0f ? 0.0f : 1.0f / sum) * vscale;
-    if (tid < d.d) {
-        float x = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x += s_o[i][tid];
-        store1(d.out, d.out_dtype, b * d.out_stride + (long)h * d.d + tid, x * by, d.out_inv_scale);
+    float top = -INFINITY, sum = 0.0f, v = 0.0f;
+    for (int i = 0; i < at_once; ++i) top = fmaxf(top, s_m[i]);
+    const float base = top == -INFINITY ? 0.0f : top;
+    for (int i = 0; i < at_once; ++i) {
+        const float by = __builtin_amdgcn_exp2f(s_m[i] - base);
+        sum += s_l[i] * by;
+        if (tid < d.d) v += s_o[i * d.d + tid] * by;
     }
+    const float by = (sum == 0.0f ? 0.0f : 1.0f / sum) * (d.cache_dtype == NM_DT_I8 ? d.v_scale[g] : 1.0f);
+    if (tid < d.d) store1(d.out, d.out_dtype, row.x * d.out_stride + (long)h * d.d + tid, v * by, d.out_inv_scale);
     if (tid == 0 && d.lse) d.lse[bh] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
 }
 
-template <typename C, int DP>
-static void launch_paged(const PagedArgs& a, int blocks, hipStream_t s)
+template <typename C, typename T, int DP>
+static void launch_paged(const PagedArgs& a, int blocks, bool own, hipStream_t s)
 {
-    // one term of a query where the matrix instructions' type is its own, and two of the weights where the result has 16 bits or fewer
-    const bool own = a.d.q_dtype == (std::is_same<C, f16>::value ? NM_DT_F16 : NM_DT_BF16);
-    if (own && a.d.out_dtype != NM_DT_F32) queue_kernel(paged_attention_kernel<C, DP, 1, 2>, dim3(blocks), dim3(kPagedThreads), 0, s, a);
-    else queue_kernel(paged_attention_kernel<C, DP, 3, 3>, dim3(blocks), dim3(kPagedThreads), 0, s, a);
+    if (own && a.d.out_dtype != NM_DT_F32) queue_kernel(paged_attention_kernel<C, T, DP, 1, 2>, dim3(blocks), dim3(kPagedThreads), 0, s, a);
+    else queue_kernel(paged_attention_kernel<C, T, DP, 3, 3>, dim3(blocks), dim3(kPagedThreads), 0, s, a);
 }
-template <typename C>
+// One term of a query where the matrix instructions' type is its own, and two of the weights where the result has 16 bits or fewer.
+template <typename C, typename T>
 static void launch_paged(const PagedArgs& a, int blocks, hipStream_t s)
 {
-    if (a.d.d <= 64) launch_paged<C, 64>(a, blocks, s);
-    else if (a.d.d <= 128) launch_paged<C, 128>(a, blocks, s);
-    else launch_paged<C, 256>(a, blocks, s);
+    const bool own = a.d.q_dtype == (std::is_same<T, f16>::value ? NM_DT_F16 : NM_DT_BF16);
+    if (a.d.d <= 64) launch_paged<C, T, 64>(a, blocks, own, s);
+    else if (a.d.d <= 128) launch_paged<C, T, 128>(a, blocks, own, s);
+    else launch_paged<C, T, 256>(a, blocks, own, s);
 }
 
-// What does not depend on pointers: shapes, types, and how the length is divided.
+// What does not depend on pointers: shapes, types, and how the work is shared.
 static int32_t plan_paged(const nm_paged_desc* d, PagedArgs* a, size_t* bytes, long* blocks, const char* what)
 {
     if (!d) return fail(NM_ERR_INVALID_ARG, "%s: desc is NULL", what);
@@ -364,6 +570,10 @@ static int32_t plan_paged(const nm_paged_desc* d, PagedArgs* a, size_t* bytes, l
     if (shift < 0) return fail(NM_ERR_UNSUPPORTED, "%s: page_size %d is no power of two up to 65536", what, d->page_size);
     if ((int64_t)d->num_pages << shift > 0x7fffffffLL || (int64_t)d->max_pages << shift > 0x3fffffffLL)
         return fail(NM_ERR_UNSUPPORTED, "%s: num_pages * page_size >= 2^31 or max_pages * page_size >= 2^30", what);
+    // distances into a cache are held in 16 bytes, in 31 bits (the strides are not negative: checked before any launch)
+    if ((double)d->num_pages * (double)d->page_stride + (double)d->page_size * (double)d->slot_stride >= 2147483648.0 * 16 / dtype_bytes(d->cache_dtype))
+        return fail(NM_ERR_UNSUPPORTED, "%s: a cache of more than 32 GiB", what);
+    if ((int64_t)d->B * d->hq >= 1 << 23) return fail(NM_ERR_UNSUPPORTED, "%s: B * hq >= 2^23", what);
     *a = PagedArgs{};
     a->d = *d;
     a->shift = shift;
@@ -371,16 +581,23 @@ static int32_t plan_paged(const nm_paged_desc* d, PagedArgs* a, size_t* bytes, l
     a->groups = (a->group + 15) / 16;
     long longest = (long)d->max_pages << shift;
     if (d->window && d->window < longest) longest = d->window;
-    const long rows = (long)d->B * d->hk * a->groups;
-    // pieces: as long as leaves 2048 workgroups (eight to a CU, so that ragged lengths even out), 128 positions at least
-    long piece = kRound;
-    while (piece < longest && rows * ((longest + 2 * piece - 1) / (2 * piece)) >= 2048) piece *= 2;
-    a->piece = (int)piece;
-    a->pieces = (int)(longest > 0 ? (longest + piece - 1) / piece : 1);
-    *blocks = rows * a->pieces;
-    if (*blocks >= 1L << 24 || (long)d->B * d->hq >= 1L << 24) return fail(NM_ERR_UNSUPPORTED, "%s: too many heads and pieces", what);
-    const size_t parts = (size_t)d->B * d->hq * a->pieces;
-    *bytes = a->pieces > 1 ? (parts * sizeof(float2) + 255) / 256 * 256 + parts * d->d * sizeof(float) : 0;
+    // Rows that read the same lines: the groups of a key head, and the heads whose pieces of a slot share a line of 128 bytes (as long as
+    // the other slots do not lie between them).
+    const int64_t head_bytes = d->head_stride * dtype_bytes(d->cache_dtype);
+    a->share = a->groups;
+    if (head_bytes > 0 && head_bytes < 128 && d->head_stride < d->slot_stride)
+        for (int n = 2; n * head_bytes <= 128; n *= 2)
+            if (d->hk % n == 0) a->share = a->groups * n;
+    const long sets = (long)d->B * d->hk * a->groups / a->share, most = sets * ((longest + kUnit - 1) / kUnit);
+    // Who shares: as many workgroups as run at once (twice as many took 4 % longer at 48 ragged requests and 1 to 10 % at one of 131071).
+    // Rows too short to be divided go to a workgroup each, without the second kernel: 12 heads of 512 positions of one request took 10.4 us
+    // so and 13.7 shared, of 1024 14.6 and 13.6; of 64 requests 23.3 and 29.8.
+    a->extra = 2;
+    if (longest > (sets >= 256 ? 1024 : 512)) a->workers = (int)std::min(most, std::max(8l, 256l * workgroups_of(d->d) / a->share));
+    const long teams = ((a->workers ? a->workers : sets) + 7) / 8 * 8;   // every XCD has as many
+    *blocks = teams * a->share;
+    const size_t parts = (size_t)a->share * a->workers * 2 * 16;
+    *bytes = parts * (sizeof(float2) + d->d * sizeof(float)) + parts / 32 * sizeof(int4);
     return NM_OK;
 }
 
@@ -424,17 +641,19 @@ int32_t nm_paged_attention(const nm_paged_desc* d, void* ws, size_t ws_bytes, vo
     if (need) {
         if (!ws || ws_bytes < need) return fail(NM_ERR_WORKSPACE, "nm_paged_attention: workspace of %zu bytes needed, %zu given", need, ws ? ws_bytes : (size_t)0);
         if (!aligned(ws, 256)) return fail(NM_ERR_WORKSPACE, "nm_paged_attention: workspace must be 256-byte aligned");
-        const size_t parts = (size_t)d->B * d->hq * a.pieces;
-        a.part_ml = static_cast<float2*>(ws);
-        a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + (parts * sizeof(float2) + 255) / 256 * 256);
+        const size_t runs = (size_t)a.share * a.workers;
+        a.joined = static_cast<int4*>(ws);
+        a.part_ml = reinterpret_cast<float2*>(a.joined + runs);
+        a.part_o = reinterpret_cast<float*>(a.part_ml + runs * 2 * 16);
     }
-    if (d->cache_dtype == NM_DT_BF16) launch_paged<bf16>(a, (int)blocks, (hipStream_t)stream);
-    else if (d->cache_dtype == NM_DT_F16) launch_paged<f16>(a, (int)blocks, (hipStream_t)stream);
-    else launch_paged<int8_t>(a, (int)blocks, (hipStream_t)stream);
+    if (d->cache_dtype == NM_DT_BF16) launch_paged<bf16, bf16>(a, (int)blocks, (hipStream_t)stream);
+    else if (d->cache_dtype == NM_DT_F16) launch_paged<f16, f16>(a, (int)blocks, (hipStream_t)stream);
+    else if (d->q_dtype == NM_DT_F16) launch_paged<int8_t, f16>(a, (int)blocks, (hipStream_t)stream);
+    else launch_paged<int8_t, bf16>(a, (int)blocks, (hipStream_t)stream);
     if (need) {
         const int32_t err = check_hip(hipGetLastError(), "nm_paged_attention launch");
         if (err) return err;
-        queue_kernel(paged_join_kernel, dim3(d->B * d->hq), dim3(256), 0, (hipStream_t)stream, a);
+        queue_kernel(paged_join_kernel, dim3(a.share * a.workers, a.group < 16 ? a.group : 16), dim3(kPagedThreads), 0, (hipStream_t)stream, a);
     }
     return check_hip(hipGetLastError(), "nm_paged_attention launch");
 }
