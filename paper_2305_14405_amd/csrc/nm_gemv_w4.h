@@ -1,0 +1,366 @@
+// Products of a few rows with 4-bit weights (nm_gemv_w4): the kernel.  One translation unit for each type of x.
+//
+// Bound by memory: N K / 2 bytes of weights, each read once, for 2 M operations a weight.  A workgroup has 16 or 32 columns (rows of W)
+// and all of K, which its eight wavefronts share in blocks of 128; their sums are joined through LDS, so that columns alone need not
+// fill the GPU.  K goes by chunks: x of a chunk, and the chunk's scales as fp32, lie in LDS (the next chunk's are on their way into
+// registers), and a wavefront takes a run of the chunk's blocks.  Weights go directly into LDS, a ring of blocks for each wavefront.
+//   Four neighbouring lanes load 64 bytes, 128 weights, of a row, a run of 32 each: neighbouring lanes in different rows, as the matrix
+// instruction wants them, cost the address unit four times as much (28672 x 8192: 54 us so, 2.2 TB/s).  From LDS lane (j, row) then
+// gets run j of its row.  The 16x16x32 instruction (rows of x its rows, columns its columns) adds over the four lanes of a
+// row, so to add within one run (the smallest group) these exchange words, four half swaps for 16 bytes: then register i of lane
+// group j holds weights 8 j .. 8 j + 7 of run i.
+//   int8: (v << 4) & 0xf0f0f0f0 and v & 0xf0f0f0f0 are 16 times the even and the odd weights as int8: three operations for eight
+// weights, and exact.  bf16, fp16: u = w + 8 is put under an exponent, 16 + u, exactly, in nine; a matrix instruction with the constant -24
+// in the weights' place takes the offset off again, once for all columns of a wavefront (the sum of x it subtracts is at most some 5
+// times the result's size, so fp32 loses two bits of 24).
+//   What a group's sum is multiplied by is one number per lane (its column).
+#pragma once
+
+#include <mutex>
+
+#include "nm_decode.h"
+
+namespace nm {
+
+typedef bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef f16 v8h __attribute__((ext_vector_type(8)));
+typedef unsigned v4u __attribute__((ext_vector_type(4)));
+typedef unsigned v2u __attribute__((ext_vector_type(2)));
+
+constexpr int kW4Waves = 8, kW4Threads = 64 * kW4Waves;
+
+constexpr int kW4Scales = 8;    // scales that a thread has of a chunk
+
+struct W4Args {
+    nm_w4_desc d;
+    DevTable table;
+    FastDiv per;         // blocks to a group of 128 or more
+    int chunk_shift;     // log2 of a chunk's length in K / 1024: a wavefront's blocks of a chunk
+    int chunks;
+    int x_stride;        // bytes between rows of x in LDS
+    int passes;          // over the weights: tiles of rows
+};
+constexpr int kW4Chunk = 128 * kW4Waves;
+
+// Pieces of 16 bytes of x that a thread has of a chunk: as many as 1024 columns of 16-bit rows are.
+constexpr int w4_pieces(int tiles) { return 4 * tiles; }
+// Blocks of a wavefront's ring: 16 columns are 1 KB of each.
+constexpr int w4_stages(int columns) { return columns == 1 ? 4 : 3; }
+
+template <typename X>
+int32_t launch_w4(const W4Args& a, hipStream_t s);
+
+// Register i of lane group j <-> register j of lane group i.
+__device__ __forceinline__ v4u exchange(v4u w)
+{
+    const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+    const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), e = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    return v4u{c[0], c[1], e[0], e[1]};
+}
+
+__device__ __forceinline__ unsigned in_vgpr_u(unsigned x)
+{
+    unsigned v;
+    asm("v_mov_b32 %0, %1" : "=v"(v) : "s"(x));
+    return v;
+}
+
+// What differs by the type of x: its eight values of a lane, the sum over them, and eight weights.
+template <typename X> struct W4;
+template <> struct W4<int8_t> {
+    typedef v2u Rows;
+    typedef v4i Sum;
+    // of a lane's eight values the even ones first: so the weights come out of their word
+    static __device__ __forceinline__ v4u order(v4u x)
+    {
+        return v4u{__builtin_amdgcn_perm(x[1], x[0], 0x06040200u), __builtin_amdgcn_perm(x[1], x[0], 0x07050301u),
+                   __builtin_amdgcn_perm(x[3], x[2], 0x06040200u), __builtin_amdgcn_perm(x[3], x[2], 0x07050301u)};
+    }
+    static __device__ __forceinline__ unsigned exponent() { return 0; }
+    static __device__ __forceinline__ v2u weights(unsigned w, unsigned) { return v2u{(w << 4) & 0xf0f0f0f0u, w & 0xf0f0f0f0u}; }
+    static __device__ __forceinline__ Sum add(Rows x, v2u w, Sum c) { return __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, x), __builtin_bit_cast(long, w), c, 0, 0, 0); }
+    static __device__ __forceinline__ Sum offset(Rows, Sum c) { return c; }
+    static constexpr float kUnit = 1.0f / 16.0f;
+};
+template <typename X> struct W4Half {
+    typedef v4u Rows;
+    typedef v4f Sum;
+    static constexpr bool kBf = std::is_same<X, bf16>::value;
+    // a lane's eight values in the order in which the weights come out of their word: 0 4 1 5 2 6 3 7
+    static __device__ __forceinline__ v4u order(v4u x)
+    {
+        return v4u{__builtin_amdgcn_perm(x[2], x[0], 0x05040100u), __builtin_amdgcn_perm(x[2], x[0], 0x07060302u),
+                    __builtin_amdgcn_perm(x[3], x[1], 0x05040100u), __builtin_amdgcn_perm(x[3], x[1], 0x07060302u)};
+    }
+    // 16 + u: u in the upper four bits of the mantissa (7 bits of bf16, 10 of fp16).  exponent: of 16, twice, in a vector register, so that
+    // mask and exponent are one instruction (an instruction takes one constant from elsewhere)
+    static __device__ __forceinline__ unsigned exponent() { return in_vgpr_u(kBf ? 0x41804180u : 0x4c004c00u); }
+    static __device__ __forceinline__ v4u weights(unsigned w, unsigned exponent)
+    {
+        const unsigned u = w ^ 0x88888888u;
+        if (kBf) return v4u{((u << 3) & 0x00780078u) | exponent, ((u >> 1) & 0x00780078u) | exponent,
+                            ((u >> 5) & 0x00780078u) | exponent, ((u >> 9) & 0x00780078u) | exponent};
+        return v4u{((u << 6) & 0x03c003c0u) | exponent, ((u << 2) & 0x03c003c0u) | exponent,
+                   ((u >> 2) & 0x03c003c0u) | exponent, ((u >> 6) & 0x03c003c0u) | exponent};
+    }
+    static __device__ __forceinline__ Sum add(Rows x, v4u w, Sum c)
+    {
+        if constexpr (kBf) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, w), c, 0, 0, 0);
+        else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x), __builtin_bit_cast(v8h, w), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ Sum offset(Rows x, Sum c)
+    {
+        const unsigned minus24 = kBf ? 0xc1c0c1c0u : 0xce00ce00u;
+        return add(x, v4u{minus24, minus24, minus24, minus24}, c);
+    }
+    static constexpr float kUnit = 1.0f;
+};
+template <> struct W4<bf16> : W4Half<bf16> {};
+template <> struct W4<f16> : W4Half<f16> {};
+
+// S: bits of a scale (float, or either 16-bit type); kRuns: runs of 32 weights to a scale within a block of 128 (1, 2, 4); kM: tiles of
+// 16 rows; kN: of 16 columns.
+template <typename X, typename S, int kRuns, int kM, int kN>
+__global__ __launch_bounds__(kW4Threads, kM == 1 ? 4 : 2) void gemv_w4_kernel(W4Args a)
+{
+    typedef W4<X> Q;
+    typedef typename Q::Rows Rows;
+    typedef typename Q::Sum Sum;
+    constexpr int kScales = 4 / kRuns;                        // to a block
+    constexpr int kCols = 16 * kN, kPer16 = 16 / (int)sizeof(X);
+    constexpr int kPieces = w4_pieces(kM);         // of x, 16 bytes, that a thread has of a chunk
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const nm_w4_desc& d = a.d;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, column = lane & 15, j = lane >> 4;
+    constexpr int kStages = w4_stages(kN);
+    // the passes over the same columns are neighbours on an XCD (workgroup i runs on XCD i mod 8)
+    const int pass = blockIdx.x / 8 % a.passes, n0 = (blockIdx.x / 8 / a.passes * 8 + blockIdx.x % 8) * kCols;
+    const int m0 = pass * 16 * kM, rows = min(d.M - m0, 16 * kM);
+    if (n0 >= d.N) return;
+    const int groups = d.K / d.group;
+    const int run = 1 << a.chunk_shift;                       // a wavefront's blocks of a chunk
+    const int entry_shift = a.chunk_shift + 3 + (kRuns == 4 ? 0 : kRuns == 2 ? 1 : 2), entries = 1 << entry_shift;   // scales of a column and chunk
+    const unsigned exponent = Q::exponent();
+    // LDS: the wavefronts' rings, the chunk's scales (rows one longer), the chunk's x; at the end the sums, from the start
+    char* s_w = smem + wave * kStages * 1024 * kN;
+    float* s_scale = reinterpret_cast<float*>(smem + kW4Waves * kStages * 1024 * kN);
+    char* s_x = smem + kW4Waves * kStages * 1024 * kN + (kCols * (entries + 1) * 4 + 15) / 16 * 16;
+
+    // weights: lane 4 r + i has run i ^ r / 4 % 4 of row r, so that no two banks meet when lane (j, row) reads run j of its row.  Columns
+    // behind the last read the last one's: what comes of them is not written.  Behind K the last run is repeated: it meets zeros of x.
+    const uint8_t* wrow[kN];
+#pragma unroll
+    for (int c = 0; c < kN; ++c) wrow[c] = d.W + (long)min(n0 + c * 16 + (lane >> 2), d.N - 1) * (d.K / 2);
+    const int total = a.chunks * run;                         // the wavefront's blocks
+    const unsigned ring = (unsigned)(uintptr_t)smem + wave * kStages * 1024 * kN;
+    auto request = [&](int u, int slot) {                     // block number u
+        const int kb = ((u >> a.chunk_shift) * kW4Waves + wave) * run + (u & (run - 1));
+        const int k = min(kb * 128 + ((lane & 3) ^ (lane >> 4 & 3)) * 32, d.K - 32);
+#pragma unroll
+        for (int c = 0; c < kN; ++c) dma16(wrow[c] + k / 2, ring + (slot * kN + c) * 1024);
+    };
+    const int read_at = (column * 4 + (j ^ (column >> 2))) * 16;
+
+    // x and scales of a chunk: into registers, then into LDS (x in the order that the matrix instructions want)
+    const int row_shift = a.chunk_shift + (sizeof(X) == 1 ? 6 : 7);   // pieces to a row of a chunk
+    v4u xp[kPieces];
+    S sp[kW4Scales];
+    auto fetch = [&](int chunk) {
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q) {
+            const int p = tid + q * kW4Threads, r = min(p >> row_shift, rows - 1), k = chunk * (kW4Chunk << a.chunk_shift) + (p & ((1 << row_shift) - 1)) * kPer16;
+            xp[q] = *reinterpret_cast<const v4u*>(static_cast<const X*>(d.x) + (long)(m0 + r) * d.x_stride + min(k, d.K - kPer16));
+        }
+#pragma unroll
+        for (int q = 0; q < kW4Scales; ++q) {
+            const int i = tid + q * kW4Threads, c = min(i >> entry_shift, kCols - 1), e = i & (entries - 1), block = chunk * (run * kW4Waves) + e / kScales;
+            const int g = min(kRuns == 4 ? (int)quotient(block, a.per) : block * kScales + e % kScales, groups - 1);
+            sp[q] = static_cast<const S*>(d.scales)[(long)min(n0 + c, d.N - 1) * groups + g];
+        }
+        __builtin_amdgcn_sched_barrier(0);                    // loads are waited for in their order
+    };
+    auto stage = [&](int chunk) {
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q) {
+            const int p = tid + q * kW4Threads, r = p >> row_shift, at = p & ((1 << row_shift) - 1), k = chunk * (kW4Chunk << a.chunk_shift) + at * kPer16;
+            if (r < rows) *reinterpret_cast<v4u*>(s_x + r * a.x_stride + at * 16) = k < d.K ? Q::order(xp[q]) : v4u{};
+        }
+#pragma unroll
+        for (int q = 0; q < kW4Scales; ++q) {
+            const int i = tid + q * kW4Threads, c = i >> entry_shift, e = i & (entries - 1);
+            float v;
+            if constexpr (sizeof(S) == 4) v = sp[q];
+            else v = d.scale_dtype == NM_DT_BF16 ? __uint_as_float((unsigned)sp[q] << 16) : (float)__builtin_bit_cast(f16, sp[q]);
+            if (c < kCols) s_scale[c * (entries + 1) + e] = v * Q::kUnit;
+        }
+    };
+
+    v4f sum[kM][kN];
+#pragma unroll
+    for (int t = 0; t < kM; ++t)
+#pragma unroll
+        for (int c = 0; c < kN; ++c) sum[t][c] = v4f{0, 0, 0, 0};
+    const char* xrow[kM];
+#pragma unroll
+    for (int t = 0; t < kM; ++t) xrow[t] = s_x + min(t * 16 + column, rows - 1) * a.x_stride + (wave * run * 128 + j * 8) * sizeof(X);
+    const float* srow = s_scale + column * (entries + 1) + wave * run * kScales;
+
+    auto block = [&](int at, const v4u (&now)[kN]) {          // block number at of the wavefront's run in this chunk
+#pragma unroll
+        for (int g = 0; g < kScales; ++g) {
+            float scale[kN];
+#pragma unroll
+            for (int c = 0; c < kN; ++c) scale[c] = srow[c * 16 * (entries + 1) + at * kScales + g];
+            auto rows_of = [&](int t, int i) { return *reinterpret_cast<const Rows*>(xrow[t] + (at * 128 + i * 32) * sizeof(X)); };
+            Sum acc[kM][kN];
+            if constexpr (kM <= 2) {                          // the offset is where the sums begin
+                Rows x[kM][kRuns];
+#pragma unroll
+                for (int t = 0; t < kM; ++t) {
+                    Sum off{};
+#pragma unroll
+                    for (int i = 0; i < kRuns; ++i) off = Q::offset(x[t][i] = rows_of(t, g * kRuns + i), off);
+#pragma unroll
+                    for (int c = 0; c < kN; ++c) acc[t][c] = off;
+                }
+#pragma unroll
+                for (int i = 0; i < kRuns; ++i)
+#pragma unroll
+                    for (int c = 0; c < kN; ++c) {
+                        const auto weights = Q::weights(now[c][g * kRuns + i], exponent);
+#pragma unroll
+                        for (int t = 0; t < kM; ++t) acc[t][c] = Q::add(x[t][i], weights, acc[t][c]);
+                    }
+            } else {                                          // or is added to them: fewer registers of x at a time
+                Sum off[kM];
+#pragma unroll
+                for (int i = 0; i < kRuns; ++i) {
+                    Rows x[kM];
+#pragma unroll
+                    for (int t = 0; t < kM; ++t) {
+                        x[t] = rows_of(t, g * kRuns + i);
+                        off[t] = Q::offset(x[t], i ? off[t] : Sum{});
+                    }
+#pragma unroll
+                    for (int c = 0; c < kN; ++c) {
+                        const auto weights = Q::weights(now[c][g * kRuns + i], exponent);
+#pragma unroll
+                        for (int t = 0; t < kM; ++t) acc[t][c] = Q::add(x[t], weights, i ? acc[t][c] : Sum{});
+                    }
+                }
+                if constexpr (sizeof(X) > 1) {
+#pragma unroll
+                    for (int t = 0; t < kM; ++t)
+#pragma unroll
+                        for (int c = 0; c < kN; ++c)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[t][c][e] += off[t][e];
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < kM; ++t)
+#pragma unroll
+                for (int c = 0; c < kN; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[t][c][e] = __builtin_fmaf((float)acc[t][c][e], scale[c], sum[t][c][e]);
+        }
+    };
+
+    fetch(0);
+#pragma unroll
+    for (int u = 0; u < kStages; ++u)
+        if (u < total) request(u, u);
+    for (int u = 0, slot = 0; u < total; ++u, slot = slot + 1 == kStages ? 0 : slot + 1) {
+        if (!(u & (run - 1))) {
+            const int chunk = u >> a.chunk_shift;
+            if (chunk) __syncthreads();
+            stage(chunk);
+            if (chunk + 1 < a.chunks) fetch(chunk + 1);
+            __syncthreads();
+        }
+        // what was requested behind this block may still be under way; at the end nothing is requested any more
+        if (u + kStages <= total) wait_vmcnt<(kStages - 1) * kN>();
+        else wait_vmcnt<0>();
+        v4u now[kN];
+#pragma unroll
+        for (int c = 0; c < kN; ++c) now[c] = *reinterpret_cast<const v4u*>(s_w + (slot * kN + c) * 1024 + read_at);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // the slot is read before it is written again
+        if (u + kStages < total) request(u + kStages, slot);
+#pragma unroll
+        for (int c = 0; c < kN; ++c) now[c] = exchange(now[c]);
+        block(u & (run - 1), now);
+    }
+    __syncthreads();
+    float (*s_sum)[kM][16][kCols] = reinterpret_cast<float (*)[kM][16][kCols]>(smem);
+#pragma unroll
+    for (int t = 0; t < kM; ++t)
+#pragma unroll
+        for (int c = 0; c < kN; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s_sum[wave][t][j * 4 + e][c * 16 + column] = sum[t][c][e];
+    __syncthreads();
+    for (int i = tid; i < kM * 16 * kCols; i += kW4Threads) {
+        const int c = i % kCols, r = i / kCols % 16, t = i / (16 * kCols), m = m0 + t * 16 + r, col = n0 + c;
+        if (m >= d.M || col >= d.N) continue;
+        float v = 0.0f;
+#pragma unroll
+        for (int p = 0; p < kW4Waves; ++p) v += s_sum[p][t][r][c];
+        v = __builtin_fmaf(v, d.alpha, d.bias ? d.bias[col] : 0.0f);
+        if (d.table_idx >= 0) {
+            int seg;
+            v = pwl_eval(v, a.table, a.table.kb, seg);
+        }
+        store1(d.out, d.out_dtype, (long)m * d.out_stride + col, v, d.out_inv_scale);
+    }
+}
+
+template <typename X, typename S, int kRuns, int kM, int kN>
+static int32_t launch_w4_tiles(W4Args a, hipStream_t s)
+{
+    a.passes = (a.d.M + 16 * kM - 1) / (16 * kM);
+    // the longest chunk whose x and scales a workgroup's threads hold at once, no longer than K
+    const int rows = a.d.M < 16 * kM ? a.d.M : 16 * kM;
+    const long room = (long)w4_pieces(kM) * kW4Threads * 16;
+    a.chunk_shift = 0;
+    while ((kW4Chunk << a.chunk_shift) < a.d.K && (kW4Waves << (a.chunk_shift + 1)) * (4 / kRuns) * 16 * kN <= kW4Scales * kW4Threads && rows * (long)(2 * kW4Chunk << a.chunk_shift) * (long)sizeof(X) <= room) ++a.chunk_shift;
+    const int chunk = kW4Chunk << a.chunk_shift;
+    a.chunks = (a.d.K + chunk - 1) / chunk;
+    a.x_stride = chunk * (int)sizeof(X) + 16;
+    const int entries = (chunk / 128) * (4 / kRuns);
+    const size_t used = (size_t)kW4Waves * w4_stages(kN) * 1024 * kN + (16 * kN * (entries + 1) * 4 + 15) / 16 * 16 + (size_t)rows * a.x_stride;
+    const size_t sums = (size_t)kW4Waves * kM * 16 * 16 * kN * 4, shmem = used > sums ? used : sums;
+    auto kern = gemv_w4_kernel<X, S, kRuns, kM, kN>;
+    if (shmem > 64 * 1024) {
+        static std::once_flag once;
+        static int32_t once_rc;
+        std::call_once(once, [&] {
+            once_rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024),
+                                "hipFuncSetAttribute(gemv_w4_kernel)");
+        });
+        if (once_rc) return once_rc;
+    }
+    queue_kernel(kern, dim3(((a.d.N + 16 * kN - 1) / (16 * kN) + 7) / 8 * 8 * a.passes), dim3(kW4Threads), shmem, s, a);
+    return check_hip(hipGetLastError(), "nm_gemv_w4 launch");
+}
+template <typename X, typename S, int kRuns>
+static int32_t launch_w4_rows(const W4Args& a, hipStream_t s)
+{
+    // 32 columns to a workgroup read x half as often; 16 where there would be fewer workgroups than CUs
+    if (a.d.M <= 16) return a.d.N > 32 * 255 ? launch_w4_tiles<X, S, kRuns, 1, 2>(a, s) : launch_w4_tiles<X, S, kRuns, 1, 1>(a, s);
+    // tiles of 48 rows where that saves a pass over the weights (those and x of a chunk are what LDS holds)
+    return (a.d.M + 47) / 48 < (a.d.M + 31) / 32 ? launch_w4_tiles<X, S, kRuns, 3, 2>(a, s) : launch_w4_tiles<X, S, kRuns, 2, 2>(a, s);
+}
+template <typename X, typename S>
+static int32_t launch_w4_group(const W4Args& a, hipStream_t s)
+{
+    if (a.d.group == 32) return launch_w4_rows<X, S, 1>(a, s);
+    if (a.d.group == 64) return launch_w4_rows<X, S, 2>(a, s);
+    return launch_w4_rows<X, S, 4>(a, s);
+}
+template <typename X>
+int32_t launch_w4(const W4Args& a, hipStream_t s)
+{
+    return a.d.scale_dtype == NM_DT_F32 ? launch_w4_group<X, float>(a, s) : launch_w4_group<X, unsigned short>(a, s);
+}
+
+}  // namespace nm
