@@ -3,7 +3,9 @@
 // Bound by memory: N K / 2 bytes of weights, each read once, for 2 M operations a weight.  A workgroup has 16 or 32 columns (rows of W)
 // and all of K, which its eight wavefronts share in blocks of 128; their sums are joined through LDS, so that columns alone need not
 // fill the GPU.  K goes by chunks: x of a chunk, and the chunk's scales as fp32, lie in LDS (the next chunk's are on their way into
-// registers), and a wavefront takes a run of the chunk's blocks.  Weights go directly into LDS, a ring of blocks for each wavefront.
+// registers), and a wavefront takes a run of the chunk's blocks.  Where a chunk or two are all of K (few rows), weights go
+// directly into LDS, a ring of blocks for each wavefront; with more chunks through registers, for whoever waits for a chunk's x would
+// wait for the whole ring (33 rows, 8192 x 8192: 29 us with the ring).
 //   Four neighbouring lanes load 64 bytes, 128 weights, of a row, a run of 32 each: neighbouring lanes in different rows, as the matrix
 // instruction wants them, cost the address unit four times as much (28672 x 8192: 54 us so, 2.2 TB/s).  From LDS lane (j, row) then
 // gets run j of its row.  The 16x16x32 instruction (rows of x its rows, columns its columns) adds over the four lanes of a
@@ -29,7 +31,8 @@ typedef unsigned v2u __attribute__((ext_vector_type(2)));
 
 constexpr int kW4Waves = 8, kW4Threads = 64 * kW4Waves;
 
-constexpr int kW4Scales = 8;    // scales that a thread has of a chunk
+// Scales that a thread has of a chunk.
+constexpr int w4_scales(int tiles) { return tiles == 1 ? 8 : 2; }
 
 struct W4Args {
     nm_w4_desc d;
@@ -42,10 +45,10 @@ struct W4Args {
 };
 constexpr int kW4Chunk = 128 * kW4Waves;
 
-// Pieces of 16 bytes of x that a thread has of a chunk: as many as 1024 columns of 16-bit rows are.
-constexpr int w4_pieces(int tiles) { return 4 * tiles; }
-// Blocks of a wavefront's ring: 16 columns are 1 KB of each.
-constexpr int w4_stages(int columns) { return columns == 1 ? 4 : 3; }
+// Pieces of 16 bytes of x that a thread has of a chunk: of 1024 columns of 16-bit rows and more.
+constexpr int w4_pieces(int tiles, bool ring) { return tiles == 1 && !ring ? 8 : 4 * tiles; }
+// Blocks of a wavefront's ring in LDS (16 columns are 1 KB of each), or its places for blocks in LDS where registers hold the next two.
+constexpr int w4_stages(int columns, bool ring) { return !ring ? 1 : columns == 1 ? 4 : 3; }
 
 template <typename X>
 int32_t launch_w4(const W4Args& a, hipStream_t s);
@@ -119,20 +122,20 @@ template <> struct W4<bf16> : W4Half<bf16> {};
 template <> struct W4<f16> : W4Half<f16> {};
 
 // S: bits of a scale (float, or either 16-bit type); kRuns: runs of 32 weights to a scale within a block of 128 (1, 2, 4); kM: tiles of
-// 16 rows; kN: of 16 columns.
-template <typename X, typename S, int kRuns, int kM, int kN>
-__global__ __launch_bounds__(kW4Threads, kM == 1 ? 4 : 2) void gemv_w4_kernel(W4Args a)
+// 16 rows; kN: of 16 columns; kRing: weights by a ring in LDS.
+template <typename X, typename S, int kRuns, int kM, int kN, bool kRing>
+__global__ __launch_bounds__(kW4Threads, kRing ? 4 : 2) void gemv_w4_kernel(W4Args a)
 {
     typedef W4<X> Q;
     typedef typename Q::Rows Rows;
     typedef typename Q::Sum Sum;
     constexpr int kScales = 4 / kRuns;                        // to a block
     constexpr int kCols = 16 * kN, kPer16 = 16 / (int)sizeof(X);
-    constexpr int kPieces = w4_pieces(kM);         // of x, 16 bytes, that a thread has of a chunk
+    constexpr int kPieces = w4_pieces(kM, kRing);         // of x, 16 bytes, that a thread has of a chunk
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const nm_w4_desc& d = a.d;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, column = lane & 15, j = lane >> 4;
-    constexpr int kStages = w4_stages(kN);
+    constexpr int kStages = w4_stages(kN, kRing);
     // the passes over the same columns are neighbours on an XCD (workgroup i runs on XCD i mod 8)
     const int pass = blockIdx.x / 8 % a.passes, n0 = (blockIdx.x / 8 / a.passes * 8 + blockIdx.x % 8) * kCols;
     const int m0 = pass * 16 * kM, rows = min(d.M - m0, 16 * kM);
@@ -153,23 +156,29 @@ __global__ __launch_bounds__(kW4Threads, kM == 1 ? 4 : 2) void gemv_w4_kernel(W4
     for (int c = 0; c < kN; ++c) wrow[c] = d.W + (long)min(n0 + c * 16 + (lane >> 2), d.N - 1) * (d.K / 2);
     const int total = a.chunks * run;                         // the wavefront's blocks
     const unsigned ring = (unsigned)(uintptr_t)smem + wave * kStages * 1024 * kN;
-    auto request = [&](int u, int slot) {                     // block number u
+    auto bytes_of = [&](int u) {                              // of the lane's piece of block number u, from the row's begin
         const int kb = ((u >> a.chunk_shift) * kW4Waves + wave) * run + (u & (run - 1));
-        const int k = min(kb * 128 + ((lane & 3) ^ (lane >> 4 & 3)) * 32, d.K - 32);
+        return min(kb * 128 + ((lane & 3) ^ (lane >> 4 & 3)) * 32, d.K - 32) / 2;
+    };
+    auto request = [&](int u, int slot) {
+        const int at = bytes_of(u);
 #pragma unroll
-        for (int c = 0; c < kN; ++c) dma16(wrow[c] + k / 2, ring + (slot * kN + c) * 1024);
+        for (int c = 0; c < kN; ++c) dma16(wrow[c] + at, ring + (slot * kN + c) * 1024);
     };
     const int read_at = (column * 4 + (j ^ (column >> 2))) * 16;
 
     // x and scales of a chunk: into registers, then into LDS (x in the order that the matrix instructions want)
-    const int row_shift = a.chunk_shift + (sizeof(X) == 1 ? 6 : 7);   // pieces to a row of a chunk
+    constexpr int kW4Scales = w4_scales(kM);
+    const int row_shift = a.chunk_shift + (sizeof(X) == 1 ? 6 : 7);   // pieces to a row of a chunk: 64 and more, so a wavefront's are of one row
+    const int uniform_wave = __builtin_amdgcn_readfirstlane(wave);
     v4u xp[kPieces];
     S sp[kW4Scales];
     auto fetch = [&](int chunk) {
 #pragma unroll
         for (int q = 0; q < kPieces; ++q) {
-            const int p = tid + q * kW4Threads, r = min(p >> row_shift, rows - 1), k = chunk * (kW4Chunk << a.chunk_shift) + (p & ((1 << row_shift) - 1)) * kPer16;
-            xp[q] = *reinterpret_cast<const v4u*>(static_cast<const X*>(d.x) + (long)(m0 + r) * d.x_stride + min(k, d.K - kPer16));
+            const int p = uniform_wave * 64 + q * kW4Threads, r = min(p >> row_shift, rows - 1);
+            const int k = (chunk * (kW4Chunk << a.chunk_shift) + (p & ((1 << row_shift) - 1)) * kPer16) + lane * kPer16;
+            xp[q] = *reinterpret_cast<const v4u*>(static_cast<const X*>(d.x) + (long)(m0 + r) * d.x_stride + (unsigned)min(k, d.K - kPer16));
         }
 #pragma unroll
         for (int q = 0; q < kW4Scales; ++q) {
@@ -182,8 +191,17 @@ __global__ __launch_bounds__(kW4Threads, kM == 1 ? 4 : 2) void gemv_w4_kernel(W4
     auto stage = [&](int chunk) {
 #pragma unroll
         for (int q = 0; q < kPieces; ++q) {
-            const int p = tid + q * kW4Threads, r = p >> row_shift, at = p & ((1 << row_shift) - 1), k = chunk * (kW4Chunk << a.chunk_shift) + at * kPer16;
-            if (r < rows) *reinterpret_cast<v4u*>(s_x + r * a.x_stride + at * 16) = k < d.K ? Q::order(xp[q]) : v4u{};
+            const int p = uniform_wave * 64 + q * kW4Threads, r = p >> row_shift, at = p & ((1 << row_shift) - 1);
+            if (r < rows) *reinterpret_cast<v4u*>(s_x + r * a.x_stride + at * 16 + lane * 16) = Q::order(xp[q]);
+        }
+        if ((chunk + 1) * (kW4Chunk << a.chunk_shift) > d.K) {        // zeros behind K
+            asm volatile("");
+#pragma unroll 1
+            for (int q = 0; q < kPieces; ++q) {
+                const int p = uniform_wave * 64 + q * kW4Threads, r = p >> row_shift, at = p & ((1 << row_shift) - 1);
+                if (r < rows && (chunk * (kW4Chunk << a.chunk_shift) + at * kPer16) + lane * kPer16 >= d.K)
+                    *reinterpret_cast<v4u*>(s_x + r * a.x_stride + at * 16 + lane * 16) = v4u{};
+            }
         }
 #pragma unroll
         for (int q = 0; q < kW4Scales; ++q) {
@@ -213,50 +231,23 @@ __global__ __launch_bounds__(kW4Threads, kM == 1 ? 4 : 2) void gemv_w4_kernel(W4
             for (int c = 0; c < kN; ++c) scale[c] = srow[c * 16 * (entries + 1) + at * kScales + g];
             auto rows_of = [&](int t, int i) { return *reinterpret_cast<const Rows*>(xrow[t] + (at * 128 + i * 32) * sizeof(X)); };
             Sum acc[kM][kN];
-            if constexpr (kM <= 2) {                          // the offset is where the sums begin
-                Rows x[kM][kRuns];
+            Rows x[kM][kRuns];
 #pragma unroll
-                for (int t = 0; t < kM; ++t) {
-                    Sum off{};
+            for (int t = 0; t < kM; ++t) {                    // the offset is where the sums begin
+                Sum off{};
 #pragma unroll
-                    for (int i = 0; i < kRuns; ++i) off = Q::offset(x[t][i] = rows_of(t, g * kRuns + i), off);
+                for (int i = 0; i < kRuns; ++i) off = Q::offset(x[t][i] = rows_of(t, g * kRuns + i), off);
 #pragma unroll
-                    for (int c = 0; c < kN; ++c) acc[t][c] = off;
-                }
-#pragma unroll
-                for (int i = 0; i < kRuns; ++i)
-#pragma unroll
-                    for (int c = 0; c < kN; ++c) {
-                        const auto weights = Q::weights(now[c][g * kRuns + i], exponent);
-#pragma unroll
-                        for (int t = 0; t < kM; ++t) acc[t][c] = Q::add(x[t][i], weights, acc[t][c]);
-                    }
-            } else {                                          // or is added to them: fewer registers of x at a time
-                Sum off[kM];
-#pragma unroll
-                for (int i = 0; i < kRuns; ++i) {
-                    Rows x[kM];
-#pragma unroll
-                    for (int t = 0; t < kM; ++t) {
-                        x[t] = rows_of(t, g * kRuns + i);
-                        off[t] = Q::offset(x[t], i ? off[t] : Sum{});
-                    }
-#pragma unroll
-                    for (int c = 0; c < kN; ++c) {
-                        const auto weights = Q::weights(now[c][g * kRuns + i], exponent);
-#pragma unroll
-                        for (int t = 0; t < kM; ++t) acc[t][c] = Q::add(x[t], weights, i ? acc[t][c] : Sum{});
-                    }
-                }
-                if constexpr (sizeof(X) > 1) {
-#pragma unroll
-                    for (int t = 0; t < kM; ++t)
-#pragma unroll
-                        for (int c = 0; c < kN; ++c)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[t][c][e] += off[t][e];
-                }
+                for (int c = 0; c < kN; ++c) acc[t][c] = off;
             }
+#pragma unroll
+            for (int i = 0; i < kRuns; ++i)
+#pragma unroll
+                for (int c = 0; c < kN; ++c) {
+                    const auto weights = Q::weights(now[c][g * kRuns + i], exponent);
+#pragma unroll
+                    for (int t = 0; t < kM; ++t) acc[t][c] = Q::add(x[t][i], weights, acc[t][c]);
+                }
 #pragma unroll
             for (int t = 0; t < kM; ++t)
 #pragma unroll
@@ -266,29 +257,59 @@ __global__ __launch_bounds__(kW4Threads, kM == 1 ? 4 : 2) void gemv_w4_kernel(W4
         }
     };
 
-    fetch(0);
-#pragma unroll
-    for (int u = 0; u < kStages; ++u)
-        if (u < total) request(u, u);
-    for (int u = 0, slot = 0; u < total; ++u, slot = slot + 1 == kStages ? 0 : slot + 1) {
-        if (!(u & (run - 1))) {
-            const int chunk = u >> a.chunk_shift;
-            if (chunk) __syncthreads();
-            stage(chunk);
-            if (chunk + 1 < a.chunks) fetch(chunk + 1);
-            __syncthreads();
-        }
-        // what was requested behind this block may still be under way; at the end nothing is requested any more
-        if (u + kStages <= total) wait_vmcnt<(kStages - 1) * kN>();
-        else wait_vmcnt<0>();
-        v4u now[kN];
+    auto next_chunk = [&](int chunk) {
+        if (chunk) __syncthreads();
+        stage(chunk);
+        if (chunk + 1 < a.chunks) fetch(chunk + 1);
+        __syncthreads();
+    };
+    auto read = [&](v4u (&now)[kN], int slot) {
 #pragma unroll
         for (int c = 0; c < kN; ++c) now[c] = *reinterpret_cast<const v4u*>(s_w + (slot * kN + c) * 1024 + read_at);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // the slot is read before it is written again
-        if (u + kStages < total) request(u + kStages, slot);
+    };
+    fetch(0);
+    if constexpr (kRing) {
 #pragma unroll
-        for (int c = 0; c < kN; ++c) now[c] = exchange(now[c]);
-        block(u & (run - 1), now);
+        for (int u = 0; u < kStages; ++u)
+            if (u < total) request(u, u);
+        for (int u = 0, slot = 0; u < total; ++u, slot = slot + 1 == kStages ? 0 : slot + 1) {
+            if (!(u & (run - 1))) next_chunk(u >> a.chunk_shift);
+            // what was requested behind this block may still be under way; at the end nothing is requested any more
+            if (u + kStages <= total) wait_vmcnt<(kStages - 1) * kN>();
+            else wait_vmcnt<0>();
+            v4u now[kN];
+            read(now, slot);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // the slot is read before it is written again
+            if (u + kStages < total) request(u + kStages, slot);
+#pragma unroll
+            for (int c = 0; c < kN; ++c) now[c] = exchange(now[c]);
+            block(u & (run - 1), now);
+        }
+    } else {
+        v4u w[2][kN];
+        auto load = [&](int u, v4u (&to)[kN]) {
+            const int at = bytes_of(u);
+#pragma unroll
+            for (int c = 0; c < kN; ++c) to[c] = *reinterpret_cast<const v4u*>(wrow[c] + at);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        load(0, w[0]);
+        load(1, w[1]);
+        for (int u0 = 0; u0 < total; u0 += 2)
+#pragma unroll
+            for (int odd = 0; odd < 2; ++odd) {
+                const int u = u0 + odd;
+                if (u >= total) break;
+                if (!(u & (run - 1))) next_chunk(u >> a.chunk_shift);
+#pragma unroll
+                for (int c = 0; c < kN; ++c) *reinterpret_cast<v4u*>(s_w + c * 1024 + lane * 16) = w[odd][c];
+                load(u + 2, w[odd]);                          // behind the last block: the last run, not used
+                v4u now[kN];
+                read(now, 0);
+#pragma unroll
+                for (int c = 0; c < kN; ++c) now[c] = exchange(now[c]);
+                block(u & (run - 1), now);
+            }
     }
     __syncthreads();
     float (*s_sum)[kM][16][kCols] = reinterpret_cast<float (*)[kM][16][kCols]>(smem);
@@ -314,22 +335,24 @@ __global__ __launch_bounds__(kW4Threads, kM == 1 ? 4 : 2) void gemv_w4_kernel(W4
     }
 }
 
-template <typename X, typename S, int kRuns, int kM, int kN>
+template <typename X, typename S, int kRuns, int kM, int kN, bool kRing>
 static int32_t launch_w4_tiles(W4Args a, hipStream_t s)
 {
     a.passes = (a.d.M + 16 * kM - 1) / (16 * kM);
     // the longest chunk whose x and scales a workgroup's threads hold at once, no longer than K
     const int rows = a.d.M < 16 * kM ? a.d.M : 16 * kM;
-    const long room = (long)w4_pieces(kM) * kW4Threads * 16;
+    const long room = (long)w4_pieces(kM, kRing) * kW4Threads * 16;
     a.chunk_shift = 0;
-    while ((kW4Chunk << a.chunk_shift) < a.d.K && (kW4Waves << (a.chunk_shift + 1)) * (4 / kRuns) * 16 * kN <= kW4Scales * kW4Threads && rows * (long)(2 * kW4Chunk << a.chunk_shift) * (long)sizeof(X) <= room) ++a.chunk_shift;
+    while ((kW4Chunk << a.chunk_shift) < a.d.K && (kW4Waves << (a.chunk_shift + 1)) * (4 / kRuns) * 16 * kN <= w4_scales(kM) * kW4Threads && rows * (long)(2 * kW4Chunk << a.chunk_shift) * (long)sizeof(X) <= room) ++a.chunk_shift;
     const int chunk = kW4Chunk << a.chunk_shift;
     a.chunks = (a.d.K + chunk - 1) / chunk;
+    if constexpr (kRing)
+        if (a.chunks > 2) return launch_w4_tiles<X, S, kRuns, kM, kN, false>(a, s);
     a.x_stride = chunk * (int)sizeof(X) + 16;
     const int entries = (chunk / 128) * (4 / kRuns);
-    const size_t used = (size_t)kW4Waves * w4_stages(kN) * 1024 * kN + (16 * kN * (entries + 1) * 4 + 15) / 16 * 16 + (size_t)rows * a.x_stride;
+    const size_t used = (size_t)kW4Waves * w4_stages(kN, kRing) * 1024 * kN + (16 * kN * (entries + 1) * 4 + 15) / 16 * 16 + (size_t)rows * a.x_stride;
     const size_t sums = (size_t)kW4Waves * kM * 16 * 16 * kN * 4, shmem = used > sums ? used : sums;
-    auto kern = gemv_w4_kernel<X, S, kRuns, kM, kN>;
+    auto kern = gemv_w4_kernel<X, S, kRuns, kM, kN, kRing>;
     if (shmem > 64 * 1024) {
         static std::once_flag once;
         static int32_t once_rc;
@@ -346,9 +369,9 @@ template <typename X, typename S, int kRuns>
 static int32_t launch_w4_rows(const W4Args& a, hipStream_t s)
 {
     // 32 columns to a workgroup read x half as often; 16 where there would be fewer workgroups than CUs
-    if (a.d.M <= 16) return a.d.N > 32 * 255 ? launch_w4_tiles<X, S, kRuns, 1, 2>(a, s) : launch_w4_tiles<X, S, kRuns, 1, 1>(a, s);
+    if (a.d.M <= 16) return a.d.N > 32 * 255 ? launch_w4_tiles<X, S, kRuns, 1, 2, true>(a, s) : launch_w4_tiles<X, S, kRuns, 1, 1, true>(a, s);
     // tiles of 48 rows where that saves a pass over the weights (those and x of a chunk are what LDS holds)
-    return (a.d.M + 47) / 48 < (a.d.M + 31) / 32 ? launch_w4_tiles<X, S, kRuns, 3, 2>(a, s) : launch_w4_tiles<X, S, kRuns, 2, 2>(a, s);
+    return (a.d.M + 47) / 48 < (a.d.M + 31) / 32 ? launch_w4_tiles<X, S, kRuns, 3, 2, false>(a, s) : launch_w4_tiles<X, S, kRuns, 2, 2, false>(a, s);
 }
 template <typename X, typename S>
 static int32_t launch_w4_group(const W4Args& a, hipStream_t s)
