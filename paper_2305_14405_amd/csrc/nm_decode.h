@@ -22,28 +22,30 @@ inline int page_shift(int32_t page_size)
     return -1;
 }
 
-// Four neighbouring elements.
-__device__ __forceinline__ v4f load4(const float* p) { return *reinterpret_cast<const v4f*>(p); }
-template <typename T>
-__device__ __forceinline__ v4f load4(const T* p)
+// N neighbouring elements, rounded once.  dtype is uniform, so this is a scalar branch; inv_scale for I8.
+template <typename T, int N>
+__device__ __forceinline__ void store_run_as(void* base, long at, const float (&v)[N])
 {
-    typedef T v4t __attribute__((ext_vector_type(4)));
-    return __builtin_convertvector(*reinterpret_cast<const v4t*>(p), v4f);
+    typedef T Vec __attribute__((ext_vector_type(N)));
+    Vec o;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = (T)v[i];
+    *reinterpret_cast<Vec*>(static_cast<T*>(base) + at) = o;
 }
-template <typename T>
-__device__ __forceinline__ void store4_as(void* base, long at, v4f v)
+template <int N>
+__device__ __forceinline__ void store_run(void* base, int dtype, long at, const float (&v)[N], float inv_scale)
 {
-    typedef T v4t __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<v4t*>(static_cast<T*>(base) + at) = __builtin_convertvector(v, v4t);
-}
-// dtype is uniform, so this is a scalar branch; inv_scale for I8.
-__device__ __forceinline__ void store4(void* base, int dtype, long at, v4f v, float inv_scale)
-{
-    if (dtype == NM_DT_BF16) store4_as<bf16>(base, at, v);
-    else if (dtype == NM_DT_F16) store4_as<f16>(base, at, v);
-    else if (dtype == NM_DT_F32) store4_as<float>(base, at, v);
-    else *reinterpret_cast<unsigned*>(static_cast<int8_t*>(base) + at) =
-             pack4(requant(v[0], inv_scale), requant(v[1], inv_scale), requant(v[2], inv_scale), requant(v[3], inv_scale));
+    if (dtype == NM_DT_BF16) store_run_as<bf16>(base, at, v);
+    else if (dtype == NM_DT_F16) store_run_as<f16>(base, at, v);
+    else if (dtype == NM_DT_F32) store_run_as<float>(base, at, v);
+    else {
+        typedef unsigned Vec __attribute__((ext_vector_type(N / 4)));
+        Vec o;
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i)
+            o[i] = pack4(requant(v[4 * i], inv_scale), requant(v[4 * i + 1], inv_scale), requant(v[4 * i + 2], inv_scale), requant(v[4 * i + 3], inv_scale));
+        *reinterpret_cast<Vec*>(static_cast<int8_t*>(base) + at) = o;
+    }
 }
 __device__ __forceinline__ void store1(void* base, int dtype, long at, float v, float inv_scale)
 {

@@ -1,23 +1,28 @@
 // Norms and rotation of a step's queries and keys, which leave for the cache with the values (nm_qk_norm_rope).
 //
 // Bound by memory: every element is read once and written once, with some ten operations on it.  A head's elements lie in the registers of
-// G lanes, eight to a lane as two groups of four whose members are each other's partners in the rotation (or neighbours, interleaved): the
-// sum of squares is a butterfly over G lanes, and no element crosses lanes.  The angles belong to the token: one
-// workgroup has (some of) a token's heads, rot / 2 of its threads make the sines and cosines while the first loads are under way, and all
-// heads read them from LDS.  An angle is reduced in 64 bits (position * frequency reaches 10^6 radians, where 32 bits would
-// leave 0.06 of error) and its sine taken in 32.
+// G lanes, two groups of neighbours to a lane (16 bytes each where sizes and addresses allow) that are each other's partners in the
+// rotation, or hold whole pairs: the sum of squares is a butterfly over G lanes, and no element crosses lanes.  The angles belong to the
+// token: a workgroup has up to eight tokens, a thread makes the sine and cosine of one of their angles while the first loads are
+// under way, and all heads read them from LDS.  An angle is reduced in 64 bits (position * frequency reaches 10^6
+// radians, where 32 bits would leave 0.06 of error) and its sine taken in 32.
 #include "nm_decode.h"
 
 namespace nm {
 
 constexpr int kRopeThreads = 256;
 
+constexpr int kRopeTokens = 8;
+
 struct QkArgs {
     nm_qk_desc d;
     int shift;          // log2 of page_size
     int heads;          // heads a token has here: hq + hk, and hk more of values where there is a cache
-    int per_block;      // heads a workgroup goes through
+    int tokens;         // of a workgroup, up to kRopeTokens
+    int per_block;      // heads of each that a workgroup goes through
+    FastDiv by_heads;   // by that
     unsigned slots;     // num_pages * page_size
+    float inv_d;
 };
 
 // cos and sin of position * inv_freq: whole turns are taken off in binary64.
@@ -51,100 +56,123 @@ __device__ __forceinline__ long cache_at(const nm_qk_desc& d, int shift, int slo
     return (long)(slot >> shift) * d.page_stride + (long)(slot & (d.page_size - 1)) * d.slot_stride + (long)h * d.head_stride;
 }
 
-// Whole groups of elements: d and rot multiples of 8.
-template <typename T, int G, bool kInterleaved>
+// E neighbours at once: d and rot multiples of 2 E.
+template <typename T, int E, int G, bool kInterleaved>
 __global__ __launch_bounds__(kRopeThreads) void qk_rope_kernel(QkArgs a)
 {
+    typedef T Vec __attribute__((ext_vector_type(E)));
     const nm_qk_desc& d = a.d;
-    __shared__ float2 s_cs[128];
-    const int tid = threadIdx.x, t = blockIdx.x;
-    const int l = tid % G, lanes = d.d / 8, half = d.rot / 2;
-    const bool mine = l < lanes;
-    // the lane's two groups of four elements
-    const bool turned = l * 8 < d.rot;
-    const int e0 = kInterleaved || !turned ? l * 8 : l * 4, e1 = kInterleaved || !turned ? l * 8 + 4 : half + l * 4;
-    const int slot = d.k_cache ? d.slots[t] : -1;
-    const bool kept = (unsigned)slot < a.slots;
-    const int first = blockIdx.y * a.per_block, last = min(first + a.per_block, a.heads);
-    auto wanted = [&](int head) { return head < last && mine && (head < d.hq || kept || (head < d.hq + d.hk && d.k_out)); };
+    __shared__ float2 s_cs[kRopeTokens][128];
+    __shared__ int s_slot[kRopeTokens];
+    const int tid = threadIdx.x, t0 = blockIdx.x * a.tokens, tokens = min(a.tokens, d.T - t0);
+    const int l = tid % G, half = d.rot / 2, rest = (d.d - d.rot) / 2;
+    const bool mine = l < d.d / (2 * E);
+    // the lane's two groups: of either half of the head (interleaved), of the rotated part, or of what is behind it
+    const bool turned = l * 2 * E < d.rot;
+    const int e0 = kInterleaved ? l * E : turned ? l * E : d.rot + l * E - half, e1 = e0 + (kInterleaved ? d.d / 2 : turned ? half : rest);
+    const int first = blockIdx.y * a.per_block, per = min(a.per_block, a.heads - first), all = tokens * a.per_block;
 
-    int head = first + tid / G;
-    v4f x0{}, x1{};
-    if (wanted(head)) {
-        const Head<T> at(d, t, head);
-        x0 = load4(at.in + e0);
-        x1 = load4(at.in + e1);
-    }
-    if (half) {
-        const int position = d.positions[t];
-        if (tid < half) s_cs[tid] = turn(position, d.inv_freq[tid]);
-        __syncthreads();
-    }
-    float2 cs[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) cs[i] = turned && mine ? s_cs[l * 4 + i] : make_float2(1.0f, 0.0f);
+    // item i: head first + i % per_block of token i / per_block (the last block of heads may be shorter: its items are skipped)
+    struct Item { int t, head; bool there; };
+    auto item_of = [&](int i) {
+        const int t = (int)quotient((unsigned)i, a.by_heads), head = i - t * a.per_block;
+        return Item{t, first + head, t < tokens && head < per};
+    };
+    auto load = [&](const Item& it, Vec& x0, Vec& x1) {
+        const int t = min(it.t, tokens - 1), head = min(it.head, first + per - 1);
+        const Head<T> at(d, t0 + t, head);
+        const T* from = at.in;
+        x0 = *reinterpret_cast<const Vec*>(from + (mine ? e0 : 0));
+        x1 = *reinterpret_cast<const Vec*>(from + (mine ? e1 : 0));
+    };
+    int i = tid / G;
+    Item now = item_of(i);
+    Vec n0, n1;
+    load(now, n0, n1);
 
-    for (; head - tid / G < last; head += kRopeThreads / G) {
-        const Head<T> at(d, t, head);
-        v4f n0{}, n1{};
-        const int next = head + kRopeThreads / G;
-        if (wanted(next)) {
-            const Head<T> to(d, t, next);
-            n0 = load4(to.in + e0);
-            n1 = load4(to.in + e1);
-        }
-        if (at.kind < 2 && (d.flags & NM_QK_NORM)) {
-            float sum = 0.0f;
+    typedef float Gamma __attribute__((ext_vector_type(4), aligned(4)));
+    float gq[2][E], gk[2][E];
+    if (d.flags & NM_QK_NORM) {
+        auto fetch_gamma = [&](const float* gamma, float (&g)[2][E]) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum = __builtin_fmaf(x0[i], x0[i], __builtin_fmaf(x1[i], x1[i], sum));
-            sum = group_sum<G>(sum);
-            const float r = 1.0f / sqrtf(sum / (float)d.d + d.eps);
-            const float* gamma = at.kind == 0 ? d.q_gamma : d.k_gamma;
-            v4f g0 = {1, 1, 1, 1}, g1 = g0;
-            if (gamma && mine) {
+            for (int part = 0; part < 2; ++part)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) { g0[i] = gamma[e0 + i]; g1[i] = gamma[e1 + i]; }
+                for (int e = 0; e < E; e += 4) {
+                    const Gamma v = gamma ? *reinterpret_cast<const Gamma*>(gamma + (mine ? (part ? e1 : e0) + e : 0)) : Gamma{1, 1, 1, 1};
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) g[part][e + n] = v[n];
+                }
+        };
+        fetch_gamma(d.q_gamma, gq);
+        fetch_gamma(d.k_gamma, gk);
+    }
+    for (int p = tid; p < tokens * half; p += kRopeThreads) {
+        const int t = p / half, angle = p - t * half;
+        s_cs[t][angle] = turn(d.positions[t0 + t], d.inv_freq[angle]);
+    }
+    if (tid < tokens) s_slot[tid] = d.k_cache ? d.slots[t0 + tid] : -1;
+    __syncthreads();
+
+    for (; i - tid / G < all; i += kRopeThreads / G) {
+        const Item it = now;
+        float x[2][E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) { x[0][e] = mine ? (float)n0[e] : 0.0f; x[1][e] = mine ? (float)n1[e] : 0.0f; }
+        now = item_of(i + kRopeThreads / G);
+        load(now, n0, n1);
+        if (!it.there) continue;                              // a whole group of lanes, as below
+        const Head<T> at(d, t0 + it.t, it.head);
+        if (at.kind < 2) {
+            if (d.flags & NM_QK_NORM) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum = __builtin_fmaf(x[0][e], x[0][e], __builtin_fmaf(x[1][e], x[1][e], sum));
+                sum = group_sum<G>(sum);
+                const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, a.inv_d, d.eps));
+                const bool query = at.kind == 0;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    x[0][e] = x[0][e] * r * (query ? gq[0][e] : gk[0][e]);
+                    x[1][e] = x[1][e] * r * (query ? gq[1][e] : gk[1][e]);
+                }
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { x0[i] = x0[i] * r * g0[i]; x1[i] = x1[i] * r * g1[i]; }
-        }
-        if (at.kind < 2 && half) {
             if (kInterleaved) {
-                const v4f y0 = x0, y1 = x1;
 #pragma unroll
-                for (int i = 0; i < 4; i += 2) {
-                    const float2 p = cs[i / 2], q = cs[2 + i / 2];
-                    x0[i] = y0[i] * p.x - y0[i + 1] * p.y;
-                    x0[i + 1] = y0[i + 1] * p.x + y0[i] * p.y;
-                    x1[i] = y1[i] * q.x - y1[i + 1] * q.y;
-                    x1[i + 1] = y1[i + 1] * q.x + y1[i] * q.y;
-                }
-            } else {
+                for (int part = 0; part < 2; ++part)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float p = x0[i], q = x1[i];
-                    x0[i] = p * cs[i].x - q * cs[i].y;
-                    x1[i] = q * cs[i].x + p * cs[i].y;
+                    for (int e = 0; e < E; e += 2) {
+                        const int angle = ((part ? e1 : e0) + e) / 2;
+                        const float2 cs = mine && angle < half ? s_cs[it.t][angle] : make_float2(1.0f, 0.0f);
+                        const float p = x[part][e], q = x[part][e + 1];
+                        x[part][e] = __builtin_fmaf(p, cs.x, -(q * cs.y));
+                        x[part][e + 1] = __builtin_fmaf(q, cs.x, p * cs.y);
+                    }
+            } else if (turned && mine) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float2 cs = s_cs[it.t][l * E + e];
+                    const float p = x[0][e], q = x[1][e];
+                    x[0][e] = __builtin_fmaf(p, cs.x, -(q * cs.y));
+                    x[1][e] = __builtin_fmaf(q, cs.x, p * cs.y);
                 }
             }
         }
-        if (wanted(head)) {
-            if (at.kind == 0 || (at.kind == 1 && d.k_out)) {
-                void* out = at.kind == 0 ? d.q_out : d.k_out;
-                const long to = t * (at.kind == 0 ? d.q_out_stride : d.k_out_stride) + (long)at.h * d.d;
-                store4(out, d.out_dtype, to + e0, x0, 0.0f);
-                store4(out, d.out_dtype, to + e1, x1, 0.0f);
-            }
-            if (at.kind > 0 && kept) {
-                const long to = cache_at(d, a.shift, slot, at.h);
-                void* cache = at.kind == 1 ? d.k_cache : d.v_cache;
-                const float inv = d.cache_dtype == NM_DT_I8 ? (at.kind == 1 ? d.k_inv_scale : d.v_inv_scale)[at.h] : 0.0f;
-                store4(cache, d.cache_dtype, to + e0, x0, inv);
-                store4(cache, d.cache_dtype, to + e1, x1, inv);
-            }
+        const int slot = s_slot[it.t];
+        const bool kept = (unsigned)slot < a.slots;
+        if (!mine) continue;
+        if (at.kind == 0 || (at.kind == 1 && d.k_out)) {
+            void* out = at.kind == 0 ? d.q_out : d.k_out;
+            const long to = (t0 + it.t) * (at.kind == 0 ? d.q_out_stride : d.k_out_stride) + (long)at.h * d.d;
+            store_run<E>(out, d.out_dtype, to + e0, x[0], 0.0f);
+            store_run<E>(out, d.out_dtype, to + e1, x[1], 0.0f);
         }
-        x0 = n0;
-        x1 = n1;
+        if (at.kind > 0 && kept) {
+            const long to = cache_at(d, a.shift, slot, at.h);
+            void* cache = at.kind == 1 ? d.k_cache : d.v_cache;
+            const float inv = d.cache_dtype == NM_DT_I8 ? (at.kind == 1 ? d.k_inv_scale : d.v_inv_scale)[at.h] : 0.0f;
+            store_run<E>(cache, d.cache_dtype, to + e0, x[0], inv);
+            store_run<E>(cache, d.cache_dtype, to + e1, x[1], inv);
+        }
     }
 }
 
@@ -183,7 +211,7 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_any_kernel(QkArgs a)
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[i], x[i], sum);
-            const float r = 1.0f / sqrtf(group_sum<64>(sum) / (float)d.d + d.eps);
+            const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(group_sum<64>(sum), a.inv_d, d.eps));
             const float* gamma = at.kind == 0 ? d.q_gamma : d.k_gamma;
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = x[i] * r * (gamma && e[i] < d.d ? gamma[e[i]] : 1.0f);
@@ -211,29 +239,43 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_any_kernel(QkArgs a)
     }
 }
 
-template <typename T, int G>
+template <typename T, int E, int G>
 static void launch_qk(const QkArgs& a, dim3 grid, hipStream_t s)
 {
-    if (a.d.flags & NM_ROPE_INTERLEAVED) queue_kernel(qk_rope_kernel<T, G, true>, grid, dim3(kRopeThreads), 0, s, a);
-    else queue_kernel(qk_rope_kernel<T, G, false>, grid, dim3(kRopeThreads), 0, s, a);
+    if (a.d.flags & NM_ROPE_INTERLEAVED) queue_kernel(qk_rope_kernel<T, E, G, true>, grid, dim3(kRopeThreads), 0, s, a);
+    else queue_kernel(qk_rope_kernel<T, E, G, false>, grid, dim3(kRopeThreads), 0, s, a);
 }
-
-template <typename T>
-static void launch_qk_t(QkArgs a, bool vec, hipStream_t s)
+template <typename T, int E>
+static void launch_qk_groups(QkArgs a, hipStream_t s)
 {
-    int G = 64;
-    if (vec)
-        for (G = 4; G < a.d.d / 8; G *= 2) {}
-    // workgroups that go through some heads of a token each: all of them where the tokens alone fill the GPU's 256 CUs a few times over, else
-    // one round of heads
+    int G = 4;
+    while (G < a.d.d / (2 * E)) G *= 2;
+    // Few tokens: a workgroup to a round of heads.  More: all heads of a token, of two or four, which share the sines, the gammas and the
+    // start of a workgroup.  (40 + 8 heads of 128 in bf16, us by a round / 1 / 2 / 4 / 8 tokens: 256 tokens 4.6 5.3 6.3 9.5 16, 1000 11 8.9 9.6
+    // 12 19, 2048 18 14.7 12.1 14 20, 4096 42 34 28 26 34, 16397 158 122 97 93 99.)  And as many tokens as fill a round.
     const int round = kRopeThreads / G;
-    a.per_block = a.d.T >= 1024 ? a.heads : round;
-    const dim3 grid(a.d.T, (a.heads + a.per_block - 1) / a.per_block);
-    if (!vec) queue_kernel(qk_rope_any_kernel<T>, grid, dim3(kRopeThreads), 0, s, a);
-    else if (G == 4) launch_qk<T, 4>(a, grid, s);
-    else if (G == 8) launch_qk<T, 8>(a, grid, s);
-    else if (G == 16) launch_qk<T, 16>(a, grid, s);
-    else launch_qk<T, 32>(a, grid, s);
+    a.tokens = a.d.T >= 4096 ? 4 : a.d.T >= 1536 ? 2 : 1;
+    if (round / a.heads > a.tokens) a.tokens = round / a.heads < kRopeTokens ? round / a.heads : kRopeTokens;
+    a.per_block = a.d.T >= 768 || a.heads < round ? a.heads : round;
+    a.by_heads = fast_div(a.per_block);
+    const dim3 grid((a.d.T + a.tokens - 1) / a.tokens, (a.heads + a.per_block - 1) / a.per_block);
+    if (G == 4) launch_qk<T, E, 4>(a, grid, s);
+    else if (G == 8) launch_qk<T, E, 8>(a, grid, s);
+    else if (G == 16) launch_qk<T, E, 16>(a, grid, s);
+    else if constexpr (E == 4) launch_qk<T, E, 32>(a, grid, s);
+}
+// run: neighbours that sizes and addresses allow at once, 8 or 4, or 0.
+template <typename T>
+static void launch_qk_t(QkArgs a, int run, hipStream_t s)
+{
+    if (sizeof(T) == 2 && run == 8) {
+        launch_qk_groups<T, 8>(a, s);
+    } else if (run) {
+        launch_qk_groups<T, 4>(a, s);
+    } else {
+        a.per_block = a.d.T >= 1024 ? a.heads : kRopeThreads / 64;
+        queue_kernel(qk_rope_any_kernel<T>, dim3(a.d.T, (a.heads + a.per_block - 1) / a.per_block), dim3(kRopeThreads), 0, s, a);
+    }
 }
 
 }  // namespace nm
@@ -274,15 +316,19 @@ extern "C" int32_t nm_qk_norm_rope(const nm_qk_desc* d, void* stream)
     QkArgs a{};
     a.d = *d;
     a.shift = shift;
+    a.inv_d = 1.0f / (float)d->d;
     a.heads = d->hq + d->hk + (d->k_cache ? d->hk : 0);
     a.slots = (unsigned)((int64_t)d->num_pages << shift);
-    const bool cache_vec = !d->k_cache || (aligned_rows(d->k_cache, d->page_stride, d->cache_dtype, 4) && aligned_rows(d->v_cache, d->slot_stride, d->cache_dtype, 4) &&
-                                           d->head_stride % 4 == 0 && aligned_rows(d->v, d->v_stride, d->in_dtype, 4));
-    const bool vec = d->d % 8 == 0 && d->rot % 8 == 0 && cache_vec && aligned_rows(d->q, d->q_stride, d->in_dtype, 4) &&
-                     aligned_rows(d->k, d->k_stride, d->in_dtype, 4) && aligned_rows(d->q_out, d->q_out_stride, d->out_dtype, 4) &&
-                     (!d->k_out || aligned_rows(d->k_out, d->k_out_stride, d->out_dtype, 4));
-    if (d->in_dtype == NM_DT_F32) launch_qk_t<float>(a, vec, (hipStream_t)stream);
-    else if (d->in_dtype == NM_DT_BF16) launch_qk_t<bf16>(a, vec, (hipStream_t)stream);
-    else launch_qk_t<f16>(a, vec, (hipStream_t)stream);
+    auto runs_of = [&](int n) {
+        const bool cache = !d->k_cache || (aligned_rows(d->k_cache, d->page_stride, d->cache_dtype, n) && aligned_rows(d->v_cache, d->slot_stride, d->cache_dtype, n) &&
+                                           d->head_stride % n == 0 && aligned_rows(d->v, d->v_stride, d->in_dtype, n));
+        return d->d % (2 * n) == 0 && d->rot % (2 * n) == 0 && cache && aligned_rows(d->q, d->q_stride, d->in_dtype, n) &&
+               aligned_rows(d->k, d->k_stride, d->in_dtype, n) && aligned_rows(d->q_out, d->q_out_stride, d->out_dtype, n) &&
+               (!d->k_out || aligned_rows(d->k_out, d->k_out_stride, d->out_dtype, n));
+    };
+    const int run = d->in_dtype != NM_DT_F32 && runs_of(8) ? 8 : runs_of(4) ? 4 : 0;
+    if (d->in_dtype == NM_DT_F32) launch_qk_t<float>(a, run, (hipStream_t)stream);
+    else if (d->in_dtype == NM_DT_BF16) launch_qk_t<bf16>(a, run, (hipStream_t)stream);
+    else launch_qk_t<f16>(a, run, (hipStream_t)stream);
     return check_hip(hipGetLastError(), "nm_qk_norm_rope launch");
 }
