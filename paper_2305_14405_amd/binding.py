@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libnm_hip.so")
@@ -194,11 +195,11 @@ def load(preload_torch: bool = True) -> C.CDLL:
     L.nm_encoder_stack_workspace.argtypes = [C.POINTER(LayerDesc), C.c_int32, C.POINTER(C.c_size_t)]
     L.nm_encoder_stack.argtypes = [C.POINTER(LayerDesc), C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
                                    C.c_void_p, C.c_size_t, C.c_void_p]
-    L.nm_page_plan.argtypes = [C.POINTER(PlanDesc), C.c_void_p]
-    L.nm_qk_norm_rope.argtypes = [C.POINTER(QkDesc), C.c_void_p]
-    L.nm_paged_attention_workspace.argtypes = [C.POINTER(PagedDesc), C.POINTER(C.c_size_t)]
-    L.nm_paged_attention.argtypes = [C.POINTER(PagedDesc), C.c_void_p, C.c_size_t, C.c_void_p]
-    L.nm_gemv_w4.argtypes = [C.POINTER(W4Desc), C.c_void_p]
+    L.nm_page_plan.argtypes = [C.c_void_p, C.c_void_p]   # PlanDesc, or its bytes
+    L.nm_qk_norm_rope.argtypes = [C.c_void_p, C.c_void_p]   # QkDesc, or its bytes
+    L.nm_paged_attention_workspace.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]   # PagedDesc, or its bytes
+    L.nm_paged_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    L.nm_gemv_w4.argtypes = [C.c_void_p, C.c_void_p]   # W4Desc, or its bytes
     _lib = L
     return L
 
@@ -574,162 +575,205 @@ def nm_cnn_run(ops, ws=None, stream=None, ws_bytes=None, op_array=None):
 # ---- one step of a decoder over a paged cache -----------------------------------------------------
 #
 # These calls' tensors may have strides, so what the C ABI cannot see is checked here: every tensor is on torch's current device,
-# has the type that the call wants of it, and lies as the call's addressing says.
+# has the type that the call wants of it, and lies as the call's addressing says.  A step's kernels take 4 to 10 us, so the checks are
+# written for speed: a description is packed into bytes in the layout of its structure (0.2 us; filling in a ctypes structure takes
+# 0.8) and handed over as they are.  make_*_desc makes one to keep; the calls take either it or what it is made of.
 
-_dtypes = None
+_dtypes = _f32 = _i32 = _u8 = _current = None
+_PLAN = struct.Struct("@6i6Pq6P")
+_QK = struct.Struct("@11i4x3P3q2Pf4x2PPqPq2P3q3P")
+_PAGED = struct.Struct("@10iPq2P3q2PPqPfiPqf4xP")
+_W4 = struct.Struct("@7i4xPq2Pf4x2Pi4xPqf4x")
 
 
 def _refuse(what):
     raise NmError(NM_ERR_INVALID_ARG, what)
 
 
-def _types():
-    global _dtypes
+def _here():
+    """Number of torch's current device; the types on the first call."""
+    global _dtypes, _f32, _i32, _u8, _current
     if _dtypes is None:
         import torch
-        _dtypes = {torch.int32: NM_DT_I32, torch.float32: NM_DT_F32, torch.bfloat16: NM_DT_BF16, torch.float16: NM_DT_F16,
-                   torch.int8: NM_DT_I8, torch.uint8: None}
-    return _dtypes
+        _f32, _i32, _u8 = torch.float32, torch.int32, torch.uint8
+        if torch.cuda.is_available():
+            _current_stream()                                 # also initialises the runtime
+            _current = _device or torch.cuda.current_device
+        else:
+            _current = lambda: -2  # noqa: E731  (no tensor is there)
+        _dtypes = {_i32: NM_DT_I32, _f32: NM_DT_F32, torch.bfloat16: NM_DT_BF16, torch.float16: NM_DT_F16, torch.int8: NM_DT_I8}
+    return _current()
 
 
-def _type(t, name):
+def _type(t, dev, name):
     """The library's number of a device tensor's type."""
-    if not t.is_cuda:
-        _refuse(f"{name} is not in device memory")
-    if _device is None:
-        _current_stream()
-    if _device is not None and t.get_device() != _device():
+    if t.get_device() != dev:                                 # -1 in host memory
         _refuse(f"{name} is not on the current device")
-    try:
-        return _types()[t.dtype]
-    except KeyError:
+    code = _dtypes.get(t.dtype)
+    if code is None:
         _refuse(f"{name}: no call takes {t.dtype}")
+    return code
 
 
-def _vector(t, dtype, n, name):
-    """Address of a contiguous tensor of n elements of one type; None for None."""
+def _vector(t, dtype, n, dev, name):
+    """Address of a contiguous tensor of n elements of one type; 0 for None."""
     if t is None:
-        return None
-    if _type(t, name) != dtype or t.numel() != n or not t.is_contiguous():
-        _refuse(f"{name}: a contiguous tensor of {n} elements of the call's type is wanted, got {tuple(t.shape)} of {t.dtype}")
+        return 0
+    if t.dtype is not dtype or t.get_device() != dev or t.numel() != n or not t.is_contiguous():
+        _refuse(f"{name}: a contiguous tensor of {n} elements of {dtype} on the current device is wanted, got {tuple(t.shape)} of {t.dtype} on {t.device}")
     return t.data_ptr()
 
 
 def _heads(t, T, h, d, name):
-    """Address and token stride of [T, h, d] whose heads lie one behind the other."""
-    if tuple(t.shape) != (T, h, d):
+    """Token stride of [T, h, d] whose heads lie one behind the other."""
+    if t.shape != (T, h, d):
         _refuse(f"{name}: shape {tuple(t.shape)}, wanted {(T, h, d)}")
     s0, s1, s2 = t.stride()
     if (s2 != 1 and d > 1) or (s1 != d and h > 1):
         _refuse(f"{name}: the heads of a token have to lie one behind the other")
-    return t.data_ptr(), s0 if T > 1 else max(s0, h * d)
+    return s0 if T > 1 else max(s0, h * d)
 
 
-def _cache(k_cache, v_cache, hk, d):
-    """dtype, (pages, page_size), (page, slot, head stride) of the two caches [pages, page_size, hk, d]."""
-    dtype = _type(k_cache, "k_cache")
-    pages, page, h, e = k_cache.shape
-    strides = k_cache.stride()
-    if (h, e) != (hk, d) or v_cache.shape != k_cache.shape:
-        _refuse(f"k_cache {tuple(k_cache.shape)} and v_cache {tuple(v_cache.shape)}: [pages, page_size, {hk}, {d}] is wanted")
-    if _type(v_cache, "v_cache") != dtype or v_cache.stride() != strides:
-        _refuse("k_cache and v_cache have to have one type and the same strides")
+def _cache(k_cache, v_cache, hk, d, dev):
+    """dtype, pages, page_size and strides of the two caches [pages, page_size, hk, d]."""
+    dtype = _type(k_cache, dev, "k_cache")
+    shape, strides = k_cache.shape, k_cache.stride()
+    if len(shape) != 4 or shape[2] != hk or shape[3] != d or v_cache.shape != shape:
+        _refuse(f"k_cache {tuple(shape)} and v_cache {tuple(v_cache.shape)}: [pages, page_size, {hk}, {d}] is wanted")
+    if v_cache.dtype is not k_cache.dtype or v_cache.get_device() != dev or v_cache.stride() != strides:
+        _refuse("k_cache and v_cache have to have one type and the same strides, on the current device")
     if strides[3] != 1 and d > 1:
         _refuse("the elements of a head have to be neighbours in the cache")
-    return dtype, pages, page, strides
+    return dtype, shape[0], shape[1], strides
 
 
-def nm_page_plan(cached, fresh, free_pages, free_begin, block_table, *, page_size, num_pages, free_end, slots, status, lens=None,
-                 row_start=None, positions=None, requests=None, stream=None):
-    """block_table: int32 [B, max_pages], rows may be apart; every other tensor is contiguous int32."""
-    B, i32 = cached.numel(), NM_DT_I32
-    if _type(block_table, "block_table") != i32 or block_table.dim() != 2 or block_table.shape[0] != B or \
-            (block_table.shape[1] > 1 and block_table.stride(1) != 1):
-        _refuse(f"block_table: int32 [{B}, max_pages] with neighbouring columns is wanted")
-    columns, n_free, T = block_table.shape[1], free_pages.numel(), slots.numel()
-    d = PlanDesc(B, page_size, num_pages, columns, n_free, T, _vector(cached, i32, B, "cached"), _vector(fresh, i32, B, "fresh"),
-                 _vector(free_pages, i32, n_free, "free_pages"), _vector(free_begin, i32, 1, "free_begin"), _vector(free_end, i32, 1, "free_end"),
-                 block_table.data_ptr(), block_table.stride(0) if B > 1 else columns, _vector(lens, i32, B, "lens"),
-                 _vector(row_start, i32, B + 1, "row_start"), _vector(slots, i32, T, "slots"), _vector(positions, i32, T, "positions"),
-                 _vector(requests, i32, T, "requests"), _vector(status, i32, 4, "status"))
-    _check(load().nm_page_plan(C.byref(d), _stream(stream)))
+def _table(t, B, dev):
+    """Columns and row stride of a block table."""
+    if t.dtype is not _i32 or t.get_device() != dev or t.dim() != 2 or t.shape[0] != B or (t.shape[1] > 1 and t.stride(1) != 1):
+        _refuse(f"block_table: int32 [{B}, max_pages] with neighbouring columns on the current device is wanted")
+    columns = t.shape[1]
+    return columns, t.stride(0) if B > 1 else columns
 
 
-def nm_qk_norm_rope(q, k, v, positions, inv_freq, q_out, *, k_out=None, k_cache=None, v_cache=None, slots=None, norm=False, q_gamma=None,
-                    k_gamma=None, eps=1e-6, interleaved=False, k_inv_scale=None, v_inv_scale=None, stream=None):
+def make_plan_desc(cached, fresh, free_pages, free_begin, block_table, *, page_size, num_pages, free_end, slots, status, lens=None,
+                   row_start=None, positions=None, requests=None) -> bytes:
+    """block_table: int32 [B, max_pages], rows may be apart; every other tensor is contiguous int32.  The description refers to the
+    tensors' memory: keep them."""
+    dev = _here()
+    B, n_free, T = cached.numel(), free_pages.numel(), slots.numel()
+    columns, stride = _table(block_table, B, dev)
+    return _PLAN.pack(B, page_size, num_pages, columns, n_free, T, _vector(cached, _i32, B, dev, "cached"), _vector(fresh, _i32, B, dev, "fresh"),
+                      _vector(free_pages, _i32, n_free, dev, "free_pages"), _vector(free_begin, _i32, 1, dev, "free_begin"),
+                      _vector(free_end, _i32, 1, dev, "free_end"), block_table.data_ptr(), stride, _vector(lens, _i32, B, dev, "lens"),
+                      _vector(row_start, _i32, B + 1, dev, "row_start"), _vector(slots, _i32, T, dev, "slots"),
+                      _vector(positions, _i32, T, dev, "positions"), _vector(requests, _i32, T, dev, "requests"), _vector(status, _i32, 4, dev, "status"))
+
+
+def nm_page_plan(*tensors, stream=None, **more):
+    """make_plan_desc's arguments, or a description."""
+    desc = tensors[0] if len(tensors) == 1 else make_plan_desc(*tensors, **more)
+    rc = load().nm_page_plan(desc, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def make_qk_desc(q, k, v, positions, inv_freq, q_out, *, k_out=None, k_cache=None, v_cache=None, slots=None, norm=False, q_gamma=None,
+                 k_gamma=None, eps=1e-6, interleaved=False, k_inv_scale=None, v_inv_scale=None) -> bytes:
     """q, q_out: [T, hq, d]; k, v, k_out: [T, hk, d]; caches: [pages, page_size, hk, d] with strides; inv_freq (rot / 2 numbers) and
-    positions may be None: no rotation."""
+    positions may be None: no rotation.  The description refers to the tensors' memory: keep them."""
+    dev = _here()
     T, hq, e = q.shape
-    hk, f32, i32 = k.shape[1], NM_DT_F32, NM_DT_I32
-    in_dtype, out_dtype = _type(q, "q"), _type(q_out, "q_out")
+    hk = k.shape[1]
+    in_dtype, out_dtype = _type(q, dev, "q"), _type(q_out, dev, "q_out")
     rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-    if _type(k, "k") != in_dtype or (k_out is not None and _type(k_out, "k_out") != out_dtype):
-        _refuse("q and k, and q_out and k_out, have to have one type")
-    qp, qs = _heads(q, T, hq, e, "q")
-    kp, ks = _heads(k, T, hk, e, "k")
-    op, os_ = _heads(q_out, T, hq, e, "q_out")
-    up, us = (None, 0) if k_out is None else _heads(k_out, T, hk, e, "k_out")
-    d = QkDesc(T, hq, hk, e, rot, (NM_QK_NORM if norm else 0) | (NM_ROPE_INTERLEAVED if interleaved else 0), in_dtype, out_dtype)
-    d.q, d.q_stride, d.k, d.k_stride, d.q_out, d.q_out_stride, d.k_out, d.k_out_stride = qp, qs, kp, ks, op, os_, up, us
-    d.q_gamma, d.k_gamma, d.eps = _vector(q_gamma, f32, e, "q_gamma"), _vector(k_gamma, f32, e, "k_gamma"), eps
-    if rot:
-        d.positions, d.inv_freq = _vector(positions, i32, T, "positions"), _vector(inv_freq, f32, rot // 2, "inv_freq")
+    if k.dtype is not q.dtype or k.get_device() != dev:
+        _refuse("q and k have to have one type, on the current device")
+    k_out_at = k_out_stride = v_at = v_stride = cache_dtype = pages = page = k_at = vc_at = slots_at = s0 = s1 = s2 = 0
+    if k_out is not None:
+        if _type(k_out, dev, "k_out") != out_dtype:
+            _refuse("q_out and k_out have to have one type")
+        k_out_at, k_out_stride = k_out.data_ptr(), _heads(k_out, T, hk, e, "k_out")
     if k_cache is not None or v_cache is not None:
-        if k_cache is None or v_cache is None or slots is None:
-            _refuse("k_cache, v_cache and slots belong together")
-        if _type(v, "v") != in_dtype:
-            _refuse("q, k and v have to have one type")
-        d.v, d.v_stride = _heads(v, T, hk, e, "v")
-        d.cache_dtype, d.num_pages, d.page_size, (d.page_stride, d.slot_stride, d.head_stride, _) = _cache(k_cache, v_cache, hk, e)
-        d.k_cache, d.v_cache, d.slots = k_cache.data_ptr(), v_cache.data_ptr(), _vector(slots, i32, T, "slots")
-        d.k_inv_scale, d.v_inv_scale = _vector(k_inv_scale, f32, hk, "k_inv_scale"), _vector(v_inv_scale, f32, hk, "v_inv_scale")
-    _check(load().nm_qk_norm_rope(C.byref(d), _stream(stream)))
+        if k_cache is None or v_cache is None or slots is None or v is None:
+            _refuse("v, k_cache, v_cache and slots belong together")
+        if v.dtype is not q.dtype or v.get_device() != dev:
+            _refuse("q, k and v have to have one type, on the current device")
+        v_at, v_stride = v.data_ptr(), _heads(v, T, hk, e, "v")
+        cache_dtype, pages, page, (s0, s1, s2, _) = _cache(k_cache, v_cache, hk, e, dev)
+        k_at, vc_at, slots_at = k_cache.data_ptr(), v_cache.data_ptr(), _vector(slots, _i32, T, dev, "slots")
+    return _QK.pack(T, hq, hk, e, rot, (NM_QK_NORM if norm else 0) | (NM_ROPE_INTERLEAVED if interleaved else 0), in_dtype, out_dtype, cache_dtype,
+                    pages, page, q.data_ptr(), k.data_ptr(), v_at, _heads(q, T, hq, e, "q"), _heads(k, T, hk, e, "k"), v_stride,
+                    _vector(q_gamma, _f32, e, dev, "q_gamma"), _vector(k_gamma, _f32, e, dev, "k_gamma"), eps,
+                    _vector(positions, _i32, T, dev, "positions") if rot else 0, _vector(inv_freq, _f32, rot // 2, dev, "inv_freq"),
+                    q_out.data_ptr(), _heads(q_out, T, hq, e, "q_out"), k_out_at, k_out_stride, k_at, vc_at, s0, s1, s2, slots_at,
+                    _vector(k_inv_scale, _f32, hk, dev, "k_inv_scale"), _vector(v_inv_scale, _f32, hk, dev, "v_inv_scale"))
+
+
+def nm_qk_norm_rope(*tensors, stream=None, **more):
+    """make_qk_desc's arguments, or a description."""
+    desc = tensors[0] if len(tensors) == 1 else make_qk_desc(*tensors, **more)
+    rc = load().nm_qk_norm_rope(desc, _stream(stream))
+    if rc:
+        _check(rc)
 
 
 def make_paged_desc(q, k_cache, v_cache, block_table, lens, out, *, scale, window=0, k_scale=None, v_scale=None, out_inv_scale=1.0,
-                    lse=None) -> PagedDesc:
+                    lse=None) -> bytes:
     """q, out: [B, hq, d]; caches: [pages, page_size, hk, d] with strides; block_table: int32 [B, max_pages].  The description
     refers to the tensors' memory: keep them."""
+    dev = _here()
     B, hq, e = q.shape
-    hk, f32 = k_cache.shape[2], NM_DT_F32
-    dtype, pages, page, strides = _cache(k_cache, v_cache, hk, e)
-    if _type(block_table, "block_table") != NM_DT_I32 or block_table.dim() != 2 or block_table.shape[0] != B or \
-            (block_table.shape[1] > 1 and block_table.stride(1) != 1):
-        _refuse(f"block_table: int32 [{B}, max_pages] with neighbouring columns is wanted")
-    columns = block_table.shape[1]
-    qp, qs = _heads(q, B, hq, e, "q")
-    op, os_ = _heads(out, B, hq, e, "out")
-    return PagedDesc(B, hq, hk, e, _type(q, "q"), dtype, _type(out, "out"), page, pages, columns, qp, qs, k_cache.data_ptr(), v_cache.data_ptr(),
-                     strides[0], strides[1], strides[2], _vector(k_scale, f32, hk, "k_scale"), _vector(v_scale, f32, hk, "v_scale"),
-                     block_table.data_ptr(), block_table.stride(0) if B > 1 else columns, _vector(lens, NM_DT_I32, B, "lens"), scale, window,
-                     op, os_, out_inv_scale, _vector(lse, f32, B * hq, "lse"))
+    hk = k_cache.shape[2]
+    dtype, pages, page, (s0, s1, s2, _) = _cache(k_cache, v_cache, hk, e, dev)
+    columns, table_stride = _table(block_table, B, dev)
+    return _PAGED.pack(B, hq, hk, e, _type(q, dev, "q"), dtype, _type(out, dev, "out"), page, pages, columns, q.data_ptr(), _heads(q, B, hq, e, "q"),
+                       k_cache.data_ptr(), v_cache.data_ptr(), s0, s1, s2, _vector(k_scale, _f32, hk, dev, "k_scale"),
+                       _vector(v_scale, _f32, hk, dev, "v_scale"), block_table.data_ptr(), table_stride, _vector(lens, _i32, B, dev, "lens"), scale,
+                       window, out.data_ptr(), _heads(out, B, hq, e, "out"), out_inv_scale, _vector(lse, _f32, B * hq, dev, "lse"))
 
 
 def nm_paged_attention_workspace(*tensors, **more) -> int:
     """Bytes; takes what nm_paged_attention takes, or a description."""
-    desc = tensors[0] if isinstance(tensors[0], PagedDesc) else make_paged_desc(*tensors, **more)
+    desc = tensors[0] if len(tensors) == 1 else make_paged_desc(*tensors, **more)
     n = C.c_size_t()
-    _check(load().nm_paged_attention_workspace(C.byref(desc), C.byref(n)))
+    _check(load().nm_paged_attention_workspace(desc, C.byref(n)))
     return n.value
 
 
 def nm_paged_attention(*tensors, ws=None, stream=None, ws_bytes=None, **more):
     """make_paged_desc's arguments, or a description."""
-    desc = tensors[0] if isinstance(tensors[0], PagedDesc) else make_paged_desc(*tensors, **more)
-    nbytes = 0 if ws is None else ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
-    _check(load().nm_paged_attention(C.byref(desc), _ptr(ws), nbytes, _stream(stream)))
+    desc = tensors[0] if len(tensors) == 1 else make_paged_desc(*tensors, **more)
+    at = 0
+    if ws is not None:
+        if ws.get_device() != _here() or not ws.is_contiguous():
+            _refuse("ws: contiguous memory on the current device is wanted")
+        at, ws_bytes = ws.data_ptr(), ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+    rc = load().nm_paged_attention(desc, at, ws_bytes or 0, _stream(stream))
+    if rc:
+        _check(rc)
 
 
-def nm_gemv_w4(x, W, scales, out, *, group, alpha=1.0, bias=None, tables: Tables | None = None, table_idx=-1, out_inv_scale=1.0, stream=None):
-    """x: [M, K], out: [M, N], rows may be apart; W: uint8 [N, K / 2]; scales: [N, K / group], both contiguous."""
+def make_w4_desc(x, W, scales, out, *, group, alpha=1.0, bias=None, tables: Tables | None = None, table_idx=-1, out_inv_scale=1.0) -> bytes:
+    """x: [M, K], out: [M, N], rows may be apart; W: uint8 [N, K / 2]; scales: [N, K / group], both contiguous.  The description
+    refers to the tensors' memory: keep them."""
+    dev = _here()
     (M, K), N = x.shape, W.shape[0]
-    if _type(W, "W") is not None or tuple(W.shape) != (N, K // 2) or not W.is_contiguous() or K % 2:
-        _refuse(f"W: contiguous uint8 [N, {K // 2}] is wanted, got {tuple(W.shape)} of {W.dtype}")
-    if group < 1 or K % group or tuple(scales.shape) != (N, K // group) or not scales.is_contiguous():
+    if W.dtype is not _u8 or W.get_device() != dev or W.shape != (N, K // 2) or not W.is_contiguous() or K % 2:
+        _refuse(f"W: contiguous uint8 [N, {K // 2}] on the current device is wanted, got {tuple(W.shape)} of {W.dtype}")
+    if group < 1 or K % group or scales.shape != (N, K // group) or not scales.is_contiguous():
         _refuse(f"scales: contiguous [{N}, {K} / group] is wanted, got {tuple(scales.shape)}, group {group}")
-    if tuple(out.shape) != (M, N) or (out.stride(1) != 1 and N > 1) or (x.stride(1) != 1 and K > 1):
+    x0, x1 = x.stride()
+    o0, o1 = out.stride() if out.dim() == 2 else (0, 0)
+    if out.shape != (M, N) or (o1 != 1 and N > 1) or (x1 != 1 and K > 1):
         _refuse(f"x and out: rows of neighbouring elements are wanted, out of shape {(M, N)}, got {tuple(out.shape)}")
-    d = W4Desc(M, N, K, group, _type(x, "x"), _type(scales, "scales"), _type(out, "out"), x.data_ptr(), x.stride(0) if M > 1 else K, W.data_ptr(),
-               scales.data_ptr(), alpha, _vector(bias, NM_DT_F32, N, "bias"), tables.handle if tables is not None else None, table_idx,
-               out.data_ptr(), out.stride(0) if M > 1 else N, out_inv_scale)
-    _check(load().nm_gemv_w4(C.byref(d), _stream(stream)))
+    return _W4.pack(M, N, K, group, _type(x, dev, "x"), _type(scales, dev, "scales"), _type(out, dev, "out"), x.data_ptr(), x0 if M > 1 else K,
+                    W.data_ptr(), scales.data_ptr(), alpha, _vector(bias, _f32, N, dev, "bias"), (tables.handle or 0) if tables is not None else 0,
+                    table_idx, out.data_ptr(), o0 if M > 1 else N, out_inv_scale)
+
+
+def nm_gemv_w4(*tensors, stream=None, **more):
+    """make_w4_desc's arguments, or a description."""
+    desc = tensors[0] if len(tensors) == 1 else make_w4_desc(*tensors, **more)
+    rc = load().nm_gemv_w4(desc, _stream(stream))
+    if rc:
+        _check(rc)

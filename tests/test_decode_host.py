@@ -162,6 +162,14 @@ def test_gemv_w4_null_and_empty(lib):
     assert lib.nm_gemv_w4(C.byref(d), Z) == nm.NM_OK
 
 
+@pytest.mark.parametrize("packed,desc", [(nm._PLAN, nm.PlanDesc), (nm._QK, nm.QkDesc), (nm._PAGED, nm.PagedDesc), (nm._W4, nm.W4Desc)])
+def test_packed_descriptions_lie_as_the_structures(packed, desc):
+    values = [float(i + 1) if t is C.c_float else i + 1 for i, (_, t) in enumerate(desc._fields_)]
+    assert packed.size == C.sizeof(desc)
+    d = desc.from_buffer_copy(packed.pack(*values))
+    assert [getattr(d, n) for n, _ in desc._fields_] == values
+
+
 def test_binding_refuses_host_tensors():
     import torch
     i = torch.zeros(4, dtype=torch.int32)
