@@ -42,6 +42,7 @@ struct W4Args {
     int chunks;
     int x_stride;        // bytes between rows of x in LDS
     int passes;          // over the weights: tiles of rows
+    int second;          // where a second buffer of a chunk's scales and x begins behind the first; 0: there is one
 };
 constexpr int kW4Chunk = 128 * kW4Waves;
 
@@ -188,11 +189,12 @@ __global__ __launch_bounds__(kW4Threads, kRing ? 4 : 2) void gemv_w4_kernel(W4Ar
         }
         __builtin_amdgcn_sched_barrier(0);                    // loads are waited for in their order
     };
+    int flip = 0;                                             // of the buffer in use
     auto stage = [&](int chunk) {
 #pragma unroll
         for (int q = 0; q < kPieces; ++q) {
             const int p = uniform_wave * 64 + q * kW4Threads, r = p >> row_shift, at = p & ((1 << row_shift) - 1);
-            if (r < rows) *reinterpret_cast<v4u*>(s_x + r * a.x_stride + at * 16 + lane * 16) = Q::order(xp[q]);
+            if (r < rows) *reinterpret_cast<v4u*>(s_x + flip + r * a.x_stride + at * 16 + lane * 16) = Q::order(xp[q]);
         }
         if ((chunk + 1) * (kW4Chunk << a.chunk_shift) > d.K) {        // zeros behind K
             asm volatile("");
@@ -200,7 +202,7 @@ __global__ __launch_bounds__(kW4Threads, kRing ? 4 : 2) void gemv_w4_kernel(W4Ar
             for (int q = 0; q < kPieces; ++q) {
                 const int p = uniform_wave * 64 + q * kW4Threads, r = p >> row_shift, at = p & ((1 << row_shift) - 1);
                 if (r < rows && (chunk * (kW4Chunk << a.chunk_shift) + at * kPer16) + lane * kPer16 >= d.K)
-                    *reinterpret_cast<v4u*>(s_x + r * a.x_stride + at * 16 + lane * 16) = v4u{};
+                    *reinterpret_cast<v4u*>(s_x + flip + r * a.x_stride + at * 16 + lane * 16) = v4u{};
             }
         }
 #pragma unroll
@@ -209,7 +211,7 @@ __global__ __launch_bounds__(kW4Threads, kRing ? 4 : 2) void gemv_w4_kernel(W4Ar
             float v;
             if constexpr (sizeof(S) == 4) v = sp[q];
             else v = d.scale_dtype == NM_DT_BF16 ? __uint_as_float((unsigned)sp[q] << 16) : (float)__builtin_bit_cast(f16, sp[q]);
-            if (c < kCols) s_scale[c * (entries + 1) + e] = v * Q::kUnit;
+            if (c < kCols) *reinterpret_cast<float*>(reinterpret_cast<char*>(s_scale + c * (entries + 1) + e) + flip) = v * Q::kUnit;
         }
     };
 
@@ -228,8 +230,8 @@ __global__ __launch_bounds__(kW4Threads, kRing ? 4 : 2) void gemv_w4_kernel(W4Ar
         for (int g = 0; g < kScales; ++g) {
             float scale[kN];
 #pragma unroll
-            for (int c = 0; c < kN; ++c) scale[c] = srow[c * 16 * (entries + 1) + at * kScales + g];
-            auto rows_of = [&](int t, int i) { return *reinterpret_cast<const Rows*>(xrow[t] + (at * 128 + i * 32) * sizeof(X)); };
+            for (int c = 0; c < kN; ++c) scale[c] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(srow + c * 16 * (entries + 1) + at * kScales + g) + flip);
+            auto rows_of = [&](int t, int i) { return *reinterpret_cast<const Rows*>(xrow[t] + flip + (at * 128 + i * 32) * sizeof(X)); };
             Sum acc[kM][kN];
             Rows x[kM][kRuns];
 #pragma unroll
@@ -258,7 +260,8 @@ __global__ __launch_bounds__(kW4Threads, kRing ? 4 : 2) void gemv_w4_kernel(W4Ar
     };
 
     auto next_chunk = [&](int chunk) {
-        if (chunk) __syncthreads();
+        if (chunk && !a.second) __syncthreads();              // the chunk before is not read any more
+        flip = !kRing && (chunk & 1) ? a.second : 0;
         stage(chunk);
         if (chunk + 1 < a.chunks) fetch(chunk + 1);
         __syncthreads();
@@ -350,7 +353,13 @@ static int32_t launch_w4_tiles(W4Args a, hipStream_t s)
         if (a.chunks > 2) return launch_w4_tiles<X, S, kRuns, kM, kN, false>(a, s);
     a.x_stride = chunk * (int)sizeof(X) + 16;
     const int entries = (chunk / 128) * (4 / kRuns);
-    const size_t used = (size_t)kW4Waves * w4_stages(kN, kRing) * 1024 * kN + (16 * kN * (entries + 1) * 4 + 15) / 16 * 16 + (size_t)rows * a.x_stride;
+    const size_t one = (size_t)(16 * kN * (entries + 1) * 4 + 15) / 16 * 16 + (size_t)rows * a.x_stride;
+    size_t used = (size_t)kW4Waves * w4_stages(kN, kRing) * 1024 * kN + one;
+    // with two buffers a wavefront may write the next chunk's while another still reads this one's: one barrier a chunk instead of two
+    if (!kRing && a.chunks > 1 && used + one <= 160 * 1024) {
+        a.second = (int)one;
+        used += one;
+    }
     const size_t sums = (size_t)kW4Waves * kM * 16 * 16 * kN * 4, shmem = used > sums ? used : sums;
     auto kern = gemv_w4_kernel<X, S, kRuns, kM, kN, kRing>;
     if (shmem > 64 * 1024) {

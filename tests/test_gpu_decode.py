@@ -619,3 +619,165 @@ def test_gemv_w4_binding_refuses():
         changed[at] = bad
         with pytest.raises(nm.NmError):
             nm.nm_gemv_w4(*changed, group=group)
+
+
+# ---- a step as it is used: plan, QKV product, norms and rotation into the cache, attention, output product -----------------
+
+def step_64(x_codes, weights, s, table, positions, lens, page, cache, hq, hk, d):
+    """A decoder's attention block for one token a request, in binary64 on the given (rounded) weights and cache."""
+    qkv = x_codes.double() @ weights["qkv"].double().t().contiguous() * s["alpha_qkv"] + weights["bqkv"].double()
+    B = x_codes.shape[0]
+    q, k, v = (qkv[:, a * d:b * d].view(B, -1, d) for a, b in ((0, hq), (hq, hq + hk), (hq + hk, hq + 2 * hk)))
+    q, _ = rotate_64(q, positions, s["inv_freq"], s["gq"], True, False)
+    k, _ = rotate_64(k, positions, s["inv_freq"], s["gk"], True, False)
+    out = torch.zeros((B, hq, d), dtype=torch.float64, device=DEV)
+    cache = cache.clone()
+    for b in range(B):
+        n = int(lens[b])
+        where = torch.arange(n, device=DEV)
+        row = table[b].long()[where // page]
+        cache[0, row[-1], (n - 1) % page], cache[1, row[-1], (n - 1) % page] = k[b], v[b]
+        kk, vv = (cache[i][row, where % page].repeat_interleave(hq // hk, 1).transpose(0, 1) for i in (0, 1))
+        w = torch.softmax((kk * q[b][:, None]).sum(-1) * d ** -0.5, -1)
+        out[b] = (w[:, :, None] * vv).sum(1)
+    return out, cache
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_a_decoder_step(graph):
+    """Three steps one after the other on one set of buffers, eager or captured once and replayed (twice each: a step is idempotent): the
+    framework's int8 product writes q, k, v in fp32; attention writes int8 codes, which a 4-bit product reads.  Every step against binary64."""
+    B, hq, hk, d, H, page, columns = 5, 8, 2, 64, 256, 16, 40
+    g, cached = gen(77), [0, 15, 16, 300, 627]
+    pages = B * columns + 3
+    s = dict(alpha_qkv=2e-4, inv_freq=(10000.0 ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)).float().to(DEV),
+             gq=(1 + 0.1 * torch.randn(d, generator=g)).to(DEV), gk=(1 + 0.1 * torch.randn(d, generator=g)).to(DEV))
+    weights = dict(qkv=torch.randint(-127, 128, ((hq + 2 * hk) * d, H), generator=g, dtype=torch.int8).to(DEV), bqkv=(0.1 * torch.randn((hq + 2 * hk) * d, generator=g)).to(DEV))
+    wo = torch.randint(-8, 8, (H, hq * d), generator=g)
+    wo_packed, wo_scales = ((wo[:, 0::2] & 15) | ((wo[:, 1::2] & 15) << 4)).to(torch.uint8).to(DEV), (0.01 + 0.01 * torch.rand((H, hq * d // 64), generator=g)).to(DEV)
+    cache = torch.randn((2, pages, page, hk, d), generator=g).to(torch.bfloat16).to(DEV)
+    order = torch.randperm(pages, generator=g).to(torch.int32)
+    table = torch.full((B, columns), -1, dtype=torch.int32)
+    at = 0
+    for b, n in enumerate(cached):
+        held = -(-n // page)
+        table[b, :held] = order[at:at + held]
+        at += held
+    table, free = table.to(DEV), order[at:].to(DEV)
+    x = torch.empty((B, H), dtype=torch.int8, device=DEV)
+    now, fresh, begin, end, lens, status = i32(cached), i32([1] * B), i32([0]), i32([0]), i32([0] * B), i32([9] * 4)
+    slots, positions = i32([0] * (B + 2)), i32([0] * (B + 2))               # two rows more than there are tokens: a padded batch
+    qkv = torch.zeros((B + 2, (hq + 2 * hk) * d), device=DEV)
+    q = torch.zeros((B + 2, hq, d), dtype=torch.bfloat16, device=DEV)
+    ctx = torch.empty((B, hq, d), dtype=torch.int8, device=DEV)
+    y, lse = torch.empty((B, H), device=DEV), torch.empty((B, hq), device=DEV)
+    third = lambda a, b: qkv[:, a * d:b * d].view(B + 2, -1, d)  # noqa: E731
+    paged = nm.make_paged_desc(q[:B], cache[0], cache[1], table, lens, ctx, scale=d ** -0.5, out_inv_scale=60.0, lse=lse)
+    ws = torch.empty(nm.nm_paged_attention_workspace(paged), dtype=torch.uint8, device=DEV)
+
+    def step():
+        nm.nm_page_plan(now, fresh, free, begin, table, page_size=page, num_pages=pages, free_end=end, lens=lens, slots=slots, positions=positions, status=status)
+        nm.nm_gemm_pwl(x, weights["qkv"], bias=weights["bqkv"], alpha=s["alpha_qkv"], out_f32=qkv[:B])
+        nm.nm_qk_norm_rope(third(0, hq), third(hq, hq + hk), third(hq + hk, hq + 2 * hk), positions, s["inv_freq"], q, norm=True, q_gamma=s["gq"],
+                           k_gamma=s["gk"], k_cache=cache[0], v_cache=cache[1], slots=slots)
+        nm.nm_paged_attention(paged, ws=ws)
+        nm.nm_gemv_w4(ctx.view(B, hq * d), wo_packed, wo_scales, y, group=64, alpha=1 / 60.0)
+
+    captured = None
+    for _ in range(3):
+        x.copy_(torch.randint(-127, 128, (B, H), generator=g, dtype=torch.int8))
+        before = cache.double()
+        if graph and captured is None:
+            step()
+            torch.cuda.synchronize()
+            captured = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(captured):
+                step()
+        for _ in range(2):
+            (captured.replay if graph else step)()
+            torch.cuda.synchronize()
+        assert status.tolist()[0] == 0 and lens.tolist() == [n + 1 for n in now.tolist()] and slots.tolist()[B:] == [-1, -1]
+        want, full = step_64(x, weights, s, table, positions[:B], lens, page, before, hq, hk, d)
+        # q and the new keys and values are rounded to bf16 (2^-8 relative: |score| / 8 at most sqrt(d) gammas, so 8 * 2^-7 * 1.4^2 / 2 on a score, which
+        # is that on a weight, twice; 2^-8 on a value of some 4), then the context to codes of 1 / 60
+        off = (ctx.double() / 60 - want.clamp(-127 / 60, 127 / 60)).abs()
+        assert float(off.max()) <= 0.5 / 60 + 4 * (2 * 8 * 2.0 ** -7 + 2.0 ** -8), float(off.max())
+        assert float(off.mean()) < 0.01                                       # half a code is 0.0083
+        w = wo.to(DEV).double() * wo_scales.double().repeat_interleave(64, 1)
+        product = ctx.view(B, -1).double() @ w.t().contiguous() / 60
+        bound = (hq * d / 1024 + 13) * U * (ctx.view(B, -1).double().abs() @ w.abs().t().contiguous()) / 60 + 2 * U * product.abs()
+        assert bool(((y.double() - product).abs() <= bound).all())
+        assert float((cache.double() - full).abs().max()) <= 2.0 ** -8 * float(full.abs().max()) + 1e-4
+        now.copy_(lens)
+        begin.copy_(end)
+
+
+def test_two_calls_at_once_and_replays():
+    """Each call twice at once on two streams, with outputs (and workspaces) of their own, and captured and replayed: the same bits every time."""
+    a = paged_case(31, [3000, 17, 900, 0, 2500], 8, 2, 128, torch.bfloat16, torch.bfloat16, page=64)
+    w = w4_case(32, 20, 200, 2048, 128, torch.bfloat16, torch.bfloat16)
+    qk = [qk_case(33, 300, 8, 2, 128, 128, torch.bfloat16, torch.bfloat16) for _ in range(2)]
+    outs = [dict(o=torch.zeros((5, 8, 128), dtype=torch.bfloat16, device=DEV), y=torch.zeros((20, 200), dtype=torch.bfloat16, device=DEV),
+                 q=torch.zeros((300, 8, 128), dtype=torch.bfloat16, device=DEV)) for _ in range(2)]
+    descs = [nm.make_paged_desc(a["q"], a["cache"][0], a["cache"][1], a["table"], a["lens"], o["o"], scale=0.1) for o in outs]
+    wss = [torch.empty(nm.nm_paged_attention_workspace(x), dtype=torch.uint8, device=DEV) for x in descs]
+
+    def calls(i):
+        nm.nm_paged_attention(descs[i], ws=wss[i])
+        nm.nm_gemv_w4(w["x"], w["W"], w["scales"], outs[i]["y"], group=128, bias=w["bias"])
+        c = qk[i]
+        nm.nm_qk_norm_rope(c["q"], c["k"], c["v"], c["positions"], c["inv_freq"], outs[i]["q"], norm=True, k_cache=c["cache"][0], v_cache=c["cache"][1], slots=c["slots"])
+
+    calls(0)
+    torch.cuda.synchronize()
+    want = {n: t.clone() for n, t in outs[0].items()}
+    want_cache = qk[0]["cache"].clone()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for o in outs:
+            for t in o.values():
+                t.zero_()
+        torch.cuda.synchronize()
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                calls(i)
+        torch.cuda.synchronize()
+        for i in (0, 1):
+            assert all(torch.equal(outs[i][n], want[n]) for n in want) and torch.equal(qk[i]["cache"], want_cache)
+    graphs = []
+    for i in (0, 1):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            calls(i)
+        graphs.append(graph)
+    for _ in range(4):
+        for o in outs:
+            for t in o.values():
+                t.zero_()
+        torch.cuda.synchronize()
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                graphs[i].replay()
+        torch.cuda.synchronize()
+        for i in (0, 1):
+            assert all(torch.equal(outs[i][n], want[n]) for n in want) and torch.equal(qk[i]["cache"], want_cache)
+
+
+def test_a_graph_follows_the_lengths():
+    """A captured call reads lengths and tables when it is replayed: other lengths, and back."""
+    c = paged_case(41, [5, 700, 3000, 64], 8, 2, 64, torch.bfloat16, torch.int8)
+    out = torch.zeros((4, 8, 64), dtype=torch.bfloat16, device=DEV)
+    desc = nm.make_paged_desc(c["q"], c["cache"][0], c["cache"][1], c["table"], c["lens"], out, scale=0.125, k_scale=c["scales"][0], v_scale=c["scales"][1])
+    ws = torch.empty(nm.nm_paged_attention_workspace(desc), dtype=torch.uint8, device=DEV)
+    nm.nm_paged_attention(desc, ws=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        nm.nm_paged_attention(desc, ws=ws)
+    for lens in ([5, 700, 3000, 64], [1, 0, 2999, 63], [0, 0, 0, 0], [5, 700, 1, 64], [5, 700, 3000, 64]):
+        c["lens"].copy_(torch.tensor(lens, dtype=torch.int32))
+        ws.fill_(0xff)
+        graph.replay()
+        torch.cuda.synchronize()
+        want, _, error, _ = attention_64(c, 0.125)
+        assert_rounded(out, want, error, str(lens))
