@@ -477,10 +477,12 @@ int32_t nm_cnn_run(const nm_cnn_op* ops, int32_t n_ops, void* ws, size_t ws_byte
  * laid out by tokens or by heads.  All of a step's numbers (lengths, slots, tables) are device memory, so that a step can
  * be captured once and replayed while they change.
  *
- * Unlike the calls above, these three compute the functions themselves, not tables of them: a softmax that is split over the cache's
- * length and joined relies on exp(a + b) = exp(a) exp(b), which a piecewise-linear exp does not have.  nm_gemv_w4 takes tables.
+ * nm_qk_norm_rope and nm_paged_attention compute the functions themselves, not tables of them: a softmax that is split over the
+ * cache's length and joined relies on exp(a + b) = exp(a) exp(b), which a piecewise-linear exp does not have.  nm_gemv_w4 takes tables.
  * Sums and statistics are binary32 (integer products exact int32); outputs are rounded once, to nearest even; int8 codes
- * as above.  Results do not depend on timing (no atomics) and agree with the formulas to rounding; they are not specified bit for bit.
+ * as above.  The same call gives the same bits (no atomics); against the formulas results are right to rounding, not bit for bit.
+ * Which kernels run depends on shapes and types alone, so every call can be captured; calls that overlap in time share nothing but
+ * what the caller gives both.
  * --------------------------------------------------------------------------------------------- */
 
 /*
@@ -498,7 +500,7 @@ int32_t nm_cnn_run(const nm_cnn_op* ops, int32_t n_ops, void* ws, size_t ws_byte
  * cached, fresh: device [B].  free_pages: device [n_free].  block_table: device [B] rows of max_pages entries, table_stride
  * apart.  slots, positions, requests: [max_tokens].  lens, row_start, positions, requests may be NULL.  No output may be an input
  * (one workgroup writes while another still reads): *free_end and lens need memory of their own.
- * Limits: B <= NM_PLAN_MAX_REQUESTS; num_pages * page_size < 2^31; page_size <= 65536.
+ * Limits: B <= NM_PLAN_MAX_REQUESTS; num_pages * page_size < 2^31; page_size <= 65536; max_tokens, n_free <= 2^30.
  */
 #define NM_PLAN_MAX_REQUESTS 4096
 enum { NM_PLAN_NO_PAGES = 1,      /* the free list is too short */
@@ -536,7 +538,7 @@ int32_t nm_page_plan(const nm_plan_desc* desc, void* stream);
  * q, k, v: device, a token's heads one behind the other, tokens q_stride, k_stride, v_stride elements apart (the thirds of a fused
  * projection's rows, for instance); in_dtype F32, BF16 or F16.  q_out, k_out likewise, out_dtype the same three; q_out may be q itself
  * (same type and stride), k_out k.  cache_dtype F32, BF16, F16 or I8.  positions, slots: device int32 [T] (positions may be NULL for rot = 0,
- * slots without a cache).  inv_freq: device fp32 [rot / 2].  gammas: device fp32 [d].  k_inv_scale, v_inv_scale: device fp32 [hk], for int8.
+ * slots without a cache).  Rows without a slot are computed into q_out and k_out like the others.  inv_freq: device fp32 [rot / 2].  gammas: device fp32 [d].  k_inv_scale, v_inv_scale: device fp32 [hk], for int8.
  * Limits: T <= 2^23; 1 <= d <= 256; rot even, 0 <= rot <= d; hq, hk >= 1, hq + 2 hk <= 65535; strides cover a token's heads.  Where the rows and the cache are
  * 16-byte aligned, d is a multiple of 8 and rot of 8 (or 0), whole groups of elements move at once.
  */
@@ -580,10 +582,10 @@ int32_t nm_qk_norm_rope(const nm_qk_desc* desc, void* stream);
  * q is split into as many terms of the matrix instructions' type as hold it, the weights into two (fp32 results: three), so nothing
  * but the outputs is rounded to fewer than 16 bits.
  * Workspace: query nm_paged_attention_workspace (it looks at the shape and the types only, never at device memory; 0: none); 256-byte
- * aligned, contents are scratch, calls that overlap in time need one each.  A cache is split over its length by max_pages (the
- * lengths are on the device), so a table much wider than the lengths costs launches of empty workgroups.
+ * aligned, contents are scratch, calls that overlap in time need one each.  Lengths may be as ragged, and the table as much wider
+ * than they are, as it happens: the work is shared by the lengths as they are when the call runs.
  * Limits: hq % hk == 0; d a multiple of 16 up to 256; cache addresses and strides multiples of 16 bytes; page_size a power of
- * two up to 65536; num_pages * page_size < 2^31; B * hk * groups of 16 query heads * pieces of the length < 2^24.
+ * two up to 65536; num_pages * page_size < 2^31; max_pages * page_size < 2^30; each cache at most 32 GiB; B * hq < 2^23.
  */
 typedef struct {
     int32_t B, hq, hk, d;
@@ -617,9 +619,10 @@ int32_t nm_paged_attention(const nm_paged_desc* desc, void* ws, size_t ws_bytes,
  * x: device [M, K], rows x_stride elements apart, x_dtype I8, BF16 or F16.  W: device [N, K / 2], contiguous: byte i of a row holds
  * w[n, 2 i] in its low and w[n, 2 i + 1] in its high four bits, two's complement (-8 .. 7).  scales: device [N, K / group], contiguous,
  * scale_dtype F32, BF16 or F16.  bias: device fp32 [N] or NULL.  out: device [M, N], rows out_stride apart, out_dtype F32, BF16, F16
- * or I8.  Any M: rows are taken 64 at a time, and the weights read again for each 64 (nm_gemm_pwl is the call for many rows).
+ * or I8.  Any M: rows are taken up to 48 at a time, and the weights read again for each (nm_gemm_pwl is the call for many rows).
+ * A row of bf16 or fp16 with an infinity or NaN comes out NaN; other rows are not touched by it.
  * Limits: group 32, 64 or a multiple of 128; K a multiple of group, at most 65536; x and W 16-byte aligned, x_stride a multiple of 16
- * bytes; M <= 2^20, N < 2^26.
+ * bytes; M <= 2^20, N < 2^26, (N / 16) (M / 32) < 2^23.
  */
 typedef struct {
     int32_t M, N, K, group;

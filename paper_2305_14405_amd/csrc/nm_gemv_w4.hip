@@ -19,6 +19,7 @@ extern "C" int32_t nm_gemv_w4(const nm_w4_desc* d, void* stream)
     if (d->group != 32 && d->group != 64 && d->group % 128) return fail(NM_ERR_UNSUPPORTED, "nm_gemv_w4: group %d is not 32, 64 or a multiple of 128", d->group);
     if (d->K % d->group) return fail(NM_ERR_INVALID_ARG, "nm_gemv_w4: K is no multiple of group");
     if (d->K > 65536 || d->M > 1 << 20 || d->N >= 1 << 26) return fail(NM_ERR_UNSUPPORTED, "nm_gemv_w4: K > 65536, M > 2^20 or N >= 2^26");
+    if ((((int64_t)d->N + 15) / 16 + 7) / 8 * 8 * ((d->M + 31) / 32) >= 1 << 23) return fail(NM_ERR_UNSUPPORTED, "nm_gemv_w4: N / 16 times M / 32 >= 2^23");
     if (d->x_stride < d->K || d->out_stride < d->N) return fail(NM_ERR_INVALID_ARG, "nm_gemv_w4: a stride is shorter than a row");
     if (!(d->alpha == d->alpha) || __builtin_isinf(d->alpha)) return fail(NM_ERR_INVALID_ARG, "nm_gemv_w4: alpha must be finite");
     W4Args a{};

@@ -130,6 +130,7 @@ extern "C" int32_t nm_page_plan(const nm_plan_desc* d, void* stream)
     if (d->B < 0 || d->num_pages < 0 || d->max_pages < 0 || d->n_free < 0 || d->max_tokens < 0)
         return fail(NM_ERR_INVALID_ARG, "nm_page_plan: negative size");
     if (d->B > NM_PLAN_MAX_REQUESTS) return fail(NM_ERR_UNSUPPORTED, "nm_page_plan: B %d > %d", d->B, NM_PLAN_MAX_REQUESTS);
+    if (d->max_tokens > 1 << 30 || d->n_free > 1 << 30) return fail(NM_ERR_UNSUPPORTED, "nm_page_plan: max_tokens or n_free > 2^30");
     const int shift = page_shift(d->page_size);
     if (shift < 0) return fail(NM_ERR_UNSUPPORTED, "nm_page_plan: page_size %d is no power of two up to 65536", d->page_size);
     if ((int64_t)d->num_pages << shift > 0x7fffffffLL) return fail(NM_ERR_UNSUPPORTED, "nm_page_plan: num_pages * page_size >= 2^31");

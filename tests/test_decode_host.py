@@ -44,7 +44,8 @@ def test_page_plan_refuses(lib, changes):
 
 
 @pytest.mark.parametrize("changes", [dict(B=nm.NM_PLAN_MAX_REQUESTS + 1), dict(page_size=0), dict(page_size=24), dict(page_size=1 << 17),
-                                     dict(num_pages=1 << 27)])
+                                     dict(num_pages=1 << 27),
+                                     dict(max_tokens=(1 << 30) + 1), dict(n_free=(1 << 30) + 1)])
 def test_page_plan_does_not_cover(lib, changes):
     refused(lib.nm_page_plan, plan(), nm.NM_ERR_UNSUPPORTED, **changes)
 
@@ -114,7 +115,7 @@ def test_paged_attention_refuses(lib, changes):
 
 @pytest.mark.parametrize("changes", [
     dict(d=72), dict(d=272, q_stride=4000, out_stride=4000), dict(page_size=3), dict(num_pages=1 << 27), dict(max_pages=1 << 26, table_stride=1 << 26),
-    dict(k_cache=P + 8), dict(v_cache=P + 4), dict(page_stride=2056), dict(slot_stride=136), dict(head_stride=72), dict(B=1 << 23, hq=2)])
+    dict(k_cache=P + 8), dict(v_cache=P + 4), dict(page_stride=2056), dict(slot_stride=136), dict(head_stride=72), dict(B=1 << 23, hq=2), dict(num_pages=1 << 20, page_stride=1 << 15), dict(num_pages=1 << 20, page_stride=1 << 14, cache_dtype=nm.NM_DT_BF16)])
 def test_paged_attention_does_not_cover(lib, changes):
     refused(attend(lib), paged(), nm.NM_ERR_UNSUPPORTED, **changes)
 
@@ -150,7 +151,7 @@ def test_gemv_w4_refuses(lib, changes):
 
 
 @pytest.mark.parametrize("changes", [dict(group=16), dict(group=96, K=192), dict(K=65536 + 64, x_stride=1 << 17), dict(M=(1 << 20) + 1), dict(N=1 << 26, out_stride=1 << 26),
-                                     dict(x=P + 8), dict(W=P + 8), dict(x_stride=260)])
+                                     dict(x=P + 8), dict(W=P + 8), dict(x_stride=260), dict(M=1 << 20, N=1 << 13, out_stride=1 << 13)])
 def test_gemv_w4_does_not_cover(lib, changes):
     refused(lib.nm_gemv_w4, w4(), nm.NM_ERR_UNSUPPORTED, **changes)
 

@@ -781,3 +781,23 @@ def test_a_graph_follows_the_lengths():
         torch.cuda.synchronize()
         want, _, error, _ = attention_64(c, 0.125)
         assert_rounded(out, want, error, str(lens))
+
+
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 1e-3])
+@pytest.mark.parametrize("q_dtype,cache_dtype", [(torch.float32, torch.float16), (torch.bfloat16, torch.bfloat16), (torch.float16, torch.int8)])
+def test_paged_attention_scales(scale, q_dtype, cache_dtype):
+    check_attention(paged_case(12, [1, 40, 900, 0], 4, 2, 64, q_dtype, cache_dtype), torch.float32, scale=scale)
+
+
+@pytest.mark.parametrize("hq,hk,d,cache_dtype,by_head", [(16, 8, 16, torch.int8, False), (8, 8, 32, torch.int8, False), (40, 2, 32, torch.bfloat16, False),
+                                                         (6, 6, 16, torch.float16, True), (64, 4, 32, torch.int8, False)])
+@pytest.mark.parametrize("lens", [[2000, 1, 0, 700, 129], [0, 0, 0], [3], [130] * 40])
+def test_paged_attention_heads_that_share_lines(hq, hk, d, cache_dtype, by_head, lens):
+    check_attention(paged_case(13, lens, hq, hk, d, torch.float32, cache_dtype, page=32, by_head=by_head, columns=64), torch.float32)
+
+
+def test_paged_attention_many_short_requests():
+    r = np.random.default_rng(5)
+    lens = [int(n) if n > 3 else 0 for n in r.integers(0, 60, 700)]
+    lens[350] = 2500
+    check_attention(paged_case(14, lens, 2, 1, 64, torch.bfloat16, torch.bfloat16, columns=200), torch.bfloat16)
