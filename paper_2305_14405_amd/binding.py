@@ -655,7 +655,7 @@ def _table(t, B, dev):
     return columns, t.stride(0) if B > 1 else columns
 
 
-def make_plan_desc(cached, fresh, free_pages, free_begin, block_table, *, page_size, num_pages, free_end, slots, status, lens=None,
+def make_plan_desc(cached, fresh, free_pages, free_begin, block_table, page_size, num_pages, free_end, slots, status, lens=None,
                    row_start=None, positions=None, requests=None) -> bytes:
     """block_table: int32 [B, max_pages], rows may be apart; every other tensor is contiguous int32.  The description refers to the
     tensors' memory: keep them."""
@@ -669,15 +669,17 @@ def make_plan_desc(cached, fresh, free_pages, free_begin, block_table, *, page_s
                       _vector(positions, _i32, T, dev, "positions"), _vector(requests, _i32, T, dev, "requests"), _vector(status, _i32, 4, dev, "status"))
 
 
-def nm_page_plan(*tensors, stream=None, **more):
-    """make_plan_desc's arguments, or a description."""
-    desc = tensors[0] if len(tensors) == 1 else make_plan_desc(*tensors, **more)
+def nm_page_plan(cached, fresh=None, free_pages=None, free_begin=None, block_table=None, *, page_size=0, num_pages=0, free_end=None, slots=None,
+                 status=None, lens=None, row_start=None, positions=None, requests=None, stream=None):
+    """make_plan_desc's arguments, or a description alone."""
+    desc = cached if cached.__class__ is bytes else make_plan_desc(cached, fresh, free_pages, free_begin, block_table, page_size, num_pages, free_end,
+                                                                   slots, status, lens, row_start, positions, requests)
     rc = load().nm_page_plan(desc, _stream(stream))
     if rc:
         _check(rc)
 
 
-def make_qk_desc(q, k, v, positions, inv_freq, q_out, *, k_out=None, k_cache=None, v_cache=None, slots=None, norm=False, q_gamma=None,
+def make_qk_desc(q, k, v, positions, inv_freq, q_out, k_out=None, k_cache=None, v_cache=None, slots=None, norm=False, q_gamma=None,
                  k_gamma=None, eps=1e-6, interleaved=False, k_inv_scale=None, v_inv_scale=None) -> bytes:
     """q, q_out: [T, hq, d]; k, v, k_out: [T, hk, d]; caches: [pages, page_size, hk, d] with strides; inv_freq (rot / 2 numbers) and
     positions may be None: no rotation.  The description refers to the tensors' memory: keep them."""
@@ -703,25 +705,30 @@ def make_qk_desc(q, k, v, positions, inv_freq, q_out, *, k_out=None, k_cache=Non
         k_at, vc_at, slots_at = k_cache.data_ptr(), v_cache.data_ptr(), _vector(slots, _i32, T, dev, "slots")
     return _QK.pack(T, hq, hk, e, rot, (NM_QK_NORM if norm else 0) | (NM_ROPE_INTERLEAVED if interleaved else 0), in_dtype, out_dtype, cache_dtype,
                     pages, page, q.data_ptr(), k.data_ptr(), v_at, _heads(q, T, hq, e, "q"), _heads(k, T, hk, e, "k"), v_stride,
-                    _vector(q_gamma, _f32, e, dev, "q_gamma"), _vector(k_gamma, _f32, e, dev, "k_gamma"), eps,
+                    0 if q_gamma is None else _vector(q_gamma, _f32, e, dev, "q_gamma"), 0 if k_gamma is None else _vector(k_gamma, _f32, e, dev, "k_gamma"), eps,
                     _vector(positions, _i32, T, dev, "positions") if rot else 0, _vector(inv_freq, _f32, rot // 2, dev, "inv_freq"),
                     q_out.data_ptr(), _heads(q_out, T, hq, e, "q_out"), k_out_at, k_out_stride, k_at, vc_at, s0, s1, s2, slots_at,
-                    _vector(k_inv_scale, _f32, hk, dev, "k_inv_scale"), _vector(v_inv_scale, _f32, hk, dev, "v_inv_scale"))
+                    0 if k_inv_scale is None else _vector(k_inv_scale, _f32, hk, dev, "k_inv_scale"),
+                    0 if v_inv_scale is None else _vector(v_inv_scale, _f32, hk, dev, "v_inv_scale"))
 
 
-def nm_qk_norm_rope(*tensors, stream=None, **more):
-    """make_qk_desc's arguments, or a description."""
-    desc = tensors[0] if len(tensors) == 1 else make_qk_desc(*tensors, **more)
+def nm_qk_norm_rope(q, k=None, v=None, positions=None, inv_freq=None, q_out=None, *, k_out=None, k_cache=None, v_cache=None, slots=None, norm=False,
+                    q_gamma=None, k_gamma=None, eps=1e-6, interleaved=False, k_inv_scale=None, v_inv_scale=None, stream=None):
+    """make_qk_desc's arguments, or a description alone."""
+    desc = q if q.__class__ is bytes else make_qk_desc(q, k, v, positions, inv_freq, q_out, k_out, k_cache, v_cache, slots, norm, q_gamma, k_gamma, eps,
+                                                       interleaved, k_inv_scale, v_inv_scale)
     rc = load().nm_qk_norm_rope(desc, _stream(stream))
     if rc:
         _check(rc)
 
 
-def make_paged_desc(q, k_cache, v_cache, block_table, lens, out, *, scale, window=0, k_scale=None, v_scale=None, out_inv_scale=1.0,
+def make_paged_desc(q, k_cache, v_cache, block_table, lens, out, scale, window=0, k_scale=None, v_scale=None, out_inv_scale=1.0,
                     lse=None) -> bytes:
     """q, out: [B, hq, d]; caches: [pages, page_size, hk, d] with strides; block_table: int32 [B, max_pages].  The description
     refers to the tensors' memory: keep them."""
     dev = _here()
+    if scale is None:
+        _refuse("scale is wanted")
     B, hq, e = q.shape
     hk = k_cache.shape[2]
     dtype, pages, page, (s0, s1, s2, _) = _cache(k_cache, v_cache, hk, e, dev)
@@ -734,15 +741,16 @@ def make_paged_desc(q, k_cache, v_cache, block_table, lens, out, *, scale, windo
 
 def nm_paged_attention_workspace(*tensors, **more) -> int:
     """Bytes; takes what nm_paged_attention takes, or a description."""
-    desc = tensors[0] if len(tensors) == 1 else make_paged_desc(*tensors, **more)
+    desc = tensors[0] if tensors[0].__class__ is bytes else make_paged_desc(*tensors, **more)
     n = C.c_size_t()
     _check(load().nm_paged_attention_workspace(desc, C.byref(n)))
     return n.value
 
 
-def nm_paged_attention(*tensors, ws=None, stream=None, ws_bytes=None, **more):
-    """make_paged_desc's arguments, or a description."""
-    desc = tensors[0] if len(tensors) == 1 else make_paged_desc(*tensors, **more)
+def nm_paged_attention(q, k_cache=None, v_cache=None, block_table=None, lens=None, out=None, *, scale=None, window=0, k_scale=None, v_scale=None,
+                       out_inv_scale=1.0, lse=None, ws=None, stream=None, ws_bytes=None):
+    """make_paged_desc's arguments, or a description alone; and the workspace."""
+    desc = q if q.__class__ is bytes else make_paged_desc(q, k_cache, v_cache, block_table, lens, out, scale, window, k_scale, v_scale, out_inv_scale, lse)
     at = 0
     if ws is not None:
         if ws.get_device() != _here() or not ws.is_contiguous():
@@ -753,7 +761,7 @@ def nm_paged_attention(*tensors, ws=None, stream=None, ws_bytes=None, **more):
         _check(rc)
 
 
-def make_w4_desc(x, W, scales, out, *, group, alpha=1.0, bias=None, tables: Tables | None = None, table_idx=-1, out_inv_scale=1.0) -> bytes:
+def make_w4_desc(x, W, scales, out, group, alpha=1.0, bias=None, tables: Tables | None = None, table_idx=-1, out_inv_scale=1.0) -> bytes:
     """x: [M, K], out: [M, N], rows may be apart; W: uint8 [N, K / 2]; scales: [N, K / group], both contiguous.  The description
     refers to the tensors' memory: keep them."""
     dev = _here()
@@ -771,9 +779,10 @@ def make_w4_desc(x, W, scales, out, *, group, alpha=1.0, bias=None, tables: Tabl
                     table_idx, out.data_ptr(), o0 if M > 1 else N, out_inv_scale)
 
 
-def nm_gemv_w4(*tensors, stream=None, **more):
-    """make_w4_desc's arguments, or a description."""
-    desc = tensors[0] if len(tensors) == 1 else make_w4_desc(*tensors, **more)
+def nm_gemv_w4(x, W=None, scales=None, out=None, *, group=0, alpha=1.0, bias=None, tables: Tables | None = None, table_idx=-1, out_inv_scale=1.0,
+               stream=None):
+    """make_w4_desc's arguments, or a description alone."""
+    desc = x if x.__class__ is bytes else make_w4_desc(x, W, scales, out, group, alpha, bias, tables, table_idx, out_inv_scale)
     rc = load().nm_gemv_w4(desc, _stream(stream))
     if rc:
         _check(rc)
