@@ -2,8 +2,9 @@
 //
 // What is needed of all requests is two prefix sums, over the new tokens and over the new pages.  Every workgroup makes both for itself
 // (two numbers of each request, from L2) and keeps them in LDS, so that no workgroup waits for another and one launch does;
-// then each token, and each new page, finds its request by bisection.  Bound by latency: four dependent reads (lengths, list
-// position, table or list, store) and a launch.  A token costs 12 written bytes, so long prompts are bound by the stores.
+// then each token, and each new page, finds its request by bisection.  Bound by latency: a launch, and dependent steps (lengths, the
+// scan, a bisection, an entry of the table or the list, a store): 4.1 us for 8 requests of one token, of which an empty launch is 2.5.
+// 500000 tokens of 500 requests, 6 MB of stores, take 8.3 us (1.2 at the rate of a copy).
 #include "nm_decode.h"
 
 namespace nm {
@@ -26,7 +27,9 @@ __device__ __forceinline__ int owner(const int* start, int n, int x)
 
 __device__ __forceinline__ int saturated(long x) { return (int)(x < 0x7fffffffL ? x : 0x7fffffffL); }
 
-__global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(nm_plan_desc d, int shift, int tokens_per_block)
+// V: neighbouring tokens of a thread, 1 or 4.
+template <int V>
+__global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(nm_plan_desc d, int shift, int tokens_per_block, int whole)
 {
     extern __shared__ int s_start[];          // [B + 1] tokens in front of a request, [B + 1] pages
     int* s_tok = s_start;
@@ -103,20 +106,47 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(nm_plan_desc d,
             const int column = (int)(((long)d.cached[b] + round) >> shift) + k - s_page[b];
             d.block_table[b * d.table_stride + column] = d.free_pages[begin + k];
         }
+    // Of a thread's tokens the first is looked up, another only where the request ends among them; one entry of the table does as long
+    // as the page is the same.
     const int t0 = (int)min((long)block * tokens_per_block, (long)d.max_tokens), t1 = (int)min((long)t0 + tokens_per_block, (long)d.max_tokens);
-    for (int t = t0 + tid; t < t1; t += kPlanThreads) {
-        int slot = -1, position = 0, request = -1;
-        if (ok && t < (int)tokens) {
-            request = owner(s_tok, d.B, t);
-            const int c = d.cached[request];
-            position = c + t - s_tok[request];
-            const int at = position >> shift, held = (int)(((long)c + round) >> shift);
-            const int entry = at < held ? d.block_table[request * d.table_stride + at] : d.free_pages[begin + s_page[request] + at - held];
-            if (entry >= 0 && entry < d.num_pages) slot = (entry << shift) + (position & (int)round);
+    for (int t = t0 + tid * V; t < t1; t += kPlanThreads * V) {
+        int slot[V], position[V], request[V];
+        int r = -1, at = -1, entry = -1, c = 0, first = 0, end = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            slot[i] = request[i] = -1;
+            position[i] = 0;
+            if (!ok || t + i >= (int)tokens) continue;
+            if (t + i >= end) {
+                r = owner(s_tok, d.B, t + i);
+                first = s_tok[r];
+                end = s_tok[r + 1];
+                c = d.cached[r];
+                at = -1;
+            }
+            const int p = c + t + i - first;
+            if (p >> shift != at) {
+                at = p >> shift;
+                const int held = (int)(((long)c + round) >> shift);
+                entry = at < held ? d.block_table[r * d.table_stride + at] : d.free_pages[begin + s_page[r] + at - held];
+            }
+            request[i] = r;
+            position[i] = p;
+            if (entry >= 0 && entry < d.num_pages) slot[i] = (entry << shift) + (p & (int)round);
         }
-        d.slots[t] = slot;
-        if (d.positions) d.positions[t] = position;
-        if (d.requests) d.requests[t] = request;
+        if (V == 4 && whole && t + V <= t1) {
+            *reinterpret_cast<int4*>(d.slots + t) = make_int4(slot[0], slot[V / 4], slot[V / 2], slot[V - 1]);
+            if (d.positions) *reinterpret_cast<int4*>(d.positions + t) = make_int4(position[0], position[V / 4], position[V / 2], position[V - 1]);
+            if (d.requests) *reinterpret_cast<int4*>(d.requests + t) = make_int4(request[0], request[V / 4], request[V / 2], request[V - 1]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (t + i < t1) {
+                    d.slots[t + i] = slot[i];
+                    if (d.positions) d.positions[t + i] = position[i];
+                    if (d.requests) d.requests[t + i] = request[i];
+                }
+        }
     }
 }
 
@@ -145,9 +175,13 @@ extern "C" int32_t nm_page_plan(const nm_plan_desc* d, void* stream)
     for (const int32_t* p : in)
         for (const int32_t* q : out)
             if (p && p == q) return fail(NM_ERR_INVALID_ARG, "nm_page_plan: an output is an input");
-    // a workgroup's scan costs it a few microseconds whatever it then writes: 1024 tokens (16 KB of stores) each, more from 512 workgroups on
-    const int per = d->max_tokens <= 512 * 1024 ? 1024 : (d->max_tokens + 511) / 512;
+    // A workgroup's scan costs it a few microseconds whatever it then writes.  Few tokens: 256 to a workgroup, one to a thread (8 tokens of 8
+    // requests 4.1 us so, 5.9 by four to a thread).  Many: 1024 and more, four to a thread (500000 tokens of 500 requests 8.3 us so, 9.5 by one).
+    const bool few = d->max_tokens <= 65536;
+    const int per = few ? 256 : d->max_tokens <= 512 * 1024 ? 1024 : ((d->max_tokens + 511) / 512 + 3) / 4 * 4;
     const int blocks = d->max_tokens ? (d->max_tokens + per - 1) / per : 1;
-    queue_kernel(page_plan_kernel, dim3(blocks), dim3(kPlanThreads), sizeof(int) * 2 * ((size_t)d->B + 1), (hipStream_t)stream, *d, shift, per);
+    const int whole = aligned(d->slots, 16) && aligned(d->positions, 16) && aligned(d->requests, 16);
+    queue_kernel(few ? page_plan_kernel<1> : page_plan_kernel<4>, dim3(blocks), dim3(kPlanThreads), sizeof(int) * 2 * ((size_t)d->B + 1), (hipStream_t)stream, *d,
+                 shift, per, whole);
     return check_hip(hipGetLastError(), "nm_page_plan launch");
 }

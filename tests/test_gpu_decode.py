@@ -801,3 +801,17 @@ def test_paged_attention_many_short_requests():
     lens = [int(n) if n > 3 else 0 for n in r.integers(0, 60, 700)]
     lens[350] = 2500
     check_attention(paged_case(14, lens, 2, 1, 64, torch.bfloat16, torch.bfloat16, columns=200), torch.bfloat16)
+
+
+def test_page_plan_outputs_at_odd_addresses():
+    cached, fresh, free, table, pages = random_plan(21, 30, 16, 100, 9)
+    T = sum(fresh) + 3
+    want = plan_in_python(cached, fresh, free, 0, table, 16, pages, T)
+    a = torch.full((3, T + 9), -5, dtype=torch.int32, device=DEV)
+    o = [a[i, i + 1:i + 1 + T] for i in range(3)]
+    nm.nm_page_plan(i32(cached), i32(fresh), i32(free), i32([0]), torch.from_numpy(table).to(DEV), page_size=16, num_pages=pages, free_end=i32([0]), slots=o[0],
+                    positions=o[1], requests=o[2], status=i32([0] * 4))
+    torch.cuda.synchronize()
+    assert [x.cpu().tolist() for x in o] == [want["slots"], want["positions"], want["requests"]]
+    for i in range(3):
+        assert bool((a[i, :i + 1] == -5).all()) and bool((a[i, i + 1 + T:] == -5).all())
