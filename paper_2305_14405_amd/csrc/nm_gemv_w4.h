@@ -1,11 +1,13 @@
 // Products of a few rows with 4-bit weights (nm_gemv_w4): the kernel.  One translation unit for each type of x.
 //
 // Bound by memory: N K / 2 bytes of weights, each read once, for 2 M operations a weight.  A workgroup has 16 or 32 columns (rows of W)
-// and all of K, which its eight wavefronts share in blocks of 128; their sums are joined through LDS, so that columns alone need not
+// and all of K, which eight or sixteen wavefronts share in blocks of 128; their sums are joined through LDS, so that columns alone need not
 // fill the GPU.  K goes by chunks: x of a chunk, and the chunk's scales as fp32, lie in LDS (the next chunk's are on their way into
 // registers), and a wavefront takes a run of the chunk's blocks.  Where a chunk or two are all of K (few rows), weights go
 // directly into LDS, a ring of blocks for each wavefront; with more chunks through registers, for whoever waits for a chunk's x would
-// wait for the whole ring (33 rows, 8192 x 8192: 29 us with the ring).
+// wait for the whole ring (33 rows, 8192 x 8192: 29 us with the ring).  Then 32 columns are two sets of eight wavefronts, four to a
+// SIMD: fetching and ordering x, unpacking weights and the matrix instructions of one run under another's (8192 x 8192: 33 rows 21.0 us, 22.8
+// with eight wavefronts of 32 columns; 48: 24.1 and 26.4; 17: 15.6 and 16.9; 16: 13.7 and 14.7).
 //   Four neighbouring lanes load 64 bytes, 128 weights, of a row, a run of 32 each: neighbouring lanes in different rows, as the matrix
 // instruction wants them, cost the address unit four times as much (28672 x 8192: 54 us so, 2.2 TB/s).  From LDS lane (j, row) then
 // gets run j of its row.  The 16x16x32 instruction (rows of x its rows, columns its columns) adds over the four lanes of a
@@ -31,8 +33,8 @@ typedef unsigned v2u __attribute__((ext_vector_type(2)));
 
 constexpr int kW4Waves = 8, kW4Threads = 64 * kW4Waves;
 
-// Scales that a thread has of a chunk.
-constexpr int w4_scales(int tiles) { return tiles == 1 ? 8 : 2; }
+// Scales that a thread has of a chunk; threads: eight wavefronts times this.
+constexpr int w4_scales(int tiles, int threads) { return ((tiles == 1 ? 8 : 2) + threads - 1) / threads; }
 
 struct W4Args {
     nm_w4_desc d;
@@ -46,8 +48,8 @@ struct W4Args {
 };
 constexpr int kW4Chunk = 128 * kW4Waves;
 
-// Pieces of 16 bytes of x that a thread has of a chunk: of 1024 columns of 16-bit rows and more.
-constexpr int w4_pieces(int tiles, bool ring) { return tiles == 1 && !ring ? 8 : 4 * tiles; }
+// Pieces of 16 bytes of x that a thread has of a chunk: of the shortest chunk of 16-bit rows and more.
+constexpr int w4_pieces(int tiles, bool ring, int sets, int shares) { return tiles == 1 && !ring ? 8 / (sets * shares) : 4 * tiles / sets; }
 // Blocks of a wavefront's ring in LDS (16 columns are 1 KB of each), or its places for blocks in LDS where registers hold the next two.
 constexpr int w4_stages(int columns, bool ring) { return !ring ? 1 : columns == 1 ? 4 : 3; }
 
@@ -123,19 +125,22 @@ template <> struct W4<bf16> : W4Half<bf16> {};
 template <> struct W4<f16> : W4Half<f16> {};
 
 // S: bits of a scale (float, or either 16-bit type); kRuns: runs of 32 weights to a scale within a block of 128 (1, 2, 4); kM: tiles of
-// 16 rows; kN: of 16 columns; kRing: weights by a ring in LDS.
-template <typename X, typename S, int kRuns, int kM, int kN, bool kRing>
-__global__ __launch_bounds__(kW4Threads, kRing ? 4 : 2) void gemv_w4_kernel(W4Args a)
+// 16 rows; kN: of 16 columns that a wavefront has; kRing: weights by a ring in LDS; kC: sets of wavefronts with columns of their own;
+// kK: times eight wavefronts share K.
+template <typename X, typename S, int kRuns, int kM, int kN, bool kRing, int kC, int kK>
+__global__ __launch_bounds__(kW4Threads * kC * kK, kRing ? 4 : 2 * kC * kK) void gemv_w4_kernel(W4Args a)
 {
     typedef W4<X> Q;
     typedef typename Q::Rows Rows;
     typedef typename Q::Sum Sum;
     constexpr int kScales = 4 / kRuns;                        // to a block
-    constexpr int kCols = 16 * kN, kPer16 = 16 / (int)sizeof(X);
-    constexpr int kPieces = w4_pieces(kM, kRing);         // of x, 16 bytes, that a thread has of a chunk
+    constexpr int kThreads = kW4Threads * kC * kK, kParts = kW4Waves * kK, kWaves = kParts * kC, kLength = kW4Chunk * kK;   // kLength: of the shortest chunk
+    constexpr int kCols = 16 * kN * kC, kPer16 = 16 / (int)sizeof(X);
+    constexpr int kPieces = w4_pieces(kM, kRing, kC, kK), kW4Scales = w4_scales(kM, kC * kK);   // that a thread has of a chunk
+    static_assert(kPieces * kThreads * 16 >= 16 * kM * kLength * 2 && kW4Scales * kThreads >= kLength / 128 * (4 / kRuns) * kCols, "the shortest chunk");
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const nm_w4_desc& d = a.d;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, column = lane & 15, j = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, number = tid >> 6, wave = number % kParts, side = number / kParts, column = lane & 15, j = lane >> 4;
     constexpr int kStages = w4_stages(kN, kRing);
     // the passes over the same columns are neighbours on an XCD (workgroup i runs on XCD i mod 8)
     const int pass = blockIdx.x / 8 % a.passes, n0 = (blockIdx.x / 8 / a.passes * 8 + blockIdx.x % 8) * kCols;
@@ -143,22 +148,22 @@ __global__ __launch_bounds__(kW4Threads, kRing ? 4 : 2) void gemv_w4_kernel(W4Ar
     if (n0 >= d.N) return;
     const int groups = d.K / d.group;
     const int run = 1 << a.chunk_shift;                       // a wavefront's blocks of a chunk
-    const int entry_shift = a.chunk_shift + 3 + (kRuns == 4 ? 0 : kRuns == 2 ? 1 : 2), entries = 1 << entry_shift;   // scales of a column and chunk
+    const int entry_shift = a.chunk_shift + (kK == 2 ? 4 : 3) + (kRuns == 4 ? 0 : kRuns == 2 ? 1 : 2), entries = 1 << entry_shift;   // scales of a column and chunk
     const unsigned exponent = Q::exponent();
     // LDS: the wavefronts' rings, the chunk's scales (rows one longer), the chunk's x; at the end the sums, from the start
-    char* s_w = smem + wave * kStages * 1024 * kN;
-    float* s_scale = reinterpret_cast<float*>(smem + kW4Waves * kStages * 1024 * kN);
-    char* s_x = smem + kW4Waves * kStages * 1024 * kN + (kCols * (entries + 1) * 4 + 15) / 16 * 16;
+    char* s_w = smem + number * kStages * 1024 * kN;
+    float* s_scale = reinterpret_cast<float*>(smem + kWaves * kStages * 1024 * kN);
+    char* s_x = smem + kWaves * kStages * 1024 * kN + (kCols * (entries + 1) * 4 + 15) / 16 * 16;
 
     // weights: lane 4 r + i has run i ^ r / 4 % 4 of row r, so that no two banks meet when lane (j, row) reads run j of its row.  Columns
     // behind the last read the last one's: what comes of them is not written.  Behind K the last run is repeated: it meets zeros of x.
     const uint8_t* wrow[kN];
 #pragma unroll
-    for (int c = 0; c < kN; ++c) wrow[c] = d.W + (long)min(n0 + c * 16 + (lane >> 2), d.N - 1) * (d.K / 2);
+    for (int c = 0; c < kN; ++c) wrow[c] = d.W + (long)min(n0 + (side * kN + c) * 16 + (lane >> 2), d.N - 1) * (d.K / 2);
     const int total = a.chunks * run;                         // the wavefront's blocks
-    const unsigned ring = (unsigned)(uintptr_t)smem + wave * kStages * 1024 * kN;
+    const unsigned ring = (unsigned)(uintptr_t)smem + number * kStages * 1024 * kN;
     auto bytes_of = [&](int u) {                              // of the lane's piece of block number u, from the row's begin
-        const int kb = ((u >> a.chunk_shift) * kW4Waves + wave) * run + (u & (run - 1));
+        const int kb = ((u >> a.chunk_shift) * kParts + wave) * run + (u & (run - 1));
         return min(kb * 128 + ((lane & 3) ^ (lane >> 4 & 3)) * 32, d.K - 32) / 2;
     };
     auto request = [&](int u, int slot) {
@@ -169,21 +174,20 @@ __global__ __launch_bounds__(kW4Threads, kRing ? 4 : 2) void gemv_w4_kernel(W4Ar
     const int read_at = (column * 4 + (j ^ (column >> 2))) * 16;
 
     // x and scales of a chunk: into registers, then into LDS (x in the order that the matrix instructions want)
-    constexpr int kW4Scales = w4_scales(kM);
-    const int row_shift = a.chunk_shift + (sizeof(X) == 1 ? 6 : 7);   // pieces to a row of a chunk: 64 and more, so a wavefront's are of one row
-    const int uniform_wave = __builtin_amdgcn_readfirstlane(wave);
+    const int row_shift = a.chunk_shift + (sizeof(X) == 1 ? 6 : 7) + (kK == 2);   // pieces to a row of a chunk: 64 and more, so a wavefront's are of one row
+    const int uniform_wave = __builtin_amdgcn_readfirstlane(number);
     v4u xp[kPieces];
     S sp[kW4Scales];
     auto fetch = [&](int chunk) {
 #pragma unroll
         for (int q = 0; q < kPieces; ++q) {
-            const int p = uniform_wave * 64 + q * kW4Threads, r = min(p >> row_shift, rows - 1);
-            const int k = (chunk * (kW4Chunk << a.chunk_shift) + (p & ((1 << row_shift) - 1)) * kPer16) + lane * kPer16;
+            const int p = uniform_wave * 64 + q * kThreads, r = min(p >> row_shift, rows - 1);
+            const int k = (chunk * (kLength << a.chunk_shift) + (p & ((1 << row_shift) - 1)) * kPer16) + lane * kPer16;
             xp[q] = *reinterpret_cast<const v4u*>(static_cast<const X*>(d.x) + (long)(m0 + r) * d.x_stride + (unsigned)min(k, d.K - kPer16));
         }
 #pragma unroll
         for (int q = 0; q < kW4Scales; ++q) {
-            const int i = tid + q * kW4Threads, c = min(i >> entry_shift, kCols - 1), e = i & (entries - 1), block = chunk * (run * kW4Waves) + e / kScales;
+            const int i = tid + q * kThreads, c = min(i >> entry_shift, kCols - 1), e = i & (entries - 1), block = chunk * (run * kParts) + e / kScales;
             const int g = min(kRuns == 4 ? (int)quotient(block, a.per) : block * kScales + e % kScales, groups - 1);
             sp[q] = static_cast<const S*>(d.scales)[(long)min(n0 + c, d.N - 1) * groups + g];
         }
@@ -191,23 +195,25 @@ __global__ __launch_bounds__(kW4Threads, kRing ? 4 : 2) void gemv_w4_kernel(W4Ar
     };
     int flip = 0;                                             // of the buffer in use
     auto stage = [&](int chunk) {
+        int lane_at = lane * 16;
+        asm volatile("" : "+v"(lane_at));                      // not every piece's address in a register of its own from the start
 #pragma unroll
         for (int q = 0; q < kPieces; ++q) {
-            const int p = uniform_wave * 64 + q * kW4Threads, r = p >> row_shift, at = p & ((1 << row_shift) - 1);
-            if (r < rows) *reinterpret_cast<v4u*>(s_x + flip + r * a.x_stride + at * 16 + lane * 16) = Q::order(xp[q]);
+            const int p = uniform_wave * 64 + q * kThreads, r = p >> row_shift, at = p & ((1 << row_shift) - 1);
+            if (r < rows) *reinterpret_cast<v4u*>(s_x + flip + r * a.x_stride + at * 16 + lane_at) = Q::order(xp[q]);
         }
-        if ((chunk + 1) * (kW4Chunk << a.chunk_shift) > d.K) {        // zeros behind K
+        if ((chunk + 1) * (kLength << a.chunk_shift) > d.K) {        // zeros behind K
             asm volatile("");
 #pragma unroll 1
             for (int q = 0; q < kPieces; ++q) {
-                const int p = uniform_wave * 64 + q * kW4Threads, r = p >> row_shift, at = p & ((1 << row_shift) - 1);
-                if (r < rows && (chunk * (kW4Chunk << a.chunk_shift) + at * kPer16) + lane * kPer16 >= d.K)
+                const int p = uniform_wave * 64 + q * kThreads, r = p >> row_shift, at = p & ((1 << row_shift) - 1);
+                if (r < rows && (chunk * (kLength << a.chunk_shift) + at * kPer16) + lane * kPer16 >= d.K)
                     *reinterpret_cast<v4u*>(s_x + flip + r * a.x_stride + at * 16 + lane * 16) = v4u{};
             }
         }
 #pragma unroll
         for (int q = 0; q < kW4Scales; ++q) {
-            const int i = tid + q * kW4Threads, c = i >> entry_shift, e = i & (entries - 1);
+            const int i = tid + q * kThreads, c = i >> entry_shift, e = i & (entries - 1);
             float v;
             if constexpr (sizeof(S) == 4) v = sp[q];
             else v = d.scale_dtype == NM_DT_BF16 ? __uint_as_float((unsigned)sp[q] << 16) : (float)__builtin_bit_cast(f16, sp[q]);
@@ -223,39 +229,57 @@ __global__ __launch_bounds__(kW4Threads, kRing ? 4 : 2) void gemv_w4_kernel(W4Ar
     const char* xrow[kM];
 #pragma unroll
     for (int t = 0; t < kM; ++t) xrow[t] = s_x + min(t * 16 + column, rows - 1) * a.x_stride + (wave * run * 128 + j * 8) * sizeof(X);
-    const float* srow = s_scale + column * (entries + 1) + wave * run * kScales;
+    const float* srow = s_scale + (side * kN * 16 + column) * (entries + 1) + wave * run * kScales;
 
+    // x and scales of a block for one tile of rows: they do not wait for its weights
+    constexpr bool kEarly = kM == 1 && !kRing;
+    Rows x1[4];
+    float scale1[kScales][kN];
+    auto rows_of = [&](int t, int at, int i) { return *reinterpret_cast<const Rows*>(xrow[t] + flip + (at * 128 + i * 32) * sizeof(X)); };
+    auto scale_of = [&](int c, int at, int g) { return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(srow + c * 16 * (entries + 1) + at * kScales + g) + flip); };
+    auto ahead = [&](int at) {
+        if constexpr (kEarly) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x1[i] = rows_of(0, at, i);
+#pragma unroll
+            for (int g = 0; g < kScales; ++g)
+#pragma unroll
+                for (int c = 0; c < kN; ++c) scale1[g][c] = scale_of(c, at, g);
+        }
+    };
     auto block = [&](int at, const v4u (&now)[kN]) {          // block number at of the wavefront's run in this chunk
 #pragma unroll
         for (int g = 0; g < kScales; ++g) {
             float scale[kN];
 #pragma unroll
-            for (int c = 0; c < kN; ++c) scale[c] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(srow + c * 16 * (entries + 1) + at * kScales + g) + flip);
-            auto rows_of = [&](int t, int i) { return *reinterpret_cast<const Rows*>(xrow[t] + flip + (at * 128 + i * 32) * sizeof(X)); };
-            Sum acc[kM][kN];
-            Rows x[kM][kRuns];
+            for (int c = 0; c < kN; ++c) scale[c] = kEarly ? scale1[g][c] : scale_of(c, at, g);
+            decltype(Q::weights(0u, 0u)) weights[kM > 1 ? kRuns : 1][kN];   // made once for all tiles of rows
+            if constexpr (kM > 1) {
 #pragma unroll
-            for (int t = 0; t < kM; ++t) {                    // the offset is where the sums begin
-                Sum off{};
+                for (int i = 0; i < kRuns; ++i)
 #pragma unroll
-                for (int i = 0; i < kRuns; ++i) off = Q::offset(x[t][i] = rows_of(t, g * kRuns + i), off);
-#pragma unroll
-                for (int c = 0; c < kN; ++c) acc[t][c] = off;
+                    for (int c = 0; c < kN; ++c) weights[i][c] = Q::weights(now[c][g * kRuns + i], exponent);
             }
 #pragma unroll
-            for (int i = 0; i < kRuns; ++i)
+            for (int t = 0; t < kM; ++t) {
+                Rows x[kRuns];
+                Sum off{}, acc[kN];
 #pragma unroll
-                for (int c = 0; c < kN; ++c) {
-                    const auto weights = Q::weights(now[c][g * kRuns + i], exponent);
+                for (int i = 0; i < kRuns; ++i) off = Q::offset(x[i] = kEarly ? x1[g * kRuns + i] : rows_of(t, at, g * kRuns + i), off);
 #pragma unroll
-                    for (int t = 0; t < kM; ++t) acc[t][c] = Q::add(x[t][i], weights, acc[t][c]);
-                }
+                for (int c = 0; c < kN; ++c) acc[c] = off;    // the offset is where the sums begin
 #pragma unroll
-            for (int t = 0; t < kM; ++t)
+                for (int i = 0; i < kRuns; ++i)
+#pragma unroll
+                    for (int c = 0; c < kN; ++c) {
+                        if constexpr (kM == 1) acc[c] = Q::add(x[i], Q::weights(now[c][g * kRuns + i], exponent), acc[c]);
+                        else acc[c] = Q::add(x[i], weights[i][c], acc[c]);
+                    }
 #pragma unroll
                 for (int c = 0; c < kN; ++c)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[t][c][e] = __builtin_fmaf((float)acc[t][c][e], scale[c], sum[t][c][e]);
+                    for (int e = 0; e < 4; ++e) sum[t][c][e] = __builtin_fmaf((float)acc[c][e], scale[c], sum[t][c][e]);
+            }
         }
     };
 
@@ -277,6 +301,7 @@ __global__ __launch_bounds__(kW4Threads, kRing ? 4 : 2) void gemv_w4_kernel(W4Ar
             if (u < total) request(u, u);
         for (int u = 0, slot = 0; u < total; ++u, slot = slot + 1 == kStages ? 0 : slot + 1) {
             if (!(u & (run - 1))) next_chunk(u >> a.chunk_shift);
+            ahead(u & (run - 1));
             // what was requested behind this block may still be under way; at the end nothing is requested any more
             if (u + kStages <= total) wait_vmcnt<(kStages - 1) * kN>();
             else wait_vmcnt<0>();
@@ -304,6 +329,7 @@ __global__ __launch_bounds__(kW4Threads, kRing ? 4 : 2) void gemv_w4_kernel(W4Ar
                 const int u = u0 + odd;
                 if (u >= total) break;
                 if (!(u & (run - 1))) next_chunk(u >> a.chunk_shift);
+                ahead(u & (run - 1));
 #pragma unroll
                 for (int c = 0; c < kN; ++c) *reinterpret_cast<v4u*>(s_w + c * 1024 + lane * 16) = w[odd][c];
                 load(u + 2, w[odd]);                          // behind the last block: the last run, not used
@@ -321,14 +347,14 @@ __global__ __launch_bounds__(kW4Threads, kRing ? 4 : 2) void gemv_w4_kernel(W4Ar
 #pragma unroll
         for (int c = 0; c < kN; ++c)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s_sum[wave][t][j * 4 + e][c * 16 + column] = sum[t][c][e];
+            for (int e = 0; e < 4; ++e) s_sum[wave][t][j * 4 + e][(side * kN + c) * 16 + column] = sum[t][c][e];
     __syncthreads();
-    for (int i = tid; i < kM * 16 * kCols; i += kW4Threads) {
+    for (int i = tid; i < kM * 16 * kCols; i += kThreads) {
         const int c = i % kCols, r = i / kCols % 16, t = i / (16 * kCols), m = m0 + t * 16 + r, col = n0 + c;
         if (m >= d.M || col >= d.N) continue;
         float v = 0.0f;
 #pragma unroll
-        for (int p = 0; p < kW4Waves; ++p) v += s_sum[p][t][r][c];
+        for (int p = 0; p < kParts; ++p) v += s_sum[p][t][r][c];
         v = __builtin_fmaf(v, d.alpha, d.bias ? d.bias[col] : 0.0f);
         if (d.table_idx >= 0) {
             int seg;
@@ -338,30 +364,33 @@ __global__ __launch_bounds__(kW4Threads, kRing ? 4 : 2) void gemv_w4_kernel(W4Ar
     }
 }
 
-template <typename X, typename S, int kRuns, int kM, int kN, bool kRing>
+template <typename X, typename S, int kRuns, int kM>
+static int32_t launch_w4_registers(const W4Args& a, hipStream_t s);
+template <typename X, typename S, int kRuns, int kM, int kN, bool kRing, int kC = 1, int kK = 1>
 static int32_t launch_w4_tiles(W4Args a, hipStream_t s)
 {
     a.passes = (a.d.M + 16 * kM - 1) / (16 * kM);
     // the longest chunk whose x and scales a workgroup's threads hold at once, no longer than K
     const int rows = a.d.M < 16 * kM ? a.d.M : 16 * kM;
-    const long room = (long)w4_pieces(kM, kRing) * kW4Threads * 16;
+    constexpr int kCols = 16 * kN * kC, kWaves = kW4Waves * kC * kK, kLength = kW4Chunk * kK;
+    const long room = (long)w4_pieces(kM, kRing, kC, kK) * kWaves * 64 * 16, scales = (long)w4_scales(kM, kC * kK) * kWaves * 64;
     a.chunk_shift = 0;
-    while ((kW4Chunk << a.chunk_shift) < a.d.K && (kW4Waves << (a.chunk_shift + 1)) * (4 / kRuns) * 16 * kN <= w4_scales(kM) * kW4Threads && rows * (long)(2 * kW4Chunk << a.chunk_shift) * (long)sizeof(X) <= room) ++a.chunk_shift;
-    const int chunk = kW4Chunk << a.chunk_shift;
+    while ((kLength << a.chunk_shift) < a.d.K && (2 * kLength << a.chunk_shift) / 128 * (4 / kRuns) * kCols <= scales && rows * (long)(2 * kLength << a.chunk_shift) * (long)sizeof(X) <= room) ++a.chunk_shift;
+    const int chunk = kLength << a.chunk_shift;
     a.chunks = (a.d.K + chunk - 1) / chunk;
     if constexpr (kRing)
-        if (a.chunks > 2) return launch_w4_tiles<X, S, kRuns, kM, kN, false>(a, s);
+        if (a.chunks > 2 / kK) return launch_w4_registers<X, S, kRuns, 1>(a, s);   // (4 rows of 4096 x 11008: 11.4 us, 12.6 as two chunks of the ring)
     a.x_stride = chunk * (int)sizeof(X) + 16;
     const int entries = (chunk / 128) * (4 / kRuns);
-    const size_t one = (size_t)(16 * kN * (entries + 1) * 4 + 15) / 16 * 16 + (size_t)rows * a.x_stride;
-    size_t used = (size_t)kW4Waves * w4_stages(kN, kRing) * 1024 * kN + one;
+    const size_t one = (size_t)(kCols * (entries + 1) * 4 + 15) / 16 * 16 + (size_t)rows * a.x_stride;
+    size_t used = (size_t)kWaves * w4_stages(kN, kRing) * 1024 * kN + one;
     // with two buffers a wavefront may write the next chunk's while another still reads this one's: one barrier a chunk instead of two
     if (!kRing && a.chunks > 1 && used + one <= 160 * 1024) {
         a.second = (int)one;
         used += one;
     }
-    const size_t sums = (size_t)kW4Waves * kM * 16 * 16 * kN * 4, shmem = used > sums ? used : sums;
-    auto kern = gemv_w4_kernel<X, S, kRuns, kM, kN, kRing>;
+    const size_t sums = (size_t)kW4Waves * kK * kM * 16 * kCols * 4, shmem = used > sums ? used : sums;
+    auto kern = gemv_w4_kernel<X, S, kRuns, kM, kN, kRing, kC, kK>;
     if (shmem > 64 * 1024) {
         static std::once_flag once;
         static int32_t once_rc;
@@ -371,16 +400,39 @@ static int32_t launch_w4_tiles(W4Args a, hipStream_t s)
         });
         if (once_rc) return once_rc;
     }
-    queue_kernel(kern, dim3(((a.d.N + 16 * kN - 1) / (16 * kN) + 7) / 8 * 8 * a.passes), dim3(kW4Threads), shmem, s, a);
+    queue_kernel(kern, dim3(((a.d.N + kCols - 1) / kCols + 7) / 8 * 8 * a.passes), dim3(64 * kWaves), shmem, s, a);
     return check_hip(hipGetLastError(), "nm_gemv_w4 launch");
+}
+// Weights through registers, tiles of 16 kM rows: 16 columns to a workgroup where no more than a CU's worth come of it, 32 where there
+// are more.  A chunk of x fills LDS either way, so one workgroup has a CU and more than 256 are a second round (16 columns of 7168 x 8192
+// took 18.4 us at 16 rows, 32 take 12.6).  With 16 columns sixteen wavefronts share K, unless it is a chunk of eight's
+// (4096 x 11008, 16 rows: 13.5 us, eight 15.7).
+template <typename X, typename S, int kRuns, int kM>
+static int32_t launch_w4_registers(const W4Args& a, hipStream_t s)
+{
+    const long passes = (a.d.M + 16 * kM - 1) / (16 * kM), columns = (a.d.N + 15) / 16;
+    if constexpr (kM < 3)
+        if (passes * columns <= 256) {
+            if constexpr (kM == 2)
+                if (a.d.K <= 2048) return launch_w4_tiles<X, S, kRuns, kM, 1, false>(a, s);
+            return launch_w4_tiles<X, S, kRuns, kM, 1, false, 1, 2>(a, s);   // (one tile of rows has a ring for so short a K)
+        }
+    return launch_w4_tiles<X, S, kRuns, kM, 1, false, 2>(a, s);
 }
 template <typename X, typename S, int kRuns>
 static int32_t launch_w4_rows(const W4Args& a, hipStream_t s)
 {
-    // 32 columns to a workgroup read x half as often; 16 where there would be fewer workgroups than CUs
-    if (a.d.M <= 16) return a.d.N > 32 * 255 ? launch_w4_tiles<X, S, kRuns, 1, 2, true>(a, s) : launch_w4_tiles<X, S, kRuns, 1, 1, true>(a, s);
-    // tiles of 48 rows where that saves a pass over the weights (those and x of a chunk are what LDS holds)
-    return (a.d.M + 47) / 48 < (a.d.M + 31) / 32 ? launch_w4_tiles<X, S, kRuns, 3, 2, false>(a, s) : launch_w4_tiles<X, S, kRuns, 2, 2, false>(a, s);
+    // The fewest rows and columns to a workgroup that leave it a CU of its own, for rows are what a workgroup's time grows with (40 rows of
+    // 4096 x 11008: 28.7 us as one tile of 48, 20.3 as two of 32; of 768 x 768 6.5 and, as three of 16, 4.4).  Where there are more workgroups
+    // than CUs anyway, tiles of 48 rows if they save a pass over the weights (those and x of a chunk are what LDS holds).
+    // A ring of eight wavefronts has 4096 columns of x under way at once; beyond, sixteen (one row of 4096 x 11008 10.9 us, 11.5 with eight; of
+    // 4096 x 4096 5.6 and 5.3).
+    const long M = a.d.M, columns = (a.d.N + 15) / 16;
+    if ((M + 15) / 16 * columns <= 256)
+        return a.d.K <= 4096 ? launch_w4_tiles<X, S, kRuns, 1, 1, true>(a, s) : launch_w4_tiles<X, S, kRuns, 1, 1, true, 1, 2>(a, s);
+    if (M <= 16) return launch_w4_tiles<X, S, kRuns, 1, 2, true>(a, s);
+    if ((M + 31) / 32 * ((columns + 1) / 2) > 256 && (M + 47) / 48 < (M + 31) / 32) return launch_w4_registers<X, S, kRuns, 3>(a, s);
+    return launch_w4_registers<X, S, kRuns, 2>(a, s);
 }
 template <typename X, typename S>
 static int32_t launch_w4_group(const W4Args& a, hipStream_t s)

@@ -556,6 +556,16 @@ def test_gemv_w4(x_dtype, scale_dtype, out_dtype, M, N, K, group):
     check_w4(w4_case(M + K, M, N, K, group, x_dtype, scale_dtype), out_dtype, bias=N % 2 == 0)
 
 
+@pytest.mark.parametrize("x_dtype,scale_dtype,out_dtype", [(torch.int8, torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16, torch.bfloat16),
+                                                           (torch.float16, torch.float32, torch.float32)])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,N,K", [(1, 70, 2304), (16, 50, 11008), (33, 100, 2432), (2, 4100, 384), (16, 4097, 4224), (17, 2100, 896), (32, 2070, 4992), (40, 3001, 2176),
+                                   (41, 8193, 1152), (48, 8200, 2560), (130, 1031, 2304)])
+def test_gemv_w4_shares_of_the_work(x_dtype, scale_dtype, out_dtype, group, M, N, K):
+    """Either side of 256 workgroups and of 2048 columns of x, with one, two and three tiles of rows."""
+    check_w4(w4_case(M + N, M, N, K, group, x_dtype, scale_dtype), out_dtype)
+
+
 @pytest.mark.parametrize("x_dtype", [torch.int8, torch.bfloat16, torch.float16])
 def test_gemv_w4_every_weight_in_every_place(x_dtype):
     """Rows of x with a single one read one weight each: exact, so every place of a word and every one of the 16 weights is seen."""
