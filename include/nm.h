@@ -7,7 +7,7 @@
  * every nonlinear operator (GELU, the exponential and the reciprocal of softmax, the reciprocal
  * square root of LayerNorm) is a piecewise-linear table y = k[s]*x + b[s] whose segment s is found
  * by quantising x (Section 3.2, Post-Training Approximation; Algorithm 3 for k, b; Algorithm 2
- * for merged segments).
+ * for merged segments).  The last section adds a decoder's step over a paged key-value cache.
  *
  * Conventions
  *   - Plain C.  Every function returns an nm_status (0 = NM_OK, negative = error) unless stated.

@@ -3,8 +3,9 @@
 // What is needed of all requests is two prefix sums, over the new tokens and over the new pages.  Every workgroup makes both for itself
 // (two numbers of each request, from L2) and keeps them in LDS, so that no workgroup waits for another and one launch does;
 // then each token, and each new page, finds its request by bisection.  Bound by latency: a launch, and dependent steps (lengths, the
-// scan, a bisection, an entry of the table or the list, a store): 4.1 us for 8 requests of one token, of which an empty launch is 2.5.
-// 500000 tokens of 500 requests, 6 MB of stores, take 8.3 us (1.2 at the rate of a copy).
+// scan, a bisection, an entry of the table or the list, a store): 4.1 us for 8 requests of one token, where a kernel that fills one
+// line takes 1.8.  500000 tokens of 500 requests, 6 MB of stores, take 8.3 us (1.2 at the rate of a copy): as long a chain, with a scan of
+// two requests a thread and a bisection of nine steps.
 #include "nm_decode.h"
 
 namespace nm {

@@ -6,6 +6,8 @@
 // token: a workgroup has up to eight tokens, a thread makes the sine and cosine of one of their angles while the first loads are
 // under way, and all heads read them from LDS.  An angle is reduced in 64 bits (position * frequency reaches 10^6
 // radians, where 32 bits would leave 0.06 of error) and its sine taken in 32.
+//   16397 tokens of 32 + 8 + 8 bf16 heads of 128 (403 MB): 93 us, 4.3 TB/s, 80 us at a copy's 5.06 TB/s; vector instructions are issued in 46 %
+// of the cycles.  8 bytes of either half at a time and one token to a workgroup took 114.  One token of 36 heads: 3.5 us, a launch and three dependent loads.
 #include "nm_decode.h"
 
 namespace nm {
