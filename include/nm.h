@@ -500,7 +500,7 @@ int32_t nm_cnn_run(const nm_cnn_op* ops, int32_t n_ops, void* ws, size_t ws_byte
  * cached, fresh: device [B].  free_pages: device [n_free].  block_table: device [B] rows of max_pages entries, table_stride
  * apart.  slots, positions, requests: [max_tokens].  lens, row_start, positions, requests may be NULL.  No output may be an input
  * (one workgroup writes while another still reads): *free_end and lens need memory of their own.
- * Limits: B <= NM_PLAN_MAX_REQUESTS; num_pages * page_size < 2^31; page_size <= 65536; max_tokens, n_free <= 2^30.
+ * Limits: B <= NM_PLAN_MAX_REQUESTS; num_pages * page_size and max_pages * page_size < 2^31; page_size <= 65536; max_tokens, n_free <= 2^30.
  */
 #define NM_PLAN_MAX_REQUESTS 4096
 enum { NM_PLAN_NO_PAGES = 1,      /* the free list is too short */

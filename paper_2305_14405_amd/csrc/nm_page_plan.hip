@@ -165,6 +165,7 @@ extern "C" int32_t nm_page_plan(const nm_plan_desc* d, void* stream)
     const int shift = page_shift(d->page_size);
     if (shift < 0) return fail(NM_ERR_UNSUPPORTED, "nm_page_plan: page_size %d is no power of two up to 65536", d->page_size);
     if ((int64_t)d->num_pages << shift > 0x7fffffffLL) return fail(NM_ERR_UNSUPPORTED, "nm_page_plan: num_pages * page_size >= 2^31");
+    if ((int64_t)d->max_pages << shift > 0x7fffffffLL) return fail(NM_ERR_UNSUPPORTED, "nm_page_plan: max_pages * page_size >= 2^31");   // a position is an int
     if (d->B && d->table_stride < d->max_pages) return fail(NM_ERR_INVALID_ARG, "nm_page_plan: table_stride < max_pages");
     if (!d->free_begin || !d->free_end || !d->status || (d->max_tokens && !d->slots))
         return fail(NM_ERR_INVALID_ARG, "nm_page_plan: free_begin, free_end, status or slots is NULL");

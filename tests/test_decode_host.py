@@ -50,6 +50,10 @@ def test_page_plan_does_not_cover(lib, changes):
     refused(lib.nm_page_plan, plan(), nm.NM_ERR_UNSUPPORTED, **changes)
 
 
+def test_page_plan_positions_of_31_bits(lib):
+    refused(lib.nm_page_plan, plan(), nm.NM_ERR_UNSUPPORTED, page_size=1 << 16, max_pages=1 << 15, table_stride=1 << 15)
+
+
 def test_page_plan_null(lib):
     assert lib.nm_page_plan(None, Z) == nm.NM_ERR_INVALID_ARG
 
