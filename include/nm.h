@@ -578,7 +578,7 @@ int32_t nm_qk_norm_rope(const nm_qk_desc* desc, void* stream);
  * q: device [B, hq, d], requests q_stride elements apart, q_dtype F32, BF16 or F16.  Cache: as above, cache_dtype BF16, F16 or I8
  * (then k_scale, v_scale: device fp32 [hk]).  block_table: device int32, rows of max_pages entries table_stride apart.  lens:
  * device int32 [B].  out: device [B, hq, d], requests out_stride apart, out_dtype F32, BF16, F16 or I8 (codes with
- * out_inv_scale: what nm_gemm_pwl reads).  lse: device fp32 [B, hq] or NULL.
+ * out_inv_scale: what nm_gemm_pwl reads); out may be q itself (same type and stride).  lse: device fp32 [B, hq] or NULL.
  * q is split into as many terms of the matrix instructions' type as hold it, the weights into two (fp32 results: three), so nothing
  * but the outputs is rounded to fewer than 16 bits.
  * Workspace: query nm_paged_attention_workspace (it looks at the shape and the types only, never at device memory; 0: none); 256-byte
@@ -619,7 +619,7 @@ int32_t nm_paged_attention(const nm_paged_desc* desc, void* ws, size_t ws_bytes,
  * x: device [M, K], rows x_stride elements apart, x_dtype I8, BF16 or F16.  W: device [N, K / 2], contiguous: byte i of a row holds
  * w[n, 2 i] in its low and w[n, 2 i + 1] in its high four bits, two's complement (-8 .. 7).  scales: device [N, K / group], contiguous,
  * scale_dtype F32, BF16 or F16.  bias: device fp32 [N] or NULL.  out: device [M, N], rows out_stride apart, out_dtype F32, BF16, F16
- * or I8.  Any M: rows are taken up to 48 at a time, and the weights read again for each (nm_gemm_pwl is the call for many rows).
+ * or I8; out is none of the inputs.  Any M: rows are taken up to 48 at a time, and the weights read again for each (nm_gemm_pwl is the call for many rows).
  * A row of bf16 or fp16 with an infinity or NaN comes out NaN; other rows are not touched by it.
  * Limits: group 32, 64 or a multiple of 128; K a multiple of group, at most 65536; x and W 16-byte aligned, x_stride a multiple of 16
  * bytes; M <= 2^20, N < 2^26, (N / 16) (M / 32) < 2^23.

@@ -167,6 +167,13 @@ def test_gemv_w4_null_and_empty(lib):
     assert lib.nm_gemv_w4(C.byref(d), Z) == nm.NM_OK
 
 
+def test_outputs_that_are_inputs(lib):
+    for n, at in (("x", P), ("W", 2 * P), ("scales", 3 * P)):
+        refused(lib.nm_gemv_w4, w4(), nm.NM_ERR_INVALID_ARG, out=at)
+    refused(attend(lib), paged(), nm.NM_ERR_INVALID_ARG, out=P)
+    refused(attend(lib), paged(), nm.NM_ERR_INVALID_ARG, out=P, out_dtype=nm.NM_DT_F32, out_stride=520)
+
+
 @pytest.mark.parametrize("packed,desc", [(nm._PLAN, nm.PlanDesc), (nm._QK, nm.QkDesc), (nm._PAGED, nm.PagedDesc), (nm._W4, nm.W4Desc)])
 def test_packed_descriptions_lie_as_the_structures(packed, desc):
     values = [float(i + 1) if t is C.c_float else i + 1 for i, (_, t) in enumerate(desc._fields_)]

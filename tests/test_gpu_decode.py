@@ -490,6 +490,17 @@ def test_paged_attention_codes_strides_and_stream():
     assert torch.equal(wide[:, 2:10], want) and bool((wide[:, :2] == 5).all()) and bool((wide[:, 10:] == 5).all())
 
 
+@pytest.mark.parametrize("lens", [[300, 1, 0, 77], [5000, 2, 0, 1999, 640]])
+def test_paged_attention_in_place(lens):
+    c = paged_case(12, lens, 8, 2, 64, torch.bfloat16, torch.bfloat16)
+    want, _ = attend(c, torch.bfloat16, 0.125)
+    want = want.clone()
+    q = c["q"].clone()
+    got, _ = attend({**c, "q": q}, torch.bfloat16, 0.125, out=q)
+    torch.cuda.synchronize()
+    assert torch.equal(q, want)
+
+
 def test_paged_attention_offsets_beyond_32_bits():
     """A cache of more than 2^32 bytes (and elements): the last pages of the pool."""
     pages, page, d = (1 << 32) // (16 * 64) + 40, 16, 64
