@@ -4,7 +4,7 @@
 // request's key head with up to 16 query heads of its group; its length is counted in units of 128 positions.  A fixed number of
 // workgroups share all rows' units evenly, each a contiguous run of them, whatever the lengths are: a run may begin and end inside a
 // row, and only those two pieces of it need joining by a second kernel; rows inside a run are written at once.  (Where no row can be long,
-// a workgroup takes a row and there is no second kernel.)  The four wavefronts of a workgroup walk a unit's four tiles of 32
+// a workgroup takes a row, of eight wavefronts if rows are few, and there is no second kernel.)  The four wavefronts of a workgroup walk a unit's four tiles of 32
 // positions, each with a running maximum, sum and output of its own, and are joined through LDS at the end of the row's piece.
 // The next tile's keys and values are on their way into registers while one is computed.
 //   Scores: keys are the rows of the 16x16x32 matrix instruction, query heads its columns, so a lane has eight positions of one head:
@@ -18,7 +18,7 @@
 //   bf16, 32 query and 8 key heads of 128: one request of 131071 positions (537 MB) 105 us and 8 for the second kernel, 5.1 TB/s in the first, a
 // copy's rate; 48 requests of up to 8192 (649 MB) 120 + 5, 5.4 TB/s.  int8, 16 heads of 64, 64 requests of up to 4097 (216 MB): 58 + 4.5,
 // 3.7 TB/s: a run has 17 units or so, and begins and ends two rows in them; codes become 16-bit numbers in vector instructions (issued in 47 % of the
-// cycles).  12 heads of 300 positions of one request: 10.4 us, a chain of dependent loads (length, page, keys) and code that runs once.
+// cycles).  12 heads of 300 positions of one request: 9.4 us (one position 7.6), a chain of dependent loads (length, page, keys) and code that runs once.
 #include <algorithm>
 
 #include "nm_decode.h"
@@ -45,6 +45,7 @@ struct PagedArgs {
     int groups;           // of up to 16 of them
     int share;            // rows that read the same lines of the cache: a team of so many workgroups of one XCD takes them side by side
     int workers;          // teams that share the units; 0: one team to a set of rows
+    int wide;             // a workgroup to a set of rows, of eight wavefronts
     int extra;            // units that starting and ending a row costs
     float* part_o;        // [share, workers, 2, 16, d]: a run's first and last piece, not yet divided by the sum
     float2* part_ml;      // [share, workers, 2, 16]: maximum (of scores in units of log 2) and sum
@@ -163,22 +164,23 @@ __device__ __forceinline__ void fetch_rows(const char* base, unsigned place, v4u
 }
 
 // C: type of the cache; T: of the matrix instructions; DP: d rounded up to 64, 128 or 256; kQ: terms of a query (1 or 3); kP: of the weights
-// (2 or 3).
-template <typename C, typename T, int DP, int kQ, int kP>
-__global__ __launch_bounds__(kPagedThreads, workgroups_of(DP)) void paged_attention_kernel(PagedArgs a)
+// (2 or 3); W: wavefronts (more than kPagedWaves: each workgroup has a row whole).
+template <typename C, typename T, int DP, int kQ, int kP, int W>
+__global__ __launch_bounds__(64 * W, W == kPagedWaves ? workgroups_of(DP) : W / 4) void paged_attention_kernel(PagedArgs a)
 {
     constexpr int kRowPieces = DP * (int)sizeof(C) / 16;      // 16-byte pieces of a row: lanes to a row
     constexpr int kPer16 = 16 / (int)sizeof(C);               // elements of one
     constexpr int kRowsAtOnce = 64 / kRowPieces, kLoads = kTile / kRowsAtOnce;
     constexpr int kStride = DP + 8;                           // elements between rows in LDS
     constexpr int kSteps = DP / 32, kBlocks = DP / 16;
+    constexpr int kStep = kTile * W;                          // positions of all wavefronts' tiles
     constexpr float kLift = std::is_same<T, f16>::value ? 10.0f : 0.0f;   // fp16 weights are held times 2^10, where small ones have more bits
     __shared__ __attribute__((aligned(16))) union {
-        short tile[kPagedWaves][kTile * kStride];
-        float o[kPagedWaves][16][DP];
+        short tile[W][kTile * kStride];
+        float o[W][16][DP];
     } s;
     __shared__ __attribute__((aligned(16))) short s_q[kQ][16 * kStride];
-    __shared__ float s_qscale[16], s_m[kPagedWaves][16], s_l[kPagedWaves][16];
+    __shared__ float s_qscale[16], s_m[W][16], s_l[W][16];
     __shared__ long s_scan[kPagedWaves], s_before;
     __shared__ int s_b;
 
@@ -201,7 +203,9 @@ __global__ __launch_bounds__(kPagedThreads, workgroups_of(DP)) void paged_attent
     int b;
     long u, u1, first, before, each = 0, longer = 0;
     int4 joined = make_int4(0, 0, 0, 0);
-    if (a.workers) {
+    bool early = false;
+    int early_entry = 0;
+    if (W == kPagedWaves && a.workers) {
         const Scan scan = scan_units(a, s_scan);
         const long all = scan.all * rows;
         const Shares shares(all, a.workers);
@@ -229,6 +233,9 @@ __global__ __launch_bounds__(kPagedThreads, workgroups_of(DP)) void paged_attent
         before = 0;
         u = first = worker % rows;                            // a row of no positions is written too
         u1 = u + 1;
+        // the first tile's pages, while the length is under way
+        early = !d.window && d.max_pages;
+        if (early) early_entry = d.block_table[b * d.table_stride + min((wave * kTile + my_position) >> a.shift, d.max_pages - 1)];
     }
 
     // The next piece of a row in this workgroup's run.
@@ -324,7 +331,7 @@ __global__ __launch_bounds__(kPagedThreads, workgroups_of(DP)) void paged_attent
         return;
     }
     int t0 = now.k0 + wave * kTile;
-    int entry = entry_of(now, t0), entry2 = entry_of(now, t0 + kUnit);
+    int entry = early ? early_entry : entry_of(now, t0), entry2 = entry_of(now, t0 + kStep);
     fetch_queries(now);
     v4u kr[kLoads], vr[kLoads];
     unsigned long valid;
@@ -336,7 +343,7 @@ __global__ __launch_bounds__(kPagedThreads, workgroups_of(DP)) void paged_attent
     while (true) {
         const Piece then = advance();
         const int then_t0 = then.k0 + wave * kTile;
-        const int then_entry = entry_of(then, then_t0), then_entry2 = entry_of(then, then_t0 + kUnit);
+        const int then_entry = entry_of(then, then_t0), then_entry2 = entry_of(then, then_t0 + kStep);
         entry = entry2;
         const int b = now.b, g = now.g, h0 = now.h0, heads = now.heads, k1 = now.k1;
 
@@ -352,6 +359,7 @@ __global__ __launch_bounds__(kPagedThreads, workgroups_of(DP)) void paged_attent
             up = __uint_as_float((unsigned)(127 + e) << 23);
         }
         __syncthreads();                                      // the piece before is done with LDS
+        if (W == kPagedWaves || qrow < 16)
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) {
             float rest = copysignf(down, by) * x[i];
@@ -362,7 +370,7 @@ __global__ __launch_bounds__(kPagedThreads, workgroups_of(DP)) void paged_attent
                 s_q[q][qrow * kStride + qc + 16 * i] = __builtin_bit_cast(short, t);
             }
         }
-        if (qc == 0) s_qscale[qrow] = up;
+        if (qc == 0 && (W == kPagedWaves || qrow < 16)) s_qscale[qrow] = up;
         __syncthreads();
         // never 0, so that it takes a masked score, minus infinity, for what it is
         const float factor = fmaxf(fabsf(by) * s_qscale[column], 1.17549435e-38f);
@@ -376,12 +384,12 @@ __global__ __launch_bounds__(kPagedThreads, workgroups_of(DP)) void paged_attent
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) o[i] = v4f{0, 0, 0, 0};
         float m = -INFINITY, l = 0.0f;
-        for (; t0 < k1; t0 += kUnit) {
+        for (; t0 < k1; t0 += kStep) {
             unsigned long next_valid;
-            const bool more = t0 + kUnit < k1;
+            const bool more = t0 + kStep < k1;
             const Piece& of = more ? now : then;
-            const unsigned next = place_of(of, more ? t0 + kUnit : then_t0, more ? entry : then_entry, next_valid);
-            entry = entry_of(now, t0 + 2 * kUnit);
+            const unsigned next = place_of(of, more ? t0 + kStep : then_t0, more ? entry : then_entry, next_valid);
+            entry = entry_of(now, t0 + 2 * kStep);
             // scores
             stage(kr, valid);
             fetch(d.k_cache, of, next, kr);
@@ -449,12 +457,12 @@ __global__ __launch_bounds__(kPagedThreads, workgroups_of(DP)) void paged_attent
         fetch_queries(then);
         l = __int_as_float(butterfly_step<32>(butterfly_step<16>(__float_as_int(l), AddF32{}), AddF32{}));
 
-        // the four wavefronts' results as one
+        // the wavefronts' results as one
         if (j == 0) { s_m[wave][column] = m; s_l[wave][column] = l; }
         __syncthreads();                                      // also: no tile is read any more
         float top = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kPagedWaves; ++w) top = fmaxf(top, s_m[w][column]);
+        for (int w = 0; w < W; ++w) top = fmaxf(top, s_m[w][column]);
         const float base = top == -INFINITY ? 0.0f : top;
         const float mine = __builtin_amdgcn_exp2f(m - base - kLift);
 #pragma unroll
@@ -467,10 +475,10 @@ __global__ __launch_bounds__(kPagedThreads, workgroups_of(DP)) void paged_attent
         if (row < heads) {
             float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kPagedWaves; ++w) top = fmaxf(top, s_m[w][row]);
+            for (int w = 0; w < W; ++w) top = fmaxf(top, s_m[w][row]);
             const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-            for (int w = 0; w < kPagedWaves; ++w) sum += s_l[w][row] * __builtin_amdgcn_exp2f(s_m[w][row] - base - kLift);
+            for (int w = 0; w < W; ++w) sum += s_l[w][row] * __builtin_amdgcn_exp2f(s_m[w][row] - base - kLift);
             if ((tid & 15) == 0) {
                 if (now.slot >= 0) a.part_ml[part_of(a, member, worker, now.slot) + row] = make_float2(top, sum);
                 else if (d.lse) d.lse[(long)b * d.hq + h0 + row] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
@@ -479,7 +487,7 @@ __global__ __launch_bounds__(kPagedThreads, workgroups_of(DP)) void paged_attent
             for (int c = (tid & 15) * 4; c < d.d; c += 64) {
                 v4f x{0, 0, 0, 0};
 #pragma unroll
-                for (int w = 0; w < kPagedWaves; ++w) x += *reinterpret_cast<const v4f*>(&s.o[w][row][c]);
+                for (int w = 0; w < W; ++w) x += *reinterpret_cast<const v4f*>(&s.o[w][row][c]);
                 if (now.slot >= 0) {
                     *reinterpret_cast<v4f*>(a.part_o + (part_of(a, member, worker, now.slot) + row) * d.d + c) = x;
                 } else {
@@ -544,20 +552,20 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_kernel(PagedArgs a)
     if (tid == 0 && d.lse) d.lse[bh] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
 }
 
-template <typename C, typename T, int DP>
+template <typename C, typename T, int DP, int W>
 static void launch_paged(const PagedArgs& a, int blocks, bool own, hipStream_t s)
 {
-    if (own && a.d.out_dtype != NM_DT_F32) queue_kernel(paged_attention_kernel<C, T, DP, 1, 2>, dim3(blocks), dim3(kPagedThreads), 0, s, a);
-    else queue_kernel(paged_attention_kernel<C, T, DP, 3, 3>, dim3(blocks), dim3(kPagedThreads), 0, s, a);
+    if (own && a.d.out_dtype != NM_DT_F32) queue_kernel(paged_attention_kernel<C, T, DP, 1, 2, W>, dim3(blocks), dim3(64 * W), 0, s, a);
+    else queue_kernel(paged_attention_kernel<C, T, DP, 3, 3, W>, dim3(blocks), dim3(64 * W), 0, s, a);
 }
 // One term of a query where the matrix instructions' type is its own, and two of the weights where the result has 16 bits or fewer.
 template <typename C, typename T>
 static void launch_paged(const PagedArgs& a, int blocks, hipStream_t s)
 {
     const bool own = a.d.q_dtype == (std::is_same<T, f16>::value ? NM_DT_F16 : NM_DT_BF16);
-    if (a.d.d <= 64) launch_paged<C, T, 64>(a, blocks, own, s);
-    else if (a.d.d <= 128) launch_paged<C, T, 128>(a, blocks, own, s);
-    else launch_paged<C, T, 256>(a, blocks, own, s);
+    if (a.d.d <= 64) a.wide ? launch_paged<C, T, 64, 2 * kPagedWaves>(a, blocks, own, s) : launch_paged<C, T, 64, kPagedWaves>(a, blocks, own, s);
+    else if (a.d.d <= 128) launch_paged<C, T, 128, kPagedWaves>(a, blocks, own, s);
+    else launch_paged<C, T, 256, kPagedWaves>(a, blocks, own, s);
 }
 
 // What does not depend on pointers: shapes, types, and how the work is shared.
@@ -594,10 +602,13 @@ static int32_t plan_paged(const nm_paged_desc* d, PagedArgs* a, size_t* bytes, l
             if (d->hk % n == 0) a->share = a->groups * n;
     const long sets = (long)d->B * d->hk * a->groups / a->share, most = sets * ((longest + kUnit - 1) / kUnit);
     // Who shares: as many workgroups as run at once (twice as many took 4 % longer at 48 ragged requests and 1 to 10 % at one of 131071).
-    // Rows too short to be divided go to a workgroup each, without the second kernel: 12 heads of 512 positions of one request took 10.4 us
-    // so and 13.7 shared, of 1024 14.6 and 13.6; of 64 requests 23.3 and 29.8.
+    // Rows too short to be divided go to a workgroup each, without the second kernel, and where that leaves CUs without one, to one of eight
+    // wavefronts (heads of up to 64: larger ones gained less than the second four cost).  12 heads of 64, 300 positions of one request 9.3 us
+    // so, 10.3 with four wavefronts, 14.1 divided; 512 positions 9.4, 10.8, 13.9; 1024 12.0, 15.0, 13.9; 2048 17.1, 23.2, 13.9.  252 heads, 1024
+    // positions: 17.5, 17.1, 24.2.  Heads of 128, 512 and 1024 positions: 8 heads 14.1 and 19.7 alone, 15.3 and 15.3 divided; 64 15.4 and 20.9, 17.7 and 20.2.
     a->extra = 2;
-    if (longest > (sets >= 256 ? 1024 : 512)) a->workers = (int)std::min(most, std::max(8l, 256l * workgroups_of(d->d) / a->share));
+    if (longest > (d->d <= 64 || sets >= 128 ? 1024 : 512)) a->workers = (int)std::min(most, std::max(8l, 256l * workgroups_of(d->d) / a->share));
+    a->wide = !a->workers && d->d <= 64 && longest > kUnit && sets * a->share <= 256;
     const long teams = ((a->workers ? a->workers : sets) + 7) / 8 * 8;   // every XCD has as many
     *blocks = teams * a->share;
     const size_t parts = (size_t)a->share * a->workers * 2 * 16;

@@ -445,6 +445,14 @@ def test_paged_attention_long_and_split(lens, hk, columns):
     check_attention(paged_case(len(lens), lens, hk * 4, hk, 128, torch.bfloat16, torch.bfloat16, page=64, columns=columns), torch.bfloat16)
 
 
+@pytest.mark.parametrize("lens,hq,hk,d,columns", [([1023, 0, 1, 129, 256, 257, 640], 5, 5, 64, 64), ([300], 12, 12, 48, 19), ([140, 7], 34, 2, 16, 9), ([1000] * 3, 8, 2, 64, 63),
+                                                  ([900, 3] * 45, 3, 3, 64, 64), ([1024, 130, 0, 700] * 10, 8, 4, 96, 64), ([1025, 1024, 1], 4, 4, 32, 65)])
+@pytest.mark.parametrize("q_dtype,cache_dtype,window", [(torch.float32, torch.bfloat16, 0), (torch.bfloat16, torch.int8, 0), (torch.float16, torch.float16, 200)])
+def test_paged_attention_rows_whole_or_divided(q_dtype, cache_dtype, window, lens, hq, hk, d, columns):
+    """Tables of up to 1024 positions and a little more: a row to a workgroup of four or eight wavefronts, or divided."""
+    check_attention(paged_case(hk + d, lens, hq, hk, d, q_dtype, cache_dtype, columns=columns), q_dtype, window=window)
+
+
 def test_paged_attention_bad_tables_and_lengths():
     """Entries that are no pages take no part, lengths beyond the table count as the table's, negative ones as none."""
     c = paged_case(3, [100, 200, 64, 33, 50], 4, 2, 64, torch.bfloat16, torch.bfloat16, columns=13)
