@@ -602,12 +602,12 @@ static int32_t plan_paged(const nm_paged_desc* d, PagedArgs* a, size_t* bytes, l
             if (d->hk % n == 0) a->share = a->groups * n;
     const long sets = (long)d->B * d->hk * a->groups / a->share, most = sets * ((longest + kUnit - 1) / kUnit);
     // Who shares: as many workgroups as run at once (twice as many took 4 % longer at 48 ragged requests and 1 to 10 % at one of 131071).
-    // Rows too short to be divided go to a workgroup each, without the second kernel, and where that leaves CUs without one, to one of eight
-    // wavefronts (heads of up to 64: larger ones gained less than the second four cost).  12 heads of 64, 300 positions of one request 9.3 us
-    // so, 10.3 with four wavefronts, 14.1 divided; 512 positions 9.4, 10.8, 13.9; 1024 12.0, 15.0, 13.9; 2048 17.1, 23.2, 13.9.  252 heads, 1024
-    // positions: 17.5, 17.1, 24.2.  Heads of 128, 512 and 1024 positions: 8 heads 14.1 and 19.7 alone, 15.3 and 15.3 divided; 64 15.4 and 20.9, 17.7 and 20.2.
+    // Rows too short to be divided go to a workgroup each, without the second kernel: tables of up to 512 positions (heads of 128, 8 rows: 14.1 us,
+    // 15.3 divided), 1024 where rows go round half of the CUs (64 rows: 20.9 and 20.2; 128: 21.9 and 25.3, 22.3 if ragged; 252 of 64: 17.1 and 24.2;
+    // 12 of 64 would gain too, 12.0 and 13.9, 8 of 128 lose more, 19.7 and 15.3).  Where that leaves CUs without one, heads of up to 64 have eight
+    // wavefronts (12 heads, 300 positions: 9.3 us, 10.3 with four; heads of 128 gain less, and lose as much at one tile, by the second four).
     a->extra = 2;
-    if (longest > (d->d <= 64 || sets >= 128 ? 1024 : 512)) a->workers = (int)std::min(most, std::max(8l, 256l * workgroups_of(d->d) / a->share));
+    if (longest > (sets >= 128 ? 1024 : 512)) a->workers = (int)std::min(most, std::max(8l, 256l * workgroups_of(d->d) / a->share));
     a->wide = !a->workers && d->d <= 64 && longest > kUnit && sets * a->share <= 256;
     const long teams = ((a->workers ? a->workers : sets) + 7) / 8 * 8;   // every XCD has as many
     *blocks = teams * a->share;
