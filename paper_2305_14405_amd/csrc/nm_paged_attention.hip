@@ -16,9 +16,8 @@
 // shows; three terms where the result is fp32), queries that are no 16-bit numbers of the matrix instructions' type as three terms of it, scaled by a
 // power of two so that nothing overflows.  int8 codes are exact in either 16-bit type.
 //   bf16, 32 query and 8 key heads of 128: one request of 131071 positions (537 MB) 105 us and 8 for the second kernel, 5.1 TB/s in the first, a
-// copy's rate; 48 requests of up to 8192 (649 MB) 120 + 5, 5.4 TB/s.  int8, 16 heads of 64, 64 requests of up to 4097 (216 MB): 58 + 4.5,
-// 3.7 TB/s: a run has 17 units or so, and begins and ends two rows in them; codes become 16-bit numbers in vector instructions (issued in 47 % of the
-// cycles).  12 heads of 300 positions of one request: 9.4 us (one position 7.6), a chain of dependent loads (length, page, keys) and code that runs once.
+// copy's rate; 48 requests of up to 8192 (649 MB) 120 + 5, 5.4 TB/s.  int8, 16 heads of 64, two taken as one, 64 requests of up to 4097 (216 MB): 53 + 5,
+// 4.1 TB/s: a run has 13 units or so, and begins and ends two rows in them; codes become 16-bit numbers in vector instructions.  12 heads of 300 positions of one request: 9.4 us (one position 7.6), a chain of dependent loads (length, page, keys) and code that runs once.
 #include <algorithm>
 
 #include "nm_decode.h"
@@ -41,11 +40,11 @@ constexpr int workgroups_of(int dp) { return dp <= 64 ? 3 : dp <= 128 ? 2 : 1; }
 struct PagedArgs {
     nm_paged_desc d;
     int shift;            // log2 of page_size
-    int group;            // query heads of a key head
+    int pack;             // neighbouring key heads that a workgroup takes as one, of int8
+    int group;            // query heads of a key head, packed
     int groups;           // of up to 16 of them
     int share;            // rows that read the same lines of the cache: a team of so many workgroups of one XCD takes them side by side
     int workers;          // teams that share the units; 0: one team to a set of rows
-    int wide;             // a workgroup to a set of rows, of eight wavefronts
     int extra;            // units that starting and ending a row costs
     float* part_o;        // [share, workers, 2, 16, d]: a run's first and last piece, not yet divided by the sum
     float2* part_ml;      // [share, workers, 2, 16]: maximum (of scores in units of log 2) and sum
@@ -188,16 +187,19 @@ __global__ __launch_bounds__(64 * W, W == kPagedWaves ? workgroups_of(DP) : W / 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int column = lane & 15, j = lane >> 4;              // head (and row of an operand), lane group
     const int row_piece = lane % kRowPieces, row_first = lane / kRowPieces;
-    const bool in_row = row_piece * kPer16 < d.d;
     // Position in a tile of a group of lanes' i-th row: the lanes of a row have the places of their rows between them, and two groups that
     // share a line of 128 bytes (rows of 64) have neighbouring rows at a time.
     constexpr bool kPairs = kRowPieces == 4;
     auto position_of = [](int group, int i) { return kPairs ? (group >> 1) * 2 * kLoads + 2 * i + (group & 1) : group * kLoads + i; };
     const int my_position = position_of(row_first, lane % kLoads);
     short* tile = s.tile[wave];
-    const int rows = d.hk * a.groups / a.share;               // sets of rows of a request
+    constexpr bool kPack = sizeof(C) == 1 && DP == 128;
+    const int pack = kPack ? a.pack : 1, width = d.d * pack;
+    const int rows = (kPack ? d.hk / pack : d.hk) * a.groups / a.share;               // sets of rows of a request
     // workgroup i runs on XCD i mod 8: a team's members are neighbours there
     const int member = blockIdx.x / 8 % a.share, worker = blockIdx.x / 8 / a.share * 8 + blockIdx.x % 8;
+
+    const bool in_row = row_piece * kPer16 < width;
 
     // this workgroup's units [u, u1); before: the units of the requests in front of b
     int b;
@@ -285,7 +287,7 @@ __global__ __launch_bounds__(64 * W, W == kPagedWaves ? workgroups_of(DP) : W / 
     };
     const int lane_bytes = in_row ? row_piece * 16 : 0;
     auto fetch = [&](const void* cache, const Piece& n, unsigned place, v4u (&to)[kLoads]) {
-        const char* base = d.num_pages ? static_cast<const char*>(cache) + (long)n.g * d.head_stride * sizeof(C) + lane_bytes : reinterpret_cast<const char*>(g_zero_line);
+        const char* base = d.num_pages ? static_cast<const char*>(cache) + (long)n.g * (pack * d.head_stride) * sizeof(C) + lane_bytes : reinterpret_cast<const char*>(g_zero_line);
         fetch_rows<kLoads>(base, place, to, std::make_integer_sequence<int, kLoads>{});
         __builtin_amdgcn_sched_barrier(0);                    // the order of the loads is what is waited for
     };
@@ -294,7 +296,7 @@ __global__ __launch_bounds__(64 * W, W == kPagedWaves ? workgroups_of(DP) : W / 
         short* to = tile + position_of(row_first, 0) * kStride + row_piece * kPer16;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) put<C, T>(to + i * kStep, from[i]);
-        if (valid != ~0ul || d.d != DP) {
+        if (valid != ~0ul || width != DP) {
 #pragma unroll 1
             for (int i = 0; i < kLoads; ++i)
                 if (!in_row || !(valid >> (lane - row_piece + i) & 1)) {
@@ -312,15 +314,26 @@ __global__ __launch_bounds__(64 * W, W == kPagedWaves ? workgroups_of(DP) : W / 
 
     // Queries of a piece: 16 rows (zeros behind the group's), 16 lanes each.
     const int qrow = tid >> 4, qc = tid & 15;
-    float x[DP / 16];
+    // Packed key heads are one whose query rows are zero but in their own head's part (codes are finite): this thread's row's, and column's.
+    const int each_group = kPack ? a.group / pack : 1;
+    const int row_part = kPack ? min(qrow / each_group, pack - 1) : 0, column_part = kPack ? min(column / each_group, pack - 1) : 0;
+    // They stay as they were read until they are used: to convert one earlier would be to wait for the tiles that are under way.
+    constexpr bool kLater = W == kPagedWaves;                 // (a workgroup with one row has none yet)
+    unsigned q_raw[DP / 16];
+    auto query = [&](unsigned raw) {
+        return d.q_dtype == NM_DT_F32 ? __uint_as_float(raw) : d.q_dtype == NM_DT_BF16 ? __uint_as_float(raw << 16) : (float)__builtin_bit_cast(f16, (unsigned short)raw);
+    };
     auto fetch_queries = [&](const Piece& n) {
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) {
-            const int c = qc + 16 * i;
+            const int c = qc + 16 * i - row_part * d.d;
             const long at = n.b * d.q_stride + (long)(n.h0 + qrow) * d.d + c;
-            const bool there = n.b >= 0 && qrow < n.heads && c < d.d;
-            x[i] = !there ? 0.0f : d.q_dtype == NM_DT_F32 ? static_cast<const float*>(d.q)[at] : d.q_dtype == NM_DT_BF16 ? (float)static_cast<const bf16*>(d.q)[at]
-                                                                                                                        : (float)static_cast<const f16*>(d.q)[at];
+            const bool there = n.b >= 0 && qrow < n.heads && (unsigned)c < (unsigned)d.d;
+            if (kLater)
+                q_raw[i] = !there ? 0u : d.q_dtype == NM_DT_F32 ? static_cast<const unsigned*>(d.q)[at] : (unsigned)static_cast<const unsigned short*>(d.q)[at];
+            else
+                q_raw[i] = __float_as_uint(!there ? 0.0f : d.q_dtype == NM_DT_F32 ? static_cast<const float*>(d.q)[at]
+                                                         : d.q_dtype == NM_DT_BF16 ? (float)static_cast<const bf16*>(d.q)[at] : (float)static_cast<const f16*>(d.q)[at]);
         }
     };
 
@@ -348,8 +361,13 @@ __global__ __launch_bounds__(64 * W, W == kPagedWaves ? workgroups_of(DP) : W / 
         const int b = now.b, g = now.g, h0 = now.h0, heads = now.heads, k1 = now.k1;
 
         // the sign of the scale goes with the queries
-        const float by = d.scale * 1.44269504088896340736f * (sizeof(C) == 1 ? d.k_scale[g] : 1.0f);
-        float top_q = 0.0f, down = 1.0f, up = 1.0f;
+        const float by = d.scale * 1.44269504088896340736f * (sizeof(C) == 1 ? d.k_scale[g * pack + row_part] : 1.0f);
+        const float by_column = kPack ? d.scale * 1.44269504088896340736f * d.k_scale[g * pack + column_part] : by;
+        float x[DP / 16], top_q = 0.0f, down = 1.0f, up = 1.0f;
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            x[i] = kLater ? query(q_raw[i]) : __uint_as_float(q_raw[i]);
+        }
         if (kQ > 1) {
 #pragma unroll
             for (int i = 0; i < DP / 16; ++i) top_q = fmaxf(top_q, fabsf(x[i]));
@@ -373,7 +391,7 @@ __global__ __launch_bounds__(64 * W, W == kPagedWaves ? workgroups_of(DP) : W / 
         if (qc == 0 && (W == kPagedWaves || qrow < 16)) s_qscale[qrow] = up;
         __syncthreads();
         // never 0, so that it takes a masked score, minus infinity, for what it is
-        const float factor = fmaxf(fabsf(by) * s_qscale[column], 1.17549435e-38f);
+        const float factor = fmaxf(fabsf(by_column) * s_qscale[column], 1.17549435e-38f);
 
         if (t0 >= k1) {                                       // no tile for this wavefront
             const unsigned place = place_of(then, then_t0, then_entry, valid);
@@ -470,7 +488,7 @@ __global__ __launch_bounds__(64 * W, W == kPagedWaves ? workgroups_of(DP) : W / 
 #pragma unroll
             for (int i = 0; i < 4; ++i) s.o[wave][column][blk * 16 + j * 4 + i] = o[blk][i] * mine;
         __syncthreads();
-        const float vscale = sizeof(C) == 1 ? d.v_scale[g] : 1.0f;
+        const float vscale = sizeof(C) == 1 ? d.v_scale[g * pack + row_part] : 1.0f;
         const int row = tid >> 4;
         if (row < heads) {
             float top = -INFINITY, sum = 0.0f;
@@ -487,7 +505,7 @@ __global__ __launch_bounds__(64 * W, W == kPagedWaves ? workgroups_of(DP) : W / 
             for (int c = (tid & 15) * 4; c < d.d; c += 64) {
                 v4f x{0, 0, 0, 0};
 #pragma unroll
-                for (int w = 0; w < W; ++w) x += *reinterpret_cast<const v4f*>(&s.o[w][row][c]);
+                for (int w = 0; w < W; ++w) x += *reinterpret_cast<const v4f*>(&s.o[w][row][row_part * d.d + c]);
                 if (now.slot >= 0) {
                     *reinterpret_cast<v4f*>(a.part_o + (part_of(a, member, worker, now.slot) + row) * d.d + c) = x;
                 } else {
@@ -547,7 +565,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_kernel(PagedArgs a)
         sum += s_l[i] * by;
         if (tid < d.d) v += s_o[i * d.d + tid] * by;
     }
-    const float by = (sum == 0.0f ? 0.0f : 1.0f / sum) * (d.cache_dtype == NM_DT_I8 ? d.v_scale[g] : 1.0f);
+    const float by = (sum == 0.0f ? 0.0f : 1.0f / sum) * (d.cache_dtype == NM_DT_I8 ? d.v_scale[h / (d.hq / d.hk)] : 1.0f);
     if (tid < d.d) store1(d.out, d.out_dtype, row.x * d.out_stride + (long)h * d.d + tid, v * by, d.out_inv_scale);
     if (tid == 0 && d.lse) d.lse[bh] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
 }
@@ -558,13 +576,20 @@ static void launch_paged(const PagedArgs& a, int blocks, bool own, hipStream_t s
     if (own && a.d.out_dtype != NM_DT_F32) queue_kernel(paged_attention_kernel<C, T, DP, 1, 2, W>, dim3(blocks), dim3(64 * W), 0, s, a);
     else queue_kernel(paged_attention_kernel<C, T, DP, 3, 3, W>, dim3(blocks), dim3(64 * W), 0, s, a);
 }
+// Positions that a request may have.
+static long longest_of(const nm_paged_desc& d, int shift)
+{
+    const long longest = (long)d.max_pages << shift;
+    return d.window && d.window < longest ? d.window : longest;
+}
 // One term of a query where the matrix instructions' type is its own, and two of the weights where the result has 16 bits or fewer.
 template <typename C, typename T>
 static void launch_paged(const PagedArgs& a, int blocks, hipStream_t s)
 {
     const bool own = a.d.q_dtype == (std::is_same<T, f16>::value ? NM_DT_F16 : NM_DT_BF16);
-    if (a.d.d <= 64) a.wide ? launch_paged<C, T, 64, 2 * kPagedWaves>(a, blocks, own, s) : launch_paged<C, T, 64, kPagedWaves>(a, blocks, own, s);
-    else if (a.d.d <= 128) launch_paged<C, T, 128, kPagedWaves>(a, blocks, own, s);
+    const bool wide = !a.workers && blocks <= 256 && longest_of(a.d, a.shift) > kUnit;   // eight wavefronts to a row
+    if (a.pack * a.d.d <= 64) wide ? launch_paged<C, T, 64, 2 * kPagedWaves>(a, blocks, own, s) : launch_paged<C, T, 64, kPagedWaves>(a, blocks, own, s);
+    else if (a.pack * a.d.d <= 128) launch_paged<C, T, 128, kPagedWaves>(a, blocks, own, s);
     else launch_paged<C, T, 256, kPagedWaves>(a, blocks, own, s);
 }
 
@@ -591,24 +616,35 @@ static int32_t plan_paged(const nm_paged_desc* d, PagedArgs* a, size_t* bytes, l
     a->shift = shift;
     a->group = d->hq / d->hk;
     a->groups = (a->group + 15) / 16;
-    long longest = (long)d->max_pages << shift;
-    if (d->window && d->window < longest) longest = d->window;
+    a->pack = 1;
+    const long longest = longest_of(*d, shift);
     // Rows that read the same lines: the groups of a key head, and the heads whose pieces of a slot share a line of 128 bytes (as long as
     // the other slots do not lie between them).
-    const int64_t head_bytes = d->head_stride * dtype_bytes(d->cache_dtype);
-    a->share = a->groups;
-    if (head_bytes > 0 && head_bytes < 128 && d->head_stride < d->slot_stride)
-        for (int n = 2; n * head_bytes <= 128; n *= 2)
-            if (d->hk % n == 0) a->share = a->groups * n;
-    const long sets = (long)d->B * d->hk * a->groups / a->share, most = sets * ((longest + kUnit - 1) / kUnit);
+    auto share_rows = [&] {
+        const int64_t head_bytes = a->pack * d->head_stride * dtype_bytes(d->cache_dtype);
+        a->share = a->groups;
+        if (head_bytes > 0 && head_bytes < 128 && a->pack * d->head_stride < d->slot_stride)
+            for (int n = 2; n * head_bytes <= 128; n *= 2)
+                if (d->hk / a->pack % n == 0) a->share = a->groups * n;
+        return (long)d->B * (d->hk / a->pack) * a->groups / a->share;
+    };
+    long sets = share_rows();
+    const bool divided = longest > (sets >= 128 ? 1024 : 512);
+    // Neighbouring heads of int8 as one of up to 128 elements: whole lines, and one softmax for all their queries.  Where they are too few, rows that
+    // begin and end at a second kernel's cost more (heads of 64, us apart and packed: 64 requests of up to 4097 positions 69 and 62, 48 54 and 49, 32 36 and
+    // 35, 16 25 and 26; heads of 32, 64 requests 60 and 38).  Not of floating-point types, where an infinity times zero is none.
+    if (divided && d->cache_dtype == NM_DT_I8 && d->head_stride == d->d && (long)d->B * d->hk * ((longest + kUnit - 1) / kUnit) >= 32 * 768) {
+        while (2 * a->pack * d->d <= 128 && d->hk % (2 * a->pack) == 0 && 2 * a->group <= 16) a->pack *= 2, a->group *= 2;
+        sets = share_rows();
+    }
+    const long most = sets * ((longest + kUnit - 1) / kUnit);
     // Who shares: as many workgroups as run at once (twice as many took 4 % longer at 48 ragged requests and 1 to 10 % at one of 131071).
     // Rows too short to be divided go to a workgroup each, without the second kernel: tables of up to 512 positions (heads of 128, 8 rows: 14.1 us,
     // 15.3 divided), 1024 where rows go round half of the CUs (64 rows: 20.9 and 20.2; 128: 21.9 and 25.3, 22.3 if ragged; 252 of 64: 17.1 and 24.2;
     // 12 of 64 would gain too, 12.0 and 13.9, 8 of 128 lose more, 19.7 and 15.3).  Where that leaves CUs without one, heads of up to 64 have eight
     // wavefronts (12 heads, 300 positions: 9.3 us, 10.3 with four; heads of 128 gain less, and lose as much at one tile, by the second four).
     a->extra = 2;
-    if (longest > (sets >= 128 ? 1024 : 512)) a->workers = (int)std::min(most, std::max(8l, 256l * workgroups_of(d->d) / a->share));
-    a->wide = !a->workers && d->d <= 64 && longest > kUnit && sets * a->share <= 256;
+    if (divided) a->workers = (int)std::min(most, std::max(8l, 256l * workgroups_of(a->pack * d->d) / a->share));
     const long teams = ((a->workers ? a->workers : sets) + 7) / 8 * 8;   // every XCD has as many
     *blocks = teams * a->share;
     const size_t parts = (size_t)a->share * a->workers * 2 * 16;

@@ -453,6 +453,17 @@ def test_paged_attention_rows_whole_or_divided(q_dtype, cache_dtype, window, len
     check_attention(paged_case(hk + d, lens, hq, hk, d, q_dtype, cache_dtype, columns=columns), q_dtype, window=window)
 
 
+@pytest.mark.parametrize("B,hq,hk,d,by_head,window", [(48, 16, 16, 64, False, 0), (48, 16, 16, 64, True, 0), (40, 32, 16, 32, False, 0), (130, 24, 6, 48, False, 333), (100, 8, 8, 16, False, 0),
+                                                       (100, 64, 8, 64, False, 1000), (99, 128, 8, 64, False, 0), (60, 14, 14, 64, False, 0), (9, 96, 96, 16, False, 0), (130, 16, 16, 16, False, 2000)])
+@pytest.mark.parametrize("q_dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_paged_attention_many_heads_of_codes(q_dtype, B, hq, hk, d, by_head, window):
+    """Enough rows and columns of the table that neighbouring key heads are taken as one, where they lie next to each other; ragged lengths."""
+    lens = [(i * i * 37) % 700 if i % 5 else 4000 * (i % 10 == 5) for i in range(B)]
+    c = paged_case(B + d, lens, hq, hk, d, q_dtype, torch.int8, page=32, by_head=by_head, columns=130)
+    c["q"][1, :, 0] *= 100.0
+    check_attention(c, q_dtype, window=window)
+
+
 def test_paged_attention_bad_tables_and_lengths():
     """Entries that are no pages take no part, lengths beyond the table count as the table's, negative ones as none."""
     c = paged_case(3, [100, 200, 64, 33, 50], 4, 2, 64, torch.bfloat16, torch.bfloat16, columns=13)
