@@ -581,7 +581,7 @@ int32_t nm_qk_norm_rope(const nm_qk_desc* desc, void* stream);
  * out_inv_scale: what nm_gemm_pwl reads); out may be q itself (same type and stride).  lse: device fp32 [B, hq] or NULL.
  * q is split into as many terms of the matrix instructions' type as hold it, the weights into two (fp32 results: three), so nothing
  * but the outputs is rounded to fewer than 16 bits.
- * Workspace: query nm_paged_attention_workspace (it looks at the shape and the types only, never at device memory; 0: none); 256-byte
+ * Workspace: query nm_paged_attention_workspace (it looks at the description's sizes, strides and types, never at device memory; 0: none); 256-byte
  * aligned, contents are scratch, calls that overlap in time need one each.  Lengths may be as ragged, and the table as much wider
  * than they are, as it happens: the work is shared by the lengths as they are when the call runs.
  * Limits: hq % hk == 0; d a multiple of 16 up to 256; cache addresses and strides multiples of 16 bytes; page_size a power of
