@@ -18,9 +18,8 @@
 //   bf16, 32 query and 8 key heads of 128: one request of 131071 positions (537 MB) 105 us and 8 for the second kernel, 5.1 TB/s in the first, a
 // copy's rate; 48 requests of up to 8192 (649 MB) 120 + 5, 5.4 TB/s.  int8, 16 heads of 64, two taken as one, 64 requests of up to 4097 (216 MB): 53 + 5,
 // 4.1 TB/s: a run has 13 units or so, and begins and ends two rows in them; codes become 16-bit numbers in vector instructions.  12 heads of 300 positions of one request: 9.4 us (one position 7.6), a chain of dependent loads (length, page, keys) and code that runs once.
-#include <algorithm>
-
 #include "nm_decode.h"
+#include "nm_paged_choice.h"
 
 namespace nm {
 
@@ -31,20 +30,9 @@ typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
-constexpr int kPagedWaves = 4, kPagedThreads = 64 * kPagedWaves;
-constexpr int kTile = 32;                       // positions a wavefront takes at once
-constexpr int kUnit = kTile * kPagedWaves;      // and a workgroup
-// Workgroups of the kernel for heads of up to dp elements that a CU has registers for (a wavefront on each SIMD each).
-constexpr int workgroups_of(int dp) { return dp <= 64 ? 3 : dp <= 128 ? 2 : 1; }
-
-struct PagedArgs {
+struct PagedArgs : PagedSplit {
     nm_paged_desc d;
     int shift;            // log2 of page_size
-    int pack;             // neighbouring key heads that a workgroup takes as one, of int8
-    int group;            // query heads of a key head, packed
-    int groups;           // of up to 16 of them
-    int share;            // rows that read the same lines of the cache: a team of so many workgroups of one XCD takes them side by side
-    int workers;          // teams that share the units; 0: one team to a set of rows
     int extra;            // units that starting and ending a row costs
     float* part_o;        // [share, workers, 2, 16, d]: a run's first and last piece, not yet divided by the sum
     float2* part_ml;      // [share, workers, 2, 16]: maximum (of scores in units of log 2) and sum
@@ -193,9 +181,9 @@ __global__ __launch_bounds__(64 * W, W == kPagedWaves ? workgroups_of(DP) : W / 
     auto position_of = [](int group, int i) { return kPairs ? (group >> 1) * 2 * kLoads + 2 * i + (group & 1) : group * kLoads + i; };
     const int my_position = position_of(row_first, lane % kLoads);
     short* tile = s.tile[wave];
-    constexpr bool kPack = sizeof(C) == 1 && DP == 128;
+    constexpr bool kPack = paged_packs(sizeof(C), DP);
     const int pack = kPack ? a.pack : 1, width = d.d * pack;
-    const int rows = (kPack ? d.hk / pack : d.hk) * a.groups / a.share;               // sets of rows of a request
+    const int rows = (kPack ? paged_rows(d.hk, pack, a.groups) : d.hk * a.groups) / a.share;   // sets of rows of a request
     // workgroup i runs on XCD i mod 8: a team's members are neighbours there
     const int member = blockIdx.x / 8 % a.share, worker = blockIdx.x / 8 / a.share * 8 + blockIdx.x % 8;
 
@@ -260,10 +248,10 @@ __global__ __launch_bounds__(64 * W, W == kPagedWaves ? workgroups_of(DP) : W / 
             Piece n;
             n.b = b;
             // requests begin with different heads, so that workgroups in step with one another do not read the same part of every page
-            const int row = (r + b) % rows * a.share + member;
-            n.g = row / a.groups;
-            n.h0 = n.g * a.group + row % a.groups * 16;
-            n.heads = min((n.g + 1) * a.group - n.h0, 16);
+            const PagedRow row = paged_row((r + b) % rows * a.share + member, a.group, a.groups);
+            n.g = row.g;
+            n.h0 = row.h0;
+            n.heads = row.heads;
             n.k0 = span.low + from * kUnit;
             n.k1 = (int)min((long)span.low + (long)to * kUnit, (long)span.n);
             n.slot = from == 0 && to == units ? -1 : begin > first;
@@ -315,8 +303,7 @@ __global__ __launch_bounds__(64 * W, W == kPagedWaves ? workgroups_of(DP) : W / 
     // Queries of a piece: 16 rows (zeros behind the group's), 16 lanes each.
     const int qrow = tid >> 4, qc = tid & 15;
     // Packed key heads are one whose query rows are zero but in their own head's part (codes are finite): this thread's row's, and column's.
-    const int each_group = kPack ? a.group / pack : 1;
-    const int row_part = kPack ? min(qrow / each_group, pack - 1) : 0, column_part = kPack ? min(column / each_group, pack - 1) : 0;
+    const int row_part = kPack ? paged_part(qrow, a.group, pack) : 0, column_part = kPack ? paged_part(column, a.group, pack) : 0;
     // They stay as they were read until they are used: to convert one earlier would be to wait for the tiles that are under way.
     constexpr bool kLater = W == kPagedWaves;                 // (a workgroup with one row has none yet)
     unsigned q_raw[DP / 16];
@@ -588,8 +575,9 @@ static void launch_paged(const PagedArgs& a, int blocks, hipStream_t s)
 {
     const bool own = a.d.q_dtype == (std::is_same<T, f16>::value ? NM_DT_F16 : NM_DT_BF16);
     const bool wide = !a.workers && blocks <= 256 && longest_of(a.d, a.shift) > kUnit;   // eight wavefronts to a row
-    if (a.pack * a.d.d <= 64) wide ? launch_paged<C, T, 64, 2 * kPagedWaves>(a, blocks, own, s) : launch_paged<C, T, 64, kPagedWaves>(a, blocks, own, s);
-    else if (a.pack * a.d.d <= 128) launch_paged<C, T, 128, kPagedWaves>(a, blocks, own, s);
+    const int width = paged_width(a.pack * a.d.d);
+    if (width == 64) wide ? launch_paged<C, T, 64, 2 * kPagedWaves>(a, blocks, own, s) : launch_paged<C, T, 64, kPagedWaves>(a, blocks, own, s);
+    else if (width == 128) launch_paged<C, T, 128, kPagedWaves>(a, blocks, own, s);
     else launch_paged<C, T, 256, kPagedWaves>(a, blocks, own, s);
 }
 
@@ -614,38 +602,9 @@ static int32_t plan_paged(const nm_paged_desc* d, PagedArgs* a, size_t* bytes, l
     *a = PagedArgs{};
     a->d = *d;
     a->shift = shift;
-    a->group = d->hq / d->hk;
-    a->groups = (a->group + 15) / 16;
-    a->pack = 1;
-    const long longest = longest_of(*d, shift);
-    // Rows that read the same lines: the groups of a key head, and the heads whose pieces of a slot share a line of 128 bytes (as long as
-    // the other slots do not lie between them).
-    auto share_rows = [&] {
-        const int64_t head_bytes = a->pack * d->head_stride * dtype_bytes(d->cache_dtype);
-        a->share = a->groups;
-        if (head_bytes > 0 && head_bytes < 128 && a->pack * d->head_stride < d->slot_stride)
-            for (int n = 2; n * head_bytes <= 128; n *= 2)
-                if (d->hk / a->pack % n == 0) a->share = a->groups * n;
-        return (long)d->B * (d->hk / a->pack) * a->groups / a->share;
-    };
-    long sets = share_rows();
-    const bool divided = longest > (sets >= 128 ? 1024 : 512);
-    // Neighbouring heads of int8 as one of up to 128 elements: whole lines, and one softmax for all their queries.  Where they are too few, rows that
-    // begin and end at a second kernel's cost more (heads of 64, us apart and packed: 64 requests of up to 4097 positions 69 and 62, 48 54 and 49, 32 36 and
-    // 35, 16 25 and 26; heads of 32, 64 requests 60 and 38).  Not of floating-point types, where an infinity times zero is none.
-    if (divided && d->cache_dtype == NM_DT_I8 && d->head_stride == d->d && (long)d->B * d->hk * ((longest + kUnit - 1) / kUnit) >= 32 * 768) {
-        while (2 * a->pack * d->d <= 128 && d->hk % (2 * a->pack) == 0 && 2 * a->group <= 16) a->pack *= 2, a->group *= 2;
-        sets = share_rows();
-    }
-    const long most = sets * ((longest + kUnit - 1) / kUnit);
-    // Who shares: as many workgroups as run at once (twice as many took 4 % longer at 48 ragged requests and 1 to 10 % at one of 131071).
-    // Rows too short to be divided go to a workgroup each, without the second kernel: tables of up to 512 positions (heads of 128, 8 rows: 14.1 us,
-    // 15.3 divided), 1024 where rows go round half of the CUs (64 rows: 20.9 and 20.2; 128: 21.9 and 25.3, 22.3 if ragged; 252 of 64: 17.1 and 24.2;
-    // 12 of 64 would gain too, 12.0 and 13.9, 8 of 128 lose more, 19.7 and 15.3).  Where that leaves CUs without one, heads of up to 64 have eight
-    // wavefronts (12 heads, 300 positions: 9.3 us, 10.3 with four; heads of 128 gain less, and lose as much at one tile, by the second four).
+    static_cast<PagedSplit&>(*a) = paged_split({d->B, d->hq, d->hk, d->d, dtype_bytes(d->cache_dtype), d->slot_stride, d->head_stride, longest_of(*d, shift)});
     a->extra = 2;
-    if (divided) a->workers = (int)std::min(most, std::max(8l, 256l * workgroups_of(a->pack * d->d) / a->share));
-    const long teams = ((a->workers ? a->workers : sets) + 7) / 8 * 8;   // every XCD has as many
+    const long teams = ((a->workers ? a->workers : a->sets) + 7) / 8 * 8;   // every XCD has as many
     *blocks = teams * a->share;
     const size_t parts = (size_t)a->share * a->workers * 2 * 16;
     *bytes = parts * (sizeof(float2) + d->d * sizeof(float)) + parts / 32 * sizeof(int4);
