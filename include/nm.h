@@ -620,7 +620,8 @@ int32_t nm_paged_attention(const nm_paged_desc* desc, void* ws, size_t ws_bytes,
  * w[n, 2 i] in its low and w[n, 2 i + 1] in its high four bits, two's complement (-8 .. 7).  scales: device [N, K / group], contiguous,
  * scale_dtype F32, BF16 or F16.  bias: device fp32 [N] or NULL.  out: device [M, N], rows out_stride apart, out_dtype F32, BF16, F16
  * or I8; out is none of the inputs.  Any M: rows are taken up to 48 at a time, and the weights read again for each (nm_gemm_pwl is the call for many rows).
- * A row of bf16 or fp16 with an infinity or NaN comes out NaN; other rows are not touched by it.
+ * bf16 and fp16 rows meet the weights themselves, in exact products: a value whose weight is zero leaves no error, an infinity follows the
+ * formula (times a weight of zero: NaN), and neither it nor a NaN reaches another row.
  * Limits: group 32, 64 or a multiple of 128; K a multiple of group, at most 65536; x and W 16-byte aligned, x_stride a multiple of 16
  * bytes; M <= 2^20, N < 2^26, (N / 16) (M / 32) < 2^23.
  */

@@ -14,9 +14,10 @@
 // row, so to add within one run (the smallest group) these exchange words, four half swaps for 16 bytes: then register i of lane
 // group j holds weights 8 j .. 8 j + 7 of run i.
 //   int8: (v << 4) & 0xf0f0f0f0 and v & 0xf0f0f0f0 are 16 times the even and the odd weights as int8: three operations for eight
-// weights, and exact.  bf16, fp16: u = w + 8 is put under an exponent, 16 + u, exactly, in nine; a matrix instruction with the constant -24
-// in the weights' place takes the offset off again, once for all columns of a wavefront (the sum of x it subtracts is at most some 5
-// times the result's size, so fp32 loses two bits of 24).
+// weights, and exact.  fp16: u = w + 8 is put under an exponent, 16 + u, and 24 taken off, both exact, in thirteen.  bf16: one
+// conversion of the lower four bits of a byte for each weight, to w / 16 in fp32, whose upper half is taken; thirteen too.  The matrix instructions so
+// have the weights themselves: what x they meet a zero with is not in the sum (with 16 + u there, and 24 times the sum of x taken off by
+// further matrix instructions, a value 30000 times the others left an error 14000 times fp32's).
 //   What a group's sum is multiplied by is one number per lane (its column).
 #pragma once
 
@@ -28,6 +29,7 @@ namespace nm {
 
 typedef bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef f16 v8h __attribute__((ext_vector_type(8)));
+typedef f16 v2h __attribute__((ext_vector_type(2)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 typedef unsigned v2u __attribute__((ext_vector_type(2)));
 
@@ -71,7 +73,8 @@ __device__ __forceinline__ unsigned in_vgpr_u(unsigned x)
     return v;
 }
 
-// What differs by the type of x: its eight values of a lane, the sum over them, and eight weights.
+// What differs by the type of x: its eight values of a lane, the sum over them, and eight weights times 1 / (kUnit kEnd): kUnit goes with the
+// scales, kEnd with the whole sum (a scale times 16 might overflow, a sum of w / 16 can only where that of w does).
 template <typename X> struct W4;
 template <> struct W4<int8_t> {
     typedef v2u Rows;
@@ -85,44 +88,51 @@ template <> struct W4<int8_t> {
     static __device__ __forceinline__ unsigned exponent() { return 0; }
     static __device__ __forceinline__ v2u weights(unsigned w, unsigned) { return v2u{(w << 4) & 0xf0f0f0f0u, w & 0xf0f0f0f0u}; }
     static __device__ __forceinline__ Sum add(Rows x, v2u w, Sum c) { return __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, x), __builtin_bit_cast(long, w), c, 0, 0, 0); }
-    static __device__ __forceinline__ Sum offset(Rows, Sum c) { return c; }
-    static constexpr float kUnit = 1.0f / 16.0f;
+    static constexpr float kUnit = 1.0f / 16.0f, kEnd = 1.0f;
 };
-template <typename X> struct W4Half {
+template <> struct W4<f16> {
     typedef v4u Rows;
     typedef v4f Sum;
-    static constexpr bool kBf = std::is_same<X, bf16>::value;
     // a lane's eight values in the order in which the weights come out of their word: 0 4 1 5 2 6 3 7
     static __device__ __forceinline__ v4u order(v4u x)
     {
         return v4u{__builtin_amdgcn_perm(x[2], x[0], 0x05040100u), __builtin_amdgcn_perm(x[2], x[0], 0x07060302u),
                     __builtin_amdgcn_perm(x[3], x[1], 0x05040100u), __builtin_amdgcn_perm(x[3], x[1], 0x07060302u)};
     }
-    // 16 + u: u in the upper four bits of the mantissa (7 bits of bf16, 10 of fp16).  exponent: of 16, twice, in a vector register, so that
-    // mask and exponent are one instruction (an instruction takes one constant from elsewhere)
-    static __device__ __forceinline__ unsigned exponent() { return in_vgpr_u(kBf ? 0x41804180u : 0x4c004c00u); }
+    // 16 + u: u in the upper four bits of the mantissa of 10.  exponent: of 16, twice, in a vector register, so that mask and exponent are
+    // one instruction (an instruction takes one constant from elsewhere)
+    static __device__ __forceinline__ unsigned exponent() { return in_vgpr_u(0x4c004c00u); }
     static __device__ __forceinline__ v4u weights(unsigned w, unsigned exponent)
     {
         const unsigned u = w ^ 0x88888888u;
-        if (kBf) return v4u{((u << 3) & 0x00780078u) | exponent, ((u >> 1) & 0x00780078u) | exponent,
-                            ((u >> 5) & 0x00780078u) | exponent, ((u >> 9) & 0x00780078u) | exponent};
-        return v4u{((u << 6) & 0x03c003c0u) | exponent, ((u << 2) & 0x03c003c0u) | exponent,
-                   ((u >> 2) & 0x03c003c0u) | exponent, ((u >> 6) & 0x03c003c0u) | exponent};
+        auto less24 = [](unsigned p) { return __builtin_bit_cast(unsigned, (v2h)(__builtin_bit_cast(v2h, p) - v2h{(f16)24.0f, (f16)24.0f})); };
+        return v4u{less24(((u << 6) & 0x03c003c0u) | exponent), less24(((u << 2) & 0x03c003c0u) | exponent),
+                   less24(((u >> 2) & 0x03c003c0u) | exponent), less24(((u >> 6) & 0x03c003c0u) | exponent)};
     }
-    static __device__ __forceinline__ Sum add(Rows x, v4u w, Sum c)
-    {
-        if constexpr (kBf) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, w), c, 0, 0, 0);
-        else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x), __builtin_bit_cast(v8h, w), c, 0, 0, 0);
-    }
-    static __device__ __forceinline__ Sum offset(Rows x, Sum c)
-    {
-        const unsigned minus24 = kBf ? 0xc1c0c1c0u : 0xce00ce00u;
-        return add(x, v4u{minus24, minus24, minus24, minus24}, c);
-    }
-    static constexpr float kUnit = 1.0f;
+    static __device__ __forceinline__ Sum add(Rows x, v4u w, Sum c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x), __builtin_bit_cast(v8h, w), c, 0, 0, 0); }
+    static constexpr float kUnit = 1.0f, kEnd = 1.0f;
 };
-template <> struct W4<bf16> : W4Half<bf16> {};
-template <> struct W4<f16> : W4Half<f16> {};
+template <> struct W4<bf16> {
+    typedef v4u Rows;
+    typedef v4f Sum;
+    static __device__ __forceinline__ v4u order(v4u x) { return x; }
+    static __device__ __forceinline__ unsigned exponent() { return 0; }
+    static __device__ __forceinline__ v4u weights(unsigned w, unsigned)
+    {
+        unsigned odd = w >> 4;
+        asm("" : "+v"(odd));   // as a number of its own, so that its bytes are operands as they lie and not shifts of w
+        v4u o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {   // byte i has weights 2 i and 2 i + 1; their sixteenths have four bits or fewer, so nothing is in the lower halves
+            const unsigned a = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(w >> (8 * i) & 0xffu)));
+            const unsigned b = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(odd >> (8 * i) & 0xffu)));
+            o[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        }
+        return o;
+    }
+    static __device__ __forceinline__ Sum add(Rows x, v4u w, Sum c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, w), c, 0, 0, 0); }
+    static constexpr float kUnit = 1.0f, kEnd = 16.0f;
+};
 
 // S: bits of a scale (float, or either 16-bit type); kRuns: runs of 32 weights to a scale within a block of 128 (1, 2, 4); kM: tiles of
 // 16 rows; kN: of 16 columns that a wavefront has; kRing: weights by a ring in LDS; kC: sets of wavefronts with columns of their own;
@@ -263,11 +273,11 @@ __global__ __launch_bounds__(kW4Threads * kC * kK, kRing ? 4 : 2 * kC * kK) void
 #pragma unroll
             for (int t = 0; t < kM; ++t) {
                 Rows x[kRuns];
-                Sum off{}, acc[kN];
+                Sum acc[kN];
 #pragma unroll
-                for (int i = 0; i < kRuns; ++i) off = Q::offset(x[i] = kEarly ? x1[g * kRuns + i] : rows_of(t, at, g * kRuns + i), off);
+                for (int i = 0; i < kRuns; ++i) x[i] = kEarly ? x1[g * kRuns + i] : rows_of(t, at, g * kRuns + i);
 #pragma unroll
-                for (int c = 0; c < kN; ++c) acc[c] = off;    // the offset is where the sums begin
+                for (int c = 0; c < kN; ++c) acc[c] = Sum{};
 #pragma unroll
                 for (int i = 0; i < kRuns; ++i)
 #pragma unroll
@@ -355,6 +365,7 @@ __global__ __launch_bounds__(kW4Threads * kC * kK, kRing ? 4 : 2 * kC * kK) void
         float v = 0.0f;
 #pragma unroll
         for (int p = 0; p < kParts; ++p) v += s_sum[p][t][r][c];
+        v *= Q::kEnd;
         v = __builtin_fmaf(v, d.alpha, d.bias ? d.bias[col] : 0.0f);
         if (d.table_idx >= 0) {
             int seg;
