@@ -1,6 +1,8 @@
 // What the kernels of a decode step share: the types of their tensors, groups of four elements, the cache's layout.
 #pragma once
 
+#include <initializer_list>
+
 #include "nm_device.h"
 
 namespace nm {
@@ -20,6 +22,14 @@ inline int page_shift(int32_t page_size)
     for (int s = 0; s <= 16; ++s)
         if (page_size == 1 << s) return s;
     return -1;
+}
+
+// Whether something that is written begins where one of the others does (NULL: not there).
+inline bool begins_as(const void* out, std::initializer_list<const void*> others)
+{
+    for (const void* p : others)
+        if (out && p == out) return true;
+    return false;
 }
 
 // N neighbouring elements, rounded once.  dtype is uniform, so this is a scalar branch; inv_scale for I8.

@@ -30,7 +30,7 @@ extern "C" int32_t nm_gemv_w4(const nm_w4_desc* d, void* stream)
     }
     if (d->M == 0) return NM_OK;   // empty tensors may be NULL pointers
     if (!d->x || !d->W || !d->scales || !d->out) return fail(NM_ERR_INVALID_ARG, "nm_gemv_w4: NULL argument");
-    if (d->out == d->x || d->out == d->W || d->out == d->scales) return fail(NM_ERR_INVALID_ARG, "nm_gemv_w4: out is an input");
+    if (begins_as(d->out, {d->x, d->W, d->scales, d->bias})) return fail(NM_ERR_INVALID_ARG, "nm_gemv_w4: out is an input");
     if (!aligned_rows(d->x, d->x_stride, d->x_dtype, 16 / dtype_bytes(d->x_dtype)) || !aligned(d->W, 16))
         return fail(NM_ERR_UNSUPPORTED, "nm_gemv_w4: x, its rows and W must be 16-byte aligned");
     a.per = fast_div(d->group >= 128 ? d->group / 128 : 1);

@@ -193,3 +193,8 @@ def test_binding_refuses_host_tensors():
         nm.nm_qk_norm_rope(x, x, x, i, None, x)
     with pytest.raises(nm.NmError):
         nm.nm_paged_attention(x, x.view(2, 1, 4, 64), x.view(2, 1, 4, 64), i.view(2, 2), i[:2], x, scale=1.0)
+
+
+@pytest.mark.parametrize("changes", [dict(out=4 * P)])
+def test_gemv_w4_out_is_the_bias(lib, changes):
+    refused(lib.nm_gemv_w4, w4(), nm.NM_ERR_INVALID_ARG, **changes)
