@@ -537,7 +537,7 @@ int32_t nm_page_plan(const nm_plan_desc* desc, void* stream);
  * A slot outside [0, num_pages * page_size) is not written.  Two tokens of one slot: every element is one of the two's.
  * q, k, v: device, a token's heads one behind the other, tokens q_stride, k_stride, v_stride elements apart (the thirds of a fused
  * projection's rows, for instance); in_dtype F32, BF16 or F16.  q_out, k_out likewise, out_dtype the same three; q_out may be q itself
- * (same type and stride), k_out k.  cache_dtype F32, BF16, F16 or I8.  positions, slots: device int32 [T] (positions may be NULL for rot = 0,
+ * (same type and stride), k_out k; no other output may be an input or another output.  cache_dtype F32, BF16, F16 or I8.  positions, slots: device int32 [T] (positions may be NULL for rot = 0,
  * slots without a cache).  Rows without a slot are computed into q_out and k_out like the others.  inv_freq: device fp32 [rot / 2].  gammas: device fp32 [d].  k_inv_scale, v_inv_scale: device fp32 [hk], for int8.
  * Limits: T <= 2^23; 1 <= d <= 256; rot even, 0 <= rot <= d; hq, hk >= 1, hq + 2 hk <= 65535; strides cover a token's heads.  Where the rows and the cache are
  * 16-byte aligned, d is a multiple of 8 and rot of 8 (or 0), whole groups of elements move at once.
@@ -578,7 +578,8 @@ int32_t nm_qk_norm_rope(const nm_qk_desc* desc, void* stream);
  * q: device [B, hq, d], requests q_stride elements apart, q_dtype F32, BF16 or F16.  Cache: as above, cache_dtype BF16, F16 or I8
  * (then k_scale, v_scale: device fp32 [hk]).  block_table: device int32, rows of max_pages entries table_stride apart.  lens:
  * device int32 [B].  out: device [B, hq, d], requests out_stride apart, out_dtype F32, BF16, F16 or I8 (codes with
- * out_inv_scale: what nm_gemm_pwl reads); out may be q itself (same type and stride).  lse: device fp32 [B, hq] or NULL.
+ * out_inv_scale: what nm_gemm_pwl reads); out may be q itself (same type and stride), and is no other input.  lse: device fp32 [B, hq] or NULL; neither an
+ * input nor out.
  * q is split into as many terms of the matrix instructions' type as hold it, the weights into two (fp32 results: three), so nothing
  * but the outputs is rounded to fewer than 16 bits.
  * Workspace: query nm_paged_attention_workspace (it looks at the description's sizes, strides and types, never at device memory; 0: none); 256-byte

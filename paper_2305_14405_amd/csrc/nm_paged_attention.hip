@@ -643,6 +643,9 @@ int32_t nm_paged_attention(const nm_paged_desc* d, void* ws, size_t ws_bytes, vo
     if (d->B == 0) return NM_OK;   // empty tensors may be NULL pointers
     if (!d->q || !d->lens || !d->out) return fail(NM_ERR_INVALID_ARG, "nm_paged_attention: q, lens or out is NULL");
     if (d->out == d->q && (d->out_dtype != d->q_dtype || d->out_stride != d->q_stride)) return fail(NM_ERR_INVALID_ARG, "nm_paged_attention: in place with another type or stride");
+    const std::initializer_list<const void*> read = {d->k_cache, d->v_cache, d->k_scale, d->v_scale, d->block_table, d->lens};
+    if (begins_as(d->out, read) || begins_as(d->lse, read) || begins_as(d->lse, {d->q, d->out}))
+        return fail(NM_ERR_INVALID_ARG, "nm_paged_attention: out or lse is an input, or lse is out");
     if ((d->max_pages && !d->block_table) || (d->max_pages && d->num_pages && (!d->k_cache || !d->v_cache)))
         return fail(NM_ERR_INVALID_ARG, "nm_paged_attention: block_table or a cache is NULL");
     if (d->cache_dtype == NM_DT_I8 && (!d->k_scale || !d->v_scale)) return fail(NM_ERR_INVALID_ARG, "nm_paged_attention: int8 cache without scales");

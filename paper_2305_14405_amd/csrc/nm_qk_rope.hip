@@ -315,6 +315,12 @@ extern "C" int32_t nm_qk_norm_rope(const nm_qk_desc* d, void* stream)
     if ((d->q_out == d->q && (d->out_dtype != d->in_dtype || d->q_out_stride != d->q_stride)) ||
         (d->k_out == d->k && (d->out_dtype != d->in_dtype || d->k_out_stride != d->k_stride)))
         return fail(NM_ERR_INVALID_ARG, "nm_qk_norm_rope: in place with another type or stride");
+    const void* v = d->k_cache ? d->v : nullptr;              // read only then
+    const std::initializer_list<const void*> read = {v, d->q_gamma, d->k_gamma, d->positions, d->inv_freq, d->slots, d->k_inv_scale, d->v_inv_scale};
+    if (begins_as(d->q_out, read) || begins_as(d->q_out, {d->k, d->k_out, d->k_cache, d->v_cache}) || begins_as(d->k_out, read) ||
+        begins_as(d->k_out, {d->q, d->k_cache, d->v_cache}) || begins_as(d->k_cache, read) || begins_as(d->k_cache, {d->q, d->k, d->v_cache}) ||
+        begins_as(d->v_cache, read) || begins_as(d->v_cache, {d->q, d->k}))
+        return fail(NM_ERR_INVALID_ARG, "nm_qk_norm_rope: an output is an input or another output");
     QkArgs a{};
     a.d = *d;
     a.shift = shift;

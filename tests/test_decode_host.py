@@ -198,3 +198,16 @@ def test_binding_refuses_host_tensors():
 @pytest.mark.parametrize("changes", [dict(out=4 * P)])
 def test_gemv_w4_out_is_the_bias(lib, changes):
     refused(lib.nm_gemv_w4, w4(), nm.NM_ERR_INVALID_ARG, **changes)
+
+
+@pytest.mark.parametrize("changes", [*(dict(out=n * P) for n in range(2, 8)), *(dict(lse=n * P) for n in range(1, 9))])
+def test_paged_attention_outputs_are_no_inputs(lib, changes):
+    """Caches, scales, table and lengths are read while results are written; out may be q, but lse neither of them."""
+    refused(attend(lib), paged(), nm.NM_ERR_INVALID_ARG, **changes)
+
+
+@pytest.mark.parametrize("changes", [*(dict(q_out=n * P) for n in (2, 3, 4, 5, 6, 7, 9, 10, 11, 12, 13, 14)), *(dict(k_out=n * P) for n in (1, 3, 4, 5, 6, 7, 10, 11, 12, 13, 14)),
+                                     *(dict(k_cache=n * P) for n in (1, 2, 3, 6, 11, 12, 13)), *(dict(v_cache=n * P) for n in (1, 2, 3, 6, 12, 14))])
+def test_qk_norm_rope_outputs_are_no_inputs(lib, changes):
+    """q_out may be q and k_out k; nothing else that is written may be read, or be written twice."""
+    refused(lib.nm_qk_norm_rope, qk(), nm.NM_ERR_INVALID_ARG, **changes)
