@@ -586,8 +586,23 @@ _PAGED = struct.Struct("@10iPq2P3q2PPqPfiPqf4xP")
 _W4 = struct.Struct("@7i4xPq2Pf4x2Pi4xPqf4x")
 
 
-def _refuse(what):
-    raise NmError(NM_ERR_INVALID_ARG, what)
+# What Python makes of a missing tensor, one of another rank, and a number that its field does not hold.
+_MISFITS = (AttributeError, TypeError, ValueError, IndexError, OverflowError, struct.error)
+
+
+def _refuse(what, cause=None):
+    raise NmError(NM_ERR_INVALID_ARG, what) from cause
+
+
+def _misfit(call, cause):
+    _refuse(f"{call}: an argument is missing, of another kind or out of its range ({cause})", cause)
+
+
+def _described(desc, packed, call):
+    """A description that the call was given, if it is one of this call's."""
+    if len(desc) != packed.size:
+        _refuse(f"{call}: {len(desc)} bytes are no description of this call")
+    return desc
 
 
 def _here():
@@ -659,20 +674,23 @@ def make_plan_desc(cached, fresh, free_pages, free_begin, block_table, page_size
                    row_start=None, positions=None, requests=None) -> bytes:
     """block_table: int32 [B, max_pages], rows may be apart; every other tensor is contiguous int32.  The description refers to the
     tensors' memory: keep them."""
-    dev = _here()
-    B, n_free, T = cached.numel(), free_pages.numel(), slots.numel()
-    columns, stride = _table(block_table, B, dev)
-    return _PLAN.pack(B, page_size, num_pages, columns, n_free, T, _vector(cached, _i32, B, dev, "cached"), _vector(fresh, _i32, B, dev, "fresh"),
-                      _vector(free_pages, _i32, n_free, dev, "free_pages"), _vector(free_begin, _i32, 1, dev, "free_begin"),
-                      _vector(free_end, _i32, 1, dev, "free_end"), block_table.data_ptr(), stride, _vector(lens, _i32, B, dev, "lens"),
-                      _vector(row_start, _i32, B + 1, dev, "row_start"), _vector(slots, _i32, T, dev, "slots"),
-                      _vector(positions, _i32, T, dev, "positions"), _vector(requests, _i32, T, dev, "requests"), _vector(status, _i32, 4, dev, "status"))
+    try:
+        dev = _here()
+        B, n_free, T = cached.numel(), free_pages.numel(), slots.numel()
+        columns, stride = _table(block_table, B, dev)
+        return _PLAN.pack(B, page_size, num_pages, columns, n_free, T, _vector(cached, _i32, B, dev, "cached"), _vector(fresh, _i32, B, dev, "fresh"),
+                          _vector(free_pages, _i32, n_free, dev, "free_pages"), _vector(free_begin, _i32, 1, dev, "free_begin"),
+                          _vector(free_end, _i32, 1, dev, "free_end"), block_table.data_ptr(), stride, _vector(lens, _i32, B, dev, "lens"),
+                          _vector(row_start, _i32, B + 1, dev, "row_start"), _vector(slots, _i32, T, dev, "slots"),
+                          _vector(positions, _i32, T, dev, "positions"), _vector(requests, _i32, T, dev, "requests"), _vector(status, _i32, 4, dev, "status"))
+    except _MISFITS as e:
+        _misfit("nm_page_plan", e)
 
 
 def nm_page_plan(cached, fresh=None, free_pages=None, free_begin=None, block_table=None, *, page_size=0, num_pages=0, free_end=None, slots=None,
                  status=None, lens=None, row_start=None, positions=None, requests=None, stream=None):
     """make_plan_desc's arguments, or a description alone."""
-    desc = cached if cached.__class__ is bytes else make_plan_desc(cached, fresh, free_pages, free_begin, block_table, page_size, num_pages, free_end,
+    desc = _described(cached, _PLAN, "nm_page_plan") if cached.__class__ is bytes else make_plan_desc(cached, fresh, free_pages, free_begin, block_table, page_size, num_pages, free_end,
                                                                    slots, status, lens, row_start, positions, requests)
     rc = load().nm_page_plan(desc, _stream(stream))
     if rc:
@@ -683,39 +701,42 @@ def make_qk_desc(q, k, v, positions, inv_freq, q_out, k_out=None, k_cache=None, 
                  k_gamma=None, eps=1e-6, interleaved=False, k_inv_scale=None, v_inv_scale=None) -> bytes:
     """q, q_out: [T, hq, d]; k, v, k_out: [T, hk, d]; caches: [pages, page_size, hk, d] with strides; inv_freq (rot / 2 numbers) and
     positions may be None: no rotation.  The description refers to the tensors' memory: keep them."""
-    dev = _here()
-    T, hq, e = q.shape
-    hk = k.shape[1]
-    in_dtype, out_dtype = _type(q, dev, "q"), _type(q_out, dev, "q_out")
-    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-    if k.dtype is not q.dtype or k.get_device() != dev:
-        _refuse("q and k have to have one type, on the current device")
-    k_out_at = k_out_stride = v_at = v_stride = cache_dtype = pages = page = k_at = vc_at = slots_at = s0 = s1 = s2 = 0
-    if k_out is not None:
-        if _type(k_out, dev, "k_out") != out_dtype:
-            _refuse("q_out and k_out have to have one type")
-        k_out_at, k_out_stride = k_out.data_ptr(), _heads(k_out, T, hk, e, "k_out")
-    if k_cache is not None or v_cache is not None:
-        if k_cache is None or v_cache is None or slots is None or v is None:
-            _refuse("v, k_cache, v_cache and slots belong together")
-        if v.dtype is not q.dtype or v.get_device() != dev:
-            _refuse("q, k and v have to have one type, on the current device")
-        v_at, v_stride = v.data_ptr(), _heads(v, T, hk, e, "v")
-        cache_dtype, pages, page, (s0, s1, s2, _) = _cache(k_cache, v_cache, hk, e, dev)
-        k_at, vc_at, slots_at = k_cache.data_ptr(), v_cache.data_ptr(), _vector(slots, _i32, T, dev, "slots")
-    return _QK.pack(T, hq, hk, e, rot, (NM_QK_NORM if norm else 0) | (NM_ROPE_INTERLEAVED if interleaved else 0), in_dtype, out_dtype, cache_dtype,
-                    pages, page, q.data_ptr(), k.data_ptr(), v_at, _heads(q, T, hq, e, "q"), _heads(k, T, hk, e, "k"), v_stride,
-                    0 if q_gamma is None else _vector(q_gamma, _f32, e, dev, "q_gamma"), 0 if k_gamma is None else _vector(k_gamma, _f32, e, dev, "k_gamma"), eps,
-                    _vector(positions, _i32, T, dev, "positions") if rot else 0, _vector(inv_freq, _f32, rot // 2, dev, "inv_freq"),
-                    q_out.data_ptr(), _heads(q_out, T, hq, e, "q_out"), k_out_at, k_out_stride, k_at, vc_at, s0, s1, s2, slots_at,
-                    0 if k_inv_scale is None else _vector(k_inv_scale, _f32, hk, dev, "k_inv_scale"),
-                    0 if v_inv_scale is None else _vector(v_inv_scale, _f32, hk, dev, "v_inv_scale"))
+    try:
+        dev = _here()
+        T, hq, e = q.shape
+        hk = k.shape[1]
+        in_dtype, out_dtype = _type(q, dev, "q"), _type(q_out, dev, "q_out")
+        rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+        if k.dtype is not q.dtype or k.get_device() != dev:
+            _refuse("q and k have to have one type, on the current device")
+        k_out_at = k_out_stride = v_at = v_stride = cache_dtype = pages = page = k_at = vc_at = slots_at = s0 = s1 = s2 = 0
+        if k_out is not None:
+            if _type(k_out, dev, "k_out") != out_dtype:
+                _refuse("q_out and k_out have to have one type")
+            k_out_at, k_out_stride = k_out.data_ptr(), _heads(k_out, T, hk, e, "k_out")
+        if k_cache is not None or v_cache is not None:
+            if k_cache is None or v_cache is None or slots is None or v is None:
+                _refuse("v, k_cache, v_cache and slots belong together")
+            if v.dtype is not q.dtype or v.get_device() != dev:
+                _refuse("q, k and v have to have one type, on the current device")
+            v_at, v_stride = v.data_ptr(), _heads(v, T, hk, e, "v")
+            cache_dtype, pages, page, (s0, s1, s2, _) = _cache(k_cache, v_cache, hk, e, dev)
+            k_at, vc_at, slots_at = k_cache.data_ptr(), v_cache.data_ptr(), _vector(slots, _i32, T, dev, "slots")
+        return _QK.pack(T, hq, hk, e, rot, (NM_QK_NORM if norm else 0) | (NM_ROPE_INTERLEAVED if interleaved else 0), in_dtype, out_dtype, cache_dtype,
+                        pages, page, q.data_ptr(), k.data_ptr(), v_at, _heads(q, T, hq, e, "q"), _heads(k, T, hk, e, "k"), v_stride,
+                        0 if q_gamma is None else _vector(q_gamma, _f32, e, dev, "q_gamma"), 0 if k_gamma is None else _vector(k_gamma, _f32, e, dev, "k_gamma"), eps,
+                        _vector(positions, _i32, T, dev, "positions") if rot else 0, _vector(inv_freq, _f32, rot // 2, dev, "inv_freq"),
+                        q_out.data_ptr(), _heads(q_out, T, hq, e, "q_out"), k_out_at, k_out_stride, k_at, vc_at, s0, s1, s2, slots_at,
+                        0 if k_inv_scale is None else _vector(k_inv_scale, _f32, hk, dev, "k_inv_scale"),
+                        0 if v_inv_scale is None else _vector(v_inv_scale, _f32, hk, dev, "v_inv_scale"))
+    except _MISFITS as e:
+        _misfit("nm_qk_norm_rope", e)
 
 
 def nm_qk_norm_rope(q, k=None, v=None, positions=None, inv_freq=None, q_out=None, *, k_out=None, k_cache=None, v_cache=None, slots=None, norm=False,
                     q_gamma=None, k_gamma=None, eps=1e-6, interleaved=False, k_inv_scale=None, v_inv_scale=None, stream=None):
     """make_qk_desc's arguments, or a description alone."""
-    desc = q if q.__class__ is bytes else make_qk_desc(q, k, v, positions, inv_freq, q_out, k_out, k_cache, v_cache, slots, norm, q_gamma, k_gamma, eps,
+    desc = _described(q, _QK, "nm_qk_norm_rope") if q.__class__ is bytes else make_qk_desc(q, k, v, positions, inv_freq, q_out, k_out, k_cache, v_cache, slots, norm, q_gamma, k_gamma, eps,
                                                        interleaved, k_inv_scale, v_inv_scale)
     rc = load().nm_qk_norm_rope(desc, _stream(stream))
     if rc:
@@ -726,22 +747,28 @@ def make_paged_desc(q, k_cache, v_cache, block_table, lens, out, scale, window=0
                     lse=None) -> bytes:
     """q, out: [B, hq, d]; caches: [pages, page_size, hk, d] with strides; block_table: int32 [B, max_pages].  The description
     refers to the tensors' memory: keep them."""
-    dev = _here()
-    if scale is None:
-        _refuse("scale is wanted")
-    B, hq, e = q.shape
-    hk = k_cache.shape[2]
-    dtype, pages, page, (s0, s1, s2, _) = _cache(k_cache, v_cache, hk, e, dev)
-    columns, table_stride = _table(block_table, B, dev)
-    return _PAGED.pack(B, hq, hk, e, _type(q, dev, "q"), dtype, _type(out, dev, "out"), page, pages, columns, q.data_ptr(), _heads(q, B, hq, e, "q"),
-                       k_cache.data_ptr(), v_cache.data_ptr(), s0, s1, s2, _vector(k_scale, _f32, hk, dev, "k_scale"),
-                       _vector(v_scale, _f32, hk, dev, "v_scale"), block_table.data_ptr(), table_stride, _vector(lens, _i32, B, dev, "lens"), scale,
-                       window, out.data_ptr(), _heads(out, B, hq, e, "out"), out_inv_scale, _vector(lse, _f32, B * hq, dev, "lse"))
+    try:
+        dev = _here()
+        if scale is None:
+            _refuse("scale is wanted")
+        B, hq, e = q.shape
+        hk = k_cache.shape[2]
+        dtype, pages, page, (s0, s1, s2, _) = _cache(k_cache, v_cache, hk, e, dev)
+        columns, table_stride = _table(block_table, B, dev)
+        return _PAGED.pack(B, hq, hk, e, _type(q, dev, "q"), dtype, _type(out, dev, "out"), page, pages, columns, q.data_ptr(), _heads(q, B, hq, e, "q"),
+                           k_cache.data_ptr(), v_cache.data_ptr(), s0, s1, s2, _vector(k_scale, _f32, hk, dev, "k_scale"),
+                           _vector(v_scale, _f32, hk, dev, "v_scale"), block_table.data_ptr(), table_stride, _vector(lens, _i32, B, dev, "lens"), scale,
+                           window, out.data_ptr(), _heads(out, B, hq, e, "out"), out_inv_scale, _vector(lse, _f32, B * hq, dev, "lse"))
+    except _MISFITS as e:
+        _misfit("nm_paged_attention", e)
 
 
 def nm_paged_attention_workspace(*tensors, **more) -> int:
     """Bytes; takes what nm_paged_attention takes, or a description."""
-    desc = tensors[0] if tensors[0].__class__ is bytes else make_paged_desc(*tensors, **more)
+    try:
+        desc = _described(tensors[0], _PAGED, "nm_paged_attention_workspace") if tensors and tensors[0].__class__ is bytes else make_paged_desc(*tensors, **more)
+    except TypeError as e:                                    # not as many arguments
+        _misfit("nm_paged_attention_workspace", e)
     n = C.c_size_t()
     _check(load().nm_paged_attention_workspace(desc, C.byref(n)))
     return n.value
@@ -750,7 +777,7 @@ def nm_paged_attention_workspace(*tensors, **more) -> int:
 def nm_paged_attention(q, k_cache=None, v_cache=None, block_table=None, lens=None, out=None, *, scale=None, window=0, k_scale=None, v_scale=None,
                        out_inv_scale=1.0, lse=None, ws=None, stream=None, ws_bytes=None):
     """make_paged_desc's arguments, or a description alone; and the workspace."""
-    desc = q if q.__class__ is bytes else make_paged_desc(q, k_cache, v_cache, block_table, lens, out, scale, window, k_scale, v_scale, out_inv_scale, lse)
+    desc = _described(q, _PAGED, "nm_paged_attention") if q.__class__ is bytes else make_paged_desc(q, k_cache, v_cache, block_table, lens, out, scale, window, k_scale, v_scale, out_inv_scale, lse)
     at = 0
     if ws is not None:
         if ws.get_device() != _here() or not ws.is_contiguous():
@@ -764,25 +791,28 @@ def nm_paged_attention(q, k_cache=None, v_cache=None, block_table=None, lens=Non
 def make_w4_desc(x, W, scales, out, group, alpha=1.0, bias=None, tables: Tables | None = None, table_idx=-1, out_inv_scale=1.0) -> bytes:
     """x: [M, K], out: [M, N], rows may be apart; W: uint8 [N, K / 2]; scales: [N, K / group], both contiguous.  The description
     refers to the tensors' memory: keep them."""
-    dev = _here()
-    (M, K), N = x.shape, W.shape[0]
-    if W.dtype is not _u8 or W.get_device() != dev or W.shape != (N, K // 2) or not W.is_contiguous() or K % 2:
-        _refuse(f"W: contiguous uint8 [N, {K // 2}] on the current device is wanted, got {tuple(W.shape)} of {W.dtype}")
-    if group < 1 or K % group or scales.shape != (N, K // group) or not scales.is_contiguous():
-        _refuse(f"scales: contiguous [{N}, {K} / group] is wanted, got {tuple(scales.shape)}, group {group}")
-    x0, x1 = x.stride()
-    o0, o1 = out.stride() if out.dim() == 2 else (0, 0)
-    if out.shape != (M, N) or (o1 != 1 and N > 1) or (x1 != 1 and K > 1):
-        _refuse(f"x and out: rows of neighbouring elements are wanted, out of shape {(M, N)}, got {tuple(out.shape)}")
-    return _W4.pack(M, N, K, group, _type(x, dev, "x"), _type(scales, dev, "scales"), _type(out, dev, "out"), x.data_ptr(), x0 if M > 1 else K,
-                    W.data_ptr(), scales.data_ptr(), alpha, _vector(bias, _f32, N, dev, "bias"), (tables.handle or 0) if tables is not None else 0,
-                    table_idx, out.data_ptr(), o0 if M > 1 else N, out_inv_scale)
+    try:
+        dev = _here()
+        (M, K), N = x.shape, W.shape[0]
+        if W.dtype is not _u8 or W.get_device() != dev or W.shape != (N, K // 2) or not W.is_contiguous() or K % 2:
+            _refuse(f"W: contiguous uint8 [N, {K // 2}] on the current device is wanted, got {tuple(W.shape)} of {W.dtype}")
+        if group < 1 or K % group or scales.shape != (N, K // group) or not scales.is_contiguous():
+            _refuse(f"scales: contiguous [{N}, {K} / group] is wanted, got {tuple(scales.shape)}, group {group}")
+        x0, x1 = x.stride()
+        o0, o1 = out.stride() if out.dim() == 2 else (0, 0)
+        if out.shape != (M, N) or (o1 != 1 and N > 1) or (x1 != 1 and K > 1):
+            _refuse(f"x and out: rows of neighbouring elements are wanted, out of shape {(M, N)}, got {tuple(out.shape)}")
+        return _W4.pack(M, N, K, group, _type(x, dev, "x"), _type(scales, dev, "scales"), _type(out, dev, "out"), x.data_ptr(), x0 if M > 1 else K,
+                        W.data_ptr(), scales.data_ptr(), alpha, _vector(bias, _f32, N, dev, "bias"), (tables.handle or 0) if tables is not None else 0,
+                        table_idx, out.data_ptr(), o0 if M > 1 else N, out_inv_scale)
+    except _MISFITS as e:
+        _misfit("nm_gemv_w4", e)
 
 
 def nm_gemv_w4(x, W=None, scales=None, out=None, *, group=0, alpha=1.0, bias=None, tables: Tables | None = None, table_idx=-1, out_inv_scale=1.0,
                stream=None):
     """make_w4_desc's arguments, or a description alone."""
-    desc = x if x.__class__ is bytes else make_w4_desc(x, W, scales, out, group, alpha, bias, tables, table_idx, out_inv_scale)
+    desc = _described(x, _W4, "nm_gemv_w4") if x.__class__ is bytes else make_w4_desc(x, W, scales, out, group, alpha, bias, tables, table_idx, out_inv_scale)
     rc = load().nm_gemv_w4(desc, _stream(stream))
     if rc:
         _check(rc)

@@ -211,3 +211,60 @@ def test_paged_attention_outputs_are_no_inputs(lib, changes):
 def test_qk_norm_rope_outputs_are_no_inputs(lib, changes):
     """q_out may be q and k_out k; nothing else that is written may be read, or be written twice."""
     refused(lib.nm_qk_norm_rope, qk(), nm.NM_ERR_INVALID_ARG, **changes)
+
+
+@pytest.fixture
+def host_tensors(monkeypatch):
+    """Descriptions of tensors in host memory can be made (none is given to a call that would run)."""
+    import torch
+    nm._here()
+    monkeypatch.setattr(nm, "_current", lambda: -1)
+    i, x = torch.zeros(8, dtype=torch.int32), torch.zeros((2, 4, 64))
+    cache = torch.zeros((3, 16, 4, 64), dtype=torch.bfloat16)
+    w = torch.zeros((2, 64), dtype=torch.bfloat16)
+    return {
+        nm.make_plan_desc: dict(cached=i[:2], fresh=i[:2], free_pages=i, free_begin=i[:1], block_table=i.view(2, 4), page_size=16, num_pages=4, free_end=i[:1],
+                                slots=i, status=i[:4]),
+        nm.make_qk_desc: dict(q=x, k=x, v=x, positions=i[:2], inv_freq=torch.zeros(32), q_out=x, k_cache=cache, v_cache=cache, slots=i[:2]),
+        nm.make_paged_desc: dict(q=x, k_cache=cache, v_cache=cache, block_table=i.view(2, 4), lens=i[:2], out=x, scale=1.0),
+        nm.make_w4_desc: dict(x=w, W=torch.zeros((5, 32), dtype=torch.uint8), scales=torch.zeros((5, 2)), out=torch.zeros((2, 5)), group=32)}
+
+
+def test_calls_refuse_what_is_missing_or_misshapen(host_tensors):
+    """A wanted tensor that is None or a number, or one of another rank, is refused as everything else is."""
+    calls = {nm.make_plan_desc: nm.nm_page_plan, nm.make_qk_desc: nm.nm_qk_norm_rope, nm.make_paged_desc: nm.nm_paged_attention, nm.make_w4_desc: nm.nm_gemv_w4}
+    for make, good in host_tensors.items():
+        assert len(make(**good)) > 0
+        for name, value in good.items():
+            if name in ("inv_freq", "positions", "free_pages") or (make is nm.make_plan_desc and name == "slots"):
+                continue                                                      # may be None, or of any length
+            for bad in [None, "3"] + ([value[0], value[None], 3] if hasattr(value, "shape") else []):
+                if hasattr(bad, "shape") and value.dim() == 1 and bad.numel() == value.numel():
+                    continue                                                  # a list of numbers may have any shape
+                with pytest.raises(nm.NmError) as e:
+                    calls[make](make(**{**good, name: bad}), stream=0)
+                assert e.value.status == nm.NM_ERR_INVALID_ARG and str(e.value), (make.__name__, name)
+
+
+def test_calls_refuse_numbers_that_do_not_fit(host_tensors):
+    calls = {nm.make_plan_desc: nm.nm_page_plan, nm.make_qk_desc: nm.nm_qk_norm_rope, nm.make_paged_desc: nm.nm_paged_attention, nm.make_w4_desc: nm.nm_gemv_w4}
+    for make, name, value in ((nm.make_plan_desc, "page_size", 1 << 31), (nm.make_plan_desc, "num_pages", 1 << 40), (nm.make_plan_desc, "page_size", 16.5), (nm.make_qk_desc, "eps", 1e300),
+                              (nm.make_paged_desc, "window", 1 << 31), (nm.make_paged_desc, "scale", 1e300), (nm.make_w4_desc, "alpha", 1e300), (nm.make_w4_desc, "table_idx", 1 << 31)):
+        with pytest.raises(nm.NmError) as e:
+            calls[make](make(**{**host_tensors[make], **dict.fromkeys(("norm",) if name == "eps" else (), True), name: value}), stream=0)
+        assert e.value.status == nm.NM_ERR_INVALID_ARG, name
+
+
+def test_calls_refuse_missing_arguments_and_other_calls_descriptions(host_tensors):
+    descs = [make(**good) for make, good in host_tensors.items()]
+    calls = [nm.nm_page_plan, nm.nm_qk_norm_rope, nm.nm_paged_attention, nm.nm_gemv_w4]
+    for i, call in enumerate(calls):
+        for bad in [None, 3, b""] + [d for j, d in enumerate(descs) if j != i]:
+            with pytest.raises(nm.NmError) as e:
+                call(bad, stream=0)
+            assert e.value.status == nm.NM_ERR_INVALID_ARG
+    with pytest.raises(nm.NmError):
+        nm.nm_paged_attention_workspace(descs[0])
+    with pytest.raises(nm.NmError):
+        nm.nm_paged_attention_workspace()
+    assert nm.nm_paged_attention_workspace(descs[2]) >= 0
