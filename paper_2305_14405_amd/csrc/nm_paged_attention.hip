@@ -30,8 +30,8 @@ typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
-struct PagedArgs : PagedSplit {
-    nm_paged_desc d;
+struct PagedDesc { nm_paged_desc d; };
+struct PagedArgs : PagedDesc, PagedSplit {
     int shift;            // log2 of page_size
     int extra;            // units that starting and ending a row costs
     float* part_o;        // [share, workers, 2, 16, d]: a run's first and last piece, not yet divided by the sum
@@ -604,7 +604,7 @@ static int32_t plan_paged(const nm_paged_desc* d, PagedArgs* a, size_t* bytes, l
     a->shift = shift;
     static_cast<PagedSplit&>(*a) = paged_split({d->B, d->hq, d->hk, d->d, dtype_bytes(d->cache_dtype), d->slot_stride, d->head_stride, longest_of(*d, shift)});
     a->extra = 2;
-    const long teams = ((a->workers ? a->workers : a->sets) + 7) / 8 * 8;   // every XCD has as many
+    const long teams = ((a->workers ? a->workers : paged_sets(d->B, d->hk, *a)) + 7) / 8 * 8;   // every XCD has as many
     *blocks = teams * a->share;
     const size_t parts = (size_t)a->share * a->workers * 2 * 16;
     *bytes = parts * (sizeof(float2) + d->d * sizeof(float)) + parts / 32 * sizeof(int4);

@@ -29,12 +29,13 @@ struct PagedSplit {
     int groups;           // of up to 16 of them
     int share;            // rows that read the same lines of the cache: a team of so many workgroups of one XCD takes them side by side
     int workers;          // teams that share the units; 0: one team to a set of rows
-    long sets;            // of rows, share rows each
 };
+// Sets of rows of all requests, a.share rows each.
+inline long paged_sets(int B, int hk, const PagedSplit& a) { return (long)B * (hk / a.pack) * a.groups / a.share; }
 
 inline PagedSplit paged_split(const PagedShape& p)
 {
-    PagedSplit a{1, p.hq / p.hk, (p.hq / p.hk + 15) / 16, 1, 0, 0};
+    PagedSplit a{1, p.hq / p.hk, (p.hq / p.hk + 15) / 16, 1, 0};
     // Rows that read the same lines: the groups of a key head, and the heads whose pieces of a slot share a line of 128 bytes (as long as
     // the other slots do not lie between them).
     auto share_rows = [&] {
@@ -43,10 +44,9 @@ inline PagedSplit paged_split(const PagedShape& p)
         if (head_bytes > 0 && head_bytes < 128 && a.pack * p.head_stride < p.slot_stride)
             for (int n = 2; n * head_bytes <= 128; n *= 2)
                 if (p.hk / a.pack % n == 0) a.share = a.groups * n;
-        a.sets = (long)p.B * (p.hk / a.pack) * a.groups / a.share;
     };
     share_rows();
-    const bool divided = p.longest > (a.sets >= 128 ? 1024 : 512);
+    const bool divided = p.longest > (paged_sets(p.B, p.hk, a) >= 128 ? 1024 : 512);
     // Neighbouring heads of int8 as one of up to 128 elements: whole lines, and one softmax for all their queries.  Where they are too few, rows that
     // begin and end at a second kernel's cost more (heads of 64, us apart and packed: 64 requests of up to 4097 positions 69 and 62, 48 54 and 49, 32 36 and
     // 35, 16 25 and 26; heads of 32, 64 requests 60 and 38).  Not of floating-point types, where an infinity times zero is none.
@@ -56,7 +56,7 @@ inline PagedSplit paged_split(const PagedShape& p)
         if (!paged_packs(p.cache_bytes, paged_width(a.pack * p.d))) a.pack = 1, a.group = p.hq / p.hk;
         share_rows();
     }
-    const long most = a.sets * ((p.longest + kUnit - 1) / kUnit);
+    const long most = paged_sets(p.B, p.hk, a) * ((p.longest + kUnit - 1) / kUnit);
     // Who shares: as many workgroups as run at once (twice as many took 4 % longer at 48 ragged requests and 1 to 10 % at one of 131071).
     // Rows too short to be divided go to a workgroup each, without the second kernel: tables of up to 512 positions (heads of 128, 8 rows: 14.1 us,
     // 15.3 divided), 1024 where rows go round half of the CUs (64 rows: 20.9 and 20.2; 128: 21.9 and 25.3, 22.3 if ragged; 252 of 64: 17.1 and 24.2;

@@ -18,7 +18,7 @@ static bool covers(const PagedShape& p)
     if (pack > 1) ++packed_shapes;
     if (a.workers) ++divided_shapes;
     const int rows = paged_rows(p.hk, pack, a.groups);
-    bool ok = a.pack * p.d <= 256 && a.groups * 16 >= a.group && a.share >= 1 && rows % a.share == 0 && a.sets * a.share == (long)p.B * rows &&
+    bool ok = a.pack * p.d <= 256 && a.groups * 16 >= a.group && a.share >= 1 && rows % a.share == 0 && paged_sets(p.B, p.hk, a) * a.share == (long)p.B * rows &&
               (a.groups == 1 || a.pack == 1) && a.group % pack == 0;
     std::vector<int> seen(p.hq, 0);
     for (int set = 0; ok && set < rows / a.share; ++set)
