@@ -479,7 +479,7 @@ int32_t nm_cnn_run(const nm_cnn_op* ops, int32_t n_ops, void* ws, size_t ws_byte
  *
  * nm_qk_norm_rope and nm_paged_attention compute the functions themselves, not tables of them: a softmax that is split over the
  * cache's length and joined relies on exp(a + b) = exp(a) exp(b), which a piecewise-linear exp does not have.  nm_gemv_w4 takes tables.
- * Sums and statistics are binary32 (integer products exact int32); outputs are rounded once, to nearest even; int8 codes
+ * Sums and statistics are binary32 (sums of up to 128 integer products exact int32); outputs are rounded once, to nearest even; int8 codes
  * as above.  The same call gives the same bits (no atomics); against the formulas results are right to rounding, not bit for bit.
  * Which kernels run depends on shapes and types alone, so every call can be captured; calls that overlap in time share nothing but
  * what the caller gives both.
@@ -615,7 +615,7 @@ int32_t nm_paged_attention(const nm_paged_desc* desc, void* ws, size_t ws_bytes,
 
 /*
  * nm_gemv_w4: product of a few rows with 4-bit weights, the projections of a step.
- *   acc[m,n] = sum over groups g of scales[n,g] * sum_{k in g} x[m,k] * w[n,k]      (int8 x: the inner sums are exact int32)
+ *   acc[m,n] = sum over groups g of scales[n,g] * sum_{k in g} x[m,k] * w[n,k]      (int8 x: of a group, or of 128 of its products at a time, exact in int32)
  *   v = fma(acc, alpha, bias_n);  v = PWL_table(v) if table_idx >= 0;  out[m,n] = v, or its int8 code with out_inv_scale
  * x: device [M, K], rows x_stride elements apart, x_dtype I8, BF16 or F16.  W: device [N, K / 2], contiguous: byte i of a row holds
  * w[n, 2 i] in its low and w[n, 2 i + 1] in its high four bits, two's complement (-8 .. 7).  scales: device [N, K / group], contiguous,

@@ -5,9 +5,9 @@
 // fill the GPU.  K goes by chunks: x of a chunk, and the chunk's scales as fp32, lie in LDS (the next chunk's are on their way into
 // registers), and a wavefront takes a run of the chunk's blocks.  Where a chunk or two are all of K (few rows), weights go
 // directly into LDS, a ring of blocks for each wavefront; with more chunks through registers, for whoever waits for a chunk's x would
-// wait for the whole ring (33 rows, 8192 x 8192: 29 us with the ring).  Then 32 columns are two sets of eight wavefronts, four to a
-// SIMD: fetching and ordering x, unpacking weights and the matrix instructions of one run under another's (8192 x 8192: 33 rows 21.0 us, 22.8
-// with eight wavefronts of 32 columns; 48: 24.1 and 26.4; 17: 15.6 and 16.9; 16: 13.7 and 14.7).
+// wait for the whole ring (33 rows, 8192 x 8192: 46 us with the ring).  Then 32 columns are two sets of eight wavefronts, four to a
+// SIMD: fetching and ordering x, unpacking weights and the matrix instructions of one run under another's (8192 x 8192: 33 rows 20.0 us, 21.8
+// with eight wavefronts of 32 columns; 48: 22.3 and 25.4; 17: 15.4 and 16.7; 16: 14.6 and 15.9).
 //   Four neighbouring lanes load 64 bytes, 128 weights, of a row, a run of 32 each: neighbouring lanes in different rows, as the matrix
 // instruction wants them, cost the address unit four times as much (28672 x 8192: 54 us so, 2.2 TB/s).  From LDS lane (j, row) then
 // gets run j of its row.  The 16x16x32 instruction (rows of x its rows, columns its columns) adds over the four lanes of a
@@ -17,7 +17,7 @@
 // weights, and exact.  fp16: u = w + 8 is put under an exponent, 16 + u, and 24 taken off, both exact, in thirteen.  bf16: one
 // conversion of the lower four bits of a byte for each weight, to w / 16 in fp32, whose upper half is taken; thirteen too.  The matrix instructions so
 // have the weights themselves: what x they meet a zero with is not in the sum (with 16 + u there, and 24 times the sum of x taken off by
-// further matrix instructions, a value 30000 times the others left an error 14000 times fp32's).
+// further matrix instructions, a value 30000 times the others that met a zero left an error some 1000 times that of an fp32 sum).
 //   What a group's sum is multiplied by is one number per lane (its column).
 #pragma once
 
@@ -390,7 +390,7 @@ static int32_t launch_w4_tiles(W4Args a, hipStream_t s)
     const int chunk = kLength << a.chunk_shift;
     a.chunks = (a.d.K + chunk - 1) / chunk;
     if constexpr (kRing)
-        if (a.chunks > 2 / kK) return launch_w4_registers<X, S, kRuns, 1>(a, s);   // (4 rows of 4096 x 11008: 11.4 us, 12.6 as two chunks of the ring)
+        if (a.chunks > 2 / kK) return launch_w4_registers<X, S, kRuns, 1>(a, s);   // (4 rows of 4096 x 11008: 11.9 us, 13.2 as two chunks of the ring)
     a.x_stride = chunk * (int)sizeof(X) + 16;
     const int entries = (chunk / 128) * (4 / kRuns);
     const size_t one = (size_t)(kCols * (entries + 1) * 4 + 15) / 16 * 16 + (size_t)rows * a.x_stride;
@@ -416,8 +416,8 @@ static int32_t launch_w4_tiles(W4Args a, hipStream_t s)
 }
 // Weights through registers, tiles of 16 kM rows: 16 columns to a workgroup where no more than a CU's worth come of it, 32 where there
 // are more.  A chunk of x fills LDS either way, so one workgroup has a CU and more than 256 are a second round (16 columns of 7168 x 8192
-// took 18.4 us at 16 rows, 32 take 12.6).  With 16 columns sixteen wavefronts share K, unless it is a chunk of eight's
-// (4096 x 11008, 16 rows: 13.5 us, eight 15.7).
+// took 18.9 us at 16 rows, 32 take 13.6).  With 16 columns sixteen wavefronts share K, unless it is a chunk of eight's
+// (4096 x 11008, 16 rows: 13.3 us, eight 14.9).
 template <typename X, typename S, int kRuns, int kM>
 static int32_t launch_w4_registers(const W4Args& a, hipStream_t s)
 {
@@ -434,10 +434,10 @@ template <typename X, typename S, int kRuns>
 static int32_t launch_w4_rows(const W4Args& a, hipStream_t s)
 {
     // The fewest rows and columns to a workgroup that leave it a CU of its own, for rows are what a workgroup's time grows with (40 rows of
-    // 4096 x 11008: 28.7 us as one tile of 48, 20.3 as two of 32; of 768 x 768 6.5 and, as three of 16, 4.4).  Where there are more workgroups
+    // 4096 x 11008: 26.8 us as one tile of 48, 19.4 as two of 32; of 768 x 768 5.9 and, as three of 16, 4.1).  Where there are more workgroups
     // than CUs anyway, tiles of 48 rows if they save a pass over the weights (those and x of a chunk are what LDS holds).
-    // A ring of eight wavefronts has 4096 columns of x under way at once; beyond, sixteen (one row of 4096 x 11008 10.9 us, 11.5 with eight; of
-    // 4096 x 4096 5.6 and 5.3).
+    // A ring of eight wavefronts has 4096 columns of x under way at once; beyond, sixteen (one row of 4096 x 11008 11.3 us, 11.8 with eight; at
+    // 4096 x 4096 either, 5.4 and 5.6).
     const long M = a.d.M, columns = (a.d.N + 15) / 16;
     if ((M + 15) / 16 * columns <= 256)
         return a.d.K <= 4096 ? launch_w4_tiles<X, S, kRuns, 1, 1, true>(a, s) : launch_w4_tiles<X, S, kRuns, 1, 1, true, 1, 2>(a, s);

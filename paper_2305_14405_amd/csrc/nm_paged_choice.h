@@ -60,7 +60,8 @@ inline PagedSplit paged_split(const PagedShape& p)
     // Who shares: as many workgroups as run at once (twice as many took 4 % longer at 48 ragged requests and 1 to 10 % at one of 131071).
     // Rows too short to be divided go to a workgroup each, without the second kernel: tables of up to 512 positions (heads of 128, 8 rows: 14.1 us,
     // 15.3 divided), 1024 where rows go round half of the CUs (64 rows: 20.9 and 20.2; 128: 21.9 and 25.3, 22.3 if ragged; 252 of 64: 17.1 and 24.2;
-    // 12 of 64 would gain too, 12.0 and 13.9, 8 of 128 lose more, 19.7 and 15.3).  Where that leaves CUs without one, heads of up to 64 have eight
+    // 12 of 64 would gain too, 12.0 and 13.9, 8 of 128 lose more, 19.7 and 15.3: the line does not look at the heads' size, so that a table of 513
+    // positions or more has a workspace with few rows of any).  Where that leaves CUs without one, heads of up to 64 have eight
     // wavefronts (12 heads, 300 positions: 9.3 us, 10.3 with four; heads of 128 gain less, and lose as much at one tile, by the second four).
     if (divided) a.workers = (int)std::min(most, std::max(8l, 256l * workgroups_of(paged_width(a.pack * p.d)) / a.share));
     return a;
