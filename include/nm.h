@@ -620,7 +620,8 @@ int32_t nm_paged_attention(const nm_paged_desc* desc, void* ws, size_t ws_bytes,
  * x: device [M, K], rows x_stride elements apart, x_dtype I8, BF16 or F16.  W: device [N, K / 2], contiguous: byte i of a row holds
  * w[n, 2 i] in its low and w[n, 2 i + 1] in its high four bits, two's complement (-8 .. 7).  scales: device [N, K / group], contiguous,
  * scale_dtype F32, BF16 or F16.  bias: device fp32 [N] or NULL.  out: device [M, N], rows out_stride apart, out_dtype F32, BF16, F16
- * or I8; out is none of the inputs.  Any M: rows are taken up to 48 at a time, and the weights read again for each (nm_gemm_pwl is the call for many rows).
+ * or I8; out is none of the inputs.  Any M: rows are taken up to 48 at a time, and the weights read again for each (many rows are better off with nm_gemm_pwl
+ * and int8 weights).
  * bf16 and fp16 rows meet the weights themselves, in exact products: a value whose weight is zero leaves no error, an infinity follows the
  * formula (times a weight of zero: NaN), and neither it nor a NaN reaches another row.
  * Limits: group 32, 64 or a multiple of 128; K a multiple of group, at most 65536; x and W 16-byte aligned, x_stride a multiple of 16

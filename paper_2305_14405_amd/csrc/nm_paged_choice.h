@@ -48,8 +48,9 @@ inline PagedSplit paged_split(const PagedShape& p)
     share_rows();
     const bool divided = p.longest > (paged_sets(p.B, p.hk, a) >= 128 ? 1024 : 512);
     // Neighbouring heads of int8 as one of up to 128 elements: whole lines, and one softmax for all their queries.  Where they are too few, rows that
-    // begin and end at a second kernel's cost more (heads of 64, us apart and packed: 64 requests of up to 4097 positions 69 and 62, 48 54 and 49, 32 36 and
-    // 35, 16 25 and 26; heads of 32, 64 requests 60 and 38).  Not of floating-point types, where an infinity times zero is none.
+    // begin and end at a second kernel's cost more (us apart and packed, requests of up to 4097 positions: 16 heads of 64, 64 requests 68 and 61, 32
+    // 36 and 37, 16 25 and 27; 12 of 48, 64 requests 55 and 53, 32 34 and 37; 16 of 32 61 and 39, 16 of 16 64 and 33, which gain with 32 requests too,
+    // 39 and 30, 42 and 28: the line is that of 64 for all).  Not of floating-point types, where an infinity times zero is none.
     if (divided && p.cache_bytes == 1 && p.head_stride == p.d && (long)p.B * p.hk * ((p.longest + kUnit - 1) / kUnit) >= 32 * 768) {
         while (2 * a.pack * p.d <= 128 && p.hk % (2 * a.pack) == 0 && 2 * a.group <= 16) a.pack *= 2, a.group *= 2;
         // heads of 16 or 32 that are too few, or have too many queries, to fill that width: the kernel for it takes them one by one
