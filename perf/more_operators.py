@@ -296,7 +296,7 @@ def _own_attn(s):
 def _plain_beam(s):
     c = s["case"]
     R, W, K, V = (c[n] for n in ("R", "W", "K", "V"))
-    x = s["x"].float()
+    x = s["x"].float() + 0.0                                                  # zeros of either sign are one value
     top = x.amax(-1, keepdim=True)
     lse = top[:, 0].double() + torch.exp(x - top).double().sum(-1).log()
     bits = x.view(torch.int32)
