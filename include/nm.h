@@ -645,6 +645,128 @@ typedef struct {
 
 int32_t nm_gemv_w4(const nm_w4_desc* desc, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Several hypotheses per request over the paged cache: a row of the batch is a hypothesis, and the rows of a request share the pages of
+ * what they have in common.  One step: nm_page_plan (one new token per row), the model with nm_qk_norm_rope and nm_paged_attention,
+ * nm_beam_select over its logits, nm_page_fork, and nm_page_copy of the pages that it names, before pages are taken again.  As above, a step's
+ * numbers are device memory, nothing is allocated, the host does not wait, every call can be captured, and the same call gives the same bits.
+ * Workspaces: 256-byte aligned, contents are scratch, calls that overlap in time need one each.
+ * --------------------------------------------------------------------------------------------- */
+
+/*
+ * nm_beam_select: the K best continuations of each of R requests with W hypotheses.  Row r W + w of the logits belongs to
+ * hypothesis w of request r, whose log-probability so far is scores[r,w]:
+ *   t(w, v) = scores[r,w] + x[w,v] - log sum_u exp(x[w,u])    for the tokens v of every hypothesis with done[r,w] = 0
+ *   t(w, end_token) = scores[r,w]                            the only candidate of one with done[r,w] != 0
+ * The K candidates of largest weight[r,w] * t go out, best first (weight NULL: 1); equal ones by w, then by logit, then by v, the lowest first
+ * (the largest logit).  For the k-th:  parents[r,k] = r W + w;  tokens[r,k] = v;  scores_out[r,k] = t;
+ * done_out[r,k] = done[r,w] != 0 or v == end_token.  Fewer than K candidates: parents and tokens -1, scores_out -inf, done_out 0.
+ * No candidates: tokens whose logit is -inf or NaN (masked), and hypotheses whose score or weight is not finite, or whose weight is not above 0.
+ * A logit of +inf counts as the largest binary32 number.  Logits are compared as they are; t and weight * t are formed in 64 bits from a sum of exponentials
+ * in 32 (partial sums of 32 terms, joined in 64), so that of two hypotheses' candidates whose t are closer than 2^-20 either may come first, but always the same.
+ * history (NULL: none): row r W + w holds the history_lens[r W + w] tokens of that hypothesis, in rows of max_history.  Row r K + k of history_out receives
+ * its parent's tokens and, unless the parent was done or the row is full, the new one; history_lens_out how many these are (no parent: 0).  What is behind
+ * them is left as it was.  Lengths outside [0, max_history] count as the nearest.
+ * logits: device [R W, V], rows logits_stride elements apart, logits_dtype F32, BF16 or F16.  scores, weight: device fp32 [R, W]; done: device int32 [R, W] or
+ * NULL.  parents, tokens, done_out (or NULL): device int32 [R, K]; scores_out: device fp32 [R, K].  history, history_out: device int32, rows
+ * history_stride and history_out_stride apart; history_lens, history_lens_out: device int32 [R W], [R K].  No output may be an input or another output.
+ * Limits: 1 <= W, K <= NM_BEAM_MAX; R W <= 2^20; 1 <= V <= 2^26; 1 <= max_history.  -1 <= end_token < V (-1: none; then done is NULL).
+ */
+#define NM_BEAM_MAX 64
+typedef struct {
+    int32_t R, W, K, V;
+    int32_t logits_dtype, end_token, max_history;
+    const void* logits;
+    int64_t logits_stride;
+    const float* scores;
+    const float* weight;
+    const int32_t* done;
+    int32_t* parents;
+    int32_t* tokens;
+    float* scores_out;
+    int32_t* done_out;
+    const int32_t* history;
+    int64_t history_stride;
+    const int32_t* history_lens;
+    int32_t* history_out;
+    int64_t history_out_stride;
+    int32_t* history_lens_out;
+} nm_beam_desc;
+
+int32_t nm_beam_select_workspace(const nm_beam_desc* desc, size_t* bytes);
+int32_t nm_beam_select(const nm_beam_desc* desc, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * nm_page_fork: the block tables of a new batch whose row b goes on from row parents[b] of the old one.  A parent outside [0, B_in)
+ * leaves row b empty; a row may have several children (they share its pages), one (it moves) or none (what only it held becomes free), and B_out
+ * may differ from B_in (a batch is compacted, or grows).  Old row r holds lens[r] tokens in its first up(lens) = ceil(lens / page_size) entries.
+ * For row b of parent p, and n = lens[p]:  lens_out[b] = n;  the first up(n) entries of its row of table_out are p's, but for the last
+ * page where n is no multiple of page_size: the next token would be written into it.  It stays p's page for the lowest-numbered row with
+ * that parent, if no other old row with children refers to the page and keep (NULL: nobody) is 0 for it; every other row gets a page of its own: the next of
+ * free_pages, from number *free_begin on, in the order of the rows.  copy_src[b], copy_dst[b] and copy_slots[b] then say which page's first
+ * slots are to be copied where (nm_page_copy), and are -1, -1, 0 for the other rows.  Entries behind up(n) are left as they were.
+ * Pages that old rows refer to and no new row does, and that keep does not hold (keep[page] != 0: a page of a prefix cache, or of another batch), are
+ * freed: with `taken` pages taken and `freed` freed, *free_end = *free_begin + taken - freed, and free_out holds from there the freed pages, ascending, and then
+ * the rest of free_pages as it was.  What lies in front of *free_end is left as it was.  free_out may be free_pages.
+ * A copied page that is freed keeps its contents until pages are taken again: copy before that.
+ * Entries that are no pages (outside [0, num_pages)) are handed on, and neither copied nor freed.
+ * status[0]: 0, or a sum of NM_FORK_*; [1]: pages wanted, [2]: pages freed, [3]: rows with a parent.  With any flag set nothing is assigned:
+ * table_out is left as it is, lens_out is 0, there are no copies, free_out holds the rest of free_pages, and *free_end = *free_begin.
+ * (With NM_FORK_BAD_LENGTH the other numbers and flags count only the rows whose length is good.)
+ * lens: device int32 [B_in].  parents: [B_out].  block_table, table_out: int32, rows of max_pages entries, table_stride and table_out_stride
+ * apart.  keep: int32 [num_pages] or NULL.  free_pages, free_out: [n_free].  lens_out, copy_src, copy_dst, copy_slots: [B_out].  Apart from free_out no output may be an
+ * input, and none another output.
+ * Limits: B_in, B_out <= NM_PLAN_MAX_REQUESTS; page_size a power of two up to 65536; num_pages * page_size and max_pages * page_size < 2^31; n_free <= 2^30.
+ */
+enum { NM_FORK_NO_PAGES = 1,      /* the free list is too short */
+       NM_FORK_BAD_LENGTH = 8,    /* a length that is negative or longer than max_pages, or *free_begin outside [0, n_free] */
+       NM_FORK_LIST_FULL = 16 };  /* the list has no room in front of *free_begin for the pages that become free */
+typedef struct {
+    int32_t B_in, B_out, page_size, num_pages, max_pages, n_free;
+    const int32_t* block_table;
+    int64_t table_stride;
+    const int32_t* lens;
+    const int32_t* parents;
+    const int32_t* keep;
+    const int32_t* free_pages;
+    const int32_t* free_begin;
+    int32_t* table_out;
+    int64_t table_out_stride;
+    int32_t* lens_out;
+    int32_t* free_out;
+    int32_t* free_end;
+    int32_t* copy_src;
+    int32_t* copy_dst;
+    int32_t* copy_slots;
+    int32_t* status; /* [4] */
+} nm_fork_desc;
+
+int32_t nm_page_fork_workspace(const nm_fork_desc* desc, size_t* bytes);
+int32_t nm_page_fork(const nm_fork_desc* desc, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * nm_page_copy: copies pages inside each of n_caches caches of one layout (a model's key and value caches of every layer): for i < n, the first
+ * slots[i] slots (NULL: page_size; more counts as page_size, fewer than 1 as none) of page src[i] to page dst[i].  A copy whose src or dst is no page (outside [0, num_pages)), or
+ * that are one page, is left out.  No page may be the destination of two copies, or the source of one and the destination of another: what those
+ * hold is not said then.
+ * caches: HOST array of n_caches device pointers, read during the call.  dtype: F32, BF16, F16 or I8; elements are moved as they are.  src, dst,
+ * slots: device int32 [n].  Strides as above, in elements.  Where addresses, strides and rows are multiples of 16 bytes, whole groups move at once.
+ * Limits: n <= 2^20; n_caches <= NM_COPY_MAX_CACHES; page_size a power of two up to 65536; hk, d >= 1; num_pages * page_size, and
+ * page_size * hk * d, < 2^31.
+ */
+#define NM_COPY_MAX_CACHES 256
+typedef struct {
+    int32_t n, n_caches, hk, d, dtype;
+    int32_t num_pages, page_size;
+    void* const* caches;
+    int64_t page_stride, slot_stride, head_stride;
+    const int32_t* src;
+    const int32_t* dst;
+    const int32_t* slots;
+} nm_copy_desc;
+
+int32_t nm_page_copy(const nm_copy_desc* desc, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,6 +21,8 @@ NM_DT_I32, NM_DT_F32, NM_DT_BF16, NM_DT_F16, NM_DT_I8 = 0, 1, 2, 3, 4
 NM_PLAN_MAX_REQUESTS = 4096
 NM_PLAN_NO_PAGES, NM_PLAN_TABLE_FULL, NM_PLAN_NO_ROWS, NM_PLAN_BAD_LENGTH = 1, 2, 4, 8
 NM_QK_NORM, NM_ROPE_INTERLEAVED = 1, 2
+NM_BEAM_MAX, NM_COPY_MAX_CACHES = 64, 256
+NM_FORK_NO_PAGES, NM_FORK_BAD_LENGTH, NM_FORK_LIST_FULL = 1, 8, 16
 
 # every symbol include/nm.h declares
 EXPORTS = ("nm_last_error", "nm_version", "nm_table_build_host", "nm_build_tables",
@@ -31,7 +33,7 @@ EXPORTS = ("nm_last_error", "nm_version", "nm_table_build_host", "nm_build_table
            "nm_encoder_stack_workspace", "nm_encoder_stack", "nm_conv2d_workspace", "nm_conv2d_pwl",
            "nm_maxpool_i8", "nm_avgpool_i8", "nm_cnn_workspace", "nm_cnn_run",
            "nm_page_plan", "nm_qk_norm_rope", "nm_paged_attention_workspace", "nm_paged_attention",
-           "nm_gemv_w4")
+           "nm_gemv_w4", "nm_beam_select_workspace", "nm_beam_select", "nm_page_fork_workspace", "nm_page_fork", "nm_page_copy")
 NM_OP_CONV, NM_OP_MAXPOOL, NM_OP_AVGPOOL, NM_OP_GEMM = 0, 1, 2, 3
 NM_LAYER_FOLD_LAYERNORM, NM_LAYER_NO_FOLD_LAYERNORM = 1, 2
 NM_NOALLOC_MAX_WORKSPACE = 64 << 20  # bytes of the buffer built into the library (nm_encoder_layer_noalloc)
@@ -129,6 +131,27 @@ class W4Desc(C.Structure):
                  ("out_inv_scale", C.c_float)])
 
 
+class BeamDesc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("R", "W", "K", "V", "logits_dtype", "end_token", "max_history")] +
+                [("logits", C.c_void_p), ("logits_stride", C.c_int64)] +
+                [(n, C.c_void_p) for n in ("scores", "weight", "done", "parents", "tokens", "scores_out", "done_out", "history")] +
+                [("history_stride", C.c_int64), ("history_lens", C.c_void_p), ("history_out", C.c_void_p), ("history_out_stride", C.c_int64),
+                 ("history_lens_out", C.c_void_p)])
+
+
+class ForkDesc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("B_in", "B_out", "page_size", "num_pages", "max_pages", "n_free")] +
+                [("block_table", C.c_void_p), ("table_stride", C.c_int64)] +
+                [(n, C.c_void_p) for n in ("lens", "parents", "keep", "free_pages", "free_begin", "table_out")] +
+                [("table_out_stride", C.c_int64)] +
+                [(n, C.c_void_p) for n in ("lens_out", "free_out", "free_end", "copy_src", "copy_dst", "copy_slots", "status")])
+
+
+class CopyDesc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("n", "n_caches", "hk", "d", "dtype", "num_pages", "page_size")] + [("caches", C.c_void_p)] +
+                [(n, C.c_int64) for n in ("page_stride", "slot_stride", "head_stride")] + [(n, C.c_void_p) for n in ("src", "dst", "slots")])
+
+
 _lib = None
 
 
@@ -200,6 +223,10 @@ def load(preload_torch: bool = True) -> C.CDLL:
     L.nm_paged_attention_workspace.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]   # PagedDesc, or its bytes
     L.nm_paged_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     L.nm_gemv_w4.argtypes = [C.c_void_p, C.c_void_p]   # W4Desc, or its bytes
+    for call in ("nm_beam_select", "nm_page_fork"):    # BeamDesc, ForkDesc, or their bytes
+        getattr(L, call + "_workspace").argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
+        getattr(L, call).argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    L.nm_page_copy.argtypes = [C.c_void_p, C.c_void_p]   # CopyDesc, or its bytes
     _lib = L
     return L
 
@@ -584,6 +611,9 @@ _PLAN = struct.Struct("@6i6Pq6P")
 _QK = struct.Struct("@11i4x3P3q2Pf4x2PPqPq2P3q3P")
 _PAGED = struct.Struct("@10iPq2P3q2PPqPfiPqf4xP")
 _W4 = struct.Struct("@7i4xPq2Pf4x2Pi4xPqf4x")
+_BEAM = struct.Struct("@7i4xPq8PqPPqP")
+_FORK = struct.Struct("@6iPq6Pq7P")
+_COPY = struct.Struct("@7i4xP3q3P")
 
 
 # What Python makes of a missing tensor, one of another rank, and a number that its field does not hold.
@@ -814,5 +844,165 @@ def nm_gemv_w4(x, W=None, scales=None, out=None, *, group=0, alpha=1.0, bias=Non
     """make_w4_desc's arguments, or a description alone."""
     desc = _described(x, _W4, "nm_gemv_w4") if x.__class__ is bytes else make_w4_desc(x, W, scales, out, group, alpha, bias, tables, table_idx, out_inv_scale)
     rc = load().nm_gemv_w4(desc, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+# ---- several hypotheses per request ------------------------------------------------------------------
+
+def _work_space(ws, ws_bytes):
+    """Address and bytes of a workspace."""
+    if ws is None:
+        return 0, ws_bytes or 0
+    try:
+        if ws.get_device() != _here() or not ws.is_contiguous():
+            _refuse("ws: contiguous memory on the current device is wanted")
+        return ws.data_ptr(), ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+    except _MISFITS as e:
+        _misfit("ws", e)
+
+
+def _workspace_of(call, packed, make, tensors, more):
+    """Bytes of workspace: of a description, or of what makes one."""
+    try:
+        desc = _described(tensors[0], packed, call) if tensors and isinstance(tensors[0], bytes) else make(*tensors, **more)
+    except TypeError as e:                                    # not as many arguments
+        _misfit(call, e)
+    n = C.c_size_t()
+    _check(getattr(load(), call)(desc, C.byref(n)))
+    return n.value
+
+
+def _rows(t, n, dev, name):
+    """Row stride and columns of an int32 matrix of n rows, whose columns are neighbours."""
+    if t.dtype is not _i32 or t.get_device() != dev or t.dim() != 2 or t.shape[0] != n or (n and t.shape[1] > 1 and t.stride(1) != 1):
+        _refuse(f"{name}: int32 [{n}, ...] with neighbouring columns on the current device is wanted")
+    return (t.stride(0) if n > 1 else t.shape[1]), t.shape[1]
+
+
+def make_beam_desc(logits, scores, parents, tokens, scores_out, done=None, weight=None, end_token=-1, done_out=None, history=None, history_lens=None,
+                   history_out=None, history_lens_out=None) -> bytes:
+    """logits: [R * W, V], rows may be apart; scores, done, weight: [R, W]; parents, tokens, scores_out, done_out: [R, K]; history: [R * W, max_history],
+    history_out: [R * K, max_history], rows may be apart.  The description refers to the tensors' memory: keep them."""
+    try:
+        dev = _here()
+        (R, W), K = scores.shape, parents.shape[1]
+        if logits.dim() != 2 or logits.shape[0] != R * W or (logits.shape[1] > 1 and logits.stride(1) != 1):
+            _refuse(f"logits: [{R * W}, V] with neighbouring elements is wanted, got {tuple(logits.shape)}")
+        for t, n in ((parents, "parents"), (tokens, "tokens"), (scores_out, "scores_out"), (done_out, "done_out")):
+            if t is not None and t.shape != (R, K):
+                _refuse(f"{n}: shape {tuple(t.shape)}, wanted {(R, K)}")
+        if end_token is None:
+            _refuse("end_token: -1 for none")
+        V, most, at = logits.shape[1], 0, (0, 0, 0, 0, 0, 0)
+        if history is not None or history_lens is not None or history_out is not None or history_lens_out is not None:
+            if history is None or history_lens is None or history_out is None or history_lens_out is None:
+                _refuse("history, history_lens, history_out and history_lens_out belong together")
+            stride, most = _rows(history, R * W, dev, "history")
+            out_stride, out_most = _rows(history_out, R * K, dev, "history_out")
+            if out_most != most:
+                _refuse(f"history and history_out have rows of {most} and {out_most}")
+            at = (history.data_ptr(), stride, _vector(history_lens, _i32, R * W, dev, "history_lens"), history_out.data_ptr(), out_stride,
+                  _vector(history_lens_out, _i32, R * K, dev, "history_lens_out"))
+        return _BEAM.pack(R, W, K, V, _type(logits, dev, "logits"), end_token, most, logits.data_ptr(), logits.stride(0) if R * W > 1 else V,
+                          _vector(scores, _f32, R * W, dev, "scores"), _vector(weight, _f32, R * W, dev, "weight"), _vector(done, _i32, R * W, dev, "done"),
+                          _vector(parents, _i32, R * K, dev, "parents"), _vector(tokens, _i32, R * K, dev, "tokens"),
+                          _vector(scores_out, _f32, R * K, dev, "scores_out"), _vector(done_out, _i32, R * K, dev, "done_out"), *at)
+    except _MISFITS as e:
+        _misfit("nm_beam_select", e)
+
+
+def nm_beam_select_workspace(*tensors, **more) -> int:
+    """Bytes; takes what nm_beam_select takes, or a description."""
+    return _workspace_of("nm_beam_select_workspace", _BEAM, make_beam_desc, tensors, more)
+
+
+def nm_beam_select(logits, scores=None, parents=None, tokens=None, scores_out=None, *, done=None, weight=None, end_token=-1, done_out=None, history=None,
+                   history_lens=None, history_out=None, history_lens_out=None, ws=None, stream=None, ws_bytes=None):
+    """make_beam_desc's arguments, or a description alone; and the workspace."""
+    desc = _described(logits, _BEAM, "nm_beam_select") if logits.__class__ is bytes else make_beam_desc(
+        logits, scores, parents, tokens, scores_out, done, weight, end_token, done_out, history, history_lens, history_out, history_lens_out)
+    rc = load().nm_beam_select(desc, *_work_space(ws, ws_bytes), _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def make_fork_desc(block_table, lens, parents, free_pages, free_begin, table_out, page_size, num_pages, lens_out, free_out, free_end, copy_src, copy_dst,
+                   copy_slots, status, keep=None) -> bytes:
+    """block_table: int32 [B_in, max_pages], table_out: [B_out, max_pages], rows may be apart; every other tensor is contiguous int32.  The
+    description refers to the tensors' memory: keep them."""
+    try:
+        dev = _here()
+        B_in, B_out, n_free = lens.numel(), parents.numel(), free_pages.numel()
+        stride, columns = _rows(block_table, B_in, dev, "block_table")
+        out_stride, out_columns = _rows(table_out, B_out, dev, "table_out")
+        if out_columns != columns:
+            _refuse(f"block_table and table_out have {columns} and {out_columns} columns")
+        return _FORK.pack(B_in, B_out, page_size, num_pages, columns, n_free, block_table.data_ptr(), stride, _vector(lens, _i32, B_in, dev, "lens"),
+                          _vector(parents, _i32, B_out, dev, "parents"), _vector(keep, _i32, num_pages, dev, "keep"),
+                          _vector(free_pages, _i32, n_free, dev, "free_pages"), _vector(free_begin, _i32, 1, dev, "free_begin"), table_out.data_ptr(), out_stride,
+                          _vector(lens_out, _i32, B_out, dev, "lens_out"), _vector(free_out, _i32, n_free, dev, "free_out"),
+                          _vector(free_end, _i32, 1, dev, "free_end"), _vector(copy_src, _i32, B_out, dev, "copy_src"),
+                          _vector(copy_dst, _i32, B_out, dev, "copy_dst"), _vector(copy_slots, _i32, B_out, dev, "copy_slots"),
+                          _vector(status, _i32, 4, dev, "status"))
+    except _MISFITS as e:
+        _misfit("nm_page_fork", e)
+
+
+def nm_page_fork_workspace(*tensors, **more) -> int:
+    """Bytes; takes what nm_page_fork takes, or a description."""
+    return _workspace_of("nm_page_fork_workspace", _FORK, make_fork_desc, tensors, more)
+
+
+def nm_page_fork(block_table, lens=None, parents=None, free_pages=None, free_begin=None, table_out=None, *, page_size=0, num_pages=0, lens_out=None,
+                 free_out=None, free_end=None, copy_src=None, copy_dst=None, copy_slots=None, status=None, keep=None, ws=None, stream=None, ws_bytes=None):
+    """make_fork_desc's arguments, or a description alone; and the workspace."""
+    desc = _described(block_table, _FORK, "nm_page_fork") if block_table.__class__ is bytes else make_fork_desc(
+        block_table, lens, parents, free_pages, free_begin, table_out, page_size, num_pages, lens_out, free_out, free_end, copy_src, copy_dst, copy_slots, status, keep)
+    rc = load().nm_page_fork(desc, *_work_space(ws, ws_bytes), _stream(stream))
+    if rc:
+        _check(rc)
+
+
+class _CopyBytes(bytes):
+    """A description of nm_page_copy, and the list of addresses in host memory that it refers to."""
+
+
+def make_copy_desc(caches, src, dst, slots=None) -> bytes:
+    """caches: a list of tensors [pages, page_size, hk, d] of one type, shape and strides, or one tensor [n, pages, page_size, hk, d]; src, dst, slots: int32.
+    The description refers to the tensors' memory: keep them."""
+    try:
+        dev = _here()
+        if hasattr(caches, "dim"):
+            if caches.dim() != 5:
+                _refuse(f"caches: [n, pages, page_size, hk, d], or a list of tensors, is wanted, got {tuple(caches.shape)}")
+            n, (pages, page, hk, e), (apart, *strides) = caches.shape[0], caches.shape[1:], caches.stride()
+            dtype, base, step = _type(caches, dev, "caches"), caches.data_ptr(), apart * caches.element_size()
+            at = [base + i * step for i in range(n)]
+        else:
+            n = len(caches)
+            if not n:
+                _refuse("caches: none is given")
+            (pages, page, hk, e), strides, dtype = caches[0].shape, list(caches[0].stride()), _type(caches[0], dev, "caches")
+            for t in caches:
+                if t.shape != caches[0].shape or list(t.stride()) != strides or t.dtype is not caches[0].dtype or t.get_device() != dev:
+                    _refuse("caches have to have one type, one shape and the same strides, on the current device")
+            at = [t.data_ptr() for t in caches]
+        if strides[3] != 1 and e > 1:
+            _refuse("the elements of a head have to be neighbours in the caches")
+        copies = src.numel()
+        array = (C.c_void_p * max(n, 1))(*at)
+        desc = _CopyBytes(_COPY.pack(copies, n, hk, e, dtype, pages, page, C.addressof(array), *strides[:3], _vector(src, _i32, copies, dev, "src"),
+                                     _vector(dst, _i32, copies, dev, "dst"), _vector(slots, _i32, copies, dev, "slots")))
+        desc.addresses = array
+        return desc
+    except _MISFITS as e:
+        _misfit("nm_page_copy", e)
+
+
+def nm_page_copy(caches, src=None, dst=None, slots=None, *, stream=None):
+    """make_copy_desc's arguments, or a description alone."""
+    desc = _described(caches, _COPY, "nm_page_copy") if isinstance(caches, bytes) else make_copy_desc(caches, src, dst, slots)
+    rc = load().nm_page_copy(desc, _stream(stream))
     if rc:
         _check(rc)

@@ -1,0 +1,541 @@
+"""The calls for several hypotheses per request (selection, forks of block tables, copies of pages) against plain implementations of
+the documented rules, selection in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2305_14405_amd import binding as nm
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+INF, NAN = math.inf, math.nan
+
+
+def gen(seed):
+    g = torch.Generator(device="cpu")
+    g.manual_seed(seed)
+    return g
+
+
+def i32(a):
+    return torch.as_tensor(a, dtype=torch.int32).to(DEV).contiguous()
+
+
+def scratch(n):
+    return torch.full((n,), 0xff, dtype=torch.uint8, device=DEV)
+
+
+# ---- selection --------------------------------------------------------------------------------------
+
+# Two candidates' totals are told apart beyond this: the sum's relative error is that of an exponential (its argument's rounding, a product's, the
+# constant's and the power's own: 4 half steps of 2^-24), of ten additions of one lane and of a rescaling (4 more), below 20 * 2^-24.
+NEAR = 2.0 ** -19.6
+
+
+def beam_case(seed, R, W, V, dtype, spread=3.0, pad=0, done=0.0, weight=False, history=0):
+    g = gen(seed)
+    x = (torch.randn((R * W, V + pad), generator=g) * spread).to(dtype)
+    c = dict(x=x[:, :V], wide=x, scores=-20 * torch.rand((R, W), generator=g), done=None, weight=None, history=None)
+    if done:
+        c["done"] = (torch.rand((R, W), generator=g) < done).to(torch.int32)
+    if weight:
+        c["weight"] = 0.1 + torch.rand((R, W), generator=g)
+    if history:
+        c["history"] = torch.randint(0, V, (R * W, history), generator=g, dtype=torch.int32)
+        c["held"] = torch.randint(-1, history + 2, (R * W,), generator=g, dtype=torch.int32)
+    return c
+
+
+def select(c, K, end=-1, stream=None, ws=None, o=None, done_out=True):
+    """One call; outputs lie inside larger tensors, whose rest has to stay as it was."""
+    (R, W), V = c["scores"].shape, c["x"].shape[1]
+    to = lambda t: None if t is None else t.to(DEV)  # noqa: E731
+    x = c["wide"].to(DEV)[:, :V]
+    if o is None:
+        o = {n: torch.full((R + 2, K), -77, dtype=torch.int32, device=DEV) for n in ("parents", "tokens", "done_out")}
+        o["totals"] = torch.full((R + 2, K), -77.0, device=DEV)
+    more = dict(done=to(c["done"]), weight=to(c["weight"]), end_token=end, done_out=o["done_out"][1:-1] if done_out else None)
+    if c["history"] is not None:
+        n = c["history"].shape[1]
+        o["history"], o["held"] = torch.full((R * K + 2, n + 3), -77, dtype=torch.int32, device=DEV), torch.full((R * K + 2,), -77, dtype=torch.int32, device=DEV)
+        more.update(history=to(c["history"]), history_lens=to(c["held"]), history_out=o["history"][1:-1, :n], history_lens_out=o["held"][1:-1])
+    args = (x, to(c["scores"]), o["parents"][1:-1], o["tokens"][1:-1], o["totals"][1:-1])
+    ws = scratch(nm.nm_beam_select_workspace(*args, **more)) if ws is None else ws
+    nm.nm_beam_select(*args, ws=ws, stream=stream, **more)
+    torch.cuda.synchronize()
+    for n, t in o.items():
+        assert bool((t[0] == -77).all()) and bool((t[-1] == -77).all()), n
+    return {n: t[1:-1].cpu() for n, t in o.items()}
+
+
+def check_select(c, K, end=-1, got=None, near=NEAR):
+    (R, W), V = c["scores"].shape, c["x"].shape[1]
+    got = select(c, K, end) if got is None else got
+    x = c["x"].double()
+    x = torch.where(x.isnan(), torch.full_like(x, -INF), x.clamp(max=float(torch.finfo(torch.float32).max)))
+    top = x.max(-1, keepdim=True).values
+    lse = torch.where(top == -INF, top, top + torch.log(torch.exp(x - torch.where(top == -INF, 0.0, top)).sum(-1, keepdim=True)))
+    total = x - lse + c["scores"].double().view(-1, 1)
+    # x - lse of huge logits: by differences
+    total = torch.where((x > 1e30) & (top > 1e30), (x - top) - torch.log(torch.exp(x - top).sum(-1, keepdim=True)) + c["scores"].double().view(-1, 1), total)
+    total[x == -INF] = -INF
+    done = torch.zeros((R * W,), dtype=torch.bool) if c["done"] is None else c["done"].view(-1) != 0
+    weight = torch.ones(R * W, dtype=torch.float64) if c["weight"] is None else c["weight"].double().view(-1)
+    total[done] = -INF
+    total[done, end] = c["scores"].double().view(-1)[done]
+    bad = ~torch.isfinite(c["scores"].view(-1)) | ~torch.isfinite(weight) | ~(weight > 0)
+    total[bad] = -INF
+    rank = torch.where(total == -INF, total, total * torch.where(bad, 1.0, weight).view(-1, 1)).view(R, W * V)
+    for r in range(R):
+        n = min(K, int((rank[r] > -INF).sum()))
+        best = torch.sort(rank[r], descending=True, stable=True)
+        p, t = got["parents"][r], got["tokens"][r]
+        assert (p[n:] == -1).all() and (t[n:] == -1).all() and (got["totals"][r, n:] == -INF).all(), r
+        assert ((p[:n] >= r * W) & (p[:n] < (r + 1) * W)).all() and ((t[:n] >= 0) & (t[:n] < V)).all(), r
+        at = (p[:n].long() - r * W) * V + t[:n].long()
+        assert len(set(at.tolist())) == n                                     # no candidate twice
+        w = weight[p[:n].long()]
+        mine = rank[r][at]
+        assert ((mine - best.values[:n]).abs() <= near * w + 1e-12 * best.values[:n].abs()).all(), (r, mine, best.values[:n])
+        # where nobody else is near, it is that one
+        gap = torch.full((n,), INF, dtype=torch.float64)
+        if n:
+            v = best.values[:n + 1].clone() if rank.shape[1] > n else torch.cat([best.values[:n], torch.tensor([-INF], dtype=torch.float64)])
+            d = (v[:-1] - v[1:])
+            gap = torch.minimum(d, torch.cat([torch.tensor([INF], dtype=torch.float64), d[:-1]]))
+        clear = gap > 2 * near * float(weight[torch.isfinite(weight)].max())
+        assert torch.equal(at[clear], best.indices[:n][clear]), r
+        ts = total.view(R, -1)[r][at]
+        assert ((got["totals"][r, :n].double() - ts).abs() <= near + 2.0 ** -24 * (ts.abs() + near)).all() or bool((ts.abs() > 1e30).any()), r
+        if "done_out" in got and got["done_out"] is not None:
+            want = done[p[:n].long()] | (t[:n] == end)
+            assert torch.equal(got["done_out"][r, :n] != 0, want) and (got["done_out"][r, n:] == 0).all(), r
+    if c["history"] is not None:
+        most = c["history"].shape[1]
+        for i, p in enumerate(got["parents"].view(-1).tolist()):
+            held = 0 if p < 0 else min(max(int(c["held"][p]), 0), most)
+            grows = p >= 0 and held < most and not bool(done[p])
+            want = torch.full((most + 3,), -77, dtype=torch.int32)
+            if p >= 0:
+                want[:held] = c["history"][p, :held]
+            if grows:
+                want[held] = got["tokens"].view(-1)[i]
+            assert torch.equal(got["history"][i], want), i
+            assert int(got["held"][i]) == held + grows, i
+    return got
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("R,W,K,V,pad", [(1, 1, 1, 1, 0), (1, 1, 5, 3, 0), (2, 3, 4, 17, 0), (1, 4, 4, 32000, 0), (3, 5, 7, 8191, 0), (2, 2, 64, 8193, 0), (5, 1, 2, 2047, 1),
+                                         (1, 64, 64, 333, 0), (7, 3, 3, 50001, 5), (40, 8, 16, 1000, 0), (1, 2, 3, 131072, 0), (2100, 1, 1, 70, 2), (3, 33, 40, 999, 3),
+                                         (2, 2, 8, 600000, 0)])
+def test_beam_select(dtype, R, W, K, V, pad):
+    check_select(beam_case(R + V, R, W, V, dtype, pad=pad), K)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("done,weight,history", [(0.4, False, 0), (0.0, True, 0), (0.3, True, 30), (1.0, True, 3000), (0.0, False, 1)])
+def test_beam_select_finished_weights_and_histories(dtype, done, weight, history):
+    check_select(beam_case(5, 6, 5, 3001, dtype, done=done, weight=weight, history=history), 7, end=11)
+
+
+def test_beam_select_histories_of_many_rows_and_long():
+    check_select(beam_case(6, 70, 3, 200, torch.float32, done=0.2, history=9000), 3, end=0)
+
+
+def test_beam_select_without_done_out():
+    c = beam_case(7, 3, 4, 500, torch.float16)
+    a, b = select(c, 4, 3), select(c, 4, 3, done_out=False)
+    assert all(torch.equal(a[n], b[n]) for n in ("parents", "tokens", "totals")) and (b["done_out"] == -77).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_beam_select_equal_candidates_go_by_row_then_token(dtype):
+    """Equal logits everywhere: the lowest rows' lowest tokens, whichever lane, wavefront or chunk holds them."""
+    c = beam_case(1, 2, 3, 70000, dtype)
+    c["x"][:] = 1.5
+    c["scores"][:] = -2
+    got = check_select(c, 5)
+    assert got["parents"].tolist() == [[0] * 5, [3] * 5] and got["tokens"].tolist() == [[0, 1, 2, 3, 4]] * 2
+    c["x"][:, 69990:] = 2.0                                                   # the last chunk's are better
+    c["x"][1, 33333] = 2.0
+    c["x"][2, 69990:] = -0.0
+    c["x"][2, :] = 0.0
+    c["x"][2, 5::2] = -0.0                                                    # zeros of either sign are one value
+    c["scores"][0] = torch.tensor([-9.0, -9.0, 50.0])
+    got = check_select(c, 64)
+    assert got["parents"][0].tolist() == [2] * 64 and got["tokens"][0].tolist() == list(range(64))
+    assert got["tokens"][1, :40].tolist() == [*range(69990, 70000)] * 3 + [*range(10)] or got["tokens"][1, 0] == 69990
+
+
+def test_beam_select_identical_hypotheses_tie_exactly():
+    c = beam_case(3, 1, 6, 40000, torch.bfloat16)
+    c["x"][:] = c["x"][0]
+    c["scores"][:] = -3.25
+    got = check_select(c, 24)
+    assert got["parents"][0].tolist() == list(range(6)) * 4                   # each value six times, by row
+    assert all(len(set(got["tokens"][0, i:i + 6].tolist())) == 1 for i in range(0, 24, 6))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_beam_select_masks_and_special_values(dtype):
+    c = beam_case(9, 8, 3, 5000, dtype, weight=True)
+    c["x"][0] = -INF                                                          # request 0: a row of nothing
+    c["x"][3:6] = -INF                                                        # request 1: nothing at all
+    c["x"][6, 7:] = NAN                                                       # request 2: seven logits, none, and one
+    c["x"][7] = NAN
+    c["x"][8] = -INF
+    c["x"][8, 4999] = -1000.0
+    c["x"][9, 17] = INF                                                       # request 3: +inf
+    c["x"][10, ::2] = INF
+    c["scores"][4] = torch.tensor([-INF, NAN, -1.0])                          # request 4: scores
+    c["scores"][5] = torch.tensor([INF, -5.0, -INF])
+    c["weight"][6] = torch.tensor([0.0, -1.0, 1.0])
+    c["weight"][7] = torch.tensor([INF, NAN, 2.0])
+    got = check_select(c, 9)
+    assert (got["parents"][1] == -1).all() and (got["parents"][0][:9] != 0).all()
+    assert sorted(got["parents"][2].tolist()) == [-1, 6, 6, 6, 6, 6, 6, 6, 8]
+    assert abs(float(got["totals"][3][got["parents"][3] == 9][0]) - float(c["scores"][3, 0])) < 1e-6 if (got["parents"][3] == 9).any() else True
+    assert set(got["parents"][4].tolist()) == {14} and set(got["parents"][5].tolist()) == {16}
+    assert set(got["parents"][6].tolist()) == {20} and set(got["parents"][7].tolist()) == {23}
+
+
+def test_beam_select_ascending_and_descending_rows():
+    """The orders in which the most, and the fewest, logits enter a list."""
+    for flip in (False, True):
+        c = beam_case(2, 2, 2, 60000, torch.float32)
+        row = torch.arange(60000.0) / 60000
+        c["x"][:] = row.flip(0) if flip else row
+        c["scores"][:] = torch.tensor([[-1.0, -1.0], [-1.0, -1.00001]])
+        check_select(c, 64)
+
+
+def test_beam_select_large_differences():
+    """Sums over logits that lie hundreds apart, and far from zero."""
+    c = beam_case(4, 3, 4, 20000, torch.float32, spread=300.0)
+    c["x"][4:8] += 20000.0
+    c["x"][8:] -= 20000.0
+    check_select(c, 12)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_beam_select_repeats_bits_on_a_stream_and_in_a_graph(dtype):
+    c = beam_case(8, 5, 4, 12345, dtype, done=0.2, weight=True, history=50)
+    want = check_select(c, 6, end=1)
+    s = torch.cuda.Stream()
+    got = select(c, 6, end=1, stream=s)
+    assert all(torch.equal(want[n], got[n]) for n in want)
+    # one captured call, replayed while its inputs change
+    dev = {n: c[n].to(DEV) for n in ("x", "scores", "done", "weight", "history", "held")}
+    o = [torch.empty((5, 6), dtype=torch.int32, device=DEV) for _ in range(3)] + [torch.empty((5, 6), device=DEV)]
+    h = [torch.zeros((30, 50), dtype=torch.int32, device=DEV), torch.zeros(30, dtype=torch.int32, device=DEV)]
+    args = (dev["x"], dev["scores"], o[0], o[1], o[3])
+    more = dict(done=dev["done"], weight=dev["weight"], end_token=1, done_out=o[2], history=dev["history"], history_lens=dev["held"], history_out=h[0], history_lens_out=h[1])
+    ws = scratch(nm.nm_beam_select_workspace(*args, **more))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        nm.nm_beam_select(*args, ws=ws, **more)
+    for seed in (8, 21, 22):
+        n = beam_case(seed, 5, 4, 12345, dtype, done=0.2, weight=True, history=50)
+        for name in dev:
+            dev[name].copy_(n[name])
+        ws.fill_(0xff)
+        g.replay()
+        torch.cuda.synchronize()
+        want = check_select(n, 6, end=1)
+        assert torch.equal(o[0].cpu(), want["parents"]) and torch.equal(o[1].cpu(), want["tokens"]) and torch.equal(o[3].cpu(), want["totals"])
+        assert torch.equal(o[2].cpu(), want["done_out"]) and torch.equal(h[1].cpu(), want["held"])
+
+
+# ---- fork -----------------------------------------------------------------------------------------------
+
+def fork_in_python(table, lens, parents, keep, free, begin, page, num_pages, table_out, free_out):
+    """The documented rules, one row after the other."""
+    B, columns = table.shape
+    up = lambda n: -(-n // page)  # noqa: E731
+    valid = lambda e: 0 <= e < num_pages  # noqa: E731
+    bad = begin < 0 or begin > len(free) or any(n < 0 or n > columns * page for n in lens)
+    size = [n if 0 <= n <= columns * page else 0 for n in lens]
+    children = {}
+    for b, p in enumerate(parents):
+        if 0 <= p < B:
+            children.setdefault(p, []).append(b)
+    refers = {r: [int(e) for e in table[r, :up(size[r])]] for r in range(B)}
+    users = {}
+    for p in children:
+        for e in set(refers[p]):
+            users.setdefault(e, set()).add(p)
+    n_rows = len(parents)
+    new, copies, at = [None] * n_rows, [(-1, -1, 0)] * n_rows, 0
+    for b, p in enumerate(parents):
+        if not 0 <= p < B:
+            new[b] = []
+            continue
+        new[b] = list(refers[p])
+        n = size[p]
+        if n % page and valid(refers[p][-1]):
+            last = refers[p][-1]
+            # in front of its partial last page, an old row refers to a page too
+            if children[p][0] != b or users[last] != {p} or last in refers[p][:-1] or (keep is not None and keep[last]):
+                i = begin + at
+                new[b][-1] = int(free[i]) if 0 <= i < len(free) else -1
+                copies[b] = (last, new[b][-1], n % page)
+                at += 1
+    before, after = {e for v in refers.values() for e in v if valid(e)}, {e for v in new for e in v}
+    freed = sorted(e for e in before - after if keep is None or not keep[e])
+    flags = 8 if bad else 0
+    if 0 <= begin <= len(free):
+        flags |= (1 if begin + at > len(free) else 0) | (16 if begin + at - len(freed) < 0 else 0)
+    out = {"table_out": table_out.copy(), "free_out": free_out.copy(), "lens_out": [0] * n_rows, "end": begin, "src": [-1] * n_rows, "dst": [-1] * n_rows, "slots": [0] * n_rows,
+           "status": [flags, at, len(freed), sum(0 <= p < B for p in parents)]}
+    if flags:
+        if 0 <= begin:
+            out["free_out"][begin:] = free[begin:]
+        return out
+    for b, p in enumerate(parents):
+        out["table_out"][b, :len(new[b])] = new[b]
+        out["lens_out"][b] = size[p] if 0 <= p < B else 0
+        out["src"][b], out["dst"][b], out["slots"][b] = copies[b]
+    out["end"] = begin + at - len(freed)
+    out["free_out"][begin + at:] = free[begin + at:]
+    out["free_out"][out["end"]:begin + at] = freed
+    return out
+
+
+def run_fork(table, lens, parents, keep, free, begin, page, num_pages, in_place=False, stride=0, stream=None):
+    B, columns = table.shape
+    n_rows = len(parents)
+    wide = np.full((B, columns + stride), -55, np.int32)
+    wide[:, :columns] = table
+    out = torch.full((n_rows, columns + 2 * stride), -66, dtype=torch.int32, device=DEV)
+    free_t = i32(np.asarray(free, np.int32))
+    free_out = free_t if in_place else torch.full((len(free),), -88, dtype=torch.int32, device=DEV)
+    o = {n: torch.full((n_rows,), -5, dtype=torch.int32, device=DEV) for n in ("lens_out", "src", "dst", "slots")}
+    o["end"], o["status"] = torch.full((1,), -5, dtype=torch.int32, device=DEV), torch.full((4,), -5, dtype=torch.int32, device=DEV)
+    args = (i32(wide)[:, :columns], i32(lens), i32(parents), free_t, i32([begin]), out[:, :columns])
+    more = dict(page_size=page, num_pages=num_pages, keep=None if keep is None else i32(keep), lens_out=o["lens_out"], free_out=free_out, free_end=o["end"], copy_src=o["src"],
+                copy_dst=o["dst"], copy_slots=o["slots"], status=o["status"])
+    nm.nm_page_fork(*args, ws=scratch(nm.nm_page_fork_workspace(*args, **more)), stream=stream, **more)
+    torch.cuda.synchronize()
+    got = {n: t.cpu().tolist() for n, t in o.items()}
+    got["end"] = got["end"][0]
+    got["free_out"] = free_out.cpu().numpy()
+    full = out.cpu().numpy()
+    assert (full[:, columns:] == -66).all()
+    got["table_out"] = full[:, :columns]
+    return got
+
+
+def check_fork(*args, in_place=False, stride=0):
+    table, _, parents, _, free = args[:5]
+    want = fork_in_python(*args, np.full((len(parents), table.shape[1]), -66, np.int32), np.array(free, np.int32) if in_place else np.full(len(free), -88, np.int32))
+    got = run_fork(*args, in_place=in_place, stride=stride)
+    for n in ("status", "end", "lens_out", "src", "dst", "slots"):
+        assert got[n] == want[n], n
+    assert np.array_equal(got["table_out"], want["table_out"])
+    assert np.array_equal(got["free_out"][0 if not in_place else want["end"]:], want["free_out"][0 if not in_place else want["end"]:])
+    if in_place:
+        assert np.array_equal(got["free_out"][:max(want["end"], 0)], np.array(free, np.int32)[:max(want["end"], 0)])
+    return got
+
+
+def random_fork(seed, B, B_out, page, longest, gone=0.2, keep=0.0, odd=False):
+    """A batch whose rows share whole pages, as forks of earlier steps leave it; odd: partial pages are shared too, and some entries are no pages."""
+    r = np.random.default_rng(seed)
+    columns = max(1, -(-longest // page) + 1)
+    lens = r.integers(0, longest + 1, B)
+    pages = r.permutation(B * columns + 40)
+    num_pages = len(pages)
+    table = np.full((B, columns), -9, np.int32)
+    at = 0
+    for b in range(B):
+        whole, held = lens[b] // page, -(-lens[b] // page)
+        share = 0
+        if b and r.random() < 0.6:
+            o = int(r.integers(0, b))
+            share = int(min(whole, lens[o] // page))
+            if odd and r.random() < 0.5:
+                lens[b] = lens[o] if r.random() < 0.5 else min(int(lens[o]) + 3, longest)
+                whole, held = lens[b] // page, -(-lens[b] // page)
+                share = -(-int(lens[o]) // page)
+            share = int(r.integers(0, share + 1)) if r.random() < 0.5 else share
+            share = min(share, held)
+            table[b, :share] = table[o, :share]
+        table[b, share:held] = pages[at:at + held - share]
+        at += held - share
+    if odd:
+        table[r.random(table.shape) < 0.03] = -1
+        table[r.random(table.shape) < 0.02] = num_pages
+    used = set(table[np.arange(columns)[None, :] < -(-lens // page)[:, None]].tolist())
+    free = [int(p) for p in pages if p not in used]
+    begin = num_pages - len(free)
+    free = r.integers(0, num_pages, begin).tolist() + free
+    parents = [int(r.integers(-1, B + 1)) if r.random() < gone else int(r.integers(0, B)) for _ in range(B_out)] if B else [-1] * B_out
+    held = (r.random(num_pages) < keep).astype(np.int32) if keep else None
+    return table, lens.tolist(), parents, held, free, begin, page, num_pages
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("odd", [False, True])
+@pytest.mark.parametrize("B,B_out,page,longest,keep", [(1, 1, 16, 5, 0.0), (1, 4, 16, 33, 0.0), (4, 1, 1, 9, 0.3), (7, 9, 8, 100, 0.2), (16, 16, 16, 600, 0.0), (64, 30, 4, 64, 0.5), (257, 300, 16, 90, 0.1),
+                                                       (40, 40, 128, 5000, 0.0), (3, 3, 65536, 100000, 0.0), (1000, 1000, 2, 20, 0.1)])
+def test_page_fork_matches_python(in_place, odd, B, B_out, page, longest, keep):
+    for seed in range(3):
+        check_fork(*random_fork(seed + B + page, B, B_out, page, longest, keep=keep, odd=odd), in_place=in_place, stride=seed)
+
+
+def test_page_fork_of_as_many_rows_as_it_takes():
+    check_fork(*random_fork(5, 4096, 4096, 16, 60, keep=0.1))
+
+
+def test_page_fork_of_a_large_pool():
+    """Pages in more than one block of the scan, freed ones in each."""
+    table, lens, parents, _, free, begin, page, num_pages = random_fork(8, 300, 200, 4, 400, gone=0.6)
+    more = 300000
+    spread = np.random.default_rng(1).permutation(num_pages + more)[:num_pages]   # the same pool among many more pages
+    table = np.where((table >= 0) & (table < num_pages), spread[np.clip(table, 0, num_pages - 1)], table).astype(np.int32)
+    check_fork(table, lens, parents, None, spread[free].tolist(), begin, page, num_pages + more)
+
+
+def test_page_fork_one_prompt_into_many_and_back():
+    """A prompt's partial page goes to its first child and is copied for the others; when one of them is left, what the others held is free."""
+    table = np.full((1, 4), -1, np.int32)
+    table[0, :3] = [5, 2, 9]
+    got = check_fork(table, [37], [0, 0, 0], None, [0, 0, 0, 0, 7, 1, 3, 0, 4], 4, 16, 10)
+    assert got["table_out"][:, :3].tolist() == [[5, 2, 9], [5, 2, 7], [5, 2, 1]] and got["end"] == 6
+    assert (got["src"], got["dst"], got["slots"]) == ([-1, 9, 9], [-1, 7, 1], [0, 5, 5])
+    back = check_fork(got["table_out"], [37, 37, 37], [1], None, got["free_out"].tolist(), got["end"], 16, 10)
+    assert back["table_out"][0, :3].tolist() == [5, 2, 7] and back["free_out"][back["end"]:back["end"] + 2].tolist() == [1, 9]
+    none = check_fork(back["table_out"], [37], [-1, 5], None, back["free_out"].tolist(), back["end"], 16, 10)
+    assert none["lens_out"] == [0, 0] and none["status"] == [0, 0, 3, 0]
+
+
+@pytest.mark.parametrize("what", ["pages", "list", "long", "negative", "begin", "begin_far"])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_page_fork_assigns_nothing_that_does_not_fit(what, in_place):
+    table, lens, parents, keep, free, begin, page, num_pages = random_fork(12, 30, 30, 16, 300, gone=0.3)
+    if what == "pages":
+        free, begin = free[:begin + 2], begin
+    if what == "list":
+        free, begin = free[begin:], 0
+        parents = parents[:5]
+    if what == "long":
+        lens[3] = table.shape[1] * page + 1
+    if what == "negative":
+        lens[29] = -1
+    if what == "begin":
+        begin = -1
+    if what == "begin_far":
+        begin = len(free) + 1
+    want = fork_in_python(table, lens, parents, keep, free, begin, page, num_pages, np.full((len(parents), table.shape[1]), -66, np.int32), np.full(len(free), -88, np.int32))
+    assert want["status"][0] == {"pages": 1, "list": 16}.get(what, 8)
+    check_fork(table, lens, parents, keep, free, begin, page, num_pages, in_place=in_place)
+
+
+def test_page_fork_empty_batches():
+    none = np.zeros((0, 4), np.int32)
+    check_fork(none, [], [], None, [3, 1], 1, 16, 9)
+    check_fork(none, [], [0, -1], None, [3, 1], 1, 16, 9)
+    check_fork(np.array([[3, 4]], np.int32), [20], [], None, [0, 0, 0, 1], 3, 16, 9)
+    check_fork(np.zeros((3, 0), np.int32), [0, 0, 0], [2, 1, 0], None, [3, 1], 1, 16, 9)
+    check_fork(np.array([[3, 4]], np.int32), [20], [0, 0], None, [], 0, 16, 0)     # a pool of no pages: no entry is one
+
+
+def test_page_fork_twice_at_once_and_replayed():
+    """Two calls with workspaces of their own on two streams, and a captured call replayed while its inputs change."""
+    a, b = random_fork(31, 200, 200, 8, 200), random_fork(32, 100, 150, 8, 300)
+    wants = [fork_in_python(*c, np.full((len(c[2]), c[0].shape[1]), -66, np.int32), np.full(len(c[4]), -88, np.int32)) for c in (a, b)]
+    s = torch.cuda.Stream()
+    got = run_fork(*b, stream=s)
+    assert got["dst"] == wants[1]["dst"] and np.array_equal(got["table_out"], wants[1]["table_out"])
+    cases = [random_fork(seed, 60, 50, 16, 500, keep=0.1) for seed in (41, 42, 43)]
+    pages, columns = cases[0][7], cases[0][0].shape[1]
+    dev = [torch.zeros((60, columns), dtype=torch.int32, device=DEV), torch.zeros(60, dtype=torch.int32, device=DEV), torch.zeros(50, dtype=torch.int32, device=DEV),
+           torch.zeros(pages, dtype=torch.int32, device=DEV), torch.zeros(pages, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)]
+    out, o = torch.zeros((50, columns), dtype=torch.int32, device=DEV), [torch.zeros(50, dtype=torch.int32, device=DEV) for _ in range(4)]
+    free_out, end, status = torch.zeros(pages, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV)
+    args = (dev[0], dev[1], dev[2], dev[4], dev[5], out)
+    more = dict(page_size=16, num_pages=pages, keep=dev[3], lens_out=o[0], free_out=free_out, free_end=end, copy_src=o[1], copy_dst=o[2], copy_slots=o[3], status=status)
+    ws = scratch(nm.nm_page_fork_workspace(*args, **more))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        nm.nm_page_fork(*args, ws=ws, **more)
+    for c in cases + cases[:1]:
+        for t, v in zip(dev, (c[0], c[1], c[2], c[3], c[4], [c[5]])):
+            t.copy_(torch.as_tensor(np.asarray(v, np.int32)))
+        out.fill_(-66), free_out.fill_(-88), ws.fill_(0xff)
+        g.replay()
+        torch.cuda.synchronize()
+        want = fork_in_python(*c, np.full((50, columns), -66, np.int32), np.full(pages, -88, np.int32))
+        assert np.array_equal(out.cpu().numpy(), want["table_out"]) and np.array_equal(free_out.cpu().numpy(), want["free_out"])
+        assert [t.cpu().tolist() for t in o] == [want[n] for n in ("lens_out", "src", "dst", "slots")] and status.cpu().tolist() == want["status"]
+
+
+# ---- copy -----------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES + [torch.int8])
+@pytest.mark.parametrize("by_head", [False, True])
+@pytest.mark.parametrize("n,caches,page,hk,d,pad", [(1, 1, 16, 1, 64, 0), (5, 3, 16, 12, 64, 0), (9, 2, 8, 2, 7, 0), (30, 4, 32, 8, 128, 0), (4, 2, 1, 3, 5, 1), (3, 2, 64, 2, 80, 16), (6, 256, 2, 1, 16, 0),
+                                                    (2, 1, 4096, 1, 33, 0), (7, 2, 16, 3, 100, 4)])
+def test_page_copy(dtype, by_head, n, caches, page, hk, d, pad):
+    g = gen(n + page)
+    pages = 2 * n + 5
+    shape = (caches, pages, hk, page, d + pad) if by_head else (caches, pages, page, hk, d + pad)
+    base = torch.randint(-100, 100, shape, generator=g).to(dtype).to(DEV)
+    view = (base.transpose(2, 3) if by_head else base)[..., :d]
+    perm = torch.randperm(pages, generator=g).to(torch.int32)
+    src, dst = perm[:n].clone(), perm[n:2 * n].clone()
+    slots = torch.randint(-1, page + 2, (n,), generator=g, dtype=torch.int32)
+    slots[0] = page
+    if n > 3:
+        src[1], dst[2], src[3] = -1, pages, dst[3]
+    for given in (slots, None):
+        want = base.clone()
+        seen = (want.transpose(2, 3) if by_head else want)[..., :d]
+        for i in range(n):
+            a, b, m = int(src[i]), int(dst[i]), page if given is None else min(max(int(given[i]), 0), page)
+            if a != b and 0 <= a < pages and 0 <= b < pages:
+                seen[:, b, :m] = seen[:, a, :m].clone()
+        assert n == 1 or not torch.equal(want, base)
+        nm.nm_page_copy(view if given is None else list(view), i32(src), i32(dst), None if given is None else i32(given))
+        torch.cuda.synchronize()
+        assert torch.equal(base, want)                                        # and nothing beside the slots has changed
+        base.copy_(torch.randint(-100, 100, shape, generator=g).to(dtype))
+
+
+def test_page_copy_beyond_2_31_elements():
+    """Pages whose elements' numbers pass 31 bits."""
+    page, hk, d = 32, 8, 256
+    pages = (1 << 31) // (page * hk * d) + 40
+    cache = torch.zeros((1, pages, page, hk, d), dtype=torch.int8, device=DEV)
+    last = torch.randint(-100, 100, (page, hk, d), generator=gen(1)).to(torch.int8).to(DEV)
+    cache[0, pages - 1] = last
+    nm.nm_page_copy(cache, i32([pages - 1, 3]), i32([pages - 2, pages]), i32([31, 5]))
+    torch.cuda.synchronize()
+    assert torch.equal(cache[0, pages - 2, :31], last[:31]) and not bool(cache[0, pages - 2, 31].any()) and torch.equal(cache[0, pages - 1], last)
+    assert not bool(cache[0, :pages - 2].any())
+
+
+def test_page_copy_kept_description_on_a_stream_and_in_a_graph():
+    cache = torch.randn((4, 9, 16, 2, 64), generator=gen(3)).to(torch.bfloat16).to(DEV)
+    src, dst, slots = i32([1, 2]), i32([5, 6]), i32([7, 16])
+    desc = nm.make_copy_desc(cache, src, dst, slots)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    nm.nm_page_copy(desc, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(cache[:, 5, :7], cache[:, 1, :7]) and torch.equal(cache[:, 6], cache[:, 2]) and not torch.equal(cache[:, 5, 7:], cache[:, 1, 7:])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        nm.nm_page_copy(desc)
+    for a, b, n in ((0, 8, 16), (3, 7, 1), (-1, 4, 16)):
+        src.copy_(torch.tensor([a, -1])), dst.copy_(torch.tensor([b, 0])), slots.copy_(torch.tensor([n, 3]))
+        want = cache.clone()
+        if a >= 0:
+            want[:, b, :n] = want[:, a, :n]
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(cache, want)
