@@ -647,7 +647,7 @@ int32_t nm_gemv_w4(const nm_w4_desc* desc, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Several hypotheses per request over the paged cache: a row of the batch is a hypothesis, and the rows of a request share the pages of
- * what they have in common.  One step: nm_page_plan (one new token per row), the model with nm_qk_norm_rope and nm_paged_attention,
+ * what they have in common.  One step: nm_page_plan (one new token per row), the model with nm_qk_norm_rope and nm_shared_attention,
  * nm_beam_select over its logits, nm_page_fork, and nm_page_copy of the pages that it names, before pages are taken again.  As above, a step's
  * numbers are device memory, nothing is allocated, the host does not wait, every call can be captured, and the same call gives the same bits.
  * Workspaces: 256-byte aligned, contents are scratch, calls that overlap in time need one each.
@@ -766,6 +766,26 @@ typedef struct {
 } nm_copy_desc;
 
 int32_t nm_page_copy(const nm_copy_desc* desc, void* stream);
+
+/*
+ * nm_shared_attention: nm_paged_attention where groups of rows share a prefix, which is read once for all of a group's rows.  Group g is the rows
+ * group_start[g] .. group_start[g + 1] - 1, and the keys and values of the first shared[g] positions are the same for all of its rows (as nm_page_fork leaves
+ * them; a shared end inside a page is possible).  Which of the rows' entries they are read through is not said.
+ * A row shorter than its group's shared[g] takes no part in that and is computed by itself, as is a row of no group.  shared[g] < 1: nothing is shared.
+ * If group_start does not ascend, or leaves [0, B], no row is in a group.
+ * desc->p: as for nm_paged_attention, its outputs and limits likewise, but window is 0 (rows of a window share little: nm_paged_attention).  group_start: device
+ * int32 [G + 1]; shared: device int32 [G].
+ * Limits besides: B <= NM_PLAN_MAX_REQUESTS, G <= NM_PLAN_MAX_REQUESTS.
+ */
+typedef struct {
+    nm_paged_desc p;
+    int32_t G;
+    const int32_t* group_start;
+    const int32_t* shared;
+} nm_shared_desc;
+
+int32_t nm_shared_attention_workspace(const nm_shared_desc* desc, size_t* bytes);
+int32_t nm_shared_attention(const nm_shared_desc* desc, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

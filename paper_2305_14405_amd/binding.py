@@ -33,7 +33,8 @@ EXPORTS = ("nm_last_error", "nm_version", "nm_table_build_host", "nm_build_table
            "nm_encoder_stack_workspace", "nm_encoder_stack", "nm_conv2d_workspace", "nm_conv2d_pwl",
            "nm_maxpool_i8", "nm_avgpool_i8", "nm_cnn_workspace", "nm_cnn_run",
            "nm_page_plan", "nm_qk_norm_rope", "nm_paged_attention_workspace", "nm_paged_attention",
-           "nm_gemv_w4", "nm_beam_select_workspace", "nm_beam_select", "nm_page_fork_workspace", "nm_page_fork", "nm_page_copy")
+           "nm_gemv_w4", "nm_beam_select_workspace", "nm_beam_select", "nm_page_fork_workspace", "nm_page_fork", "nm_page_copy",
+           "nm_shared_attention_workspace", "nm_shared_attention")
 NM_OP_CONV, NM_OP_MAXPOOL, NM_OP_AVGPOOL, NM_OP_GEMM = 0, 1, 2, 3
 NM_LAYER_FOLD_LAYERNORM, NM_LAYER_NO_FOLD_LAYERNORM = 1, 2
 NM_NOALLOC_MAX_WORKSPACE = 64 << 20  # bytes of the buffer built into the library (nm_encoder_layer_noalloc)
@@ -147,6 +148,10 @@ class ForkDesc(C.Structure):
                 [(n, C.c_void_p) for n in ("lens_out", "free_out", "free_end", "copy_src", "copy_dst", "copy_slots", "status")])
 
 
+class SharedDesc(C.Structure):
+    _fields_ = [("p", PagedDesc), ("G", C.c_int32), ("group_start", C.c_void_p), ("shared", C.c_void_p)]
+
+
 class CopyDesc(C.Structure):
     _fields_ = ([(n, C.c_int32) for n in ("n", "n_caches", "hk", "d", "dtype", "num_pages", "page_size")] + [("caches", C.c_void_p)] +
                 [(n, C.c_int64) for n in ("page_stride", "slot_stride", "head_stride")] + [(n, C.c_void_p) for n in ("src", "dst", "slots")])
@@ -223,7 +228,7 @@ def load(preload_torch: bool = True) -> C.CDLL:
     L.nm_paged_attention_workspace.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]   # PagedDesc, or its bytes
     L.nm_paged_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     L.nm_gemv_w4.argtypes = [C.c_void_p, C.c_void_p]   # W4Desc, or its bytes
-    for call in ("nm_beam_select", "nm_page_fork"):    # BeamDesc, ForkDesc, or their bytes
+    for call in ("nm_beam_select", "nm_page_fork", "nm_shared_attention"):   # BeamDesc, ForkDesc, SharedDesc, or their bytes
         getattr(L, call + "_workspace").argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
         getattr(L, call).argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     L.nm_page_copy.argtypes = [C.c_void_p, C.c_void_p]   # CopyDesc, or its bytes
@@ -614,6 +619,8 @@ _W4 = struct.Struct("@7i4xPq2Pf4x2Pi4xPqf4x")
 _BEAM = struct.Struct("@7i4xPq8PqPPqP")
 _FORK = struct.Struct("@6iPq6Pq7P")
 _COPY = struct.Struct("@7i4xP3q3P")
+_GROUPS = struct.Struct("@i4x2P")
+_SHARED = struct.Struct(_PAGED.format + _GROUPS.format[1:])
 
 
 # What Python makes of a missing tensor, one of another rank, and a number that its field does not hold.
@@ -1004,5 +1011,31 @@ def nm_page_copy(caches, src=None, dst=None, slots=None, *, stream=None):
     """make_copy_desc's arguments, or a description alone."""
     desc = _described(caches, _COPY, "nm_page_copy") if isinstance(caches, bytes) else make_copy_desc(caches, src, dst, slots)
     rc = load().nm_page_copy(desc, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def make_shared_desc(q, k_cache, v_cache, block_table, lens, group_start, shared, out, scale, k_scale=None, v_scale=None, out_inv_scale=1.0, lse=None) -> bytes:
+    """As make_paged_desc; group_start: int32 [G + 1], shared: int32 [G]."""
+    try:
+        dev = _here()
+        G = shared.numel()
+        return make_paged_desc(q, k_cache, v_cache, block_table, lens, out, scale, 0, k_scale, v_scale, out_inv_scale, lse) + _GROUPS.pack(
+            G, _vector(group_start, _i32, G + 1, dev, "group_start"), _vector(shared, _i32, G, dev, "shared"))
+    except _MISFITS as e:
+        _misfit("nm_shared_attention", e)
+
+
+def nm_shared_attention_workspace(*tensors, **more) -> int:
+    """Bytes; takes what nm_shared_attention takes, or a description."""
+    return _workspace_of("nm_shared_attention_workspace", _SHARED, make_shared_desc, tensors, more)
+
+
+def nm_shared_attention(q, k_cache=None, v_cache=None, block_table=None, lens=None, group_start=None, shared=None, out=None, *, scale=None, k_scale=None,
+                        v_scale=None, out_inv_scale=1.0, lse=None, ws=None, stream=None, ws_bytes=None):
+    """make_shared_desc's arguments, or a description alone; and the workspace."""
+    desc = _described(q, _SHARED, "nm_shared_attention") if q.__class__ is bytes else make_shared_desc(
+        q, k_cache, v_cache, block_table, lens, group_start, shared, out, scale, k_scale, v_scale, out_inv_scale, lse)
+    rc = load().nm_shared_attention(desc, *_work_space(ws, ws_bytes), _stream(stream))
     if rc:
         _check(rc)

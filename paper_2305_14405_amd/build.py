@@ -11,7 +11,8 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libnm_hip.so")
 SOURCES = ["nm_tables.cpp", "nm_rows.hip", "nm_gemm.hip", "nm_gemm_direct.hip", "nm_gemm_end.hip", "nm_gemm_long.hip", "nm_gemm_unaligned.hip", "nm_gemm_ln.hip", "nm_qkv_attention.hip", "nm_attention.hip", "nm_block.hip", "nm_conv_chain.hip", "nm_conv_taps.hip", "nm_conv.hip",
            "nm_page_plan.hip", "nm_qk_rope.hip", "nm_paged_attention.hip", "nm_gemv_w4.hip", "nm_gemv_w4_bf16.hip",
-           "nm_gemv_w4_f16.hip", "nm_beam_select.hip", "nm_page_fork.hip", "nm_page_copy.hip", "nm_layer.cpp"]
+           "nm_gemv_w4_f16.hip", "nm_beam_select.hip", "nm_page_fork.hip", "nm_page_copy.hip", "nm_shared_attention.hip",
+           "nm_layer.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

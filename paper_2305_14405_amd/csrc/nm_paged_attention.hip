@@ -18,17 +18,9 @@
 //   bf16, 32 query and 8 key heads of 128: one request of 131071 positions (537 MB) 105 us and 8 for the second kernel, 5.1 TB/s in the first, a
 // copy's rate; 48 requests of up to 8192 (649 MB) 120 + 5, 5.4 TB/s.  int8, 16 heads of 64, two taken as one, 64 requests of up to 4097 (216 MB): 53 + 5,
 // 4.1 TB/s: a run has 13 units or so, and begins and ends two rows in them; codes become 16-bit numbers in vector instructions.  12 heads of 300 positions of one request: 9.4 us (one position 7.6), a chain of dependent loads (length, page, keys) and code that runs once.
-#include "nm_decode.h"
-#include "nm_paged_choice.h"
+#include "nm_paged_parts.h"
 
 namespace nm {
-
-typedef bf16 v8bf __attribute__((ext_vector_type(8)));
-typedef f16 v8h __attribute__((ext_vector_type(8)));
-typedef f16 v2h __attribute__((ext_vector_type(2)));
-typedef short v4s __attribute__((ext_vector_type(4)));
-typedef short v8s __attribute__((ext_vector_type(8)));
-typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
 struct PagedDesc { nm_paged_desc d; };
 struct PagedArgs : PagedDesc, PagedSplit {
@@ -59,19 +51,6 @@ __device__ __forceinline__ int units_of(const PagedArgs& a, int b)
 // What one of a request's rows counts for when the work is shared: starting and ending a row costs a workgroup about as much as a.extra units.
 __device__ __forceinline__ int cost_of(const PagedArgs& a, int b) { return units_of(a, b) + a.extra; }
 
-// How a total cost is divided: worker w has [begin(w), begin(w + 1)), the first `more` workers one more than `each`.
-struct Shares {
-    long each, more;
-    __device__ __forceinline__ Shares(long all, long workers) : each(all / workers), more(all % workers) {}
-    __device__ __forceinline__ Shares(long e, long m, int) : each(e), more(m) {}
-    __device__ __forceinline__ long begin(long w) const { return each * w + min(w, more); }
-    __device__ __forceinline__ long owner(long x) const
-    {
-        const long longer = (each + 1) * more;
-        return x < longer ? x / (each + 1) : more + (x - longer) / each;
-    }
-};
-
 // The cost of one of a request's rows, summed over the requests in front of each thread's run of them, and over all.  s: LDS of one number a wavefront.
 struct Scan { long before, mine, all; int b0, b1; };
 __device__ __forceinline__ Scan scan_units(const PagedArgs& a, long* s)
@@ -101,54 +80,6 @@ __device__ __forceinline__ Scan scan_units(const PagedArgs& a, long* s)
 // What a workgroup has of a row: positions [k0, k1) of request b for key head g and query heads h0 .. h0 + heads - 1; slot: where its part goes,
 // -1 where it is the whole row.  b: -1 for none.
 struct Piece { int b, g, h0, heads, k0, k1, slot; };
-
-template <typename T> struct Mma;
-template <> struct Mma<bf16> {
-    static __device__ __forceinline__ v4f mma(v8s a, v8s b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0); }
-};
-template <> struct Mma<f16> {
-    static __device__ __forceinline__ v4f mma(v8s a, v8s b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0); }
-};
-
-// 16 bytes of a cache row as elements of the matrix instructions' type, to LDS.
-template <typename C, typename T>
-__device__ __forceinline__ void put(short* to, v4u w)
-{
-    if constexpr (sizeof(C) == 2) {
-        *reinterpret_cast<v4u*>(to) = w;
-    } else {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            v4u o;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const unsigned x = w[half * 2 + i / 2];
-                if constexpr (std::is_same<T, f16>::value) {
-                    // 1024 + (code + 128) is exact under fp16's exponent of 1024, and so is the difference
-                    const unsigned u = __builtin_amdgcn_perm(0x64646464u, x ^ 0x80808080u, i % 2 ? 0x04030402u : 0x04010400u);
-                    o[i] = __builtin_bit_cast(unsigned, (v2h)(__builtin_bit_cast(v2h, u) - v2h{(f16)1152.0f, (f16)1152.0f}));
-                } else {
-                    const unsigned y = x >> (i % 2 * 16);
-                    const unsigned a = __float_as_uint((float)(int8_t)y), b = __float_as_uint((float)(int8_t)(y >> 8));
-                    o[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);   // the upper halves: small integers have no bits below
-                }
-            }
-            *reinterpret_cast<v4u*>(to + half * 8) = o;
-        }
-    }
-}
-
-// Lane number I of a lane's row: of 16 lanes where there are eight loads or more, else of four.
-template <int kLoads, int I>
-__device__ __forceinline__ unsigned row_lane(unsigned v)
-{
-    return __builtin_amdgcn_update_dpp(0, v, kLoads >= 8 ? 0x150 + I : I * 0x55, 0xf, 0xf, false);
-}
-template <int kLoads, int... I>
-__device__ __forceinline__ void fetch_rows(const char* base, unsigned place, v4u (&to)[kLoads], std::integer_sequence<int, I...>)
-{
-    ((to[I] = *reinterpret_cast<const v4u*>(base + (unsigned long)row_lane<kLoads, I>(place) * 16)), ...);
-}
 
 // C: type of the cache; T: of the matrix instructions; DP: d rounded up to 64, 128 or 256; kQ: terms of a query (1 or 3); kP: of the weights
 // (2 or 3); W: wavefronts (more than kPagedWaves: each workgroup has a row whole).
@@ -611,6 +542,38 @@ static int32_t plan_paged(const nm_paged_desc* d, PagedArgs* a, size_t* bytes, l
     return NM_OK;
 }
 
+int32_t check_paged_shape(const nm_paged_desc* d, bool* divided, const char* what)
+{
+    PagedArgs a;
+    long blocks;
+    size_t n;
+    const int32_t rc = plan_paged(d, &a, &n, &blocks, what);
+    *divided = !rc && a.workers;
+    return rc;
+}
+
+// What a call checks of its pointers and strides (plan_paged has looked at its shapes and types).
+int32_t check_paged(const nm_paged_desc* d, const char* what)
+{
+    const int64_t row = (int64_t)d->hq * d->d;
+    if (d->q_stride < row || d->out_stride < row || d->table_stride < d->max_pages) return fail(NM_ERR_INVALID_ARG, "%s: a stride is shorter than a row", what);
+    if (d->page_stride < 0 || d->slot_stride < 0 || d->head_stride < 0) return fail(NM_ERR_INVALID_ARG, "%s: negative stride of the cache", what);
+    if (!(d->scale == d->scale) || __builtin_isinf(d->scale)) return fail(NM_ERR_INVALID_ARG, "%s: scale must be finite", what);
+    if (d->B == 0) return NM_OK;   // empty tensors may be NULL pointers
+    if (!d->q || !d->lens || !d->out) return fail(NM_ERR_INVALID_ARG, "%s: q, lens or out is NULL", what);
+    if (d->out == d->q && (d->out_dtype != d->q_dtype || d->out_stride != d->q_stride)) return fail(NM_ERR_INVALID_ARG, "%s: in place with another type or stride", what);
+    const std::initializer_list<const void*> read = {d->k_cache, d->v_cache, d->k_scale, d->v_scale, d->block_table, d->lens};
+    if (begins_as(d->out, read) || begins_as(d->lse, read) || begins_as(d->lse, {d->q, d->out}))
+        return fail(NM_ERR_INVALID_ARG, "%s: out or lse is an input, or lse is out", what);
+    if ((d->max_pages && !d->block_table) || (d->max_pages && d->num_pages && (!d->k_cache || !d->v_cache)))
+        return fail(NM_ERR_INVALID_ARG, "%s: block_table or a cache is NULL", what);
+    if (d->cache_dtype == NM_DT_I8 && (!d->k_scale || !d->v_scale)) return fail(NM_ERR_INVALID_ARG, "%s: int8 cache without scales", what);
+    const int per16 = 16 / dtype_bytes(d->cache_dtype);
+    if (!aligned(d->k_cache, 16) || !aligned(d->v_cache, 16) || d->page_stride % per16 || d->slot_stride % per16 || d->head_stride % per16)
+        return fail(NM_ERR_UNSUPPORTED, "%s: the cache's addresses and strides must be multiples of 16 bytes", what);
+    return NM_OK;
+}
+
 }  // namespace nm
 
 using namespace nm;
@@ -636,22 +599,8 @@ int32_t nm_paged_attention(const nm_paged_desc* d, void* ws, size_t ws_bytes, vo
     size_t need;
     const int32_t rc = plan_paged(d, &a, &need, &blocks, "nm_paged_attention");
     if (rc) return rc;
-    const int64_t row = (int64_t)d->hq * d->d;
-    if (d->q_stride < row || d->out_stride < row || d->table_stride < d->max_pages) return fail(NM_ERR_INVALID_ARG, "nm_paged_attention: a stride is shorter than a row");
-    if (d->page_stride < 0 || d->slot_stride < 0 || d->head_stride < 0) return fail(NM_ERR_INVALID_ARG, "nm_paged_attention: negative stride of the cache");
-    if (!(d->scale == d->scale) || __builtin_isinf(d->scale)) return fail(NM_ERR_INVALID_ARG, "nm_paged_attention: scale must be finite");
+    if (const int32_t bad = check_paged(d, "nm_paged_attention")) return bad;
     if (d->B == 0) return NM_OK;   // empty tensors may be NULL pointers
-    if (!d->q || !d->lens || !d->out) return fail(NM_ERR_INVALID_ARG, "nm_paged_attention: q, lens or out is NULL");
-    if (d->out == d->q && (d->out_dtype != d->q_dtype || d->out_stride != d->q_stride)) return fail(NM_ERR_INVALID_ARG, "nm_paged_attention: in place with another type or stride");
-    const std::initializer_list<const void*> read = {d->k_cache, d->v_cache, d->k_scale, d->v_scale, d->block_table, d->lens};
-    if (begins_as(d->out, read) || begins_as(d->lse, read) || begins_as(d->lse, {d->q, d->out}))
-        return fail(NM_ERR_INVALID_ARG, "nm_paged_attention: out or lse is an input, or lse is out");
-    if ((d->max_pages && !d->block_table) || (d->max_pages && d->num_pages && (!d->k_cache || !d->v_cache)))
-        return fail(NM_ERR_INVALID_ARG, "nm_paged_attention: block_table or a cache is NULL");
-    if (d->cache_dtype == NM_DT_I8 && (!d->k_scale || !d->v_scale)) return fail(NM_ERR_INVALID_ARG, "nm_paged_attention: int8 cache without scales");
-    const int per16 = 16 / dtype_bytes(d->cache_dtype);
-    if (!aligned(d->k_cache, 16) || !aligned(d->v_cache, 16) || d->page_stride % per16 || d->slot_stride % per16 || d->head_stride % per16)
-        return fail(NM_ERR_UNSUPPORTED, "nm_paged_attention: the cache's addresses and strides must be multiples of 16 bytes");
     if (need) {
         if (!ws || ws_bytes < need) return fail(NM_ERR_WORKSPACE, "nm_paged_attention: workspace of %zu bytes needed, %zu given", need, ws ? ws_bytes : (size_t)0);
         if (!aligned(ws, 256)) return fail(NM_ERR_WORKSPACE, "nm_paged_attention: workspace must be 256-byte aligned");

@@ -153,6 +153,55 @@ def test_page_copy_misaligned_null_and_empty(lib):
         assert lib.nm_page_copy(C.byref(d), Z) == nm.NM_OK  # nothing to do
 
 
+# ---- attention over shared prefixes -------------------------------------------------------------------
+
+def shared():
+    d = nm.SharedDesc()
+    d.p.B, d.p.hq, d.p.hk, d.p.d, d.p.q_dtype, d.p.cache_dtype, d.p.out_dtype = 3, 8, 2, 64, nm.NM_DT_F32, nm.NM_DT_I8, nm.NM_DT_BF16
+    d.p.page_size, d.p.num_pages, d.p.max_pages, d.p.q_stride, d.p.out_stride, d.p.table_stride = 16, 100, 80, 512, 512, 80
+    fill(d.p, ("q", "k_cache", "v_cache", "k_scale", "v_scale", "block_table", "lens", "out", "lse"))
+    d.p.page_stride, d.p.slot_stride, d.p.head_stride, d.p.scale, d.p.out_inv_scale = 2048, 128, 64, 0.125, 1.0
+    d.G, d.group_start, d.shared = 2, P * 20, P * 21
+    return d
+
+
+def attend(lib, desc):
+    return lib.nm_shared_attention(C.byref(desc), C.c_void_p(P * 100), 1 << 50, Z)
+
+
+@pytest.mark.parametrize("changes", [
+    dict(B=-1), dict(hq=0), dict(hk=0), dict(hq=9), dict(d=0), dict(max_pages=-1), dict(num_pages=-1), dict(window=-1), dict(q_dtype=nm.NM_DT_I8),
+    dict(cache_dtype=nm.NM_DT_F32), dict(out_dtype=nm.NM_DT_I32), dict(q_stride=511), dict(out_stride=511), dict(table_stride=79), dict(page_stride=-16),
+    dict(slot_stride=-16), dict(head_stride=-16), dict(scale=float("nan")), dict(scale=float("inf")), dict(q=None), dict(lens=None), dict(out=None),
+    dict(block_table=None), dict(k_cache=None), dict(v_cache=None), dict(k_scale=None), dict(v_scale=None), dict(G=-1), dict(group_start=None), dict(shared=None),
+    *(dict(out=n * P) for n in (1, 2, 3, 4, 5, 6, 7, 20, 21)), *(dict(lse=n * P) for n in (1, 2, 3, 4, 5, 6, 7, 8, 20, 21))])
+def test_shared_attention_refuses(lib, changes):
+    d = shared()
+    for n, v in changes.items():
+        setattr(d if n in ("G", "group_start", "shared") else d.p, n, v)
+    assert attend(lib, d) == nm.NM_ERR_INVALID_ARG and "nm_shared_attention" in nm.nm_last_error()
+
+
+@pytest.mark.parametrize("changes", [
+    dict(d=72), dict(d=272, q_stride=4000, out_stride=4000), dict(page_size=3), dict(num_pages=1 << 27), dict(max_pages=1 << 26, table_stride=1 << 26),
+    dict(k_cache=P + 8), dict(v_cache=P + 4), dict(page_stride=2056), dict(slot_stride=136), dict(head_stride=72), dict(num_pages=1 << 20, page_stride=1 << 15),
+    dict(window=5), dict(B=nm.NM_PLAN_MAX_REQUESTS + 1), dict(G=nm.NM_PLAN_MAX_REQUESTS + 1)])
+def test_shared_attention_does_not_cover(lib, changes):
+    d = shared()
+    for n, v in changes.items():
+        setattr(d if n == "G" else d.p, n, v)
+    assert attend(lib, d) == nm.NM_ERR_UNSUPPORTED and "nm_shared_attention" in nm.nm_last_error()
+
+
+def test_shared_attention_workspace_null_and_empty(lib):
+    workspace_checks(lib, "nm_shared_attention", shared())
+    d, n = shared(), C.c_size_t()
+    d.p.max_pages = d.p.table_stride = 20                                     # rows that are not divided need none
+    assert lib.nm_shared_attention_workspace(C.byref(d), C.byref(n)) == nm.NM_OK and n.value == 0
+    d.p.B, d.p.q, d.p.out, d.p.lens, d.group_start = 0, None, None, None, None
+    assert lib.nm_shared_attention(C.byref(d), None, 0, Z) == nm.NM_OK
+
+
 # ---- binding ---------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("packed,desc", [(nm._BEAM, nm.BeamDesc), (nm._FORK, nm.ForkDesc), (nm._COPY, nm.CopyDesc)])
@@ -161,6 +210,13 @@ def test_packed_descriptions_lie_as_the_structures(packed, desc):
     assert packed.size == C.sizeof(desc)
     d = desc.from_buffer_copy(packed.pack(*values))
     assert [getattr(d, n) for n, _ in desc._fields_] == values
+
+
+def test_packed_description_of_shared_attention_lies_as_the_structure():
+    values = [float(i + 1) if t is C.c_float else i + 1 for i, (_, t) in enumerate(nm.PagedDesc._fields_)]
+    d = nm.SharedDesc.from_buffer_copy(nm._PAGED.pack(*values) + nm._GROUPS.pack(901, 902, 903))
+    assert nm._SHARED.size == C.sizeof(d) and (d.G, d.group_start, d.shared) == (901, 902, 903)
+    assert [getattr(d.p, n) for n, _ in nm.PagedDesc._fields_] == values
 
 
 @pytest.fixture
@@ -176,10 +232,12 @@ def host_tensors(monkeypatch):
                                 end_token=3, done_out=o(2, 4), history=o(6, 9), history_lens=o(6), history_out=o(8, 9), history_lens_out=o(8)),
         nm.make_fork_desc: dict(block_table=o(2, 4), lens=i[:2], parents=i[:3], free_pages=o(9), free_begin=i[:1], table_out=o(3, 4), page_size=16, num_pages=9, lens_out=o(3),
                                 free_out=o(9), free_end=o(1), copy_src=o(3), copy_dst=o(3), copy_slots=o(3), status=o(4)),
+        nm.make_shared_desc: dict(q=torch.zeros((2, 4, 64)), k_cache=torch.zeros((3, 16, 4, 64), dtype=torch.bfloat16), v_cache=torch.zeros((3, 16, 4, 64), dtype=torch.bfloat16),
+                                  block_table=o(2, 4), lens=i[:2], group_start=i[:2], shared=i[:1], out=torch.zeros((2, 4, 64)), scale=1.0),
         nm.make_copy_desc: dict(caches=torch.zeros((2, 5, 16, 2, 64)), src=o(3), dst=o(3), slots=o(3))}
 
 
-CALLS = {nm.make_beam_desc: nm.nm_beam_select, nm.make_fork_desc: nm.nm_page_fork, nm.make_copy_desc: nm.nm_page_copy}
+CALLS = {nm.make_beam_desc: nm.nm_beam_select, nm.make_fork_desc: nm.nm_page_fork, nm.make_copy_desc: nm.nm_page_copy, nm.make_shared_desc: nm.nm_shared_attention}
 MAY_BE_NONE = ("done", "done_out", "slots", "keep")
 ANY_LENGTH = ("src",)
 
@@ -192,7 +250,7 @@ def test_calls_refuse_what_is_missing_or_misshapen(host_tensors):
         for name, value in good.items():
             bad = ["3"] if name in MAY_BE_NONE else [None, "3"]
             if hasattr(value, "shape"):
-                bad += [3, value.double()]
+                bad += [3] if name in ("q", "out") else [3, value.double()]
                 bad += [value[0]] if value.dim() > 1 or (value.numel() > 1 and name not in ANY_LENGTH) else []
                 bad += [value[None]] if value.dim() > 1 and name not in ("parents", "tokens", "scores_out", "done", "scores") else []
             for b in bad:
@@ -218,8 +276,9 @@ def test_calls_refuse_missing_arguments_and_other_calls_descriptions(host_tensor
             with pytest.raises(nm.NmError) as e:
                 call(bad, stream=0)
             assert e.value.status == nm.NM_ERR_INVALID_ARG
-    for ask, good, bad in ((nm.nm_beam_select_workspace, nm.make_beam_desc, nm.make_fork_desc), (nm.nm_page_fork_workspace, nm.make_fork_desc, nm.make_copy_desc)):
-        assert ask(descs[good]) > 0
+    for ask, good, bad in ((nm.nm_beam_select_workspace, nm.make_beam_desc, nm.make_fork_desc), (nm.nm_page_fork_workspace, nm.make_fork_desc, nm.make_copy_desc),
+                           (nm.nm_shared_attention_workspace, nm.make_shared_desc, nm.make_copy_desc)):
+        assert ask(descs[good]) >= 0
         with pytest.raises(nm.NmError):
             ask(descs[bad])
         with pytest.raises(nm.NmError):
