@@ -1,25 +1,30 @@
 // The best continuations of every request's hypotheses (nm_beam_select).
 //
 // One pass over the logits makes both of what is needed of a row: its sum of exponentials, and its K best logits.  (Within a row the order of
-// candidates is that of the logits, so nothing but K of a row can be among the request's K.)  A wavefront takes 2048 logits at a time into
-// registers; each lane has a running maximum and sum of its own, and the wavefront one list, sorted, an entry to a lane: an entry is one 64-bit number, the
-// logit's bits in the order of their values above the complement of the token, so that comparing it settles ties too.  Logits above the K-th
-// entry are found by a ballot and put in one by one, which few are after the first thousands.  Rows are split into chunks where there are few of them.  A
-// second kernel has a workgroup to a request: it merges the chunks' lists and sums, forms the candidates' log-probabilities in 64 bits, and
-// merges the rows' lists, W heads at a time.
+// candidates is that of the logits, so nothing but K of a row can be among the request's K.)  A workgroup goes over a chunk of a row, every lane with a
+// maximum and a sum of its own.  Each wavefront sorts its lanes' maxima; the K-th of one wavefront, and the least of the wavefronts' K/4-th, are values that at least
+// K logits of the chunk reach.  The lanes that hold such logits, K and a few more, are few: what they went over is read again, the logits that
+// reach the value are collected in LDS, and each counts how many are better: that is its place.  A candidate is one 64-bit number, the logit's bits in the order
+// of their values above the complement of the token, so that comparing it settles ties too.  Where more than LDS takes reach the value (many
+// equal logits, or all large ones in a few lanes), they are put one by one into lists, sorted, an entry to a lane.
+//   A second kernel has a workgroup to a request: it joins the chunks' sums, forms the candidates' log-probabilities in 64 bits, and chooses among
+// them in the same way; short histories it copies itself.
 #include <algorithm>
 
 #include "nm_decode.h"
 
 namespace nm {
 
-constexpr int kBeamWaves = 4, kBeamThreads = 64 * kBeamWaves;
-constexpr int kBeamLane = 32, kBeamTile = 64 * kBeamLane;      // logits of a lane, of a wavefront
-constexpr int kBeamChunks = 64;                                // of a row at most: a lane of the second kernel to each
+constexpr int kBeamWaves = 4, kBeamThreads = 64 * kBeamWaves;   // of the first kernel
+constexpr int kJoinWaves = 8, kJoinThreads = 64 * kJoinWaves;   // of the second
+constexpr int kBeamStep = 4;                                    // groups of 16 bytes that a lane asks for at a time
+constexpr int kBeamMost = 512;                                 // candidates that are ranked at once
 
 struct BeamArgs {
     nm_beam_desc d;
-    int chunks, chunk;               // of a row, and their length
+    int chunks, chunk;               // of a row, and their length, a number of kBeamStep groups of 16 bytes for every lane
+    FastDiv each;                    // candidates of a row: chunks K
+    int histories;                   // the second kernel copies them
     unsigned long* part_key;         // [R W, chunks, K], best first, 0: none
     double* part_sum;                // [R W, chunks]: sum of exp(x - max)
     float* part_max;                 // [R W, chunks], -inf: no logits
@@ -67,8 +72,73 @@ __device__ __forceinline__ Key insert_all(Key list, Key mine, int K, int lane)
     return list;
 }
 
-// exp(a) for a <= 0, by the hardware's power of two.
-__device__ __forceinline__ float exp_of(float a) { return __builtin_amdgcn_exp2f(a * 1.44269504088896340736f); }
+// The value of lane ^ MASK.
+struct Second { __device__ __forceinline__ int operator()(int, int b) const { return b; } };
+struct Differ { __device__ __forceinline__ int operator()(int a, int b) const { return a ^ b; } };
+template <int MASK>
+__device__ __forceinline__ int across(int v)
+{
+    return MASK < 16 ? butterfly_step<MASK>(v, Second{}) : butterfly_step<MASK>(v, Differ{}) ^ v;
+}
+template <int MASK>
+__device__ __forceinline__ double across(double v)
+{
+    const long u = __double_as_longlong(v);
+    return __longlong_as_double((long)across<MASK>((int)(u >> 32)) << 32 | (unsigned)across<MASK>((int)u));
+}
+__device__ __forceinline__ double wave_sum(double v)
+{
+    v += across<32>(v);
+    v += across<16>(v);
+    v += across<8>(v);
+    v += across<4>(v);
+    v += across<2>(v);
+    return v + across<1>(v);
+}
+__device__ __forceinline__ float wave_max(float v) { return __int_as_float(group_reduce<64>(__float_as_int(v), MaxF32{})); }
+
+// Sorts a wavefront's numbers, the largest into lane 0 (Batcher's bitonic order: runs of SIZE, merged over distances STEP).
+template <int SIZE, int STEP>
+__device__ __forceinline__ float sort_step(float v, int lane)
+{
+    const float other = __int_as_float(across<STEP>(__float_as_int(v)));
+    v = ((lane & STEP) == 0) == ((lane & SIZE) == 0) ? fmaxf(v, other) : fminf(v, other);
+    if constexpr (STEP > 1) v = sort_step<SIZE, STEP / 2>(v, lane);
+    return v;
+}
+__device__ __forceinline__ float sorted(float v, int lane)
+{
+    v = sort_step<2, 1>(v, lane);
+    v = sort_step<4, 2>(v, lane);
+    v = sort_step<8, 4>(v, lane);
+    v = sort_step<16, 8>(v, lane);
+    v = sort_step<32, 16>(v, lane);
+    return sort_step<64, 32>(v, lane);
+}
+
+// A value that at least K of the numbers whose maxima over disjoint sets the workgroup's threads have reach (-inf: there may be fewer).  s: LDS.
+template <int W>
+__device__ __forceinline__ float reached(float top, int K, float (&s)[2][W])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int order = __float_as_int(sorted(top, lane));
+    // with every lane active: of one that is not, a copy of the register need not have the value
+    const float last = __int_as_float(__builtin_amdgcn_readlane(order, K - 1)), share = __int_as_float(__builtin_amdgcn_readlane(order, (K - 1) / W));
+    if (lane == 0) {
+        s[0][wave] = last;
+        s[1][wave] = share;
+    }
+    __syncthreads();
+    float most = s[0][0], least = s[1][0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) {
+        most = fmaxf(most, s[0][w]);
+        least = fminf(least, s[1][w]);
+    }
+    return fmaxf(most, least);
+}
+
+constexpr float kLog2e = 1.44269504088896340736f;
 
 // NaN: -inf, +inf: the largest number.  (A median of three with -inf as a bound is folded into a minimum, which passes the number in place of a NaN.)
 __device__ __forceinline__ float logit(float x) { return x == x ? fminf(x, 3.40282346638528859812e38f) : -INFINITY; }
@@ -80,157 +150,336 @@ __device__ __forceinline__ bool offers(const nm_beam_desc& d, long row)
     return __builtin_fabsf(s) < INFINITY && w > 0.0f && w < INFINITY;
 }
 
+// The largest of three; a NaN is passed over, or left for the sum to show.
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float v;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(v) : "v"(a), "v"(b), "v"(c));
+    return v;
+}
+
+// Calls use(i, how many of n numbers are better than number i) for each of them, L lanes to a number.
+template <int L, int kThreads, typename Better, typename Use>
+__device__ __forceinline__ void places(int n, Better better, Use use)
+{
+    for (int i0 = 0; i0 < n; i0 += kThreads / L) {
+        const int i = i0 + (int)threadIdx.x / L, mine = min(i, n - 1);
+        int place = 0;
+#pragma unroll 2
+        for (int k = threadIdx.x % L; k < n; k += L) place += better(k, mine);
+        place = group_reduce<L>(place, AddI32{});
+        if (i < n && threadIdx.x % L == 0) use(i, place);
+    }
+}
+
 template <typename T>
 __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a)
 {
-    constexpr int kGroup = 16 / (int)sizeof(T), kGroups = kBeamLane / kGroup;
+    constexpr int kGroup = 16 / (int)sizeof(T), kApart = kBeamThreads * kGroup, kTile = kBeamStep * kApart;
+    constexpr int kEach = kBeamStep * kGroup;                  // logits of a lane at a time
     typedef T Vec __attribute__((ext_vector_type(kGroup)));
-    __shared__ Key s_list[kBeamWaves][64];
-    __shared__ float s_max[kBeamWaves];
+    __shared__ Key s_key[kBeamMost];
+    __shared__ float s_max[kBeamWaves], s_reached[2][kBeamWaves];
     __shared__ double s_sum[kBeamWaves];
+    __shared__ int s_count, s_lanes, s_lane[kBeamThreads];
     const nm_beam_desc& d = a.d;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = d.K;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = d.K;
     const long row = blockIdx.y;
-    if (!offers(d, row) || (d.done && d.done[row])) return;   // uniform
     const T* x = static_cast<const T*>(d.logits) + row * d.logits_stride;
     // groups of 16 bytes begin `ahead` elements in front of the row
     const int ahead = (int)(reinterpret_cast<uintptr_t>(x) % 16 / sizeof(T));
-    const int v_end = (int)min((long)d.V, (long)(blockIdx.x + 1) * a.chunk - ahead), v_begin = max((int)blockIdx.x * a.chunk - ahead, 0);
+    const int begin = (int)blockIdx.x * a.chunk - ahead, end = min(begin + a.chunk, d.V);
+    // a group of the row: a logit in front of it or behind is none
+    auto group = [&](int v) -> Vec {
+        if (v >= 0 && v + kGroup <= d.V) return *reinterpret_cast<const Vec*>(x + v);
+        Vec w;
+#pragma unroll 1
+        for (int e = 0; e < kGroup; ++e) w[e] = v + e >= 0 && v + e < d.V ? x[v + e] : (T)-INFINITY;
+        return w;
+    };
+    auto ask = [&](int t, Vec (&w)[kBeamStep]) {
+        const int v = t + tid * kGroup;
+        if (t >= 0 && t + kTile <= d.V) {                      // uniform
+#pragma unroll
+            for (int i = 0; i < kBeamStep; ++i) w[i] = *reinterpret_cast<const Vec*>(x + v + i * kApart);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kBeamStep; ++i) w[i] = group(v + i * kApart);
+        }
+    };
+    // the first are asked for before it is known whether the row matters
+    Vec w[kBeamStep];
+    ask(begin, w);
+    if (!offers(d, row) || (d.done && d.done[row])) return;    // uniform
+    if (tid == 0) s_count = s_lanes = 0;
 
+    // Logits as they are; where an infinity or a NaN turns up in the maximum or the sum, once more with what they count as.
+    float top, least, mine;
+    double sum;
+    auto sweep = [&](auto special) {
+        mine = -INFINITY;
+        sum = 0;
+        float off = 0.0f;                                      // what is subtracted from x log2(e)
+        for (int t = begin; t < end; t += kTile) {
+            float y[kEach];
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) y[i] = special ? logit((float)w[i / kGroup][i % kGroup]) : (float)w[i / kGroup][i % kGroup];
+            if (t + kTile < end) ask(t + kTile, w);
+            float now = fmaxf(mine, y[0]);
+#pragma unroll
+            for (int i = 1; i + 1 < kEach; i += 2) now = max3(now, y[i], y[i + 1]);
+            now = fmaxf(now, y[kEach - 1]);
+            float part[4] = {0, 0, 0, 0};
+            if (!special) {
+                // exp(x - m) as a power of two of x log2(e) - m log2(e), rounded once (what the second product's rounding leaves is made up for behind)
+                const float next = now == -INFINITY ? 0.0f : now * kLog2e;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) part[i % 4] += __builtin_amdgcn_exp2f(__builtin_fmaf(y[i], kLog2e, -next));
+                sum *= (double)__builtin_amdgcn_exp2f(off - next);
+                off = next;
+            } else {
+                const float base = now == -INFINITY ? 0.0f : now;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) part[i % 4] += __builtin_amdgcn_exp2f((y[i] - base) * kLog2e);
+                sum *= (double)__builtin_amdgcn_exp2f((mine - base) * kLog2e);
+            }
+            sum += (double)((part[0] + part[1]) + (part[2] + part[3]));
+            mine = now;
+        }
+        top = wave_max(mine);
+        if (lane == 0) s_max[wave] = top;
+        least = reached(mine, K, s_reached);                   // synchronises
+#pragma unroll
+        for (int i = 0; i < kBeamWaves; ++i) top = fmaxf(top, s_max[i]);
+        const float base = top == -INFINITY ? 0.0f : top;
+        float by = __builtin_amdgcn_exp2f((mine - base) * kLog2e);
+        if (!special && mine > -INFINITY) by *= __builtin_amdgcn_exp2f(-__builtin_fmaf(mine, kLog2e, -off));
+        sum = wave_sum(sum * (double)by);
+        if (lane == 0) s_sum[wave] = sum;
+        __syncthreads();
+        sum = 0;
+#pragma unroll
+        for (int i = 0; i < kBeamWaves; ++i) sum += s_sum[i];
+    };
+    sweep(std::false_type{});
+    if (!(top < 1e30f && sum < INFINITY)) {                    // uniform; NaNs too
+        __syncthreads();
+        ask(begin, w);
+        sweep(std::true_type{});
+    }
+    const long out = row * a.chunks + blockIdx.x;
+    if (tid == 0) {
+        a.part_max[out] = top;
+        a.part_sum[out] = sum;
+    }
+
+    // The lanes that hold any of those: their groups are read once more, by all lanes.  (Code for what few lanes come to is fetched for all.)
+    if (mine >= least && mine > -INFINITY) s_lane[atomicAdd(&s_lanes, 1)] = tid;
+    __syncthreads();
+    const int lanes = s_lanes, groups = lanes * (a.chunk / kApart);
+    auto number = [&](int i) { return begin + i / lanes * kApart + s_lane[i % lanes] * kGroup; };
+    for (int i = tid; i < groups; i += kBeamThreads) {
+        const int v = number(i);
+        const Vec y = group(v);
+#pragma unroll
+        for (int e = 0; e < kGroup; ++e) {
+            const float z = logit((float)y[e]);
+            if (z >= least && z > -INFINITY) {
+                const int at = atomicAdd(&s_count, 1);
+                if (at < kBeamMost) s_key[at] = key_of(z, v + e);
+            }
+        }
+    }
+    __syncthreads();
+    const int n = s_count;
+    Key* best = a.part_key + out * K;
+    if (n <= kBeamMost) {
+        if (tid >= n && tid < K) best[tid] = 0;
+        places<8, kBeamThreads>(n, [&](int k, int i) { return (int)(s_key[k] > s_key[i]); }, [&](int i, int place) {
+            if (place < K) best[place] = s_key[i];
+        });
+        return;
+    }
+    __syncthreads();
     Key list = 0;
-    float top = -INFINITY;
-    double sum = 0;
-    for (long t = (long)blockIdx.x * a.chunk - ahead + wave * kBeamTile; t < v_end; t += kBeamTile * kBeamWaves) {
-        float y[kBeamLane];
-        const int first = (int)t + lane * kGroup;
-#pragma unroll
-        for (int i = 0; i < kGroups; ++i) {
-            const int v = first + i * 64 * kGroup;
-            if (v >= v_begin && v + kGroup <= v_end) {
-                const Vec w = *reinterpret_cast<const Vec*>(x + v);
-#pragma unroll
-                for (int e = 0; e < kGroup; ++e) y[i * kGroup + e] = logit((float)w[e]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < kGroup; ++e) y[i * kGroup + e] = v + e >= v_begin && v + e < v_end ? logit((float)x[v + e]) : -INFINITY;
-            }
-        }
-        float m = y[0];
-#pragma unroll
-        for (int i = 1; i < kBeamLane; ++i) m = fmaxf(m, y[i]);
-        const float now = fmaxf(m, top), base = now == -INFINITY ? 0.0f : now;
-        float part[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < kBeamLane; ++i) part[i % 4] += exp_of(y[i] - base);
-        sum = sum * (double)exp_of(top - base) + (double)((part[0] + part[1]) + (part[2] + part[3]));
-        top = now;
-        const Key last = lane_key(list, K - 1);
-        if (__any(m > -INFINITY && (!last || m >= logit_of(last)))) {
-#pragma unroll
-            for (int i = 0; i < kBeamLane; ++i) {
-                const int v = first + i / kGroup * 64 * kGroup + i % kGroup;
-                list = insert_all(list, y[i] > -INFINITY ? key_of(y[i], v) : 0, K, lane);
-            }
+    for (int i0 = 0; i0 < groups; i0 += kBeamThreads) {        // every lane of a wavefront comes along
+        const int i = i0 + tid;
+#pragma unroll 1
+        for (int e = 0; e < kGroup; ++e) {
+            const int v = i < groups ? number(i) + e : -1;
+            const float z = v >= 0 && v < d.V ? logit((float)x[v]) : -INFINITY;
+            list = insert_all(list, z >= least && z > -INFINITY ? key_of(z, v) : 0, K, lane);
         }
     }
-    // the lanes' sums, then the wavefronts'
-    float m = top;
-    for (int step = 32; step; step >>= 1) m = fmaxf(m, __shfl_xor(m, step));
-    sum *= (double)exp_of(top - (m == -INFINITY ? 0.0f : m));
-    for (int step = 32; step; step >>= 1) sum += __shfl_xor(sum, step);
-    s_list[wave][lane] = list;
-    if (lane == 0) { s_max[wave] = m; s_sum[wave] = sum; }
+    s_key[tid] = list;
     __syncthreads();
     if (wave) return;
-    for (int w = 1; w < kBeamWaves; ++w) list = insert_all(list, lane < K ? s_list[w][lane] : 0, K, lane);
-    const long part = row * a.chunks + blockIdx.x;
-    if (lane < K) a.part_key[part * K + lane] = list;
-    if (lane == 0) {
-        float all = s_max[0];
-        for (int w = 1; w < kBeamWaves; ++w) all = fmaxf(all, s_max[w]);
-        double total = 0;
-        for (int w = 0; w < kBeamWaves; ++w) total += s_sum[w] * (double)exp_of(s_max[w] - (all == -INFINITY ? 0.0f : all));
-        a.part_max[part] = all;
-        a.part_sum[part] = total;
-    }
+#pragma unroll 1
+    for (int i = 1; i < kBeamWaves; ++i) list = insert_all(list, lane < K ? s_key[i * 64 + lane] : 0, K, lane);
+    if (lane < K) best[lane] = list;
 }
 
-// A workgroup to a request.
-__global__ __launch_bounds__(kBeamThreads) void beam_join_kernel(BeamArgs a)
-{
-    __shared__ double s_rank[NM_BEAM_MAX][NM_BEAM_MAX], s_total[NM_BEAM_MAX][NM_BEAM_MAX];   // [hypothesis][its candidates]
-    __shared__ int s_token[NM_BEAM_MAX][NM_BEAM_MAX];
-    const nm_beam_desc& d = a.d;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = d.K, r = blockIdx.x;
-    for (int w = wave; w < d.W; w += kBeamWaves) {
-        const long row = (long)r * d.W + w;
-        double total = -INFINITY;
-        int token = -1;
-        if (offers(d, row)) {
-            if (d.done && d.done[row]) {
-                if (lane == 0) { total = d.scores[row]; token = d.end_token; }
-            } else {
-                const long part = row * a.chunks;
-                const float m = lane < a.chunks ? a.part_max[part + lane] : -INFINITY;
-                float top = m;
-                for (int step = 32; step; step >>= 1) top = fmaxf(top, __shfl_xor(top, step));
-                double sum = lane < a.chunks ? a.part_sum[part + lane] * exp((double)m - (double)(top == -INFINITY ? 0.0f : top)) : 0.0;
-                for (int step = 32; step; step >>= 1) sum += __shfl_xor(sum, step);
-                Key list = 0;
-                for (int c = 0; c < a.chunks; ++c) list = insert_all(list, lane < K ? a.part_key[(part + c) * K + lane] : 0, K, lane);
-                if (list && lane < K) {
-                    total = (double)d.scores[row] + (((double)logit_of(list) - (double)top) - log(sum));
-                    token = token_of(list);
-                }
-            }
-        }
-        s_total[w][lane] = total;
-        s_rank[w][lane] = total == -INFINITY ? total : (d.weight ? (double)d.weight[row] : 1.0) * total;
-        s_token[w][lane] = token;
-    }
-    __syncthreads();
-    if (wave) return;
-    // lane w has the best candidate of hypothesis w that is left
-    int at = 0;
-    double head = lane < d.W ? s_rank[lane][0] : -INFINITY;
-    for (int k = 0; k < K; ++k) {
-        double best = head;
-        for (int step = 32; step; step >>= 1) best = fmax(best, __shfl_xor(best, step));
-        const int w = __ffsll((long long)__ballot(head == best)) - 1;
-        const long out = (long)r * K + k;
-        if (best == -INFINITY) {
-            if (lane == 0) {
-                d.parents[out] = d.tokens[out] = -1;
-                d.scores_out[out] = -INFINITY;
-                if (d.done_out) d.done_out[out] = 0;
-            }
-        } else if (lane == w) {
-            const long row = (long)r * d.W + w;
-            d.parents[out] = (int)row;
-            d.tokens[out] = s_token[w][at];
-            d.scores_out[out] = (float)s_total[w][at];
-            if (d.done_out) d.done_out[out] = (d.done && d.done[row]) || s_token[w][at] == d.end_token;
-            ++at;
-            head = at < K ? s_rank[w][at] : -INFINITY;
-        }
-    }
-}
+constexpr int kFollow = 8;
 
-// Histories: a few workgroups to a row.
-__global__ __launch_bounds__(kBeamThreads) void beam_history_kernel(nm_beam_desc d)
+// A row's history behind its choice: tokens [first, ...) of those that it takes over, every `step`-th; and the new one.
+__device__ __forceinline__ void follow(const nm_beam_desc& d, long row, int parent, int token, int first, int step)
 {
-    const long row = blockIdx.x;
-    const int parent = d.parents[row];
     const int held = parent < 0 ? 0 : min(max(d.history_lens[parent], 0), d.max_history);
     const bool grows = parent >= 0 && held < d.max_history && !(d.done && d.done[parent]);
     int* to = d.history_out + row * d.history_out_stride;
     const int* from = d.history + (long)max(parent, 0) * d.history_stride;
-    for (int i = blockIdx.y * kBeamThreads + threadIdx.x; i < held; i += gridDim.y * kBeamThreads) to[i] = from[i];
-    if (blockIdx.y == 0 && threadIdx.x == 0) {
-        if (grows) to[held] = d.tokens[row];
+    for (int i = first; i < held; i += kFollow * step) {       // that many under way
+        int x[kFollow];
+#pragma unroll
+        for (int k = 0; k < kFollow; ++k) x[k] = from[min(i + k * step, held - 1)];
+#pragma unroll
+        for (int k = 0; k < kFollow; ++k)
+            if (i + k * step < held) to[i + k * step] = x[k];
+    }
+    if (first == 0) {
+        if (grows) to[held] = token;
         d.history_lens_out[row] = held + grows;
     }
 }
+
+// A workgroup to a request.
+__global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a)
+{
+    // of a hypothesis: its largest logit, what is added to a logit's difference from that, and its weight; kind 0: offers nothing, 1: its tokens, 2: its end
+    __shared__ float s_top[NM_BEAM_MAX];
+    __shared__ double s_add[NM_BEAM_MAX], s_weight[NM_BEAM_MAX], s_rank[kBeamMost];
+    __shared__ Key s_key[kBeamMost];
+    __shared__ int s_kind[NM_BEAM_MAX], s_of[kBeamMost], s_count, s_parent[NM_BEAM_MAX], s_token[NM_BEAM_MAX];
+    __shared__ float s_reached[2][kJoinWaves];
+    const nm_beam_desc& d = a.d;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = d.K, W = d.W, r = blockIdx.x;
+    const long row0 = (long)r * W;
+    const int each = a.chunks * K, all = W * each;
+    const Key* keys = a.part_key + row0 * each;
+    // The first candidate is asked for before anything else (of a hypothesis that turns out to offer none, it is not looked at).
+    const Key ahead = keys[min(tid, all - 1)];
+    for (int w = wave; w < W; w += kJoinWaves) {
+        const long row = row0 + w, part = row * a.chunks;
+        const float m0 = a.part_max[part + min(lane, a.chunks - 1)];
+        const double l0 = a.part_sum[part + min(lane, a.chunks - 1)];
+        const int kind = !offers(d, row) ? 0 : d.done && d.done[row] ? 2 : 1;
+        float top = -INFINITY;
+        double sum = 0;
+        if (kind == 1) {
+            if (lane < a.chunks) top = m0;
+            for (int c = lane + 64; c < a.chunks; c += 64) top = fmaxf(top, a.part_max[part + c]);
+            top = wave_max(top);
+            const float base = top == -INFINITY ? 0.0f : top;
+            if (lane < a.chunks) sum = l0 * (double)__builtin_amdgcn_exp2f((m0 - base) * kLog2e);
+            for (int c = lane + 64; c < a.chunks; c += 64) sum += a.part_sum[part + c] * (double)__builtin_amdgcn_exp2f((a.part_max[part + c] - base) * kLog2e);
+            sum = wave_sum(sum);
+        }
+        if (lane == 0) {
+            s_top[w] = top;
+            s_add[w] = (double)d.scores[row] - (kind == 1 ? log(sum) : 0.0);
+            s_weight[w] = d.weight ? (double)d.weight[row] : 1.0;
+            s_kind[w] = kind;
+        }
+    }
+    if (tid == 0) s_count = 0;
+    for (int k = tid; k < K; k += kJoinThreads) s_parent[k] = s_token[k] = -1;
+    __syncthreads();
+
+    // The candidates one after the other: hypothesis, key (an end's is 1), and what it is ranked by.
+    auto candidates = [&](auto&& use) {
+#pragma unroll 1
+        for (int i = tid; i < all; i += kJoinThreads) {
+            const int w = (int)quotient(i, a.each), kind = s_kind[w];
+            const Key key = kind == 1 ? (i == tid ? ahead : keys[i]) : (Key)(kind == 2 && i == w * each);
+            if (key) use(w, key, (kind == 2 ? s_add[w] : ((double)logit_of(key) - (double)s_top[w]) + s_add[w]) * s_weight[w]);
+        }
+    };
+    float least = -INFINITY;                                   // all of few
+    if (all > 64) {
+        float top = -INFINITY;
+        candidates([&](int, Key, double rank) { top = fmaxf(top, (float)rank); });   // (rounding keeps the order)
+        least = reached(top, K, s_reached);
+    }
+    candidates([&](int w, Key key, double rank) {
+        if ((float)rank >= least) {
+            const int at = atomicAdd(&s_count, 1);
+            if (at < kBeamMost) {
+                s_rank[at] = rank;
+                s_key[at] = key;
+                s_of[at] = w;
+            }
+        }
+    });
+    __syncthreads();
+    const int n = s_count;
+    auto put = [&](int k, int w, Key key) {
+        const long out = (long)r * K + k;
+        const int kind = s_kind[w], token = kind == 2 ? d.end_token : token_of(key);
+        d.parents[out] = s_parent[k] = (int)row0 + w;
+        d.tokens[out] = s_token[k] = token;
+        d.scores_out[out] = (float)(kind == 2 ? s_add[w] : ((double)logit_of(key) - (double)s_top[w]) + s_add[w]);
+        if (d.done_out) d.done_out[out] = kind == 2 || token == d.end_token;
+    };
+    if (n <= kBeamMost) {
+        places<4, kJoinThreads>(n, [&](int k, int i) {
+            const double other = s_rank[k], rank = s_rank[i];
+            const int w = s_of[k], v = s_of[i];
+            return (int)(other > rank) | ((int)(other == rank) & ((int)(w < v) | ((int)(w == v) & (int)(s_key[k] > s_key[i]))));
+        }, [&](int i, int place) {
+            if (place < K) put(place, s_of[i], s_key[i]);
+        });
+    } else {
+        // one list after the other: the best by their place among those in front, an entry to a lane
+        __syncthreads();
+        if (wave == 0) {
+            double list_rank = -INFINITY;
+            int list_w = 0;
+            Key list_key = 0;
+            for (int w = 0; w < W; ++w) {
+                if (!s_kind[w]) continue;
+                Key row = 0;                                   // the hypothesis' own, by key
+                if (s_kind[w] == 2) row = lane == 0;
+                else
+                    for (int c = 0; c < a.chunks; ++c) row = insert_all(row, lane < K ? a.part_key[((row0 + w) * a.chunks + c) * K + lane] : 0, K, lane);
+                for (int i = 0; i < K; ++i) {
+                    const Key key = lane_key(row, i);
+                    if (!key) break;
+                    const double rank = (s_kind[w] == 2 ? s_add[w] : ((double)logit_of(key) - (double)s_top[w]) + s_add[w]) * s_weight[w];
+                    const int at = __popcll(__ballot(list_key && list_rank >= rank));   // those in front are of lower hypotheses, or better
+                    if (at >= K) break;
+                    const double up_rank = __shfl_up(list_rank, 1);
+                    const int up_w = __shfl_up(list_w, 1);
+                    const Key up_key = __shfl_up(list_key, 1);
+                    if (lane == at) { list_rank = rank; list_w = w; list_key = key; }
+                    else if (lane > at) { list_rank = up_rank; list_w = up_w; list_key = up_key; }
+                }
+            }
+            if (lane < K && list_key) put(lane, list_w, list_key);
+        }
+    }
+    __syncthreads();
+    for (int k = tid; k < K; k += kJoinThreads)
+        if (s_parent[k] < 0) {
+            const long out = (long)r * K + k;
+            d.parents[out] = d.tokens[out] = -1;
+            d.scores_out[out] = -INFINITY;
+            if (d.done_out) d.done_out[out] = 0;
+        }
+    if (a.histories)
+        for (int k = wave; k < K; k += kJoinWaves) follow(d, (long)r * K + k, s_parent[k], s_token[k], lane, 64);
+}
+
+// Long histories: a few workgroups to a row.
+__global__ __launch_bounds__(kBeamThreads) void beam_history_kernel(nm_beam_desc d)
+{
+    const long row = blockIdx.x;
+    follow(d, row, d.parents[row], d.tokens[row], blockIdx.y * kBeamThreads + threadIdx.x, gridDim.y * kBeamThreads);
+}
+
+constexpr long kBeamGroups = 1024;                             // workgroups of the first kernel, about
+// Tokens of a history, and of a request's, that its workgroup of the second kernel copies, a wavefront to a history; more go to a kernel of their own.
+constexpr int kHistory = 1024;
+constexpr long kHistories = 8192;
 
 static int32_t plan_beam(const nm_beam_desc* d, BeamArgs* a, size_t* bytes, const char* what)
 {
@@ -241,12 +490,14 @@ static int32_t plan_beam(const nm_beam_desc* d, BeamArgs* a, size_t* bytes, cons
     if ((int64_t)d->R * d->W > 1 << 20 || d->V > 1 << 26) return fail(NM_ERR_UNSUPPORTED, "%s: R * W > 2^20 or V > 2^26", what);
     *a = BeamArgs{};
     a->d = *d;
-    const long rows = (long)d->R * d->W, most = ((long)d->V + 16 + kBeamTile * kBeamWaves - 1) / (kBeamTile * kBeamWaves);
-    const long wanted = rows ? (2048 + rows - 1) / rows : 1;
-    long chunks = std::min(std::min(most, wanted), (long)kBeamChunks);
-    const long step = kBeamTile * kBeamWaves;
-    a->chunk = (int)((((long)d->V + 16 + chunks - 1) / chunks + step - 1) / step * step);
-    a->chunks = (int)(((long)d->V + 16 + a->chunk - 1) / a->chunk);
+    // chunks of one tile where there are few rows, and as many as give every CU four workgroups
+    const long rows = (long)d->R * d->W, tile = kBeamStep * kBeamThreads * 16 / dtype_bytes(d->logits_dtype);
+    const long tiles = ((long)d->V + 15 + tile - 1) / tile;    // a row's first group of 16 bytes may begin in front of it
+    const long wanted = rows ? std::min(std::max(1l, kBeamGroups / rows), tiles) : 1;
+    a->chunk = (int)((tiles + wanted - 1) / wanted * tile);
+    a->chunks = (int)((tiles * tile + a->chunk - 1) / a->chunk);
+    a->each = fast_div(a->chunks * d->K);
+    a->histories = d->history && d->max_history <= kHistory && (long)d->K * d->max_history <= kHistories;
     const size_t parts = (size_t)rows * a->chunks;
     *bytes = parts * (d->K * sizeof(Key) + sizeof(double) + sizeof(float));
     return NM_OK;
@@ -319,11 +570,11 @@ int32_t nm_beam_select(const nm_beam_desc* d, void* ws, size_t ws_bytes, void* s
         const int32_t err = check_hip(hipGetLastError(), "nm_beam_select launch");
         if (err) return err;
     }
-    queue_kernel(beam_join_kernel, dim3(d->R), dim3(kBeamThreads), 0, s, a);
-    if (d->history) {
+    queue_kernel(beam_join_kernel, dim3(d->R), dim3(kJoinThreads), 0, s, a);
+    if (d->history && !a.histories) {
         const int32_t err = check_hip(hipGetLastError(), "nm_beam_select launch");
         if (err) return err;
-        queue_kernel(beam_history_kernel, dim3(d->R * d->K, std::min((d->max_history + 4 * kBeamThreads - 1) / (4 * kBeamThreads), 64)), dim3(kBeamThreads), 0, s, *d);
+        queue_kernel(beam_history_kernel, dim3(d->R * d->K, std::min((d->max_history + kFollow * kBeamThreads - 1) / (kFollow * kBeamThreads), 64)), dim3(kBeamThreads), 0, s, *d);
     }
     return check_hip(hipGetLastError(), "nm_beam_select launch");
 }

@@ -283,6 +283,9 @@ struct AddF32 {
 struct MaxF32 {
     __device__ __forceinline__ int operator()(int a, int b) const { return __float_as_int(__builtin_fmaxf(__int_as_float(a), __int_as_float(b))); }
 };
+struct AddI32 {
+    __device__ __forceinline__ int operator()(int a, int b) const { return a + b; }
+};
 struct MaxI32 {
     __device__ __forceinline__ int operator()(int a, int b) const { return max(a, b); }
 };
