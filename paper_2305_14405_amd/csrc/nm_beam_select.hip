@@ -24,6 +24,7 @@ struct BeamArgs {
     nm_beam_desc d;
     int chunks, chunk;               // of a row, and their length, a number of kBeamStep groups of 16 bytes for every lane
     FastDiv each;                    // candidates of a row: chunks K
+    int rows;                        // of this launch of the first kernel
     int histories;                   // the second kernel copies them
     unsigned long* part_key;         // [R W, chunks, K], best first, 0: none
     double* part_sum;                // [R W, chunks]: sum of exp(x - max)
@@ -189,12 +190,18 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a)
     // groups of 16 bytes begin `ahead` elements in front of the row
     const int ahead = (int)(reinterpret_cast<uintptr_t>(x) % 16 / sizeof(T));
     const int begin = (int)blockIdx.x * a.chunk - ahead, end = min(begin + a.chunk, d.V);
-    // a group of the row: a logit in front of it or behind is none
+    // a group of the row: a logit in front of it or behind is none.  What lies between the first row's begin and the last one's end may be read.
+    const long front = -row * d.logits_stride, behind = (a.rows - 1 - row) * d.logits_stride + d.V;
     auto group = [&](int v) -> Vec {
-        if (v >= 0 && v + kGroup <= d.V) return *reinterpret_cast<const Vec*>(x + v);
         Vec w;
+        if (v >= front && v + kGroup <= behind) {
+            w = *reinterpret_cast<const Vec*>(x + v);
+#pragma unroll
+            for (int e = 0; e < kGroup; ++e) w[e] = (unsigned)(v + e) < (unsigned)d.V ? w[e] : (T)-INFINITY;
+        } else {
 #pragma unroll 1
-        for (int e = 0; e < kGroup; ++e) w[e] = v + e >= 0 && v + e < d.V ? x[v + e] : (T)-INFINITY;
+            for (int e = 0; e < kGroup; ++e) w[e] = (unsigned)(v + e) < (unsigned)d.V ? x[v + e] : (T)-INFINITY;
+        }
         return w;
     };
     auto ask = [&](int t, Vec (&w)[kBeamStep]) {
@@ -476,7 +483,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_history_kernel(nm_beam_desc
     follow(d, row, d.parents[row], d.tokens[row], blockIdx.y * kBeamThreads + threadIdx.x, gridDim.y * kBeamThreads);
 }
 
-constexpr long kBeamGroups = 1024;                             // workgroups of the first kernel, about
+constexpr long kBeamGroups = 512;                             // workgroups of the first kernel, about
 // Tokens of a history, and of a request's, that its workgroup of the second kernel copies, a wavefront to a history; more go to a kernel of their own.
 constexpr int kHistory = 1024;
 constexpr long kHistories = 8192;
@@ -556,6 +563,7 @@ int32_t nm_beam_select(const nm_beam_desc* d, void* ws, size_t ws_bytes, void* s
     for (int first = 0; first < rows; first += 65535) {
         BeamArgs b = a;
         const int n = std::min(rows - first, 65535);
+        b.rows = n;
         b.d.logits = static_cast<const char*>(d->logits) + first * d->logits_stride * dtype_bytes(d->logits_dtype);
         b.d.scores += first;
         if (b.d.weight) b.d.weight += first;
