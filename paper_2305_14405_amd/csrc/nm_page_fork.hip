@@ -1,11 +1,11 @@
 // Block tables of a new batch whose rows go on from rows of the old one (nm_page_fork).
 //
-// Nothing is counted from call to call: who refers to a page is found from the tables.  A word of the workspace for each page is marked by
-// every old row (that a row refers to it), by every row with children (that one refers to it in front of its partial last page), and counts the rows with
-// children whose partial last page it is.  From that follow which rows take a page of their own (a scan over the rows) and which pages become free (a
-// scan over the pages, in blocks).  Four kernels: clear the words and find every old row's first child; mark; decide for the rows, and count
-// the freed pages of every block; write the tables and the list.
-//   The marks are set by integer atomics, whose order does not change their result, and a mark that is there already is not set again.
+// Nothing is counted from call to call: who refers to a page is found from the tables.  Each page has marks: that an old row refers to it; that one with
+// children does so in front of its partial last page; and how many rows with children have it as that.  From them follow which rows take a page
+// of their own (a scan over the rows) and which pages become free (a scan over the pages).  The marks are set by integer atomics, whose order does not change their result.
+//   Small batches: one workgroup, marks in LDS, a chain of dependent steps.  Others: four kernels, marks in the workspace.  Clear them
+// and find every old row's first child; mark (a row leaves out what the row in front of it marks as well: hypotheses of a request share most of their
+// pages, and atomics on one word wait for one another); decide for the rows, and count the freed pages of every block; write the tables and the list.
 #include <algorithm>
 
 #include "nm_decode.h"
@@ -14,29 +14,35 @@ namespace nm {
 
 constexpr int kForkThreads = 256;
 constexpr int kForkBlocks = 1024;                  // of pages at most
+constexpr int kForkBlock = 4096;                   // pages of one at least
+constexpr int kRowThreads = 1024, kRows = NM_PLAN_MAX_REQUESTS / kRowThreads;   // the workgroup that decides for the rows
+// What one workgroup does alone: rows, entries of either table, pages, the list.
+constexpr int kSmallRows = 1024, kSmallEntries = 16384, kSmallPages = 65536, kSmallList = 65536;
 
 struct ForkArgs {
     nm_fork_desc d;
     int shift;
     int blocks, block;                             // of pages, and their length
     int list_blocks;
-    int* marks;                                    // [num_pages]
+    int* marks;                                    // [num_pages, up to a multiple of kRun]
     int* first;                                    // [B_in]: lowest-numbered child, B_out: none
+    int4* rows;                                    // [B_out]: parent (-1: none), its length, its partial last page (-1: none), whether this is its first child
     int* freed;                                    // [blocks]: pages that become free
     int* sums;                                     // [4]: flags of the rows, pages wanted, rows with a parent
 };
-enum { kOld = 1, kFull = 2, kPart = 4 };           // kPart and above: how many rows with children have it as their partial last page
+enum { kOld = 1, kFull = 2, kKept = 4, kPart = 8 };   // kKept: by keep; kPart and above: how many rows with children have it as their partial last page
+constexpr int kRun = 16;                           // neighbouring pages of a thread
 
 // Tokens of an old row, 0 where its length is bad.
-__device__ __forceinline__ int length_of(const ForkArgs& a, int r, bool* bad = nullptr)
-{
-    const int n = a.d.lens[r];
-    const bool off = n < 0 || n > (long)a.d.max_pages << a.shift;
-    if (bad) *bad = off;
-    return off ? 0 : n;
-}
+__device__ __forceinline__ int good_length(const ForkArgs& a, int n) { return n < 0 || n > (long)a.d.max_pages << a.shift ? 0 : n; }
+__device__ __forceinline__ int length_of(const ForkArgs& a, int r) { return good_length(a, a.d.lens[r]); }
+__device__ __forceinline__ int held_of(const ForkArgs& a, int n) { return (int)(((long)n + a.d.page_size - 1) >> a.shift); }
 __device__ __forceinline__ bool is_page(const ForkArgs& a, int e) { return e >= 0 && e < a.d.num_pages; }
 __device__ __forceinline__ bool is_row(const ForkArgs& a, int p) { return p >= 0 && p < a.d.B_in; }
+
+// By a page's marks: whether its one user with children may keep it as its partial last page, and whether it becomes free.
+__device__ __forceinline__ bool stays(int m) { return !(m & (kFull | kKept)) && m / kPart == 1; }
+__device__ __forceinline__ bool goes(int m) { return (m & (kOld | kFull | kKept)) == kOld && m / kPart != 1; }
 
 // Sums over the workgroup's threads in front, and over all.  s: LDS of a number for each wavefront.
 struct Sums { int before, all; };
@@ -53,121 +59,174 @@ __device__ __forceinline__ Sums scan(int mine, int* s)
     if (lane == 63) s[wave] = in;
     __syncthreads();
     Sums r{in - mine, 0};
+#pragma unroll
     for (int w = 0; w < kThreads / 64; ++w) {
-        if (w < wave) r.before += s[w];
-        r.all += s[w];
+        const int x = s[w];
+        r.before += w < wave ? x : 0;
+        r.all += x;
     }
     return r;
 }
 
-__global__ __launch_bounds__(kForkThreads) void fork_clear_kernel(ForkArgs a)
+// Flags of a call from those of its lengths, the pages wanted and the pages that become free; where the list begins behind it.
+__device__ __forceinline__ int all_flags(const ForkArgs& a, int flags, int begin, int wanted, int freed)
+{
+    if (begin >= 0 && begin <= a.d.n_free) {
+        if ((long)begin + wanted > a.d.n_free) flags |= NM_FORK_NO_PAGES;
+        if ((long)begin + wanted - freed < 0) flags |= NM_FORK_LIST_FULL;
+    }
+    return flags;
+}
+__device__ __forceinline__ void report(const ForkArgs& a, int flags, int wanted, int freed, int parents, int end)
+{
+    a.d.status[0] = flags;
+    a.d.status[1] = wanted;
+    a.d.status[2] = freed;
+    a.d.status[3] = parents;
+    *a.d.free_end = end;
+}
+
+__global__ __launch_bounds__(kRowThreads) void fork_clear_kernel(ForkArgs a)
 {
     __shared__ int s_first[NM_PLAN_MAX_REQUESTS];
     if (blockIdx.x) {
-        for (long i = (long)(blockIdx.x - 1) * kForkThreads + threadIdx.x; i < a.d.num_pages; i += (long)(gridDim.x - 1) * kForkThreads) a.marks[i] = 0;
+        const long n = ((long)a.d.num_pages + kRun - 1) / kRun * kRun;
+        for (long i = (long)(blockIdx.x - 1) * kRowThreads + threadIdx.x; i < n; i += (long)(gridDim.x - 1) * kRowThreads)
+            a.marks[i] = a.d.keep && i < a.d.num_pages && a.d.keep[i] ? kKept : 0;
         return;
     }
-    for (int r = threadIdx.x; r < a.d.B_in; r += kForkThreads) s_first[r] = a.d.B_out;
+    for (int r = threadIdx.x; r < a.d.B_in; r += kRowThreads) s_first[r] = a.d.B_out;
     __syncthreads();
-    for (int b = threadIdx.x; b < a.d.B_out; b += kForkThreads) {
-        const int p = a.d.parents[b];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int b = threadIdx.x + i * kRowThreads, p = b < a.d.B_out ? a.d.parents[b] : -1;
         if (is_row(a, p)) atomicMin(&s_first[p], b);
     }
     __syncthreads();
-    for (int r = threadIdx.x; r < a.d.B_in; r += kForkThreads) a.first[r] = s_first[r];
+    for (int r = threadIdx.x; r < a.d.B_in; r += kRowThreads) a.first[r] = s_first[r];
 }
 
-// A workgroup to an old row.
+// Workgroups: of new rows, what is to be decided for them, a thread to each; then of old rows, which set their marks, a wavefront to each.
 __global__ __launch_bounds__(kForkThreads) void fork_mark_kernel(ForkArgs a)
 {
-    const int r = blockIdx.x, n = length_of(a, r), whole = n >> a.shift, held = whole + (n & (a.d.page_size - 1) ? 1 : 0);
-    const bool lives = a.first[r] < a.d.B_out;
-    for (int i = threadIdx.x; i < held; i += kForkThreads) {
-        const int page = a.d.block_table[r * a.d.table_stride + i];
-        if (!is_page(a, page)) continue;
-        const int mark = kOld | (lives && i < whole ? kFull : 0);
-        if ((__hip_atomic_load(a.marks + page, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) & mark) != mark) atomicOr(a.marks + page, mark);
-        if (lives && i >= whole) atomicAdd(a.marks + page, kPart);
+    const nm_fork_desc& d = a.d;
+    const int news = (d.B_out + kForkThreads - 1) / kForkThreads, lane = threadIdx.x & 63;
+    if ((int)blockIdx.x < news) {
+        const int b = blockIdx.x * kForkThreads + threadIdx.x;
+        if (b >= d.B_out) return;
+        const int p = d.parents[b];
+        if (!is_row(a, p)) {
+            a.rows[b] = make_int4(-1, 0, -1, 0);
+            return;
+        }
+        const int n = length_of(a, p), page = n & (d.page_size - 1) ? d.block_table[p * d.table_stride + (n >> a.shift)] : -1;
+        a.rows[b] = make_int4(p, n, is_page(a, page) ? page : -1, a.first[p] == b);
+        return;
+    }
+    const int r = ((int)blockIdx.x - news) * (kForkThreads / 64) + (int)(threadIdx.x / 64), q = max(r - 1, 0);
+    if (r >= d.B_in) return;
+    const int n = length_of(a, r), whole = n >> a.shift, held = held_of(a, n);
+    const bool lives = a.first[r] < d.B_out;
+    // of the row in front: how many entries it marks, and how many of them as kFull
+    const int n_front = r ? length_of(a, q) : 0, held_front = held_of(a, n_front), full_front = a.first[q] < d.B_out ? n_front >> a.shift : 0;
+    const int* row = d.block_table + r * d.table_stride;
+    const int* front = d.block_table + q * d.table_stride;
+    constexpr int kAtOnce = 4;
+    for (int i0 = lane; i0 < held; i0 += 64 * kAtOnce) {
+        int page[kAtOnce], same[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int i = min(i0 + 64 * k, held - 1);
+            page[k] = row[i];
+            same[k] = front[held_front ? min(i, held_front - 1) : 0];   // (a row without entries: its first is not looked at)
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int i = i0 + 64 * k;
+            if (i >= held || !is_page(a, page[k])) continue;
+            int mark = kOld | (lives && i < whole ? kFull : 0);
+            if (i < held_front && same[k] == page[k]) mark &= i < full_front ? 0 : ~kOld;
+            if (mark) atomicOr(a.marks + page[k], mark);
+            if (lives && i >= whole) atomicAdd(a.marks + page[k], kPart);
+        }
     }
 }
 
-__device__ __forceinline__ bool becomes_free(const ForkArgs& a, int page)
+// A run of pages from p on: those that become free, as bits.
+__device__ __forceinline__ unsigned freed_of(const ForkArgs& a, long p)
 {
-    const int m = a.marks[page];
-    return (m & (kOld | kFull)) == kOld && m / kPart != 1 && !(a.d.keep && a.d.keep[page]);
+    unsigned bits = 0;
+#pragma unroll
+    for (int i = 0; i < kRun; i += 4) {
+        const int4 m = *reinterpret_cast<const int4*>(a.marks + p + i);
+        bits |= (goes(m.x) ? 1u : 0u) << i | (goes(m.y) ? 2u : 0u) << i | (goes(m.z) ? 4u : 0u) << i | (goes(m.w) ? 8u : 0u) << i;
+    }
+    return bits;
 }
 
 // Workgroup 0: the rows.  The others: a block of pages each.
-__global__ __launch_bounds__(kForkThreads) void fork_decide_kernel(ForkArgs a)
+__global__ __launch_bounds__(kRowThreads) void fork_decide_kernel(ForkArgs a)
 {
-    __shared__ int s[kForkThreads / 64];
+    __shared__ int s[kRowThreads / 64];
     const nm_fork_desc& d = a.d;
+    const int tid = threadIdx.x;
     if (blockIdx.x) {
         const int block = blockIdx.x - 1;
         const long p0 = (long)block * a.block, p1 = min(p0 + a.block, (long)d.num_pages);
         int n = 0;
-        for (long p = p0 + threadIdx.x; p < p1; p += kForkThreads) n += becomes_free(a, (int)p);
-        const Sums all = scan<kForkThreads>(n, s);
-        if (threadIdx.x == 0) a.freed[block] = all.all;
+        for (long p = p0 + tid * kRun; p < p1; p += kRowThreads * kRun) n += __popc(freed_of(a, p));
+        const Sums all = scan<kRowThreads>(n, s);
+        if (tid == 0) a.freed[block] = all.all;
         return;
     }
     const int begin = *d.free_begin;
     bool bad = begin < 0 || begin > d.n_free;
-    for (int r = threadIdx.x; r < d.B_in; r += kForkThreads) {
-        bool off;
-        length_of(a, r, &off);
-        bad |= off;
+    for (int r = tid; r < d.B_in; r += kRowThreads) {
+        const int n = d.lens[r];
+        bad |= n != good_length(a, n);
     }
-    // a thread has a run of rows
-    const int per = (d.B_out + kForkThreads - 1) / kForkThreads, b0 = min((int)threadIdx.x * per, d.B_out), b1 = min(b0 + per, d.B_out);
+    // a thread has neighbouring rows, whose loads are under way together
+    const int b0 = tid * kRows;
+    int4 row[kRows];
     int wants = 0, rows = 0;
-    for (int pass = 0; pass < 2; ++pass) {
-        int at = 0;
-        if (pass) {
-            const Sums pages = scan<kForkThreads>(wants, s), parents = scan<kForkThreads>(rows, s);
-            const bool any = __syncthreads_or(bad);
-            at = pages.before;
-            if (threadIdx.x == 0) {
-                a.sums[0] = any ? NM_FORK_BAD_LENGTH : 0;
-                a.sums[1] = pages.all;
-                a.sums[2] = parents.all;
-            }
-        }
-        for (int b = b0; b < b1; ++b) {
-            const int p = d.parents[b];
-            int src = -1, dst = -1, slots = 0;
-            if (is_row(a, p)) {
-                const int n = length_of(a, p);
-                if (!pass) ++rows;
-                if (n & (d.page_size - 1)) {
-                    const int page = d.block_table[p * d.table_stride + (n >> a.shift)];
-                    if (is_page(a, page)) {
-                        const int m = a.marks[page];
-                        if (a.first[p] != b || (m & kFull) || m / kPart != 1 || (d.keep && d.keep[page])) {
-                            if (!pass) ++wants;
-                            src = page;
-                            slots = n & (d.page_size - 1);
-                            const long i = (long)begin + at++;
-                            if (i >= 0 && i < d.n_free) dst = d.free_pages[i];
-                        }
-                    }
-                }
-            }
-            if (pass) {
-                d.copy_src[b] = src;
-                d.copy_dst[b] = dst;
-                d.copy_slots[b] = slots;
-            }
-        }
+    bool need[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) row[i] = b0 + i < d.B_out ? a.rows[b0 + i] : make_int4(-1, 0, -1, 0);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int m = row[i].z >= 0 ? a.marks[row[i].z] : 0;
+        need[i] = row[i].z >= 0 && (!row[i].w || !stays(m));
+        wants += need[i];
+        rows += row[i].x >= 0;
     }
+    const Sums pages = scan<kRowThreads>(wants, s), parents = scan<kRowThreads>(rows, s);
+    const bool any = __syncthreads_or(bad);
+    if (tid == 0) {
+        a.sums[0] = any ? NM_FORK_BAD_LENGTH : 0;
+        a.sums[1] = pages.all;
+        a.sums[2] = parents.all;
+    }
+    long at = (long)begin + pages.before;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i)
+        if (b0 + i < d.B_out) {
+            d.copy_src[b0 + i] = need[i] ? row[i].z : -1;
+            d.copy_dst[b0 + i] = need[i] && at >= 0 && at < d.n_free ? d.free_pages[at] : -1;
+            d.copy_slots[b0 + i] = need[i] ? row[i].y & (d.page_size - 1) : 0;
+            at += need[i];
+        }
 }
 
-// Workgroups: rows, then blocks of pages, then blocks of the list.
+// Workgroups: blocks of pages, then rows, a wavefront to each, then blocks of the list.
 __global__ __launch_bounds__(kForkThreads) void fork_write_kernel(ForkArgs a)
 {
     __shared__ int s[kForkThreads / 64];
     const nm_fork_desc& d = a.d;
-    const int block = (int)blockIdx.x - d.B_out, tid = threadIdx.x;
+    const int block = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+    // asked for ahead of what decides whether they are written
+    const int b = (block - a.blocks) * (kForkThreads / 64) + tid / 64;
+    const bool pages = block < a.blocks, rows = !pages && block - a.blocks < (d.B_out + kForkThreads / 64 - 1) / (kForkThreads / 64);
+    const int4 row = rows && b < d.B_out ? a.rows[b] : make_int4(-1, 0, -1, 0);
     int before = 0, all = 0;                       // freed pages of the blocks in front of this one, and of all
     for (int i = tid; i < a.blocks; i += kForkThreads) {
         const int n = a.freed[i];
@@ -175,51 +234,123 @@ __global__ __launch_bounds__(kForkThreads) void fork_write_kernel(ForkArgs a)
         before += i < block ? n : 0;
     }
     all = scan<kForkThreads>(all, s).all;
-    const int begin = *d.free_begin, wanted = a.sums[1];
-    int flags = a.sums[0];
-    if (begin >= 0 && begin <= d.n_free) {
-        if ((long)begin + wanted > d.n_free) flags |= NM_FORK_NO_PAGES;
-        if ((long)begin + wanted - all < 0) flags |= NM_FORK_LIST_FULL;
-    }
+    const int begin = *d.free_begin, wanted = a.sums[1], flags = all_flags(a, a.sums[0], begin, wanted, all);
     const bool ok = flags == 0;
     const int end = ok ? begin + wanted - all : begin;
-
-    if (blockIdx.x == 0 && tid == 0) {
-        d.status[0] = flags;
-        d.status[1] = wanted;
-        d.status[2] = all;
-        d.status[3] = a.sums[2];
-        *d.free_end = end;
-    }
-    if (block < 0) {
-        const int b = blockIdx.x, p = d.parents[b];
-        const bool lives = ok && is_row(a, p);
-        const int n = lives ? length_of(a, p) : 0, held = (int)(((long)n + d.page_size - 1) >> a.shift);
-        const int dst = lives ? d.copy_dst[b] : -1, src = lives ? d.copy_src[b] : -1;
-        __syncthreads();
-        for (int i = tid; i < held; i += kForkThreads)
-            d.table_out[b * d.table_out_stride + i] = src >= 0 && i == n >> a.shift ? dst : d.block_table[p * d.table_stride + i];
-        if (tid == 0) {
+    if (block == 0 && tid == 0) report(a, flags, wanted, all, a.sums[2], end);
+    if (pages) {
+        if (!ok) return;
+        long at = (long)end + scan<kForkThreads>(before, s).all;
+        const long p0 = (long)block * a.block, p1 = min(p0 + a.block, (long)d.num_pages);
+        for (long p = p0; p < p1; p += kForkThreads * kRun) {
+            unsigned bits = p + tid * kRun < p1 ? freed_of(a, p + tid * kRun) : 0;
+            const Sums sums = scan<kForkThreads>(__popc(bits), s);
+            for (long to = at + sums.before; bits; bits &= bits - 1) d.free_out[to++] = (int)p + tid * kRun + __ffs((int)bits) - 1;
+            at += sums.all;
+        }
+    } else if (rows) {
+        if (b >= d.B_out) return;
+        const int n = ok ? row.y : 0, held = held_of(a, n);
+        const int dst = d.copy_dst[b], src = d.copy_src[b];
+        const int* from = d.block_table + (long)max(row.x, 0) * d.table_stride;
+        int* to = d.table_out + b * d.table_out_stride;
+        constexpr int kAtOnce = 4;
+        for (int i0 = lane; i0 < held; i0 += 64 * kAtOnce) {
+            int x[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) x[k] = from[min(i0 + 64 * k, held - 1)];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k)
+                if (i0 + 64 * k < held) to[i0 + 64 * k] = src >= 0 && i0 + 64 * k == n >> a.shift ? dst : x[k];
+        }
+        if (lane == 0) {
             d.lens_out[b] = n;
             if (!ok) {
                 d.copy_src[b] = d.copy_dst[b] = -1;
                 d.copy_slots[b] = 0;
             }
         }
-    } else if (block < a.blocks) {
-        if (!ok) return;
-        long at = (long)end + scan<kForkThreads>(before, s).all;
-        const long p0 = (long)block * a.block, p1 = min(p0 + a.block, (long)d.num_pages);
-        for (long p = p0; p < p1; p += kForkThreads) {
-            const bool goes = p + tid < p1 && becomes_free(a, (int)(p + tid));
-            const Sums sums = scan<kForkThreads>(goes, s);
-            if (goes) d.free_out[at + sums.before] = (int)(p + tid);
-            at += sums.all;
-        }
     } else if (d.free_out != d.free_pages && begin >= 0) {
-        for (long i = (long)begin + (ok ? wanted : 0) + (long)(block - a.blocks) * kForkThreads + tid; i < d.n_free; i += (long)a.list_blocks * kForkThreads)
+        const int first = block - a.blocks - (d.B_out + kForkThreads / 64 - 1) / (kForkThreads / 64);
+        for (long i = (long)begin + (ok ? wanted : 0) + (long)first * kForkThreads + tid; i < d.n_free; i += (long)a.list_blocks * kForkThreads)
             d.free_out[i] = d.free_pages[i];
     }
+}
+
+// All of it in one workgroup.  A page's marks are four bits in LDS: kOld, kFull, one row's partial last page, and another's.
+__global__ __launch_bounds__(kRowThreads) void fork_small_kernel(ForkArgs a)
+{
+    extern __shared__ unsigned s_marks[];          // eight pages to a word
+    __shared__ int s_first[kSmallRows], s_n[kSmallRows], s_src[kSmallRows], s_dst[kSmallRows], s[kRowThreads / 64];
+    const nm_fork_desc& d = a.d;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, words = (d.num_pages + 7) / 8;
+    const int begin = *d.free_begin;
+    // a thread to a row, of either batch
+    const int raw = tid < d.B_in ? d.lens[tid] : 0, parent = tid < d.B_out ? d.parents[tid] : -1;
+    const bool child = is_row(a, parent);
+    for (int i = tid; i < words; i += kRowThreads) s_marks[i] = 0;
+    s_first[tid] = d.B_out;
+    s_n[tid] = good_length(a, raw);
+    const bool bad = __syncthreads_or(raw != good_length(a, raw) || begin < 0 || begin > d.n_free);
+    if (child) atomicMin(&s_first[parent], tid);
+    __syncthreads();
+    auto marks_of = [&](int page) {
+        const unsigned m = s_marks[page / 8] >> page % 8 * 4;
+        return (int)(m & (kOld | kFull)) + (int)((m >> 2 & 1) + (m >> 3 & 1)) * kPart + (d.keep && d.keep[page] ? kKept : 0);
+    };
+    for (int r = wave; r < d.B_in; r += kRowThreads / 64) {
+        const int n = s_n[r], whole = n >> a.shift, held = held_of(a, n);
+        const bool lives = s_first[r] < d.B_out;
+        for (int i = lane; i < held; i += 64) {
+            const int page = d.block_table[r * d.table_stride + i];
+            if (!is_page(a, page)) continue;
+            const int at = page % 8 * 4;
+            const bool part = lives && i >= whole;
+            const unsigned was = atomicOr(&s_marks[page / 8], (unsigned)(kOld | (part ? 4 : lives ? kFull : 0)) << at);
+            if (part && (was >> at & 4)) atomicOr(&s_marks[page / 8], 8u << at);
+        }
+    }
+    __syncthreads();
+    // the rows
+    const int n = child ? s_n[parent] : 0;
+    int page = -1;
+    if (n & (d.page_size - 1)) page = d.block_table[parent * d.table_stride + (n >> a.shift)];
+    const bool need = is_page(a, page) && (s_first[parent] != tid || !stays(marks_of(page)));
+    const Sums wanted = scan<kRowThreads>(need, s), parents = scan<kRowThreads>(child, s);
+    const long from = (long)begin + wanted.before;
+    const int dst = need && from >= 0 && from < d.n_free ? d.free_pages[from] : -1;
+    // the pages, a run of words to a thread
+    const int each = (words + kRowThreads - 1) / kRowThreads, w0 = min(tid * each, words), w1 = min(w0 + each, words);
+    auto freed = [&](int p) { return p < d.num_pages && s_marks[p / 8] >> p % 8 * 4 & kOld && goes(marks_of(p)); };
+    int mine = 0;
+    for (int p = w0 * 8; p < w1 * 8; ++p) mine += freed(p);
+    const Sums gone = scan<kRowThreads>(mine, s);
+    const int flags = all_flags(a, bad ? NM_FORK_BAD_LENGTH : 0, begin, wanted.all, gone.all);
+    const bool ok = flags == 0;
+    const int end = ok ? begin + wanted.all - gone.all : begin;
+    if (tid == 0) report(a, flags, wanted.all, gone.all, parents.all, end);
+    if (tid < d.B_out) {
+        d.lens_out[tid] = ok ? n : 0;
+        d.copy_src[tid] = ok && need ? page : -1;
+        d.copy_dst[tid] = ok ? dst : -1;
+        d.copy_slots[tid] = ok && need ? n & (d.page_size - 1) : 0;
+    }
+    s_src[tid] = need ? n >> a.shift : -1;         // the entry that is another
+    s_dst[tid] = dst;
+    __syncthreads();                               // also: what is taken has been read, where the list is written in place
+    if (ok) {
+        int to = end + gone.before;
+        for (int p = w0 * 8; mine && p < w1 * 8; ++p)
+            if (freed(p)) d.free_out[to++] = p;
+        for (int b = wave; b < d.B_out; b += kRowThreads / 64) {
+            const int p = d.parents[b];
+            if (!is_row(a, p)) continue;
+            const int held = held_of(a, s_n[p]);
+            for (int i = lane; i < held; i += 64) d.table_out[b * d.table_out_stride + i] = i == s_src[b] ? s_dst[b] : d.block_table[p * d.table_stride + i];
+        }
+    }
+    if (d.free_out != d.free_pages && begin >= 0)
+        for (long i = (long)begin + (ok ? wanted.all : 0) + tid; i < d.n_free; i += kRowThreads) d.free_out[i] = d.free_pages[i];
 }
 
 static int32_t plan_fork(const nm_fork_desc* d, ForkArgs* a, size_t* bytes, const char* what)
@@ -235,10 +366,10 @@ static int32_t plan_fork(const nm_fork_desc* d, ForkArgs* a, size_t* bytes, cons
     *a = ForkArgs{};
     a->d = *d;
     a->shift = shift;
-    a->block = std::max(4096, (d->num_pages + kForkBlocks - 1) / kForkBlocks);
+    a->block = std::max(kForkBlock, ((d->num_pages + kForkBlocks - 1) / kForkBlocks + kRun - 1) / kRun * kRun);
     a->blocks = (d->num_pages + a->block - 1) / a->block;
     a->list_blocks = std::min((d->n_free + 8 * kForkThreads - 1) / (8 * kForkThreads), 512);
-    *bytes = sizeof(int) * ((size_t)d->num_pages + d->B_in + a->blocks + 4);
+    *bytes = sizeof(int) * (((size_t)d->num_pages + kRun - 1) / kRun * kRun + 4 * (size_t)d->B_out + d->B_in + a->blocks + 4);
     return NM_OK;
 }
 
@@ -283,15 +414,21 @@ int32_t nm_page_fork(const nm_fork_desc* d, void* ws, size_t ws_bytes, void* str
     if (!ws || ws_bytes < need) return fail(NM_ERR_WORKSPACE, "nm_page_fork: workspace of %zu bytes needed, %zu given", need, ws ? ws_bytes : (size_t)0);
     if (!aligned(ws, 256)) return fail(NM_ERR_WORKSPACE, "nm_page_fork: workspace must be 256-byte aligned");
     a.marks = static_cast<int*>(ws);
-    a.first = a.marks + d->num_pages;
+    a.rows = reinterpret_cast<int4*>(a.marks + ((size_t)d->num_pages + kRun - 1) / kRun * kRun);
+    a.first = reinterpret_cast<int*>(a.rows + d->B_out);
     a.freed = a.first + d->B_in;
     a.sums = a.freed + a.blocks;
     const hipStream_t s = (hipStream_t)stream;
     const dim3 threads(kForkThreads);
-    queue_kernel(fork_clear_kernel, dim3(1 + std::min((d->num_pages + 4 * kForkThreads - 1) / (4 * kForkThreads), 2048)), threads, 0, s, a);
-    if (d->B_in) queue_kernel(fork_mark_kernel, dim3(d->B_in), threads, 0, s, a);
-    queue_kernel(fork_decide_kernel, dim3(1 + a.blocks), threads, 0, s, a);
-    queue_kernel(fork_write_kernel, dim3(std::max(1, d->B_out + a.blocks + a.list_blocks)), threads, 0, s, a);
+    if (std::max(d->B_in, d->B_out) <= kSmallRows && (long)std::max(d->B_in, d->B_out) * d->max_pages <= kSmallEntries && d->num_pages <= kSmallPages && d->n_free <= kSmallList) {
+        queue_kernel(fork_small_kernel, dim3(1), dim3(kRowThreads), sizeof(unsigned) * ((d->num_pages + 7) / 8), s, a);
+        return check_hip(hipGetLastError(), "nm_page_fork launch");
+    }
+    const int per = kForkThreads / 64, news = (d->B_out + kForkThreads - 1) / kForkThreads, olds = (d->B_in + per - 1) / per;
+    queue_kernel(fork_clear_kernel, dim3(1 + std::min((d->num_pages + kRowThreads - 1) / kRowThreads, 1024)), dim3(kRowThreads), 0, s, a);
+    if (news + olds) queue_kernel(fork_mark_kernel, dim3(news + olds), threads, 0, s, a);
+    queue_kernel(fork_decide_kernel, dim3(1 + a.blocks), dim3(kRowThreads), 0, s, a);
+    queue_kernel(fork_write_kernel, dim3(std::max(1, a.blocks + (d->B_out + per - 1) / per + a.list_blocks)), threads, 0, s, a);
     return check_hip(hipGetLastError(), "nm_page_fork launch");
 }
 
