@@ -15,7 +15,8 @@ namespace nm {
 constexpr int kForkThreads = 256;
 constexpr int kForkBlocks = 1024;                  // of pages at most
 constexpr int kForkBlock = 4096;                   // pages of one at least
-constexpr int kRowThreads = 1024, kRows = NM_PLAN_MAX_REQUESTS / kRowThreads;   // the workgroup that decides for the rows
+constexpr int kRowThreads = 1024, kRows = NM_PLAN_MAX_REQUESTS / kRowThreads;
+constexpr int kRowBlocks = NM_PLAN_MAX_REQUESTS / kForkThreads;   // of rows at most
 // What one workgroup does alone: rows, entries of either table, pages, the list.
 constexpr int kSmallRows = 1024, kSmallEntries = 16384, kSmallPages = 65536, kSmallList = 65536;
 
@@ -24,11 +25,16 @@ struct ForkArgs {
     int shift;
     int blocks, block;                             // of pages, and their length
     int list_blocks;
-    int* marks;                                    // [num_pages, up to a multiple of kRun]
+    int* marks;                                    // [num_pages, up to a multiple of kRun]: kKept, and kPart for every row with children that has it as its last
+    uint8_t* old;                                  // [2, likewise]: an old row refers to the page; one with children does, in front of its partial last page
+    long padded;                                   // num_pages up to a multiple of kRun
     int* first;                                    // [B_in]: lowest-numbered child, B_out: none
-    int4* rows;                                    // [B_out]: parent (-1: none), its length, its partial last page (-1: none), whether this is its first child
+    int4* rows;                                    // [B_out]: parent (-1: none), its length, its partial last page (-1: none), whether this is its first child;
+                                                   // then: its place among its block's rows that take a page, -1 where it does not
+    int* taken;                                    // [B_out]: what the list holds from its begin on (which may be written over before it is asked for)
     int* freed;                                    // [blocks]: pages that become free
-    int* sums;                                     // [4]: flags of the rows, pages wanted, rows with a parent
+    int* sums;                                     // [kRowBlocks]: of a block of rows, pages wanted, and rows with a parent from bit 16 on
+    int* bad;                                      // [1]: whether a length is bad
 };
 enum { kOld = 1, kFull = 2, kKept = 4, kPart = 8 };   // kKept: by keep; kPart and above: how many rows with children have it as their partial last page
 constexpr int kRun = 16;                           // neighbouring pages of a thread
@@ -90,9 +96,9 @@ __global__ __launch_bounds__(kRowThreads) void fork_clear_kernel(ForkArgs a)
 {
     __shared__ int s_first[NM_PLAN_MAX_REQUESTS];
     if (blockIdx.x) {
-        const long n = ((long)a.d.num_pages + kRun - 1) / kRun * kRun;
-        for (long i = (long)(blockIdx.x - 1) * kRowThreads + threadIdx.x; i < n; i += (long)(gridDim.x - 1) * kRowThreads)
-            a.marks[i] = a.d.keep && i < a.d.num_pages && a.d.keep[i] ? kKept : 0;
+        const long first = (long)(blockIdx.x - 1) * kRowThreads + threadIdx.x, step = (long)(gridDim.x - 1) * kRowThreads;
+        for (long i = first; i < a.padded; i += step) a.marks[i] = a.d.keep && i < a.d.num_pages && a.d.keep[i] ? kKept : 0;
+        for (long i = first; i < a.padded / 2; i += step) reinterpret_cast<int*>(a.old)[i] = 0;
         return;
     }
     for (int r = threadIdx.x; r < a.d.B_in; r += kRowThreads) s_first[r] = a.d.B_out;
@@ -115,6 +121,8 @@ __global__ __launch_bounds__(kForkThreads) void fork_mark_kernel(ForkArgs a)
         const int b = blockIdx.x * kForkThreads + threadIdx.x;
         if (b >= d.B_out) return;
         const int p = d.parents[b];
+        const long at = (long)*d.free_begin + b;
+        a.taken[b] = at >= 0 && at < d.n_free ? d.free_pages[at] : -1;
         if (!is_row(a, p)) {
             a.rows[b] = make_int4(-1, 0, -1, 0);
             return;
@@ -146,7 +154,9 @@ __global__ __launch_bounds__(kForkThreads) void fork_mark_kernel(ForkArgs a)
             if (i >= held || !is_page(a, page[k])) continue;
             int mark = kOld | (lives && i < whole ? kFull : 0);
             if (i < held_front && same[k] == page[k]) mark &= i < full_front ? 0 : ~kOld;
-            if (mark) atomicOr(a.marks + page[k], mark);
+            // one value, whoever writes it
+            if (mark & kOld) __hip_atomic_store(a.old + page[k], (uint8_t)1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (mark & kFull) __hip_atomic_store(a.old + a.padded + page[k], (uint8_t)1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             if (lives && i >= whole) atomicAdd(a.marks + page[k], kPart);
         }
     }
@@ -155,66 +165,48 @@ __global__ __launch_bounds__(kForkThreads) void fork_mark_kernel(ForkArgs a)
 // A run of pages from p on: those that become free, as bits.
 __device__ __forceinline__ unsigned freed_of(const ForkArgs& a, long p)
 {
+    const v4i old = *reinterpret_cast<const v4i*>(a.old + p), full = *reinterpret_cast<const v4i*>(a.old + a.padded + p);
     unsigned bits = 0;
 #pragma unroll
     for (int i = 0; i < kRun; i += 4) {
-        const int4 m = *reinterpret_cast<const int4*>(a.marks + p + i);
-        bits |= (goes(m.x) ? 1u : 0u) << i | (goes(m.y) ? 2u : 0u) << i | (goes(m.z) ? 4u : 0u) << i | (goes(m.w) ? 8u : 0u) << i;
+        const v4i m = *reinterpret_cast<const v4i*>(a.marks + p + i);
+        const int free = old[i / 4] & ~full[i / 4];            // a byte each, 0 or 1
+#pragma unroll
+        for (int k = 0; k < 4; ++k) bits |= free >> 8 * k & 1 && !(m[k] & kKept) && m[k] / kPart != 1 ? 1u << (i + k) : 0u;
     }
     return bits;
 }
 
-// Workgroup 0: the rows.  The others: a block of pages each.
-__global__ __launch_bounds__(kRowThreads) void fork_decide_kernel(ForkArgs a)
+// Workgroups: of blocks of pages, then of rows; and one that looks at the lengths.
+__global__ __launch_bounds__(kForkThreads) void fork_decide_kernel(ForkArgs a)
 {
-    __shared__ int s[kRowThreads / 64];
+    __shared__ int s[kForkThreads / 64];
     const nm_fork_desc& d = a.d;
-    const int tid = threadIdx.x;
-    if (blockIdx.x) {
-        const int block = blockIdx.x - 1;
+    const int tid = threadIdx.x, block = blockIdx.x, news = (d.B_out + kForkThreads - 1) / kForkThreads;
+    if (block < a.blocks) {
         const long p0 = (long)block * a.block, p1 = min(p0 + a.block, (long)d.num_pages);
         int n = 0;
-        for (long p = p0 + tid * kRun; p < p1; p += kRowThreads * kRun) n += __popc(freed_of(a, p));
-        const Sums all = scan<kRowThreads>(n, s);
+        for (long p = p0 + tid * kRun; p < p1; p += kForkThreads * kRun) n += __popc(freed_of(a, p));
+        const Sums all = scan<kForkThreads>(n, s);
         if (tid == 0) a.freed[block] = all.all;
-        return;
-    }
-    const int begin = *d.free_begin;
-    bool bad = begin < 0 || begin > d.n_free;
-    for (int r = tid; r < d.B_in; r += kRowThreads) {
-        const int n = d.lens[r];
-        bad |= n != good_length(a, n);
-    }
-    // a thread has neighbouring rows, whose loads are under way together
-    const int b0 = tid * kRows;
-    int4 row[kRows];
-    int wants = 0, rows = 0;
-    bool need[kRows];
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) row[i] = b0 + i < d.B_out ? a.rows[b0 + i] : make_int4(-1, 0, -1, 0);
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        const int m = row[i].z >= 0 ? a.marks[row[i].z] : 0;
-        need[i] = row[i].z >= 0 && (!row[i].w || !stays(m));
-        wants += need[i];
-        rows += row[i].x >= 0;
-    }
-    const Sums pages = scan<kRowThreads>(wants, s), parents = scan<kRowThreads>(rows, s);
-    const bool any = __syncthreads_or(bad);
-    if (tid == 0) {
-        a.sums[0] = any ? NM_FORK_BAD_LENGTH : 0;
-        a.sums[1] = pages.all;
-        a.sums[2] = parents.all;
-    }
-    long at = (long)begin + pages.before;
-#pragma unroll
-    for (int i = 0; i < kRows; ++i)
-        if (b0 + i < d.B_out) {
-            d.copy_src[b0 + i] = need[i] ? row[i].z : -1;
-            d.copy_dst[b0 + i] = need[i] && at >= 0 && at < d.n_free ? d.free_pages[at] : -1;
-            d.copy_slots[b0 + i] = need[i] ? row[i].y & (d.page_size - 1) : 0;
-            at += need[i];
+    } else if (block - a.blocks < news) {
+        const int b = (block - a.blocks) * kForkThreads + tid;
+        const int4 row = b < d.B_out ? a.rows[b] : make_int4(-1, 0, -1, 0);
+        bool need = false;
+        if (row.z >= 0) need = !row.w || !stays(a.marks[row.z] | (a.old[a.padded + row.z] ? kFull : 0));
+        const Sums sums = scan<kForkThreads>((int)need | (int)(row.x >= 0) << 16, s);
+        if (b < d.B_out) a.rows[b].w = need ? sums.before & 0xffff : -1;
+        if (tid == 0) a.sums[block - a.blocks] = sums.all;
+    } else {
+        const int begin = *d.free_begin;
+        bool bad = begin < 0 || begin > d.n_free;
+        for (int r = tid; r < d.B_in; r += kForkThreads) {
+            const int n = d.lens[r];
+            bad |= n != good_length(a, n);
         }
+        bad = __syncthreads_or(bad);
+        if (tid == 0) *a.bad = bad;
+    }
 }
 
 // Workgroups: blocks of pages, then rows, a wavefront to each, then blocks of the list.
@@ -233,11 +225,14 @@ __global__ __launch_bounds__(kForkThreads) void fork_write_kernel(ForkArgs a)
         all += n;
         before += i < block ? n : 0;
     }
+    // pages that rows want, and rows with a parent; what the blocks in front of this wavefront's row want
+    const int sum = lane * kForkThreads < d.B_out ? a.sums[lane] : 0, sums = group_reduce<64>(sum, AddI32{});
+    const int front = group_reduce<64>(lane < b / kForkThreads ? sum & 0xffff : 0, AddI32{});
     all = scan<kForkThreads>(all, s).all;
-    const int begin = *d.free_begin, wanted = a.sums[1], flags = all_flags(a, a.sums[0], begin, wanted, all);
+    const int begin = *d.free_begin, wanted = sums & 0xffff, flags = all_flags(a, *a.bad ? NM_FORK_BAD_LENGTH : 0, begin, wanted, all);
     const bool ok = flags == 0;
     const int end = ok ? begin + wanted - all : begin;
-    if (block == 0 && tid == 0) report(a, flags, wanted, all, a.sums[2], end);
+    if (block == 0 && tid == 0) report(a, flags, wanted, all, sums >> 16, end);
     if (pages) {
         if (!ok) return;
         long at = (long)end + scan<kForkThreads>(before, s).all;
@@ -251,7 +246,8 @@ __global__ __launch_bounds__(kForkThreads) void fork_write_kernel(ForkArgs a)
     } else if (rows) {
         if (b >= d.B_out) return;
         const int n = ok ? row.y : 0, held = held_of(a, n);
-        const int dst = d.copy_dst[b], src = d.copy_src[b];
+        const bool need = ok && row.w >= 0;
+        const int dst = need ? a.taken[front + row.w] : -1;
         const int* from = d.block_table + (long)max(row.x, 0) * d.table_stride;
         int* to = d.table_out + b * d.table_out_stride;
         constexpr int kAtOnce = 4;
@@ -261,14 +257,13 @@ __global__ __launch_bounds__(kForkThreads) void fork_write_kernel(ForkArgs a)
             for (int k = 0; k < kAtOnce; ++k) x[k] = from[min(i0 + 64 * k, held - 1)];
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k)
-                if (i0 + 64 * k < held) to[i0 + 64 * k] = src >= 0 && i0 + 64 * k == n >> a.shift ? dst : x[k];
+                if (i0 + 64 * k < held) to[i0 + 64 * k] = need && i0 + 64 * k == n >> a.shift ? dst : x[k];
         }
         if (lane == 0) {
             d.lens_out[b] = n;
-            if (!ok) {
-                d.copy_src[b] = d.copy_dst[b] = -1;
-                d.copy_slots[b] = 0;
-            }
+            d.copy_src[b] = need ? row.z : -1;
+            d.copy_dst[b] = dst;
+            d.copy_slots[b] = need ? n & (d.page_size - 1) : 0;
         }
     } else if (d.free_out != d.free_pages && begin >= 0) {
         const int first = block - a.blocks - (d.B_out + kForkThreads / 64 - 1) / (kForkThreads / 64);
@@ -316,7 +311,7 @@ __global__ __launch_bounds__(kRowThreads) void fork_small_kernel(ForkArgs a)
     int page = -1;
     if (n & (d.page_size - 1)) page = d.block_table[parent * d.table_stride + (n >> a.shift)];
     const bool need = is_page(a, page) && (s_first[parent] != tid || !stays(marks_of(page)));
-    const Sums wanted = scan<kRowThreads>(need, s), parents = scan<kRowThreads>(child, s);
+    const Sums rows = scan<kRowThreads>((int)need | (int)child << 16, s), wanted{rows.before & 0xffff, rows.all & 0xffff};
     const long from = (long)begin + wanted.before;
     const int dst = need && from >= 0 && from < d.n_free ? d.free_pages[from] : -1;
     // the pages, a run of words to a thread
@@ -328,7 +323,7 @@ __global__ __launch_bounds__(kRowThreads) void fork_small_kernel(ForkArgs a)
     const int flags = all_flags(a, bad ? NM_FORK_BAD_LENGTH : 0, begin, wanted.all, gone.all);
     const bool ok = flags == 0;
     const int end = ok ? begin + wanted.all - gone.all : begin;
-    if (tid == 0) report(a, flags, wanted.all, gone.all, parents.all, end);
+    if (tid == 0) report(a, flags, wanted.all, gone.all, rows.all >> 16, end);
     if (tid < d.B_out) {
         d.lens_out[tid] = ok ? n : 0;
         d.copy_src[tid] = ok && need ? page : -1;
@@ -366,10 +361,11 @@ static int32_t plan_fork(const nm_fork_desc* d, ForkArgs* a, size_t* bytes, cons
     *a = ForkArgs{};
     a->d = *d;
     a->shift = shift;
+    a->padded = ((long)d->num_pages + kRun - 1) / kRun * kRun;
     a->block = std::max(kForkBlock, ((d->num_pages + kForkBlocks - 1) / kForkBlocks + kRun - 1) / kRun * kRun);
     a->blocks = (d->num_pages + a->block - 1) / a->block;
     a->list_blocks = std::min((d->n_free + 8 * kForkThreads - 1) / (8 * kForkThreads), 512);
-    *bytes = sizeof(int) * (((size_t)d->num_pages + kRun - 1) / kRun * kRun + 4 * (size_t)d->B_out + d->B_in + a->blocks + 4);
+    *bytes = 6 * (size_t)a->padded + sizeof(int) * (5 * (size_t)d->B_out + d->B_in + a->blocks + kRowBlocks + 1);
     return NM_OK;
 }
 
@@ -414,10 +410,13 @@ int32_t nm_page_fork(const nm_fork_desc* d, void* ws, size_t ws_bytes, void* str
     if (!ws || ws_bytes < need) return fail(NM_ERR_WORKSPACE, "nm_page_fork: workspace of %zu bytes needed, %zu given", need, ws ? ws_bytes : (size_t)0);
     if (!aligned(ws, 256)) return fail(NM_ERR_WORKSPACE, "nm_page_fork: workspace must be 256-byte aligned");
     a.marks = static_cast<int*>(ws);
-    a.rows = reinterpret_cast<int4*>(a.marks + ((size_t)d->num_pages + kRun - 1) / kRun * kRun);
-    a.first = reinterpret_cast<int*>(a.rows + d->B_out);
+    a.old = reinterpret_cast<uint8_t*>(a.marks + a.padded);
+    a.rows = reinterpret_cast<int4*>(a.old + 2 * a.padded);
+    a.taken = reinterpret_cast<int*>(a.rows + d->B_out);
+    a.first = a.taken + d->B_out;
     a.freed = a.first + d->B_in;
     a.sums = a.freed + a.blocks;
+    a.bad = a.sums + kRowBlocks;
     const hipStream_t s = (hipStream_t)stream;
     const dim3 threads(kForkThreads);
     if (std::max(d->B_in, d->B_out) <= kSmallRows && (long)std::max(d->B_in, d->B_out) * d->max_pages <= kSmallEntries && d->num_pages <= kSmallPages && d->n_free <= kSmallList) {
@@ -427,7 +426,7 @@ int32_t nm_page_fork(const nm_fork_desc* d, void* ws, size_t ws_bytes, void* str
     const int per = kForkThreads / 64, news = (d->B_out + kForkThreads - 1) / kForkThreads, olds = (d->B_in + per - 1) / per;
     queue_kernel(fork_clear_kernel, dim3(1 + std::min((d->num_pages + kRowThreads - 1) / kRowThreads, 1024)), dim3(kRowThreads), 0, s, a);
     if (news + olds) queue_kernel(fork_mark_kernel, dim3(news + olds), threads, 0, s, a);
-    queue_kernel(fork_decide_kernel, dim3(1 + a.blocks), dim3(kRowThreads), 0, s, a);
+    queue_kernel(fork_decide_kernel, dim3(a.blocks + news + 1), threads, 0, s, a);
     queue_kernel(fork_write_kernel, dim3(std::max(1, a.blocks + (d->B_out + per - 1) / per + a.list_blocks)), threads, 0, s, a);
     return check_hip(hipGetLastError(), "nm_page_fork launch");
 }
