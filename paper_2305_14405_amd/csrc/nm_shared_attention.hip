@@ -1,12 +1,13 @@
 // Attention of one new token per row over a paged cache, where groups of rows share a prefix (nm_shared_attention).
 //
-// The rows' own positions are nm_paged_attention's work: every key and value once, bound by memory.  A group's prefix is read once for all its
-// rows: for one key head the queries of all of them, rows times heads, are as many columns of the same matrix products.  A piece
-// of work is a range of positions with up to kQueries columns; a group with more goes over its prefix again, side by side on one XCD, so
-// that its L2 serves the others.  Softmax over both ranges: each piece leaves its maximum, sum and output, and a last kernel joins a row's.
-//   A first kernel of one workgroup makes the list: of each group (its prefix, all its rows' queries) and each row (its own positions, its queries) the
-// cost, and where in their sequence each workgroup of the second begins.  As in nm_paged_attention a fixed number of workgroups share all of it evenly, whatever
-// the lengths are, and a run's first and last piece may be parts of a range.  Tiles, operand layouts and precision are that kernel's too.
+// Each row's own positions are nm_paged_attention's work: every key and value once, bound by memory.  A group's prefix is read once for all its
+// rows: for one key head the queries of all of them, rows times heads, are as many columns of the same matrix products.  Softmax over both: each piece
+// of work, a range of positions, leaves its maximum, sum and output, and a last kernel joins what a query has.
+//   A first kernel of one workgroup makes two lists.  Ranges of up to 16 queries, which the rows' own are, are taken as nm_paged_attention takes them: each of
+// a workgroup's four wavefronts has tiles of 32 positions of its own.  Ranges of more have their 128 positions at a time in LDS for all four: each has 32
+// queries, or 16 where they are three terms, of up to four times as many, and the positions that are left to it (few queries: a half or a quarter of them).
+// A fixed number of workgroups is divided among the lists by their cost, and shares each evenly, whatever the lengths are; a run's first and
+// last piece may be parts of a range.  Tiles, operand layouts and precision are nm_paged_attention's.
 #include "nm_paged_parts.h"
 
 namespace nm {
@@ -14,33 +15,39 @@ namespace nm {
 constexpr int kSharedMost = NM_PLAN_MAX_REQUESTS;     // rows, groups
 constexpr int kSharePrefix = kUnit;                   // shorter prefixes are every row's own
 constexpr int kPlanners = 1024;
+constexpr int kLists = 3;
 
-// Columns of a piece in sixteens.
-constexpr int shared_sets(int dp) { return dp <= 128 ? 2 : 1; }
+// Wavefronts of a list's workgroups; sixteens of queries that one has of a range, by the heads' size and the terms of a query; and queries of a range.
+constexpr int shared_waves(int list) { return list == 2 ? 2 * kPagedWaves : kPagedWaves; }
+constexpr int shared_sets(int list, int dp, int terms) { return list == 0 ? 1 : terms == 1 ? (dp <= 128 ? 2 : 1) : list == 2 && dp <= 64 ? 2 : 1; }
+constexpr int shared_tile(int list, int dp, int terms) { return list == 0 ? 16 : (list == 1 ? 2 : shared_waves(2)) * 16 * shared_sets(list, dp, terms); }
 
-struct SharedHead { long each, more; int workers, pad; };   // how the cost is divided
+struct SharedHead { long each[kLists], more[kLists]; int workers[kLists]; };   // how a list's cost is divided
 struct SharedArgs {
     nm_paged_desc d;
     int G;
     const int32_t* group_start;
     const int32_t* shared;
-    int shift, group, sets;      // log2 of page_size, query heads of a key head, sixteens of columns of a piece
-    int workers;                 // at most
+    int shift, group;            // log2 of page_size, query heads of a key head
+    int tile[kLists];            // queries of a range
+    int workers, last;           // of the first two lists, and of the third
+    int whole_queries;           // 8 elements of a query may be read at once
     SharedHead* head;
     int4* ent;                   // [G + B]: a group: first row, rows, the row whose table it goes by, positions; a row: itself, 1, its own first position, its length
     int* lead;                   // [B]: first row of the group whose prefix the row shares, -1: none
-    long* before;                // [workers]: cost of the entities in front of a worker's first
-    int* first;                  // [workers]: a worker's first entity
-    int4* info;                  // [2, B, hq], by a tile's first query: how many pieces it has (0: none, -1: the result is there), the first's worker and slot (-1: whole)
-    float2* part_ml;             // [workers, 2, 16 sets]: maximum (of scores in units of log 2) and sum
-    float* part_o;               // [workers, 2, 16 sets, d]: not yet divided by the sum
-    float2* whole_ml;            // [2, B, hq]
+    long* before;                // [kLists, workers]: cost of the entities in front of a worker's first
+    int* first;                  // [kLists, workers]: a worker's first entity
+    int4* info;                  // [2, B, hq], by a range's first query: how many pieces it has (0: none, -1: the result is there), where the first's part is (-1:
+                                 // whole), where the second's is, and how far apart those behind it are
+    float2* part_ml;             // [workers, 2, tile] of each list: maximum (of scores in units of log 2) and sum
+    float* part_o;               // [likewise, d]: not yet divided by the sum
+    float2* whole_ml;            // [2, B, hq]: prefixes, own positions
     float* whole_o;              // [2, B, hq, d]
 };
 
-// What an entity is, and what it costs.
+// What an entity is, which list it is on, and what it costs.
 struct Entity {
-    int row0, table, k0, k1, queries, tiles, units, unit, extra;
+    int row0, table, k0, k1, queries, list, tile, tiles, units, extra;
     __device__ __forceinline__ Entity(const SharedArgs& a, int e)
     {
         const int4 x = a.ent[e];
@@ -50,16 +57,15 @@ struct Entity {
         k0 = prefix ? 0 : x.z;
         k1 = x.w;
         queries = prefix && k1 <= 0 ? 0 : x.y * a.group;
-        tiles = (queries + 16 * a.sets - 1) / (16 * a.sets);
+        list = !prefix || queries <= a.tile[0] ? 0 : queries <= a.tile[1] ? 1 : 2;
+        tile = a.tile[list];
+        tiles = (queries + tile - 1) / tile;
         units = (k1 - k0 + kUnit - 1) / kUnit;
-        // a unit's keys and values, and its columns; beginning and ending a range
-        unit = 4 + min((queries + 15) / 16, a.sets);
-        extra = 2 * unit;
+        extra = 2;                                            // beginning and ending a range, in units
     }
-    __device__ __forceinline__ long cost() const { return (long)units * unit + extra; }               // of a key head's tile
+    __device__ __forceinline__ long cost() const { return units + extra; }                             // of a key head's tile, in units
     __device__ __forceinline__ long all(const SharedArgs& a) const { return cost() * a.d.hk * tiles; }
 };
-__device__ __forceinline__ int most_unit(const SharedArgs& a) { return 4 + a.sets; }
 
 __global__ __launch_bounds__(kPlanners) void shared_plan_kernel(SharedArgs a)
 {
@@ -100,92 +106,88 @@ __global__ __launch_bounds__(kPlanners) void shared_plan_kernel(SharedArgs a)
         const bool shares = good && s_lead[g] < B;
         a.ent[g] = make_int4(s_start[g], shares ? s_start[g + 1] - s_start[g] : 0, shares ? s_lead[g] : 0, shares ? (int)min((long)a.shared[g], cap) : 0);
     }
-    __threadfence_block();
     __syncthreads();
-    // a thread's run of entities, then the threads'
+    // a thread's run of entities, then the threads'; one list after the other (entities of the others cost nothing)
     const int n = a.G + B, per = (n + kPlanners - 1) / kPlanners, e0 = min(tid * per, n), e1 = min(e0 + per, n);
-    long mine = 0;
-    for (int e = e0; e < e1; ++e) mine += Entity(a, e).all(a);
-    long in = mine;
-    for (int step = 1; step < 64; step <<= 1) {
-        const long t = __shfl_up(in, step);
-        if (lane >= step) in += t;
-    }
-    if (lane == 63) s_wave[tid >> 6] = in;
-    __syncthreads();
-    long front = in - mine, all = 0;
-    for (int w = 0; w < kPlanners / 64; ++w) {
-        if (w < tid >> 6) front += s_wave[w];
-        all += s_wave[w];
-    }
+    long cost[kLists], front[kLists];
+    for (int list = 0; list < kLists; ++list) cost[list] = 0;
     for (int e = e0; e < e1; ++e) {
-        s_before[e] = front;
-        front += Entity(a, e).all(a);
+        const Entity x(a, e);
+        for (int list = 0; list < kLists; ++list) cost[list] += x.list == list ? x.all(a) : 0;
     }
-    if (tid == 0) s_before[n] = all;
-    __syncthreads();
-    // no share is smaller than a unit, so that every worker between a range's first and last has some of it
-    const int workers = (int)max(1l, min((long)a.workers, all / most_unit(a)));
-    const Shares shares(all, workers);
-    if (tid == 0) *a.head = SharedHead{shares.each, shares.more, workers, 0};
-    for (int w = tid; w < workers; w += kPlanners) {
-        const long x = shares.begin(w);
-        int lo = 0, hi = n;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (s_before[mid] <= x) lo = mid; else hi = mid;
+    for (int list = 0; list < kLists; ++list) {
+        const long mine = cost[list];
+        long in = mine;
+        for (int step = 1; step < 64; step <<= 1) {
+            const long t = __shfl_up(in, step);
+            if (lane >= step) in += t;
         }
-        a.first[w] = lo;
-        a.before[w] = s_before[lo];
+        __syncthreads();
+        if (lane == 63) s_wave[tid >> 6] = in;
+        __syncthreads();
+        front[list] = in - mine;
+        cost[list] = 0;
+        for (int w = 0; w < kPlanners / 64; ++w) {
+            if (w < tid >> 6) front[list] += s_wave[w];
+            cost[list] += s_wave[w];
+        }
     }
+    // the first two lists' workers by their cost
+    const long both = cost[0] + cost[1];
+    const long second = cost[1] ? min(max(1l, (long)((double)a.workers * (double)cost[1] / (double)both + 0.5)), (long)a.workers - (cost[0] > 0)) : 0;
+    const long workers[kLists] = {min((long)a.workers - second, cost[0]), min(second, cost[1]), min((long)a.last, cost[2])};
+    for (int list = 0; list < kLists; ++list) {
+        if (!workers[list]) continue;                  // uniform
+        __syncthreads();
+        long at = front[list];
+        for (int e = e0; e < e1; ++e) {
+            s_before[e] = at;
+            const Entity x(a, e);
+            at += x.list == list ? x.all(a) : 0;
+        }
+        if (tid == 0) s_before[n] = cost[list];
+        __syncthreads();
+        const Shares shares(cost[list], workers[list]);
+        if (tid == 0) {
+            a.head->each[list] = shares.each;
+            a.head->more[list] = shares.more;
+        }
+        for (int w = tid; w < workers[list]; w += kPlanners) {
+            const long x = shares.begin(w);
+            int lo = 0, hi = n;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if (s_before[mid] <= x) lo = mid; else hi = mid;
+            }
+            a.first[list * a.workers + w] = lo;
+            a.before[list * a.workers + w] = s_before[lo];
+        }
+    }
+    if (tid < kLists) a.head->workers[tid] = (int)workers[tid];
 }
 
 // What a workgroup has of a range: positions [k0, k1) by the table of row `table` (-1: none) for key head g and the n queries from number i0 on of the rows from
-// row0 on; slot: where its part goes, -1 where it is the whole range; prefix: of a group.
+// row0 on; slot: where its part goes, -1 where it is the whole range; prefix: of a group; done: its result is the query's.
 struct SharedPiece { int table, row0, g, i0, n, k0, k1, slot, prefix, done; };
 
-// C, T, DP, kQ, kP: as in nm_paged_attention; N: sixteens of columns.
-template <typename C, typename T, int DP, int kQ, int kP, int N>
-__global__ __launch_bounds__(kPagedThreads, DP <= 128 ? 2 : 1) void shared_attention_kernel(SharedArgs a)
-{
-    constexpr int W = kPagedWaves;
-    constexpr int kRowPieces = DP * (int)sizeof(C) / 16;      // 16-byte pieces of a row: lanes to a row
-    constexpr int kPer16 = 16 / (int)sizeof(C);               // elements of one
-    constexpr int kRowsAtOnce = 64 / kRowPieces, kLoads = kTile / kRowsAtOnce;
-    constexpr int kStride = DP + 8;                           // elements between rows in LDS
-    constexpr int kSteps = DP / 32, kBlocks = DP / 16;
-    constexpr int kStep = kTile * W;                          // positions of all wavefronts' tiles
-    constexpr float kLift = std::is_same<T, f16>::value ? 10.0f : 0.0f;   // fp16 weights are held times 2^10, where small ones have more bits
-    __shared__ __attribute__((aligned(16))) union {
-        short tile[W][kTile * kStride];
-        float o[W][16][DP];
-    } s;
-    __shared__ __attribute__((aligned(16))) short s_q[kQ][16 * N * kStride];
-    __shared__ float s_qscale[16 * N], s_m[W][16], s_l[W][16];
-
-    const nm_paged_desc& d = a.d;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int column = lane & 15, j = lane >> 4;              // head (and row of an operand), lane group
-    const int row_piece = lane % kRowPieces, row_first = lane / kRowPieces;
-    constexpr bool kPairs = kRowPieces == 4;
-    auto position_of = [](int group, int i) { return kPairs ? (group >> 1) * 2 * kLoads + 2 * i + (group & 1) : group * kLoads + i; };
-    const int my_position = position_of(row_first, lane % kLoads);
-    short* tile = s.tile[wave];
-    const bool in_row = row_piece * kPer16 < d.d;
-
-    // workgroup i runs on XCD i mod 8: neighbouring runs are one XCD's
-    const SharedHead head = *a.head;
-    const int each_xcd = (head.workers + 7) / 8, worker = (int)(blockIdx.x % 8) * each_xcd + (int)(blockIdx.x / 8);
-    if ((int)(blockIdx.x / 8) >= each_xcd || worker >= head.workers) return;
-    const Shares shares(head.each, head.more, 0);
-    const long first = shares.begin(worker), u1 = shares.begin(worker + 1);
-    long u = first, before = a.before[worker];
-    int e = a.first[worker];
-
-    auto advance = [&]() -> SharedPiece {
+// A worker's run through its list.
+struct Run {
+    Shares shares;
+    long first, u, u1, before;
+    int e, list, worker;
+    __device__ __forceinline__ Run(const SharedArgs& a, const SharedHead& head, int list, int worker)
+        : shares(head.each[list], head.more[list], 0), first(shares.begin(worker)), u(first), u1(shares.begin(worker + 1)),
+          before(a.before[list * a.workers + worker]), e(a.first[list * a.workers + worker]), list(list), worker(worker) {}
+    // Number of the first query's part of a worker's slot.
+    static __device__ __forceinline__ long part_of(const SharedArgs& a, int list, long worker, int slot)
+    {
+        return (list > 0 ? 2l * a.workers * a.tile[0] : 0l) + (list > 1 ? 2l * a.workers * a.tile[1] : 0l) + (worker * 2 + slot) * a.tile[list];
+    }
+    __device__ __forceinline__ SharedPiece next(const SharedArgs& a)
+    {
         while (u < u1) {
             const Entity x(a, e);
-            const long cost = x.cost(), all = x.all(a);
+            const long cost = x.cost(), all = x.list == list ? x.all(a) : 0;
             if (u >= before + all) {                          // the next entity
                 before += all;
                 ++e;
@@ -194,8 +196,7 @@ __global__ __launch_bounds__(kPagedThreads, DP <= 128 ? 2 : 1) void shared_atten
             const int r = (int)((u - before) / cost);
             const long begin = before + r * cost, end = min(u1, begin + cost);
             // a range's cost comes first, then its units
-            auto units_at = [&](long at) { return (int)min((max(at - begin - x.extra, 0l) + x.unit - 1) / x.unit, (long)x.units); };
-            const int from = units_at(u), to = units_at(end);
+            const int from = (int)max(u - begin - x.extra, 0l), to = (int)max(end - begin - x.extra, 0l);
             const bool starts = u == begin;
             u = end;
             if (x.units ? from == to : !starts) continue;     // another workgroup has what there is of it
@@ -203,46 +204,78 @@ __global__ __launch_bounds__(kPagedThreads, DP <= 128 ? 2 : 1) void shared_atten
             n.table = x.table;
             n.row0 = x.row0;
             n.g = r / x.tiles;
-            n.i0 = r % x.tiles * 16 * N;
-            n.n = min(x.queries - n.i0, 16 * N);
+            n.i0 = r % x.tiles * x.tile;
+            n.n = min(x.queries - n.i0, x.tile);
             n.k0 = x.k0 + from * kUnit;
             n.k1 = (int)min((long)x.k0 + (long)to * kUnit, (long)x.k1);
             n.slot = from == 0 && to == x.units ? -1 : begin > first;
             n.prefix = e < a.G;
             n.done = !n.prefix && x.k0 == 0 && n.slot < 0;
-            if (from == 0 && tid == 0) {
-                const int count = n.done ? -1 : x.units ? (int)(shares.owner(begin + x.extra + (long)(x.units - 1) * x.unit) - worker) + 1 : 0;
-                a.info[((long)!n.prefix * d.B + x.row0 + n.i0 / a.group) * d.hq + n.g * a.group + n.i0 % a.group] = make_int4(count, worker, n.slot, 0);
+            if (from == 0 && threadIdx.x == 0) {
+                const int count = n.done ? -1 : x.units ? (int)(shares.owner(begin + x.extra + x.units - 1) - worker) + 1 : 0;
+                a.info[((long)!n.prefix * a.d.B + x.row0 + n.i0 / a.group) * a.d.hq + n.g * a.group + n.i0 % a.group] =
+                    make_int4(count, n.slot < 0 ? -1 : (int)part_of(a, list, worker, n.slot), (int)part_of(a, list, worker + 1, 0), 2 * x.tile);
             }
             return n;
         }
         return SharedPiece{-1, 0, 0, 0, 0, 0, 0, -1, 0, 0};
-    };
+    }
+};
+
+// What both lists' code needs of a cache with elements C, for matrix instructions of T and heads of up to DP elements.
+template <typename C, typename T, int DP>
+struct Tiles {
+    static constexpr int kRowPieces = DP * (int)sizeof(C) / 16;      // 16-byte pieces of a row: lanes to a row
+    static constexpr int kPer16 = 16 / (int)sizeof(C);               // elements of one
+    static constexpr int kRowsAtOnce = 64 / kRowPieces, kLoads = kTile / kRowsAtOnce;
+    static constexpr int kStride = DP + 8;                           // elements between rows in LDS
+    static constexpr int kSteps = DP / 32, kBlocks = DP / 16;
+    static constexpr float kLift = std::is_same<T, f16>::value ? 10.0f : 0.0f;   // fp16 weights are held times 2^10, where small ones have more bits
+    static constexpr bool kPairs = kRowPieces == 4;
+
+    const SharedArgs& a;
+    int lane, column, j, row_piece, row_first, my_position, lane_bytes;
+    bool in_row;
+    static __device__ __forceinline__ int position_of(int group, int i) { return kPairs ? (group >> 1) * 2 * kLoads + 2 * i + (group & 1) : group * kLoads + i; }
+    __device__ __forceinline__ Tiles(const SharedArgs& a) : a(a)
+    {
+        lane = threadIdx.x & 63;
+        column = lane & 15;                                   // query (and row of an operand)
+        j = lane >> 4;                                        // lane group
+        row_piece = lane % kRowPieces;
+        row_first = lane / kRowPieces;
+        my_position = position_of(row_first, lane % kLoads);
+        in_row = row_piece * kPer16 < a.d.d;
+        lane_bytes = in_row ? row_piece * 16 : 0;
+    }
     // A tile's places: a lane has one position's distance into the cache in 16 bytes, 0 where it takes no part.  Loads are not
     // conditional: a lane of no part reads the first page, and zeros are put in the place of what it read.
-    auto entry_of = [&](const SharedPiece& n, int t0) {
+    __device__ __forceinline__ int entry_of(const SharedPiece& n, int t0) const
+    {
         const bool some = n.table >= 0 && n.k1 > 0;
-        const int* table = d.max_pages && some ? d.block_table + n.table * d.table_stride : reinterpret_cast<const int*>(g_zero_line);
+        const int* table = a.d.max_pages && some ? a.d.block_table + n.table * a.d.table_stride : reinterpret_cast<const int*>(g_zero_line);
         return table[some ? min(t0 + my_position, n.k1 - 1) >> a.shift : 0];
-    };
-    auto place_of = [&](const SharedPiece& n, int t0, int entry, unsigned long& valid) -> unsigned {
+    }
+    __device__ __forceinline__ unsigned place_of(const SharedPiece& n, int t0, int entry, unsigned long& valid) const
+    {
         const int k = t0 + my_position;
-        const bool ok = k < n.k1 && entry >= 0 && entry < d.num_pages;
+        const bool ok = k < n.k1 && entry >= 0 && entry < a.d.num_pages;
         valid = __ballot(ok);
-        return ok ? (unsigned)(((long)entry * d.page_stride + (long)(k & (d.page_size - 1)) * d.slot_stride) / kPer16) : 0u;
-    };
-    const int lane_bytes = in_row ? row_piece * 16 : 0;
-    auto fetch = [&](const void* cache, const SharedPiece& n, unsigned place, v4u (&to)[kLoads]) {
-        const char* base = d.num_pages ? static_cast<const char*>(cache) + (long)n.g * d.head_stride * sizeof(C) + lane_bytes : reinterpret_cast<const char*>(g_zero_line);
+        return ok ? (unsigned)(((long)entry * a.d.page_stride + (long)(k & (a.d.page_size - 1)) * a.d.slot_stride) / kPer16) : 0u;
+    }
+    __device__ __forceinline__ void fetch(const void* cache, const SharedPiece& n, unsigned place, v4u (&to)[kLoads]) const
+    {
+        const char* base = a.d.num_pages ? static_cast<const char*>(cache) + (long)n.g * a.d.head_stride * sizeof(C) + lane_bytes : reinterpret_cast<const char*>(g_zero_line);
         fetch_rows<kLoads>(base, place, to, std::make_integer_sequence<int, kLoads>{});
         __builtin_amdgcn_sched_barrier(0);                    // the order of the loads is what is waited for
-    };
-    auto stage = [&](const v4u (&from)[kLoads], unsigned long valid) {
+    }
+    __device__ __forceinline__ void stage(short* tile, const v4u (&from)[kLoads], unsigned long valid) const
+    {
         constexpr int kRow = (kPairs ? 2 : 1) * kStride;
         short* to = tile + position_of(row_first, 0) * kStride + row_piece * kPer16;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) put<C, T>(to + i * kRow, from[i]);
-        if (valid != ~0ul || d.d != DP) {
+        if (valid != ~0ul || a.d.d != DP) {
 #pragma unroll 1
             for (int i = 0; i < kLoads; ++i)
                 if (!in_row || !(valid >> (lane - row_piece + i) & 1)) {
@@ -250,223 +283,480 @@ __global__ __launch_bounds__(kPagedThreads, DP <= 128 ? 2 : 1) void shared_atten
                     for (int c = 0; c < kPer16; c += 8) *reinterpret_cast<v4u*>(to + i * kRow + c) = v4u{};
                 }
         }
-    };
+    }
     // whether the lane's score number i, of position i / 4 * 16 + j * 4 + i % 4, takes part
-    auto scored = [&](int i, unsigned long valid) {
+    __device__ __forceinline__ bool scored(int i, unsigned long valid) const
+    {
         const int at = i / 4 * 16 + j * 4 + i % 4;
         const int group = kPairs ? at / (2 * kLoads) * 2 + (at & 1) : at / kLoads, nth = kPairs ? at % (2 * kLoads) / 2 : at % kLoads;
         return valid >> (group * kRowPieces + nth) & 1;
+    }
+    __device__ __forceinline__ v8s keys_of(const short* tile, int blk, int step) const { return *reinterpret_cast<const v8s*>(tile + (blk * 16 + column) * kStride + step * 32 + j * 8); }
+    __device__ __forceinline__ v8s values_of(const short* tile, int blk) const
+    {
+        const short* at = tile + (j * 4 + column / 4) * kStride + blk * 16 + column % 4 * 4;
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at));
+        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at + 16 * kStride));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    // A tile's scores of S sixteens of queries into weights of kP terms; the queries' sums and outputs so far go along.  m is what is subtracted: a maximum, or up
+    // to kSlack less (a weight of up to 2^5 has as many bits, and with fp16's lift stays below 2^16), so that few tiles change it.
+    static constexpr float kSlack = 5.0f;
+    template <int S, int kP>
+    __device__ __forceinline__ void weigh(v4f (&sc)[S][2], unsigned long valid, const float (&factor)[S], float (&m)[S], float (&l)[S], v8s (&p)[S][kP], v4f (&o)[S][kBlocks]) const
+    {
+        if (valid != ~0ul) {
+            asm volatile("");                                 // a branch: few tiles need it
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool in = scored(i, valid);
+#pragma unroll
+                for (int t = 0; t < S; ++t) sc[t][i / 4][i % 4] = in ? sc[t][i / 4][i % 4] : -INFINITY;
+            }
+        }
+        float top[S];
+        bool over = false;
+#pragma unroll
+        for (int t = 0; t < S; ++t) {
+            top[t] = sc[t][0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top[t] = fmaxf(top[t], sc[t][i / 4][i % 4]);
+            top[t] *= factor[t];
+            over |= top[t] > m[t] + kSlack;
+        }
+        if (__any(over)) {                                    // few tiles need it
+#pragma unroll
+            for (int t = 0; t < S; ++t) {
+                const float most = __int_as_float(butterfly_step<32>(butterfly_step<16>(__float_as_int(top[t]), MaxF32{}), MaxF32{}));
+                const float next = most > m[t] + kSlack ? most : m[t];
+                const float shrink = __builtin_amdgcn_exp2f(m[t] - (next == -INFINITY ? 0.0f : next));
+                m[t] = next;
+                l[t] *= shrink;
+#pragma unroll
+                for (int blk = 0; blk < kBlocks; ++blk)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[t][blk][i] *= shrink;
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < S; ++t) {
+            const float lifted = kLift - (m[t] == -INFINITY ? 0.0f : m[t]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][i / 4][i % 4], factor[t], lifted));
+                l[t] += w;
+#pragma unroll
+                for (int q = 0; q < kP; ++q) {
+                    const T v = (T)w;
+                    w = __builtin_fmaf((float)v, -1.0f, w);
+                    p[t][q][i] = __builtin_bit_cast(short, v);
+                }
+            }
+        }
+    }
+    // Calls use(Q{}) with the queries' type: that of the matrix instructions where they are of one term.  (One branch in front of all loads: a branch at
+    // each has every one wait for the one before.)
+    template <int kQ, typename Use>
+    __device__ __forceinline__ void typed(Use use) const
+    {
+        if constexpr (kQ == 1) use(T{});
+        else if (a.d.q_dtype == NM_DT_F32) use(0.0f);
+        else if (a.d.q_dtype == NM_DT_BF16) use(bf16{});
+        else use(f16{});
+    }
+    // Number of a query's first element.
+    __device__ __forceinline__ long query_of(const SharedPiece& n, int row) const
+    {
+        const int i = n.i0 + row;
+        return (long)(n.row0 + i / a.group) * a.d.q_stride + (long)(n.g * a.group + i % a.group) * a.d.d;
+    }
+    // What a query's scores are multiplied by, but for its own scale; the sign of the scale goes with the queries.
+    __device__ __forceinline__ float scale_of(int g) const { return a.d.scale * 1.44269504088896340736f * (sizeof(C) == 1 ? a.d.k_scale[g] : 1.0f); }
+    // Powers of two that bring a query of three terms below 4, and back.
+    static __device__ __forceinline__ void level(float top, float& down, float& up)
+    {
+        const int exponent = max(-126, min((int)(__float_as_uint(top) >> 23) - 127, 126));
+        down = __uint_as_float((unsigned)(127 - exponent) << 23);
+        up = __uint_as_float((unsigned)(127 + exponent) << 23);
+    }
+    // Writes a query's part or result, its maximum and sum: elements(put) calls put(c, y) for the lane's runs of four elements, from c on.
+    template <typename Elements>
+    __device__ __forceinline__ void leave(const SharedPiece& n, int row, long part, Elements elements, float top, float sum) const
+    {
+        const nm_paged_desc& d = a.d;
+        const int i = n.i0 + row, b = n.row0 + i / a.group, h = n.g * a.group + i % a.group;
+        if (!n.done) {
+            const long at = n.slot < 0 ? ((long)!n.prefix * d.B + b) * d.hq + h : part + row;
+            float* to = (n.slot < 0 ? a.whole_o : a.part_o) + at * d.d;
+            elements([&](int c, v4f y) {
+                if (c == 0) (n.slot < 0 ? a.whole_ml : a.part_ml)[at] = make_float2(top, sum);
+                *reinterpret_cast<v4f*>(to + c) = y;
+            });
+            return;
+        }
+        const float over = (sum == 0.0f ? 0.0f : 1.0f / sum) * (sizeof(C) == 1 ? d.v_scale[n.g] : 1.0f);
+        elements([&](int c, v4f y) {
+            if (c == 0 && d.lse) d.lse[(long)b * d.hq + h] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) store1(d.out, d.out_dtype, b * d.out_stride + (long)h * d.d + c + k, y[k] * over, d.out_inv_scale);
+        });
+    }
+};
+
+// Memory of a workgroup.
+template <int DP, int kQ, int W>
+struct SharedLds {
+    union {
+        struct { short q[kQ][16 * (DP + 8)], tile[kPagedWaves][kTile * (DP + 8)]; } few;
+        struct { short k[kPagedWaves][kTile * (DP + 8)], v[kPagedWaves][kTile * (DP + 8)]; } many;
+        float o[W][16][DP];
     };
+    float m[W][16], l[W][16], q_scale[16];
+    unsigned long valid[kPagedWaves];
+};
 
-    const int qrow = tid >> 4, qc = tid & 15;                 // 16 queries at a time, 16 lanes each
-
-    // What the first tile of a piece needs is requested while the piece before is under way.
-    SharedPiece now = advance();
+// A run through the first list: ranges of up to 16 queries, tiles of a wavefront's own.  What the first tile of a piece needs is requested while the
+// piece before is under way.
+template <typename C, typename T, int DP, int kQ, int kP>
+__device__ __forceinline__ void run_few(const SharedArgs& a, Run run, SharedLds<DP, kQ, kPagedWaves>& s)
+{
+    using X = Tiles<C, T, DP>;
+    constexpr int W = kPagedWaves, kStep = kTile * W, kStride = X::kStride;
+    const X x(a);
+    const int tid = threadIdx.x, wave = tid >> 6, qrow = tid >> 4, qc = tid & 15;
+    short* tile = s.few.tile[wave];
+    SharedPiece now = run.next(a);
     if (now.table < 0) return;
     int t0 = now.k0 + wave * kTile;
-    int entry = entry_of(now, t0), entry2 = entry_of(now, t0 + kStep);
-    v4u kr[kLoads], vr[kLoads];
+    int entry = x.entry_of(now, t0), entry2 = x.entry_of(now, t0 + kStep);
+    v4u kr[X::kLoads], vr[X::kLoads];
     unsigned long valid;
     {
-        const unsigned place = place_of(now, t0, entry, valid);
-        fetch(d.k_cache, now, place, kr);
-        fetch(d.v_cache, now, place, vr);
+        const unsigned place = x.place_of(now, t0, entry, valid);
+        x.fetch(a.d.k_cache, now, place, kr);
+        x.fetch(a.d.v_cache, now, place, vr);
     }
     while (true) {
-        const SharedPiece then = advance();
+        const SharedPiece then = run.next(a);
         const int then_t0 = then.k0 + wave * kTile;
-        const int then_entry = entry_of(then, then_t0), then_entry2 = entry_of(then, then_t0 + kStep);
+        const int then_entry = x.entry_of(then, then_t0), then_entry2 = x.entry_of(then, then_t0 + kStep);
         entry = entry2;
-        const int g = now.g, k1 = now.k1, sets = (now.n + 15) / 16;
-        // the sign of the scale goes with the queries
-        const float by = d.scale * 1.44269504088896340736f * (sizeof(C) == 1 ? d.k_scale[g] : 1.0f);
+        const int g = now.g, k1 = now.k1;
+        const float by = x.scale_of(g);
         __syncthreads();                                      // the piece before is done with LDS
+        {
+            const long at = x.query_of(now, min(qrow, now.n - 1));
+            float y[DP / 16], top = 0.0f, down = 1.0f, up = 1.0f;
+            x.template typed<kQ>([&](auto type) {
+                using Q = decltype(type);
+                Q raw[DP / 16];
 #pragma unroll
-        for (int t = 0; t < N; ++t) {
-            if (t >= sets) continue;
-            const int i = now.i0 + t * 16 + qrow;
-            const bool mine = t * 16 + qrow < now.n;
-            const long at = (long)(now.row0 + i / a.group) * d.q_stride + (long)(g * a.group + i % a.group) * d.d;
-            float x[DP / 16], top_q = 0.0f, down = 1.0f, up = 1.0f;
+                for (int c = 0; c < DP / 16; ++c) raw[c] = static_cast<const Q*>(a.d.q)[at + min(qc + 16 * c, a.d.d - 1)];
 #pragma unroll
-            for (int c = 0; c < DP / 16; ++c) {
-                const int col = qc + 16 * c;
-                const bool there = mine && col < d.d;
-                x[c] = !there ? 0.0f : d.q_dtype == NM_DT_F32 ? static_cast<const float*>(d.q)[at + col]
-                              : d.q_dtype == NM_DT_BF16 ? (float)static_cast<const bf16*>(d.q)[at + col] : (float)static_cast<const f16*>(d.q)[at + col];
-            }
+                for (int c = 0; c < DP / 16; ++c) y[c] = qrow < now.n && qc + 16 * c < a.d.d ? (float)raw[c] : 0.0f;
+            });
             if (kQ > 1) {
 #pragma unroll
-                for (int c = 0; c < DP / 16; ++c) top_q = fmaxf(top_q, fabsf(x[c]));
-                top_q = __int_as_float(group_reduce<16>(__float_as_int(top_q), MaxF32{}));
-                const int exponent = max(-126, min((int)(__float_as_uint(top_q) >> 23) - 127, 126));   // the row goes below 4
-                down = __uint_as_float((unsigned)(127 - exponent) << 23);
-                up = __uint_as_float((unsigned)(127 + exponent) << 23);
+                for (int c = 0; c < DP / 16; ++c) top = fmaxf(top, fabsf(y[c]));
+                X::level(__int_as_float(group_reduce<16>(__float_as_int(top), MaxF32{})), down, up);
             }
 #pragma unroll
             for (int c = 0; c < DP / 16; ++c) {
-                float rest = copysignf(down, by) * x[c];
+                float rest = copysignf(down, by) * y[c];
 #pragma unroll
                 for (int q = 0; q < kQ; ++q) {
                     const T v = (T)rest;
                     rest -= (float)v;
-                    s_q[q][(t * 16 + qrow) * kStride + qc + 16 * c] = __builtin_bit_cast(short, v);
+                    s.few.q[q][qrow * kStride + qc + 16 * c] = __builtin_bit_cast(short, v);
                 }
             }
-            if (qc == 0) s_qscale[t * 16 + qrow] = up;
+            if (qc == 0) s.q_scale[qrow] = up;
         }
         __syncthreads();
+        // never 0, so that it takes a masked score, minus infinity, for what it is
+        const float factor[1] = {fmaxf(fabsf(by) * s.q_scale[x.column], 1.17549435e-38f)};
         if (t0 >= k1) {                                       // no tile for this wavefront
-            const unsigned place = place_of(then, then_t0, then_entry, valid);
-            fetch(d.k_cache, then, place, kr);
-            fetch(d.v_cache, then, place, vr);
+            const unsigned place = x.place_of(then, then_t0, then_entry, valid);
+            x.fetch(a.d.k_cache, then, place, kr);
+            x.fetch(a.d.v_cache, then, place, vr);
         }
-        v4f o[N][kBlocks];
-        float m[N], l[N], factor[N];
+        v4f o[1][X::kBlocks];
 #pragma unroll
-        for (int t = 0; t < N; ++t) {
-#pragma unroll
-            for (int i = 0; i < kBlocks; ++i) o[t][i] = v4f{0, 0, 0, 0};
-            m[t] = -INFINITY;
-            l[t] = 0.0f;
-            // never 0, so that it takes a masked score, minus infinity, for what it is
-            factor[t] = t < sets ? fmaxf(fabsf(by) * s_qscale[t * 16 + column], 1.17549435e-38f) : 1.0f;
-        }
+        for (int i = 0; i < X::kBlocks; ++i) o[0][i] = v4f{0, 0, 0, 0};
+        float m[1] = {-INFINITY}, l[1] = {0.0f};
         for (; t0 < k1; t0 += kStep) {
             unsigned long next_valid;
             const bool more = t0 + kStep < k1;
             const SharedPiece& of = more ? now : then;
-            const unsigned next = place_of(of, more ? t0 + kStep : then_t0, more ? entry : then_entry, next_valid);
-            entry = entry_of(now, t0 + 2 * kStep);
-            // scores
-            stage(kr, valid);
-            fetch(d.k_cache, of, next, kr);
-            v4f sc[N][2];
+            const unsigned next = x.place_of(of, more ? t0 + kStep : then_t0, more ? entry : then_entry, next_valid);
+            entry = x.entry_of(now, t0 + 2 * kStep);
+            x.stage(tile, kr, valid);
+            x.fetch(a.d.k_cache, of, next, kr);
+            v4f sc[1][2];
 #pragma unroll
-            for (int t = 0; t < N; ++t) sc[t][0] = sc[t][1] = v4f{0, 0, 0, 0};
+            for (int blk = 0; blk < 2; ++blk) {
+                sc[0][blk] = v4f{0, 0, 0, 0};
 #pragma unroll
-            for (int step = 0; step < kSteps; ++step) {
-                v8s ka[2];
+                for (int step = 0; step < X::kSteps; ++step) {
+                    const v8s ka = x.keys_of(tile, blk, step);
 #pragma unroll
-                for (int blk = 0; blk < 2; ++blk) ka[blk] = *reinterpret_cast<const v8s*>(tile + (blk * 16 + column) * kStride + step * 32 + j * 8);
-#pragma unroll
-                for (int t = 0; t < N; ++t) {
-                    if (t >= sets) continue;
-#pragma unroll
-                    for (int q = kQ - 1; q >= 0; --q) {
-                        const v8s qb = *reinterpret_cast<const v8s*>(s_q[q] + (t * 16 + column) * kStride + step * 32 + j * 8);
-#pragma unroll
-                        for (int blk = 0; blk < 2; ++blk) sc[t][blk] = Mma<T>::mma(ka[blk], qb, sc[t][blk]);
-                    }
+                    for (int q = kQ - 1; q >= 0; --q) sc[0][blk] = Mma<T>::mma(ka, *reinterpret_cast<const v8s*>(s.few.q[q] + x.column * kStride + step * 32 + x.j * 8), sc[0][blk]);
                 }
             }
-            v8s p[N][kP];
+            v8s p[1][kP];
+            x.template weigh<1, kP>(sc, valid, factor, m, l, p, o);
+            x.stage(tile, vr, valid);
+            x.fetch(a.d.v_cache, of, next, vr);
 #pragma unroll
-            for (int t = 0; t < N; ++t) {
-                if (t >= sets) continue;
-                if (valid != ~0ul) {
-                    asm volatile("");                         // a branch: few tiles need it
+            for (int blk = 0; blk < X::kBlocks; ++blk) {
+                const v8s va = x.values_of(tile, blk);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sc[t][i / 4][i % 4] = scored(i, valid) ? sc[t][i / 4][i % 4] : -INFINITY;
-                }
-                float top = sc[t][0][0];
-#pragma unroll
-                for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[t][i / 4][i % 4]);
-                top = __int_as_float(butterfly_step<32>(butterfly_step<16>(__float_as_int(top), MaxF32{}), MaxF32{}));
-                top = fmaxf(m[t], top == -INFINITY ? top : top * factor[t]);
-                const float base = top == -INFINITY ? 0.0f : top;
-                const float shrink = __builtin_amdgcn_exp2f(m[t] - base);
-                m[t] = top;
-                l[t] *= shrink;
-                const float lifted = kLift - base;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][i / 4][i % 4], factor[t], lifted));
-                    l[t] += w;
-#pragma unroll
-                    for (int q = 0; q < kP; ++q) {
-                        const T v = (T)w;
-                        w = __builtin_fmaf((float)v, -1.0f, w);
-                        p[t][q][i] = __builtin_bit_cast(short, v);
-                    }
-                }
-                if (__any(shrink != 1.0f)) {
-#pragma unroll
-                    for (int blk = 0; blk < kBlocks; ++blk)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[t][blk][i] *= shrink;
-                }
-            }
-            // values
-            stage(vr, valid);
-            fetch(d.v_cache, of, next, vr);
-#pragma unroll
-            for (int blk = 0; blk < kBlocks; ++blk) {
-                const short* at = tile + (j * 4 + column / 4) * kStride + blk * 16 + column % 4 * 4;
-                const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at));
-                const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at + 16 * kStride));
-                const v8s va = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-                for (int t = 0; t < N; ++t) {
-                    if (t >= sets) continue;
-#pragma unroll
-                    for (int q = kP - 1; q >= 0; --q) o[t][blk] = Mma<T>::mma(va, p[t][q], o[t][blk]);
-                }
+                for (int q = kP - 1; q >= 0; --q) o[0][blk] = Mma<T>::mma(va, p[0][q], o[0][blk]);
             }
             valid = next_valid;
         }
-
-        // the wavefronts' results as one, sixteen columns at a time
-#pragma unroll
-        for (int t = 0; t < N; ++t) {
-            if (t >= sets) continue;
-            const float sum_l = __int_as_float(butterfly_step<32>(butterfly_step<16>(__float_as_int(l[t]), AddF32{}), AddF32{}));
-            __syncthreads();                                  // no tile, and no columns before these, are read any more
-            if (j == 0) { s_m[wave][column] = m[t]; s_l[wave][column] = sum_l; }
-            __syncthreads();
+        // the wavefronts' results as one
+        l[0] = __int_as_float(butterfly_step<32>(butterfly_step<16>(__float_as_int(l[0]), AddF32{}), AddF32{}));
+        if (x.j == 0) { s.m[wave][x.column] = m[0]; s.l[wave][x.column] = l[0]; }
+        __syncthreads();                                      // also: no tile is read any more
+        {
             float top = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < W; ++w) top = fmaxf(top, s_m[w][column]);
-            const float mine = __builtin_amdgcn_exp2f(m[t] - (top == -INFINITY ? 0.0f : top) - kLift);
+            for (int w = 0; w < W; ++w) top = fmaxf(top, s.m[w][x.column]);
+            const float mine = __builtin_amdgcn_exp2f(m[0] - (top == -INFINITY ? 0.0f : top) - X::kLift);
 #pragma unroll
-            for (int blk = 0; blk < kBlocks; ++blk)
+            for (int blk = 0; blk < X::kBlocks; ++blk)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s.o[wave][column][blk * 16 + j * 4 + i] = o[t][blk][i] * mine;
-            __syncthreads();
-            const int row = t * 16 + qrow;
-            if (row < now.n) {
-                const int i = now.i0 + row, b = now.row0 + i / a.group, h = g * a.group + i % a.group;
-                float top = -INFINITY, sum = 0.0f;
+                for (int i = 0; i < 4; ++i) s.o[wave][x.column][blk * 16 + x.j * 4 + i] = o[0][blk][i] * mine;
+        }
+        __syncthreads();
+        if (qrow < now.n) {
+            float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-                for (int w = 0; w < W; ++w) top = fmaxf(top, s_m[w][qrow]);
-                const float base = top == -INFINITY ? 0.0f : top;
+            for (int w = 0; w < W; ++w) top = fmaxf(top, s.m[w][qrow]);
+            const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-                for (int w = 0; w < W; ++w) sum += s_l[w][qrow] * __builtin_amdgcn_exp2f(s_m[w][qrow] - base - kLift);
-                const long part = now.slot < 0 ? ((long)!now.prefix * d.B + b) * d.hq + h : ((long)worker * 2 + now.slot) * 16 * N + row;
-                if (qc == 0) {
-                    if (!now.done) (now.slot < 0 ? a.whole_ml : a.part_ml)[part] = make_float2(top, sum);
-                    else if (d.lse) d.lse[(long)b * d.hq + h] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
-                }
-                const float over = (sum == 0.0f ? 0.0f : 1.0f / sum) * (sizeof(C) == 1 ? d.v_scale[g] : 1.0f);
-                float* to = (now.slot < 0 ? a.whole_o : a.part_o) + part * d.d;
-                for (int c = qc * 4; c < d.d; c += 64) {
+            for (int w = 0; w < W; ++w) sum += s.l[w][qrow] * __builtin_amdgcn_exp2f(s.m[w][qrow] - base - X::kLift);
+            const long part = Run::part_of(a, 0, run.worker, max(now.slot, 0));
+            x.leave(now, qrow, part, [&](auto put) {
+                for (int c = qc * 4; c < a.d.d; c += 64) {
                     v4f y{0, 0, 0, 0};
 #pragma unroll
                     for (int w = 0; w < W; ++w) y += *reinterpret_cast<const v4f*>(&s.o[w][qrow][c]);
-                    if (!now.done) {
-                        *reinterpret_cast<v4f*>(to + c) = y;
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) store1(d.out, d.out_dtype, b * d.out_stride + (long)h * d.d + c + k, y[k] * over, d.out_inv_scale);
-                    }
+                    put(c, y);
                 }
-            }
+            }, top, sum);
         }
         if (then.table < 0) break;
         now = then;
         t0 = then_t0;
         entry2 = then_entry2;
     }
+}
+
+// A run through another list: 128 positions at a time in LDS, for all wavefronts' queries.  S: sixteens of a wavefront; W: wavefronts (eight: four bring
+// keys and four values).
+template <typename C, typename T, int DP, int kQ, int kP, int S, int W>
+__device__ __forceinline__ void run_many(const SharedArgs& a, Run run, SharedLds<DP, kQ, W>& s)
+{
+    using X = Tiles<C, T, DP>;
+    constexpr bool kBoth = W == kPagedWaves;
+    const X x(a);
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), qrow = tid / 16 % 16, qc = tid & 15;
+    for (SharedPiece now = run.next(a); now.table >= 0; now = run.next(a)) {
+        const int g = now.g, k1 = now.k1;
+        // wavefronts that have queries of their own, and which of them (and which part of the positions) this one has
+        const int apart = now.n <= 16 * S ? 1 : now.n <= 32 * S ? 2 : W == 4 || now.n <= 64 * S ? 4 : W, mine = wave % apart, part = wave / apart, parts = W / apart;
+        const int brings = wave % kPagedWaves;
+        const bool keys = wave < kPagedWaves;
+        int t0 = now.k0 + brings * kTile;
+        int entry = x.entry_of(now, t0), entry2 = x.entry_of(now, t0 + kUnit);
+        v4u kr[X::kLoads], vr[kBoth ? X::kLoads : 1];
+        unsigned long valid;
+        auto fetch = [&](unsigned place) {
+            x.fetch(keys ? a.d.k_cache : a.d.v_cache, now, place, kr);
+            if constexpr (kBoth) x.fetch(a.d.v_cache, now, place, vr);
+        };
+        fetch(x.place_of(now, t0, entry, valid));
+        // queries, as operands: a lane has those of column `column`, 8 elements of each step
+        const float by = x.scale_of(g);
+        v8s qb[S][kQ][X::kSteps];
+        float factor[S];
+        x.template typed<kQ>([&](auto type) {
+            using Q = decltype(type);
+            typedef Q Run8 __attribute__((ext_vector_type(8)));
+            // d is a multiple of 16: 8 elements are there, or none
+            Run8 raw[S][X::kSteps];
+            auto each = [&](auto load) {
+#pragma unroll
+                for (int t = 0; t < S; ++t) {
+                    const int row = (mine * S + t) * 16 + x.column;
+                    const Q* from = static_cast<const Q*>(a.d.q) + x.query_of(now, min(row, now.n - 1));
+#pragma unroll
+                    for (int step = 0; step < X::kSteps; ++step) {
+                        const int c = step * 32 + x.j * 8;
+                        load(t, step, from + min(c, a.d.d - 8), row < now.n && c < a.d.d);
+                    }
+                }
+            };
+            if (a.whole_queries) each([&](int t, int step, const Q* from, bool) { raw[t][step] = *reinterpret_cast<const Run8*>(from); });
+            else each([&](int t, int step, const Q* from, bool) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) raw[t][step][e] = from[e];
+            });
+            each([&](int t, int step, const Q*, bool there) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) raw[t][step][e] = there ? raw[t][step][e] : (Q)0.0f;
+            });
+#pragma unroll
+            for (int t = 0; t < S; ++t) {
+                float top = 0.0f, down = 1.0f, up = 1.0f;
+                if constexpr (kQ > 1) {
+#pragma unroll
+                    for (int step = 0; step < X::kSteps; ++step)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)raw[t][step][e]));
+                    X::level(__int_as_float(butterfly_step<32>(butterfly_step<16>(__float_as_int(top), MaxF32{}), MaxF32{})), down, up);
+                }
+                const float signed_down = copysignf(down, by);
+#pragma unroll
+                for (int step = 0; step < X::kSteps; ++step)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        float rest = signed_down * (float)raw[t][step][e];
+#pragma unroll
+                        for (int q = 0; q < kQ; ++q) {
+                            const T v = (T)rest;
+                            rest -= (float)v;
+                            qb[t][q][step][e] = __builtin_bit_cast(short, v);
+                        }
+                    }
+                factor[t] = fmaxf(fabsf(by) * up, 1.17549435e-38f);   // never 0, so that it takes a masked score, minus infinity, for what it is
+            }
+        });
+        v4f o[S][X::kBlocks];
+        float m[S], l[S];
+#pragma unroll
+        for (int t = 0; t < S; ++t) {
+#pragma unroll
+            for (int i = 0; i < X::kBlocks; ++i) o[t][i] = v4f{0, 0, 0, 0};
+            m[t] = -INFINITY;
+            l[t] = 0.0f;
+        }
+        for (int u0 = now.k0; u0 < k1; u0 += kUnit) {
+            __syncthreads();                                  // the positions before are done with
+            x.stage(keys ? s.many.k[brings] : s.many.v[brings], kr, valid);
+            if constexpr (kBoth) x.stage(s.many.v[brings], vr, valid);
+            if (keys && x.lane == 0) s.valid[brings] = valid;
+            __syncthreads();
+            const unsigned place = x.place_of(now, t0 + kUnit, entry2, valid);
+            t0 += kUnit;
+            entry2 = x.entry_of(now, t0 + kUnit);
+            fetch(place);                                     // (behind the last: the first page)
+            const int tiles = min((k1 - u0 + kTile - 1) / kTile, kPagedWaves);
+#pragma unroll 1
+            for (int n = part; n < tiles; n += parts) {
+                const unsigned long bits = s.valid[n];         // uniform, which the compiler cannot know
+                const unsigned long there = (unsigned long)(unsigned)__builtin_amdgcn_readfirstlane((int)(bits >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)bits);
+                v4f sc[S][2];
+#pragma unroll
+                for (int t = 0; t < S; ++t) sc[t][0] = sc[t][1] = v4f{0, 0, 0, 0};
+#pragma unroll
+                for (int step = 0; step < X::kSteps; ++step)
+#pragma unroll
+                    for (int blk = 0; blk < 2; ++blk) {
+                        const v8s ka = x.keys_of(s.many.k[n], blk, step);
+#pragma unroll
+                        for (int t = 0; t < S; ++t)
+#pragma unroll
+                            for (int q = kQ - 1; q >= 0; --q) sc[t][blk] = Mma<T>::mma(ka, qb[t][q][step], sc[t][blk]);
+                    }
+                v8s p[S][kP];
+                x.template weigh<S, kP>(sc, there, factor, m, l, p, o);
+#pragma unroll
+                for (int blk = 0; blk < X::kBlocks; ++blk) {
+                    const v8s va = x.values_of(s.many.v[n], blk);
+#pragma unroll
+                    for (int t = 0; t < S; ++t)
+#pragma unroll
+                        for (int q = kP - 1; q >= 0; --q) o[t][blk] = Mma<T>::mma(va, p[t][q], o[t][blk]);
+                }
+            }
+        }
+        // the wavefronts' results as one, sixteen queries of each at a time
+        const long at = Run::part_of(a, run.list, run.worker, max(now.slot, 0));
+        if (parts == 1) {                                     // each has its own: a lane has four elements of each block of its query
+#pragma unroll
+            for (int t = 0; t < S; ++t) {
+                const float sum = __int_as_float(butterfly_step<32>(butterfly_step<16>(__float_as_int(l[t]), AddF32{}), AddF32{})), down = __builtin_amdgcn_exp2f(-X::kLift);
+                const int row = (mine * S + t) * 16 + x.column;
+                if (row < now.n)
+                    x.leave(now, row, at, [&](auto put) {
+#pragma unroll
+                        for (int blk = 0; blk < X::kBlocks; ++blk)
+                            if (blk * 16 < a.d.d) put(blk * 16 + x.j * 4, o[t][blk] * down);
+                    }, m[t], sum * down);
+            }
+            continue;
+        }
+#pragma unroll
+        for (int t = 0; t < S; ++t) {
+            const float sum_l = __int_as_float(butterfly_step<32>(butterfly_step<16>(__float_as_int(l[t]), AddF32{}), AddF32{}));
+            __syncthreads();
+            if (x.j == 0) { s.m[wave][x.column] = m[t]; s.l[wave][x.column] = sum_l; }
+            __syncthreads();
+            float top = -INFINITY;
+            for (int w = mine; w < W; w += apart) top = fmaxf(top, s.m[w][x.column]);
+            const float shrink = __builtin_amdgcn_exp2f(m[t] - (top == -INFINITY ? 0.0f : top) - X::kLift);
+#pragma unroll
+            for (int blk = 0; blk < X::kBlocks; ++blk)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s.o[wave][x.column][blk * 16 + x.j * 4 + i] = o[t][blk][i] * shrink;
+            __syncthreads();
+            for (int of = tid / 256; of < apart; of += W / 4) {   // sixteen queries are 256 threads' work
+                const int row = (of * S + t) * 16 + qrow;
+                if (row >= now.n) break;
+                float top = -INFINITY, sum = 0.0f;
+                for (int w = of; w < W; w += apart) top = fmaxf(top, s.m[w][qrow]);
+                const float base = top == -INFINITY ? 0.0f : top;
+                for (int w = of; w < W; w += apart) sum += s.l[w][qrow] * __builtin_amdgcn_exp2f(s.m[w][qrow] - base - X::kLift);
+                x.leave(now, row, at, [&](auto put) {
+                    for (int c = qc * 4; c < a.d.d; c += 64) {
+                        v4f y{0, 0, 0, 0};
+                        for (int w = of; w < W; w += apart) y += *reinterpret_cast<const v4f*>(&s.o[w][qrow][c]);
+                        put(c, y);
+                    }
+                }, top, sum);
+            }
+        }
+    }
+}
+
+// The first two lists.  C, T, DP, kQ, kP: as in nm_paged_attention.
+template <typename C, typename T, int DP, int kQ, int kP>
+__global__ __launch_bounds__(kPagedThreads, DP <= 128 ? 2 : 1) void shared_attention_kernel(SharedArgs a)
+{
+    __shared__ __attribute__((aligned(16))) SharedLds<DP, kQ, kPagedWaves> s;
+    // workgroup i runs on XCD i mod 8: neighbouring runs are one XCD's, and each XCD has its share of either list
+    const SharedHead head = *a.head;
+    const int xcd = blockIdx.x % 8, i = blockIdx.x / 8, second = (head.workers[1] + 7) / 8, first = (head.workers[0] + 7) / 8;
+    if (i < second) {
+        const int worker = xcd * second + i;
+        if (worker < head.workers[1]) run_many<C, T, DP, kQ, kP, shared_sets(1, DP, kQ), kPagedWaves>(a, Run(a, head, 1, worker), s);
+    } else if (i - second < first) {
+        const int worker = xcd * first + i - second;
+        if (worker < head.workers[0]) run_few<C, T, DP, kQ, kP>(a, Run(a, head, 0, worker), s);
+    }
+}
+
+// The third: a workgroup of eight wavefronts to a CU.
+template <typename C, typename T, int DP, int kQ, int kP>
+__global__ __launch_bounds__(64 * shared_waves(2), 2) void shared_prefix_kernel(SharedArgs a)
+{
+    __shared__ __attribute__((aligned(16))) SharedLds<DP, kQ, shared_waves(2)> s;
+    const SharedHead head = *a.head;
+    const int each = (head.workers[2] + 7) / 8, worker = (int)(blockIdx.x % 8) * each + (int)(blockIdx.x / 8);
+    if ((int)(blockIdx.x / 8) < each && worker < head.workers[2]) run_many<C, T, DP, kQ, kP, shared_sets(2, DP, kQ), shared_waves(2)>(a, Run(a, head, 2, worker), s);
 }
 
 // Joins what a query has: its group's prefix and its row's own positions, each whole or in pieces.  A workgroup to a query; lanes of four elements read every
@@ -476,21 +766,17 @@ __global__ __launch_bounds__(kPagedThreads) void shared_join_kernel(SharedArgs a
     __shared__ __attribute__((aligned(16))) float s_o[kPagedThreads * 4];
     __shared__ float s_m[kPagedThreads / 4], s_l[kPagedThreads / 4];
     const nm_paged_desc& d = a.d;
-    const int tid = threadIdx.x, b = blockIdx.x / d.hq, h = blockIdx.x % d.hq, g = h / a.group, set = 16 * a.sets;
+    const int tid = threadIdx.x, b = blockIdx.x / d.hq, h = blockIdx.x % d.hq, g = h / a.group;
     const int lead = a.lead[b];
     const long bh = (long)b * d.hq + h, all = (long)d.B * d.hq;
-    // [0] the prefix, [1] the row's own: pieces, the first's worker and slot, the query's number among the piece's
+    // [0] the prefix, [1] the row's own positions; and the query's number in the range
     int4 info[2] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
-    int nth[2];
-    {
-        const int i = h % a.group;
-        nth[1] = i % set;
-        info[1] = a.info[all + (long)b * d.hq + g * a.group + i - nth[1]];
-    }
+    int nth[2] = {0, h % a.group % a.tile[0]};
+    info[1] = a.info[all + bh - nth[1]];
     if (info[1].x < 0) return;
     if (lead >= 0) {
         const int i = (b - lead) * a.group + h % a.group;
-        nth[0] = i % set;
+        nth[0] = i % a.tile[2];
         const int i0 = i - nth[0];
         info[0] = a.info[(long)(lead + i0 / a.group) * d.hq + g * a.group + i0 % a.group];
     }
@@ -503,9 +789,10 @@ __global__ __launch_bounds__(kPagedThreads) void shared_join_kernel(SharedArgs a
         for (int k = mine; k < used; k += at_once) {
             const int own = k >= info[0].x, i = own ? k - info[0].x : k;
             const int4 of = info[own];
-            const long part = of.z < 0 ? own * all + bh : ((long)(of.y + i) * 2 + (i == 0 ? of.z : 0)) * set + nth[own];
-            const float2 ml = (of.z < 0 ? a.whole_ml : a.part_ml)[part];
-            const v4f y = *reinterpret_cast<const v4f*>((of.z < 0 ? a.whole_o : a.part_o) + part * d.d + c);
+            const bool whole = of.y < 0;
+            const long part = whole ? own * all + bh : (i ? of.z + (long)(i - 1) * of.w : of.y) + nth[own];
+            const float2 ml = (whole ? a.whole_ml : a.part_ml)[part];
+            const v4f y = *reinterpret_cast<const v4f*>((whole ? a.whole_o : a.part_o) + part * d.d + c);
             const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.0f : top;
             const float shrink = __builtin_amdgcn_exp2f(m - base), by = __builtin_amdgcn_exp2f(ml.x - base);
             l = l * shrink + ml.y * by;
@@ -530,11 +817,17 @@ __global__ __launch_bounds__(kPagedThreads) void shared_join_kernel(SharedArgs a
     if (tid == 0 && d.lse) d.lse[bh] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
 }
 
+template <typename C, typename T, int DP, int kQ, int kP>
+static void launch_shared(const SharedArgs& a, hipStream_t s)
+{
+    // either list's workers rounded up to one for every XCD
+    queue_kernel(shared_attention_kernel<C, T, DP, kQ, kP>, dim3((a.workers + 7) / 8 * 8 + 8), dim3(kPagedThreads), 0, s, a);
+    if (a.G && (long)a.d.B * a.group > a.tile[1]) queue_kernel(shared_prefix_kernel<C, T, DP, kQ, kP>, dim3(a.last), dim3(64 * shared_waves(2)), 0, s, a);
+}
 template <typename C, typename T, int DP>
 static void launch_shared(const SharedArgs& a, bool own, hipStream_t s)
 {
-    if (own) queue_kernel(shared_attention_kernel<C, T, DP, 1, 2, shared_sets(DP)>, dim3((a.workers + 7) / 8 * 8), dim3(kPagedThreads), 0, s, a);
-    else queue_kernel(shared_attention_kernel<C, T, DP, 3, 3, shared_sets(DP)>, dim3((a.workers + 7) / 8 * 8), dim3(kPagedThreads), 0, s, a);
+    own ? launch_shared<C, T, DP, 1, 2>(a, s) : launch_shared<C, T, DP, 3, 3>(a, s);
 }
 // One term of a query where the matrix instructions' type is its own, and two of the weights where the result has 16 bits or fewer.
 static bool one_term(const nm_paged_desc& d)
@@ -583,15 +876,17 @@ static int32_t plan_shared(const nm_shared_desc* d, SharedArgs* a, void* ws, siz
     a->shift = page_shift(d->p.page_size);
     a->group = d->p.hq / d->p.hk;
     const int width = paged_width(d->p.d);
-    a->sets = shared_sets(width);
+    for (int list = 0; list < kLists; ++list) a->tile[list] = shared_tile(list, width, one_term(d->p) ? 1 : 3);
     a->workers = 256 * (width <= 128 ? 2 : 1);
-    const size_t parts = (size_t)a->workers * 2 * 16 * a->sets, queries = (size_t)d->p.B * d->p.hq;
+    a->whole_queries = aligned_rows(d->p.q, d->p.q_stride, d->p.q_dtype, 8);
+    a->last = 256;
+    const size_t parts = (size_t)a->workers * 2 * (a->tile[0] + a->tile[1]) + (size_t)a->last * 2 * a->tile[2], queries = (size_t)d->p.B * d->p.hq;
     Carve c{static_cast<char*>(ws)};
     c.take(a->head, 1);
     c.take(a->ent, (size_t)d->G + d->p.B);
     c.take(a->info, 2 * queries);
-    c.take(a->before, a->workers);
-    c.take(a->first, a->workers);
+    c.take(a->before, kLists * a->workers);
+    c.take(a->first, kLists * a->workers);
     c.take(a->lead, d->p.B);
     c.take(a->part_ml, parts);
     c.take(a->whole_ml, 2 * queries);
