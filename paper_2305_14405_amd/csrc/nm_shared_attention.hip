@@ -15,6 +15,7 @@ namespace nm {
 constexpr int kSharedMost = NM_PLAN_MAX_REQUESTS;     // rows, groups
 constexpr int kSharePrefix = kUnit;                   // shorter prefixes are every row's own
 constexpr int kPlanners = 1024;
+constexpr long kFewUnits = 1024;
 constexpr int kLists = 3;
 
 // Wavefronts of a list's workgroups; sixteens of queries that one has of a range, by the heads' size and the terms of a query; and queries of a range.
@@ -69,8 +70,13 @@ struct Entity {
 
 __global__ __launch_bounds__(kPlanners) void shared_plan_kernel(SharedArgs a)
 {
-    __shared__ long s_before[2 * kSharedMost + 1], s_wave[kPlanners / 64];
-    __shared__ int s_start[kSharedMost + 1], s_lead[kSharedMost];
+    // the groups' starts and first rows that take part; then, of each list, the cost of the entities in front of each (rows are on the first alone)
+    __shared__ union {
+        struct { int start[kSharedMost + 1], lead[kSharedMost]; } g;
+        struct { long rows[2 * kSharedMost + 1], groups[kLists - 1][kSharedMost + 1]; } before;
+    } s;
+    __shared__ long s_wave[kLists][kPlanners / 64];
+    int (&s_start)[kSharedMost + 1] = s.g.start, (&s_lead)[kSharedMost] = s.g.lead;
     const int tid = threadIdx.x, B = a.d.B, lane = tid & 63;
     bool good = true;
     for (int g = tid; g <= a.G; g += kPlanners) s_start[g] = a.G ? a.group_start[g] : 0;
@@ -107,63 +113,74 @@ __global__ __launch_bounds__(kPlanners) void shared_plan_kernel(SharedArgs a)
         a.ent[g] = make_int4(s_start[g], shares ? s_start[g + 1] - s_start[g] : 0, shares ? s_lead[g] : 0, shares ? (int)min((long)a.shared[g], cap) : 0);
     }
     __syncthreads();
-    // a thread's run of entities, then the threads'; one list after the other (entities of the others cost nothing)
+    // a thread's run of entities, then the threads' (an entity costs nothing on the lists that it is not on)
     const int n = a.G + B, per = (n + kPlanners - 1) / kPlanners, e0 = min(tid * per, n), e1 = min(e0 + per, n);
-    long cost[kLists], front[kLists];
-    for (int list = 0; list < kLists; ++list) cost[list] = 0;
+    long mine[kLists], in[kLists], front[kLists], cost[kLists];
+#pragma unroll
+    for (int list = 0; list < kLists; ++list) mine[list] = 0;
     for (int e = e0; e < e1; ++e) {
         const Entity x(a, e);
-        for (int list = 0; list < kLists; ++list) cost[list] += x.list == list ? x.all(a) : 0;
+        const long all = x.all(a);
+#pragma unroll
+        for (int list = 0; list < kLists; ++list) mine[list] += x.list == list ? all : 0;
     }
+#pragma unroll
+    for (int list = 0; list < kLists; ++list) in[list] = mine[list];
+#pragma unroll
+    for (int step = 1; step < 64; step <<= 1)
+#pragma unroll
+        for (int list = 0; list < kLists; ++list) {
+            const long t = __shfl_up(in[list], step);
+            if (lane >= step) in[list] += t;
+        }
+#pragma unroll
+    for (int list = 0; list < kLists; ++list)
+        if (lane == 63) s_wave[list][tid >> 6] = in[list];
+    __syncthreads();
+#pragma unroll
     for (int list = 0; list < kLists; ++list) {
-        const long mine = cost[list];
-        long in = mine;
-        for (int step = 1; step < 64; step <<= 1) {
-            const long t = __shfl_up(in, step);
-            if (lane >= step) in += t;
-        }
-        __syncthreads();
-        if (lane == 63) s_wave[tid >> 6] = in;
-        __syncthreads();
-        front[list] = in - mine;
+        front[list] = in[list] - mine[list];
         cost[list] = 0;
+#pragma unroll
         for (int w = 0; w < kPlanners / 64; ++w) {
-            if (w < tid >> 6) front[list] += s_wave[w];
-            cost[list] += s_wave[w];
+            const long t = s_wave[list][w];
+            front[list] += w < tid >> 6 ? t : 0;
+            cost[list] += t;
         }
     }
+    for (int e = e0; e < e1; ++e) {
+        s.before.rows[e] = front[0];
+        if (e < a.G) s.before.groups[0][e] = front[1], s.before.groups[1][e] = front[2];
+        const Entity x(a, e);
+        const long all = x.all(a);
+#pragma unroll
+        for (int list = 0; list < kLists; ++list) front[list] += x.list == list ? all : 0;
+    }
+    if (tid == 0) s.before.rows[n] = cost[0], s.before.groups[0][a.G] = cost[1], s.before.groups[1][a.G] = cost[2];
     // the first two lists' workers by their cost
     const long both = cost[0] + cost[1];
     const long second = cost[1] ? min(max(1l, (long)((double)a.workers * (double)cost[1] / (double)both + 0.5)), (long)a.workers - (cost[0] > 0)) : 0;
     const long workers[kLists] = {min((long)a.workers - second, cost[0]), min(second, cost[1]), min((long)a.last, cost[2])};
-    for (int list = 0; list < kLists; ++list) {
-        if (!workers[list]) continue;                  // uniform
-        __syncthreads();
-        long at = front[list];
-        for (int e = e0; e < e1; ++e) {
-            s_before[e] = at;
-            const Entity x(a, e);
-            at += x.list == list ? x.all(a) : 0;
-        }
-        if (tid == 0) s_before[n] = cost[list];
-        __syncthreads();
-        const Shares shares(cost[list], workers[list]);
-        if (tid == 0) {
+    __syncthreads();
+    for (long i = tid; i < workers[0] + workers[1] + workers[2]; i += kPlanners) {
+        const int list = i < workers[0] ? 0 : i < workers[0] + workers[1] ? 1 : 2;
+        const long w = i - (list > 0 ? workers[0] : 0) - (list > 1 ? workers[1] : 0);
+        const Shares shares(list == 0 ? cost[0] : list == 1 ? cost[1] : cost[2], list == 0 ? workers[0] : list == 1 ? workers[1] : workers[2]);
+        if (w == 0) {
             a.head->each[list] = shares.each;
             a.head->more[list] = shares.more;
         }
-        for (int w = tid; w < workers[list]; w += kPlanners) {
-            const long x = shares.begin(w);
-            int lo = 0, hi = n;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) / 2;
-                if (s_before[mid] <= x) lo = mid; else hi = mid;
-            }
-            a.first[list * a.workers + w] = lo;
-            a.before[list * a.workers + w] = s_before[lo];
+        const long x = shares.begin(w);
+        const long* before = list == 0 ? s.before.rows : s.before.groups[list - 1];
+        int lo = 0, hi = list == 0 ? n : a.G;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (before[mid] <= x) lo = mid; else hi = mid;
         }
+        a.first[list * a.workers + w] = lo;
+        a.before[list * a.workers + w] = before[lo];
     }
-    if (tid < kLists) a.head->workers[tid] = (int)workers[tid];
+    if (tid < kLists) a.head->workers[tid] = (int)(tid == 0 ? workers[0] : tid == 1 ? workers[1] : workers[2]);
 }
 
 // What a workgroup has of a range: positions [k0, k1) by the table of row `table` (-1: none) for key head g and the n queries from number i0 on of the rows from
@@ -406,13 +423,14 @@ struct Tiles {
 // Memory of a workgroup.
 template <int DP, int kQ, int W>
 struct SharedLds {
+    static constexpr int kBuffers = W > kPagedWaves && DP <= 128 ? 2 : 1;   // eight wavefronts have a CU's memory for themselves
     union {
         struct { short q[kQ][16 * (DP + 8)], tile[kPagedWaves][kTile * (DP + 8)]; } few;
-        struct { short k[kPagedWaves][kTile * (DP + 8)], v[kPagedWaves][kTile * (DP + 8)]; } many;
+        struct { short k[kPagedWaves][kTile * (DP + 8)], v[kPagedWaves][kTile * (DP + 8)]; } many[kBuffers];
         float o[W][16][DP];
     };
     float m[W][16], l[W][16], q_scale[16];
-    unsigned long valid[kPagedWaves];
+    unsigned long valid[kBuffers][kPagedWaves];
 };
 
 // A run through the first list: ranges of up to 16 queries, tiles of a wavefront's own.  What the first tile of a piece needs is requested while the
@@ -643,20 +661,35 @@ __device__ __forceinline__ void run_many(const SharedArgs& a, Run run, SharedLds
             m[t] = -INFINITY;
             l[t] = 0.0f;
         }
-        for (int u0 = now.k0; u0 < k1; u0 += kUnit) {
-            __syncthreads();                                  // the positions before are done with
-            x.stage(keys ? s.many.k[brings] : s.many.v[brings], kr, valid);
-            if constexpr (kBoth) x.stage(s.many.v[brings], vr, valid);
-            if (keys && x.lane == 0) s.valid[brings] = valid;
-            __syncthreads();
+        // 128 positions from registers into a buffer, and the next ones on their way
+        auto bring = [&](auto& to, unsigned long (&there)[kPagedWaves]) {
+            x.stage(keys ? to.k[brings] : to.v[brings], kr, valid);
+            if constexpr (kBoth) x.stage(to.v[brings], vr, valid);
+            if (keys && x.lane == 0) there[brings] = valid;
             const unsigned place = x.place_of(now, t0 + kUnit, entry2, valid);
             t0 += kUnit;
             entry2 = x.entry_of(now, t0 + kUnit);
             fetch(place);                                     // (behind the last: the first page)
+        };
+        constexpr bool kTwo = SharedLds<DP, kQ, W>::kBuffers > 1;
+        if (kTwo) {
+            __syncthreads();                                  // the piece before is done with LDS
+            bring(s.many[0], s.valid[0]);
+        }
+        int buffer = 0;
+        for (int u0 = now.k0; u0 < k1; u0 += kUnit, buffer ^= kTwo) {
+            __syncthreads();                                  // the positions before are done with, and (of two buffers) these are there
+            if (!kTwo) {
+                bring(s.many[0], s.valid[0]);
+                __syncthreads();
+            } else if (u0 + kUnit < k1) {
+                bring(s.many[buffer ^ 1], s.valid[buffer ^ 1]);
+            }
+            const auto& many = s.many[buffer];
             const int tiles = min((k1 - u0 + kTile - 1) / kTile, kPagedWaves);
 #pragma unroll 1
             for (int n = part; n < tiles; n += parts) {
-                const unsigned long bits = s.valid[n];         // uniform, which the compiler cannot know
+                const unsigned long bits = s.valid[buffer][n];         // uniform, which the compiler cannot know
                 const unsigned long there = (unsigned long)(unsigned)__builtin_amdgcn_readfirstlane((int)(bits >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)bits);
                 v4f sc[S][2];
 #pragma unroll
@@ -665,7 +698,7 @@ __device__ __forceinline__ void run_many(const SharedArgs& a, Run run, SharedLds
                 for (int step = 0; step < X::kSteps; ++step)
 #pragma unroll
                     for (int blk = 0; blk < 2; ++blk) {
-                        const v8s ka = x.keys_of(s.many.k[n], blk, step);
+                        const v8s ka = x.keys_of(many.k[n], blk, step);
 #pragma unroll
                         for (int t = 0; t < S; ++t)
 #pragma unroll
@@ -675,7 +708,7 @@ __device__ __forceinline__ void run_many(const SharedArgs& a, Run run, SharedLds
                 x.template weigh<S, kP>(sc, there, factor, m, l, p, o);
 #pragma unroll
                 for (int blk = 0; blk < X::kBlocks; ++blk) {
-                    const v8s va = x.values_of(s.many.v[n], blk);
+                    const v8s va = x.values_of(many.v[n], blk);
 #pragma unroll
                     for (int t = 0; t < S; ++t)
 #pragma unroll
@@ -867,7 +900,10 @@ static int32_t plan_shared(const nm_shared_desc* d, SharedArgs* a, void* ws, siz
     if (d->G < 0) return fail(NM_ERR_INVALID_ARG, "%s: G is negative", what);
     if (d->p.window) return fail(NM_ERR_UNSUPPORTED, "%s: a window", what);
     if (d->p.B > kSharedMost || d->G > kSharedMost) return fail(NM_ERR_UNSUPPORTED, "%s: B %d or G %d > %d", what, d->p.B, d->G, kSharedMost);
-    *alone = !divided;
+    // rows that are not divided, and few units in all, which every workgroup then has one or two of whether or not they are shared (the first kernel and the
+    // third take longer than what sharing saves)
+    const long most = (long)d->p.B * d->p.hk * ((((long)d->p.max_pages << page_shift(d->p.page_size)) + kUnit - 1) / kUnit);
+    *alone = !divided || d->G == 0 || most <= kFewUnits;
     *a = SharedArgs{};
     a->d = d->p;
     a->G = d->G;
@@ -892,8 +928,8 @@ static int32_t plan_shared(const nm_shared_desc* d, SharedArgs* a, void* ws, siz
     c.take(a->whole_ml, 2 * queries);
     c.take(a->part_o, parts * d->p.d);
     c.take(a->whole_o, 2 * queries * d->p.d);
-    *bytes = *alone ? 0 : c.used;
-    return NM_OK;
+    *bytes = c.used;
+    return *alone ? nm_paged_attention_workspace(&d->p, bytes) : NM_OK;
 }
 
 }  // namespace nm
@@ -927,9 +963,10 @@ int32_t nm_shared_attention(const nm_shared_desc* desc, void* ws, size_t ws_byte
     if (desc->G && (!desc->group_start || !desc->shared)) return fail(NM_ERR_INVALID_ARG, "nm_shared_attention: group_start or shared is NULL");
     if (begins_as(d.out, {desc->group_start, desc->shared}) || begins_as(d.lse, {desc->group_start, desc->shared}))
         return fail(NM_ERR_INVALID_ARG, "nm_shared_attention: out or lse is group_start or shared");
-    if (alone) return nm_paged_attention(&d, nullptr, 0, stream);
+    if (alone && !need) return nm_paged_attention(&d, nullptr, 0, stream);
     if (!ws || ws_bytes < need) return fail(NM_ERR_WORKSPACE, "nm_shared_attention: workspace of %zu bytes needed, %zu given", need, ws ? ws_bytes : (size_t)0);
     if (!aligned(ws, 256)) return fail(NM_ERR_WORKSPACE, "nm_shared_attention: workspace must be 256-byte aligned");
+    if (alone) return nm_paged_attention(&d, ws, ws_bytes, stream);
     const hipStream_t s = (hipStream_t)stream;
     queue_kernel(shared_plan_kernel, dim3(1), dim3(kPlanners), 0, s, a);
     if (d.cache_dtype == NM_DT_BF16) launch_shared<bf16, bf16>(a, s);

@@ -16,7 +16,8 @@ def shared_case(seed, groups, hq, hk, d, q_dtype, cache_dtype, page=16, by_head=
     prefix that ends inside a page has that page's slots in a page of every row.  Free slots, and pages that no row owns, hold NaN (codes: -128)."""
     g = gen(seed)
     lens = [n for _, rows in groups for n in rows]
-    columns = max([-(-max(n, 0) // page) for n in lens] + [1]) if columns is None else columns
+    if columns is None:                                                      # wide enough that the rows are not taken one by one
+        columns = max([-(-max(n, 0) // page) for n in lens] + [-(-1100 // (len(lens) * hk)) * 128 // page + 1])
     most = sum(-(-max(n, 0) // page) for n in lens) + 9
     B = len(lens)
     shape = (2, most, hk, page, d) if by_head else (2, most, page, hk, d)
@@ -130,10 +131,15 @@ def test_shared_attention_long_many_and_wide(groups, hq, hk, d, dtype):
 
 
 def test_shared_attention_short_tables_need_no_workspace():
-    c = shared_case(2, [(200, [201, 300, 7]), (100, [150] * 3)], 6, 3, 64, torch.float16, torch.float16)
+    c = shared_case(2, [(200, [201, 300, 7]), (100, [150] * 3)], 6, 3, 64, torch.float16, torch.float16, columns=19)
     args = (c["q"], c["cache"][0], c["cache"][1], c["table"], c["lens"], c["start"], c["shared"], torch.empty_like(c["q"]))
     assert nm.nm_shared_attention_workspace(*args, scale=1.0) == 0
     check(c, torch.float16)
+
+
+def test_shared_attention_of_few_units():
+    """Rows that are divided, but too few for sharing: taken one by one."""
+    check(shared_case(13, [(700, [701, 750, 800, 0])], 12, 12, 64, torch.float32, torch.bfloat16, columns=51), torch.float32)
 
 
 def test_shared_attention_without_groups():
@@ -152,7 +158,7 @@ def test_shared_attention_groups_that_are_none(start):
 
 def test_shared_attention_bad_tables_lengths_and_prefixes():
     """Entries that are no pages take no part, lengths beyond the table count as the table's; a prefix longer than its rows is no one's."""
-    c = shared_case(6, [(400, [500, 600, 450]), (300, [301] * 4)], 4, 2, 64, torch.bfloat16, torch.bfloat16, columns=40)
+    c = shared_case(6, [(400, [500, 600, 450]), (300, [301] * 4)], 4, 2, 64, torch.bfloat16, torch.bfloat16, columns=1200)
     for b in (0, 1, 2):
         c["table"][b, 3], c["table"][b, 7] = -5, 10 ** 6
     c["table"][1, 30] = 2 ** 31 - 1
@@ -214,7 +220,7 @@ def test_shared_attention_is_what_paged_attention_gives():
 
 def test_shared_attention_twice_at_once_and_replayed():
     """Two calls on two streams with workspaces of their own; a captured call, replayed while lengths, groups and tables change, its workspace filled anew."""
-    a = shared_case(11, [(600, [650] * 6), (300, [400] * 5)], 8, 2, 64, torch.bfloat16, torch.bfloat16, columns=60)
+    a = shared_case(11, [(600, [650] * 6), (300, [400] * 5)], 8, 2, 64, torch.bfloat16, torch.bfloat16, columns=900)
     b = shared_case(12, [(900, [950] * 3)], 8, 2, 64, torch.bfloat16, torch.bfloat16)
     wants = [attend(c, torch.bfloat16, 0.125) for c in (a, b)]
     s = torch.cuda.Stream()
