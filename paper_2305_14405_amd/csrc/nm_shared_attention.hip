@@ -302,7 +302,7 @@ struct Tiles {
         }
     }
     // whether the lane's score number i, of position i / 4 * 16 + j * 4 + i % 4, takes part
-    __device__ __forceinline__ bool scored(int i, unsigned long valid) const
+    static __device__ __forceinline__ bool scored(int i, int j, unsigned long valid)
     {
         const int at = i / 4 * 16 + j * 4 + i % 4;
         const int group = kPairs ? at / (2 * kLoads) * 2 + (at & 1) : at / kLoads, nth = kPairs ? at % (2 * kLoads) / 2 : at % kLoads;
@@ -322,11 +322,12 @@ struct Tiles {
     template <int S, int kP>
     __device__ __forceinline__ void weigh(v4f (&sc)[S][2], unsigned long valid, const float (&factor)[S], float (&m)[S], float (&l)[S], v8s (&p)[S][kP], v4f (&o)[S][kBlocks]) const
     {
-        if (valid != ~0ul) {
-            asm volatile("");                                 // a branch: few tiles need it
+        if (valid != ~0ul) {                                  // a branch: few tiles need it, and nothing of it is to be held in registers
+            int group = j;
+            asm volatile("" : "+v"(group));
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const bool in = scored(i, valid);
+                const bool in = scored(i, group, valid);
 #pragma unroll
                 for (int t = 0; t < S; ++t) sc[t][i / 4][i % 4] = in ? sc[t][i / 4][i % 4] : -INFINITY;
             }
@@ -694,25 +695,36 @@ __device__ __forceinline__ void run_many(const SharedArgs& a, Run run, SharedLds
                 v4f sc[S][2];
 #pragma unroll
                 for (int t = 0; t < S; ++t) sc[t][0] = sc[t][1] = v4f{0, 0, 0, 0};
+                // reads run ahead of the products that use them, which the compiler by itself puts next to one another
+                constexpr int kFrags = 2 * X::kSteps, kAhead = 3;
+                v8s ka[kFrags];
 #pragma unroll
-                for (int step = 0; step < X::kSteps; ++step)
+                for (int i = 0; i < kAhead; ++i) ka[i] = x.keys_of(many.k[n], i % 2, i / 2);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int blk = 0; blk < 2; ++blk) {
-                        const v8s ka = x.keys_of(many.k[n], blk, step);
-#pragma unroll
-                        for (int t = 0; t < S; ++t)
-#pragma unroll
-                            for (int q = kQ - 1; q >= 0; --q) sc[t][blk] = Mma<T>::mma(ka, qb[t][q][step], sc[t][blk]);
-                    }
-                v8s p[S][kP];
-                x.template weigh<S, kP>(sc, there, factor, m, l, p, o);
-#pragma unroll
-                for (int blk = 0; blk < X::kBlocks; ++blk) {
-                    const v8s va = x.values_of(many.v[n], blk);
+                for (int i = 0; i < kFrags; ++i) {
+                    if (i + kAhead < kFrags) ka[i + kAhead] = x.keys_of(many.k[n], (i + kAhead) % 2, (i + kAhead) / 2);
 #pragma unroll
                     for (int t = 0; t < S; ++t)
 #pragma unroll
-                        for (int q = kP - 1; q >= 0; --q) o[t][blk] = Mma<T>::mma(va, p[t][q], o[t][blk]);
+                        for (int q = kQ - 1; q >= 0; --q) sc[t][i % 2] = Mma<T>::mma(ka[i], qb[t][q][i / 2], sc[t][i % 2]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                v8s p[S][kP];
+                x.template weigh<S, kP>(sc, there, factor, m, l, p, o);
+                constexpr int kBehind = 2;
+                v8s va[X::kBlocks];
+#pragma unroll
+                for (int blk = 0; blk < kBehind; ++blk) va[blk] = x.values_of(many.v[n], blk);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int blk = 0; blk < X::kBlocks; ++blk) {
+                    if (blk + kBehind < X::kBlocks) va[blk + kBehind] = x.values_of(many.v[n], blk + kBehind);
+#pragma unroll
+                    for (int q = kP - 1; q >= 0; --q)
+#pragma unroll
+                        for (int t = 0; t < S; ++t) o[t][blk] = Mma<T>::mma(va[blk], p[t][q], o[t][blk]);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
