@@ -359,17 +359,26 @@ struct Tiles {
 #pragma unroll
         for (int t = 0; t < S; ++t) {
             const float lifted = kLift - (m[t] == -INFINITY ? 0.0f : m[t]);
+            typedef float Pair __attribute__((ext_vector_type(2)));
+            typedef T Term __attribute__((ext_vector_type(2)));
+            Pair sum = {0, 0};
+            v4u words[kP];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][i / 4][i % 4], factor[t], lifted));
-                l[t] += w;
+            for (int i = 0; i < 8; i += 2) {                  // by two: one conversion
+                Pair w;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) w[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][(i + k) / 4][(i + k) % 4], factor[t], lifted));
+                sum += w;
 #pragma unroll
                 for (int q = 0; q < kP; ++q) {
-                    const T v = (T)w;
-                    w = __builtin_fmaf((float)v, -1.0f, w);
-                    p[t][q][i] = __builtin_bit_cast(short, v);
+                    const Term v = __builtin_convertvector(w, Term);
+                    if (q + 1 < kP) w -= __builtin_convertvector(v, Pair);   // exact
+                    words[q][i / 2] = __builtin_bit_cast(unsigned, v);
                 }
             }
+#pragma unroll
+            for (int q = 0; q < kP; ++q) p[t][q] = __builtin_bit_cast(v8s, words[q]);
+            l[t] += sum[0] + sum[1];
         }
     }
     // Calls use(Q{}) with the queries' type: that of the matrix instructions where they are of one term.  (One branch in front of all loads: a branch at
