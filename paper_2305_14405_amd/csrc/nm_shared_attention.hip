@@ -29,7 +29,10 @@ struct SharedArgs {
     int G;
     const int32_t* group_start;
     const int32_t* shared;
-    int shift, group;            // log2 of page_size, query heads of a key head
+    int shift, own;              // log2 of page_size, query heads of a key head
+    // Neighbouring key heads of int8 may be taken as one, whose queries are zero but in their own head's part (codes are finite): how many there are then, their
+    // elements and query heads, and how many are one.
+    int heads, width, group, pack;
     int tile[kLists];            // queries of a range
     int workers, last;           // of the first two lists, and of the third
     int whole_queries;           // 8 elements of a query may be read at once
@@ -65,7 +68,7 @@ struct Entity {
         extra = 2;                                            // beginning and ending a range, in units
     }
     __device__ __forceinline__ long cost() const { return units + extra; }                             // of a key head's tile, in units
-    __device__ __forceinline__ long all(const SharedArgs& a) const { return cost() * a.d.hk * tiles; }
+    __device__ __forceinline__ long all(const SharedArgs& a) const { return cost() * a.heads * tiles; }
 };
 
 __global__ __launch_bounds__(kPlanners) void shared_plan_kernel(SharedArgs a)
@@ -262,7 +265,7 @@ struct Tiles {
         row_piece = lane % kRowPieces;
         row_first = lane / kRowPieces;
         my_position = position_of(row_first, lane % kLoads);
-        in_row = row_piece * kPer16 < a.d.d;
+        in_row = row_piece * kPer16 < a.width;
         lane_bytes = in_row ? row_piece * 16 : 0;
     }
     // A tile's places: a lane has one position's distance into the cache in 16 bytes, 0 where it takes no part.  Loads are not
@@ -282,7 +285,7 @@ struct Tiles {
     }
     __device__ __forceinline__ void fetch(const void* cache, const SharedPiece& n, unsigned place, v4u (&to)[kLoads]) const
     {
-        const char* base = a.d.num_pages ? static_cast<const char*>(cache) + (long)n.g * a.d.head_stride * sizeof(C) + lane_bytes : reinterpret_cast<const char*>(g_zero_line);
+        const char* base = a.d.num_pages ? static_cast<const char*>(cache) + (long)n.g * (a.pack * a.d.head_stride) * sizeof(C) + lane_bytes : reinterpret_cast<const char*>(g_zero_line);
         fetch_rows<kLoads>(base, place, to, std::make_integer_sequence<int, kLoads>{});
         __builtin_amdgcn_sched_barrier(0);                    // the order of the loads is what is waited for
     }
@@ -292,7 +295,7 @@ struct Tiles {
         short* to = tile + position_of(row_first, 0) * kStride + row_piece * kPer16;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) put<C, T>(to + i * kRow, from[i]);
-        if (valid != ~0ul || a.d.d != DP) {
+        if (valid != ~0ul || a.width != DP) {
 #pragma unroll 1
             for (int i = 0; i < kLoads; ++i)
                 if (!in_row || !(valid >> (lane - row_piece + i) & 1)) {
@@ -397,8 +400,13 @@ struct Tiles {
         const int i = n.i0 + row;
         return (long)(n.row0 + i / a.group) * a.d.q_stride + (long)(n.g * a.group + i % a.group) * a.d.d;
     }
-    // What a query's scores are multiplied by, but for its own scale; the sign of the scale goes with the queries.
-    __device__ __forceinline__ float scale_of(int g) const { return a.d.scale * 1.44269504088896340736f * (sizeof(C) == 1 ? a.d.k_scale[g] : 1.0f); }
+    // Of a range's query number `row`: which of the heads taken as one is its own, and what its scores are multiplied by, but for its own scale; the sign goes with
+    // the query.
+    __device__ __forceinline__ int part_of(const SharedPiece& n, int row) const { return sizeof(C) == 1 ? (n.i0 + row) % a.group / a.own : 0; }
+    __device__ __forceinline__ float scale_of(const SharedPiece& n, int row) const
+    {
+        return a.d.scale * 1.44269504088896340736f * (sizeof(C) == 1 ? a.d.k_scale[n.g * a.pack + part_of(n, row)] : 1.0f);
+    }
     // Powers of two that bring a query of three terms below 4, and back.
     static __device__ __forceinline__ void level(float top, float& down, float& up)
     {
@@ -421,7 +429,7 @@ struct Tiles {
             });
             return;
         }
-        const float over = (sum == 0.0f ? 0.0f : 1.0f / sum) * (sizeof(C) == 1 ? d.v_scale[n.g] : 1.0f);
+        const float over = (sum == 0.0f ? 0.0f : 1.0f / sum) * (sizeof(C) == 1 ? d.v_scale[h / a.own] : 1.0f);
         elements([&](int c, v4f y) {
             if (c == 0 && d.lse) d.lse[(long)b * d.hq + h] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
 #pragma unroll
@@ -469,19 +477,20 @@ __device__ __forceinline__ void run_few(const SharedArgs& a, Run run, SharedLds<
         const int then_t0 = then.k0 + wave * kTile;
         const int then_entry = x.entry_of(then, then_t0), then_entry2 = x.entry_of(then, then_t0 + kStep);
         entry = entry2;
-        const int g = now.g, k1 = now.k1;
-        const float by = x.scale_of(g);
+        const int k1 = now.k1, mine = min(qrow, now.n - 1), part = x.part_of(now, mine);   // this thread's query's
+        const float by = x.scale_of(now, mine);
         __syncthreads();                                      // the piece before is done with LDS
         {
-            const long at = x.query_of(now, min(qrow, now.n - 1));
+            const long at = x.query_of(now, mine);
+            const int c0 = qc - part * a.d.d;                  // the thread's first element of its own head
             float y[DP / 16], top = 0.0f, down = 1.0f, up = 1.0f;
             x.template typed<kQ>([&](auto type) {
                 using Q = decltype(type);
                 Q raw[DP / 16];
 #pragma unroll
-                for (int c = 0; c < DP / 16; ++c) raw[c] = static_cast<const Q*>(a.d.q)[at + min(qc + 16 * c, a.d.d - 1)];
+                for (int c = 0; c < DP / 16; ++c) raw[c] = static_cast<const Q*>(a.d.q)[at + min(max(c0 + 16 * c, 0), a.d.d - 1)];
 #pragma unroll
-                for (int c = 0; c < DP / 16; ++c) y[c] = qrow < now.n && qc + 16 * c < a.d.d ? (float)raw[c] : 0.0f;
+                for (int c = 0; c < DP / 16; ++c) y[c] = qrow < now.n && (unsigned)(c0 + 16 * c) < (unsigned)a.d.d ? (float)raw[c] : 0.0f;
             });
             if (kQ > 1) {
 #pragma unroll
@@ -498,11 +507,11 @@ __device__ __forceinline__ void run_few(const SharedArgs& a, Run run, SharedLds<
                     s.few.q[q][qrow * kStride + qc + 16 * c] = __builtin_bit_cast(short, v);
                 }
             }
-            if (qc == 0) s.q_scale[qrow] = up;
+            if (qc == 0) s.q_scale[qrow] = fabsf(by) * up;
         }
         __syncthreads();
         // never 0, so that it takes a masked score, minus infinity, for what it is
-        const float factor[1] = {fmaxf(fabsf(by) * s.q_scale[x.column], 1.17549435e-38f)};
+        const float factor[1] = {fmaxf(s.q_scale[x.column], 1.17549435e-38f)};
         if (t0 >= k1) {                                       // no tile for this wavefront
             const unsigned place = x.place_of(then, then_t0, then_entry, valid);
             x.fetch(a.d.k_cache, then, place, kr);
@@ -565,12 +574,11 @@ __device__ __forceinline__ void run_few(const SharedArgs& a, Run run, SharedLds<
             const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
             for (int w = 0; w < W; ++w) sum += s.l[w][qrow] * __builtin_amdgcn_exp2f(s.m[w][qrow] - base - X::kLift);
-            const long part = Run::part_of(a, 0, run.worker, max(now.slot, 0));
-            x.leave(now, qrow, part, [&](auto put) {
+            x.leave(now, qrow, Run::part_of(a, 0, run.worker, max(now.slot, 0)), [&](auto put) {
                 for (int c = qc * 4; c < a.d.d; c += 64) {
                     v4f y{0, 0, 0, 0};
 #pragma unroll
-                    for (int w = 0; w < W; ++w) y += *reinterpret_cast<const v4f*>(&s.o[w][qrow][c]);
+                    for (int w = 0; w < W; ++w) y += *reinterpret_cast<const v4f*>(&s.o[w][qrow][part * a.d.d + c]);
                     put(c, y);
                 }
             }, top, sum);
@@ -592,7 +600,7 @@ __device__ __forceinline__ void run_many(const SharedArgs& a, Run run, SharedLds
     const X x(a);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), qrow = tid / 16 % 16, qc = tid & 15;
     for (SharedPiece now = run.next(a); now.table >= 0; now = run.next(a)) {
-        const int g = now.g, k1 = now.k1;
+        const int k1 = now.k1;
         // wavefronts that have queries of their own, and which of them (and which part of the positions) this one has
         const int apart = now.n <= 16 * S ? 1 : now.n <= 32 * S ? 2 : W == 4 || now.n <= 64 * S ? 4 : W, mine = wave % apart, part = wave / apart, parts = W / apart;
         const int brings = wave % kPagedWaves;
@@ -607,7 +615,6 @@ __device__ __forceinline__ void run_many(const SharedArgs& a, Run run, SharedLds
         };
         fetch(x.place_of(now, t0, entry, valid));
         // queries, as operands: a lane has those of column `column`, 8 elements of each step
-        const float by = x.scale_of(g);
         v8s qb[S][kQ][X::kSteps];
         float factor[S];
         x.template typed<kQ>([&](auto type) {
@@ -620,10 +627,11 @@ __device__ __forceinline__ void run_many(const SharedArgs& a, Run run, SharedLds
                 for (int t = 0; t < S; ++t) {
                     const int row = (mine * S + t) * 16 + x.column;
                     const Q* from = static_cast<const Q*>(a.d.q) + x.query_of(now, min(row, now.n - 1));
+                    const int c0 = x.j * 8 - x.part_of(now, min(row, now.n - 1)) * a.d.d;   // the lane's first element of its own head
 #pragma unroll
                     for (int step = 0; step < X::kSteps; ++step) {
-                        const int c = step * 32 + x.j * 8;
-                        load(t, step, from + min(c, a.d.d - 8), row < now.n && c < a.d.d);
+                        const int c = c0 + step * 32;
+                        load(t, step, from + min(max(c, 0), a.d.d - 8), row < now.n && (unsigned)c < (unsigned)a.d.d);
                     }
                 }
             };
@@ -638,6 +646,7 @@ __device__ __forceinline__ void run_many(const SharedArgs& a, Run run, SharedLds
             });
 #pragma unroll
             for (int t = 0; t < S; ++t) {
+                const float by = x.scale_of(now, min((mine * S + t) * 16 + x.column, now.n - 1));
                 float top = 0.0f, down = 1.0f, up = 1.0f;
                 if constexpr (kQ > 1) {
 #pragma unroll
@@ -744,12 +753,14 @@ __device__ __forceinline__ void run_many(const SharedArgs& a, Run run, SharedLds
             for (int t = 0; t < S; ++t) {
                 const float sum = __int_as_float(butterfly_step<32>(butterfly_step<16>(__float_as_int(l[t]), AddF32{}), AddF32{})), down = __builtin_amdgcn_exp2f(-X::kLift);
                 const int row = (mine * S + t) * 16 + x.column;
-                if (row < now.n)
+                if (row < now.n) {
+                    const int own = x.part_of(now, row) * a.d.d;
                     x.leave(now, row, at, [&](auto put) {
 #pragma unroll
                         for (int blk = 0; blk < X::kBlocks; ++blk)
-                            if (blk * 16 < a.d.d) put(blk * 16 + x.j * 4, o[t][blk] * down);
+                            if ((unsigned)(blk * 16 - own) < (unsigned)a.d.d) put(blk * 16 - own + x.j * 4, o[t][blk] * down);
                     }, m[t], sum * down);
+                }
             }
             continue;
         }
@@ -774,10 +785,11 @@ __device__ __forceinline__ void run_many(const SharedArgs& a, Run run, SharedLds
                 for (int w = of; w < W; w += apart) top = fmaxf(top, s.m[w][qrow]);
                 const float base = top == -INFINITY ? 0.0f : top;
                 for (int w = of; w < W; w += apart) sum += s.l[w][qrow] * __builtin_amdgcn_exp2f(s.m[w][qrow] - base - X::kLift);
+                const int own = x.part_of(now, row) * a.d.d;
                 x.leave(now, row, at, [&](auto put) {
                     for (int c = qc * 4; c < a.d.d; c += 64) {
                         v4f y{0, 0, 0, 0};
-                        for (int w = of; w < W; w += apart) y += *reinterpret_cast<const v4f*>(&s.o[w][qrow][c]);
+                        for (int w = of; w < W; w += apart) y += *reinterpret_cast<const v4f*>(&s.o[w][qrow][own + c]);
                         put(c, y);
                     }
                 }, top, sum);
@@ -866,7 +878,7 @@ __global__ __launch_bounds__(kPagedThreads) void shared_join_kernel(SharedArgs a
         sum += s_l[i] * by;
         if (tid < d.d) v += s_o[i * d.d + tid] * by;
     }
-    const float by = (sum == 0.0f ? 0.0f : 1.0f / sum) * (d.cache_dtype == NM_DT_I8 ? d.v_scale[g] : 1.0f);
+    const float by = (sum == 0.0f ? 0.0f : 1.0f / sum) * (d.cache_dtype == NM_DT_I8 ? d.v_scale[h / a.own] : 1.0f);
     if (tid < d.d) store1(d.out, d.out_dtype, b * d.out_stride + (long)h * d.d + tid, v * by, d.out_inv_scale);
     if (tid == 0 && d.lse) d.lse[bh] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
 }
@@ -893,7 +905,7 @@ template <typename C, typename T>
 static void launch_shared(const SharedArgs& a, hipStream_t s)
 {
     const bool own = one_term(a.d);
-    const int width = paged_width(a.d.d);
+    const int width = paged_width(a.width);
     if (width == 64) launch_shared<C, T, 64>(a, own, s);
     else if (width == 128) launch_shared<C, T, 128>(a, own, s);
     else launch_shared<C, T, 256>(a, own, s);
@@ -931,8 +943,15 @@ static int32_t plan_shared(const nm_shared_desc* d, SharedArgs* a, void* ws, siz
     a->group_start = d->group_start;
     a->shared = d->shared;
     a->shift = page_shift(d->p.page_size);
-    a->group = d->p.hq / d->p.hk;
-    const int width = paged_width(d->p.d);
+    a->own = d->p.hq / d->p.hk;
+    // Heads of int8 as one, whole lines of 128 bytes, where their queries, of a group's rows (of so many as the groups have among them), are still few.
+    a->pack = 1;
+    if (d->p.cache_dtype == NM_DT_I8 && d->p.head_stride == d->p.d)
+        while (2 * a->pack * d->p.d <= 128 && d->p.hk % (2 * a->pack) == 0 && (d->G ? (d->p.B + d->G - 1) / d->G : 1) * a->own * 2 * a->pack <= shared_tile(0, 128, 1)) a->pack *= 2;
+    a->heads = d->p.hk / a->pack;
+    a->width = d->p.d * a->pack;
+    a->group = a->own * a->pack;
+    const int width = paged_width(a->width);
     for (int list = 0; list < kLists; ++list) a->tile[list] = shared_tile(list, width, one_term(d->p) ? 1 : 3);
     a->workers = 256 * (width <= 128 ? 2 : 1);
     a->whole_queries = aligned_rows(d->p.q, d->p.q_stride, d->p.q_dtype, 8);

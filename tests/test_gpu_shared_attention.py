@@ -107,6 +107,17 @@ def test_shared_attention(q_dtype, cache_dtype, out_dtype, hq, hk, d):
     check(c, out_dtype)
 
 
+@pytest.mark.parametrize("hq,hk,d", [(16, 16, 64), (8, 8, 32), (16, 8, 16), (12, 12, 48), (16, 16, 16), (6, 6, 64)])
+@pytest.mark.parametrize("by_head", [False, True])
+@pytest.mark.parametrize("q_dtype", TYPES)
+def test_shared_attention_neighbouring_heads_of_codes(q_dtype, by_head, hq, hk, d):
+    """int8 heads that lie next to each other are taken as one of up to 128 elements, where groups are small; some groups here are larger."""
+    c = shared_case(hq * d, [(300, [310, 301]), (512, [700, 513, 600]), (0, [40]), (900, [901]), (256, [300] * 20), (140, [141, 0]), (0, [9]), (130, [131, 2000]), (64, [65, 70])], hq, hk, d, q_dtype,
+                    torch.int8, page=32, by_head=by_head)
+    c["q"][1, :, 0] *= 100.0
+    check(c, q_dtype)
+
+
 def test_shared_attention_rows_in_front_of_and_behind_the_groups():
     c = shared_case(3, MIXED, 8, 2, 64, torch.bfloat16, torch.bfloat16)
     assert int(c["start"][0]) == 2 and int(c["start"][-1]) == c["lens"].numel() - 3
