@@ -23,6 +23,21 @@ constexpr int shared_waves(int list) { return list == 2 ? 2 * kPagedWaves : kPag
 constexpr int shared_sets(int list, int dp, int terms) { return list == 0 ? 1 : terms == 1 ? (dp <= 128 ? 2 : 1) : list == 2 && dp <= 64 ? 2 : 1; }
 constexpr int shared_tile(int list, int dp, int terms) { return list == 0 ? 16 : (list == 1 ? 2 : shared_waves(2)) * 16 * shared_sets(list, dp, terms); }
 
+// Quotients of numbers that are not negative: a division of 32 bits takes a tenth of one of 64.
+__device__ __forceinline__ long divided(long n, long by) { return (n | by) >> 31 ? n / by : (long)((unsigned)n / (unsigned)by); }
+// As Shares, by these.
+struct Portions {
+    long each, more;
+    __device__ __forceinline__ Portions(long all, long workers) : each(divided(all, workers)), more(all - each * workers) {}
+    __device__ __forceinline__ Portions(long e, long m, int) : each(e), more(m) {}
+    __device__ __forceinline__ long begin(long w) const { return each * w + min(w, more); }
+    __device__ __forceinline__ long owner(long x) const
+    {
+        const long longer = (each + 1) * more;
+        return x < longer ? divided(x, each + 1) : more + divided(x - longer, each);
+    }
+};
+
 struct SharedHead { long each[kLists], more[kLists]; int workers[kLists]; };   // how a list's cost is divided
 struct SharedArgs {
     nm_paged_desc d;
@@ -33,7 +48,8 @@ struct SharedArgs {
     // Neighbouring key heads of int8 may be taken as one, whose queries are zero but in their own head's part (codes are finite): how many there are then, their
     // elements and query heads, and how many are one.
     int heads, width, group, pack;
-    int tile[kLists];            // queries of a range
+    int tile[kLists];            // log2 of the queries of a range
+    FastDiv by_group;
     int workers, last;           // of the first two lists, and of the third
     int whole_queries;           // 8 elements of a query may be read at once
     SharedHead* head;
@@ -61,9 +77,10 @@ struct Entity {
         k0 = prefix ? 0 : x.z;
         k1 = x.w;
         queries = prefix && k1 <= 0 ? 0 : x.y * a.group;
-        list = !prefix || queries <= a.tile[0] ? 0 : queries <= a.tile[1] ? 1 : 2;
-        tile = a.tile[list];
-        tiles = (queries + tile - 1) / tile;
+        list = !prefix || queries <= 1 << a.tile[0] ? 0 : queries <= 1 << a.tile[1] ? 1 : 2;
+        const int shift = list == 0 ? a.tile[0] : list == 1 ? a.tile[1] : a.tile[2];
+        tile = 1 << shift;
+        tiles = (queries + tile - 1) >> shift;
         units = (k1 - k0 + kUnit - 1) / kUnit;
         extra = 2;                                            // beginning and ending a range, in units
     }
@@ -168,7 +185,7 @@ __global__ __launch_bounds__(kPlanners) void shared_plan_kernel(SharedArgs a)
     for (long i = tid; i < workers[0] + workers[1] + workers[2]; i += kPlanners) {
         const int list = i < workers[0] ? 0 : i < workers[0] + workers[1] ? 1 : 2;
         const long w = i - (list > 0 ? workers[0] : 0) - (list > 1 ? workers[1] : 0);
-        const Shares shares(list == 0 ? cost[0] : list == 1 ? cost[1] : cost[2], list == 0 ? workers[0] : list == 1 ? workers[1] : workers[2]);
+        const Portions shares(list == 0 ? cost[0] : list == 1 ? cost[1] : cost[2], list == 0 ? workers[0] : list == 1 ? workers[1] : workers[2]);
         if (w == 0) {
             a.head->each[list] = shares.each;
             a.head->more[list] = shares.more;
@@ -192,7 +209,7 @@ struct SharedPiece { int table, row0, g, i0, n, k0, k1, slot, prefix, done; };
 
 // A worker's run through its list.
 struct Run {
-    Shares shares;
+    Portions shares;
     long first, u, u1, before;
     int e, list, worker;
     __device__ __forceinline__ Run(const SharedArgs& a, const SharedHead& head, int list, int worker)
@@ -201,7 +218,7 @@ struct Run {
     // Number of the first query's part of a worker's slot.
     static __device__ __forceinline__ long part_of(const SharedArgs& a, int list, long worker, int slot)
     {
-        return (list > 0 ? 2l * a.workers * a.tile[0] : 0l) + (list > 1 ? 2l * a.workers * a.tile[1] : 0l) + (worker * 2 + slot) * a.tile[list];
+        return (list > 0 ? (2l * a.workers) << a.tile[0] : 0l) + (list > 1 ? (2l * a.workers) << a.tile[1] : 0l) + ((worker * 2 + slot) << (list == 0 ? a.tile[0] : list == 1 ? a.tile[1] : a.tile[2]));
     }
     __device__ __forceinline__ SharedPiece next(const SharedArgs& a)
     {
@@ -213,7 +230,7 @@ struct Run {
                 ++e;
                 continue;
             }
-            const int r = (int)((u - before) / cost);
+            const int r = (int)divided(u - before, cost);
             const long begin = before + r * cost, end = min(u1, begin + cost);
             // a range's cost comes first, then its units
             const int from = (int)max(u - begin - x.extra, 0l), to = (int)max(end - begin - x.extra, 0l);
@@ -223,8 +240,8 @@ struct Run {
             SharedPiece n;
             n.table = x.table;
             n.row0 = x.row0;
-            n.g = r / x.tiles;
-            n.i0 = r % x.tiles * x.tile;
+            n.g = x.tiles == 1 ? r : r / x.tiles;
+            n.i0 = (r - n.g * x.tiles) * x.tile;
             n.n = min(x.queries - n.i0, x.tile);
             n.k0 = x.k0 + from * kUnit;
             n.k1 = (int)min((long)x.k0 + (long)to * kUnit, (long)x.k1);
@@ -233,7 +250,8 @@ struct Run {
             n.done = !n.prefix && x.k0 == 0 && n.slot < 0;
             if (from == 0 && threadIdx.x == 0) {
                 const int count = n.done ? -1 : x.units ? (int)(shares.owner(begin + x.extra + x.units - 1) - worker) + 1 : 0;
-                a.info[((long)!n.prefix * a.d.B + x.row0 + n.i0 / a.group) * a.d.hq + n.g * a.group + n.i0 % a.group] =
+                const int row = (int)quotient(n.i0, a.by_group);
+                a.info[((long)!n.prefix * a.d.B + x.row0 + row) * a.d.hq + n.g * a.group + n.i0 - row * a.group] =
                     make_int4(count, n.slot < 0 ? -1 : (int)part_of(a, list, worker, n.slot), (int)part_of(a, list, worker + 1, 0), 2 * x.tile);
             }
             return n;
@@ -397,12 +415,12 @@ struct Tiles {
     // Number of a query's first element.
     __device__ __forceinline__ long query_of(const SharedPiece& n, int row) const
     {
-        const int i = n.i0 + row;
-        return (long)(n.row0 + i / a.group) * a.d.q_stride + (long)(n.g * a.group + i % a.group) * a.d.d;
+        const int i = n.i0 + row, b = (int)quotient(i, a.by_group);
+        return (long)(n.row0 + b) * a.d.q_stride + (long)(n.g * a.group + i - b * a.group) * a.d.d;
     }
     // Of a range's query number `row`: which of the heads taken as one is its own, and what its scores are multiplied by, but for its own scale; the sign goes with
     // the query.
-    __device__ __forceinline__ int part_of(const SharedPiece& n, int row) const { return sizeof(C) == 1 ? (n.i0 + row) % a.group / a.own : 0; }
+    __device__ __forceinline__ int part_of(const SharedPiece& n, int row) const { return sizeof(C) == 1 && a.pack > 1 ? (n.i0 + row) % a.group / a.own : 0; }
     __device__ __forceinline__ float scale_of(const SharedPiece& n, int row) const
     {
         return a.d.scale * 1.44269504088896340736f * (sizeof(C) == 1 ? a.d.k_scale[n.g * a.pack + part_of(n, row)] : 1.0f);
@@ -419,7 +437,7 @@ struct Tiles {
     __device__ __forceinline__ void leave(const SharedPiece& n, int row, long part, Elements elements, float top, float sum) const
     {
         const nm_paged_desc& d = a.d;
-        const int i = n.i0 + row, b = n.row0 + i / a.group, h = n.g * a.group + i % a.group;
+        const int i = n.i0 + row, nth = (int)quotient(i, a.by_group), b = n.row0 + nth, h = n.g * a.group + i - nth * a.group;
         if (!n.done) {
             const long at = n.slot < 0 ? ((long)!n.prefix * d.B + b) * d.hq + h : part + row;
             float* to = (n.slot < 0 ? a.whole_o : a.part_o) + at * d.d;
@@ -832,19 +850,19 @@ __global__ __launch_bounds__(kPagedThreads) void shared_join_kernel(SharedArgs a
     __shared__ __attribute__((aligned(16))) float s_o[kPagedThreads * 4];
     __shared__ float s_m[kPagedThreads / 4], s_l[kPagedThreads / 4];
     const nm_paged_desc& d = a.d;
-    const int tid = threadIdx.x, b = blockIdx.x / d.hq, h = blockIdx.x % d.hq, g = h / a.group;
+    const int tid = threadIdx.x, b = blockIdx.y, h = blockIdx.x, g = (int)quotient(h, a.by_group), in_group = h - g * a.group;
     const int lead = a.lead[b];
     const long bh = (long)b * d.hq + h, all = (long)d.B * d.hq;
     // [0] the prefix, [1] the row's own positions; and the query's number in the range
     int4 info[2] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
-    int nth[2] = {0, h % a.group % a.tile[0]};
+    int nth[2] = {0, in_group & ((1 << a.tile[0]) - 1)};
     info[1] = a.info[all + bh - nth[1]];
     if (info[1].x < 0) return;
     if (lead >= 0) {
-        const int i = (b - lead) * a.group + h % a.group;
-        nth[0] = i % a.tile[2];
-        const int i0 = i - nth[0];
-        info[0] = a.info[(long)(lead + i0 / a.group) * d.hq + g * a.group + i0 % a.group];
+        const int i = (b - lead) * a.group + in_group;
+        nth[0] = i & ((1 << a.tile[2]) - 1);
+        const int i0 = i - nth[0], row = (int)quotient(i0, a.by_group);
+        info[0] = a.info[(long)(lead + row) * d.hq + g * a.group + i0 - row * a.group];
     }
     const int used = info[0].x + info[1].x;
     const int lanes = d.d / 4, at_once = kPagedThreads / lanes, mine = tid / lanes, c = tid % lanes * 4;
@@ -888,7 +906,7 @@ static void launch_shared(const SharedArgs& a, hipStream_t s)
 {
     // either list's workers rounded up to one for every XCD
     queue_kernel(shared_attention_kernel<C, T, DP, kQ, kP>, dim3((a.workers + 7) / 8 * 8 + 8), dim3(kPagedThreads), 0, s, a);
-    if (a.G && (long)a.d.B * a.group > a.tile[1]) queue_kernel(shared_prefix_kernel<C, T, DP, kQ, kP>, dim3(a.last), dim3(64 * shared_waves(2)), 0, s, a);
+    if (a.G && (long)a.d.B * a.group > 1 << a.tile[1]) queue_kernel(shared_prefix_kernel<C, T, DP, kQ, kP>, dim3(a.last), dim3(64 * shared_waves(2)), 0, s, a);
 }
 template <typename C, typename T, int DP>
 static void launch_shared(const SharedArgs& a, bool own, hipStream_t s)
@@ -951,12 +969,13 @@ static int32_t plan_shared(const nm_shared_desc* d, SharedArgs* a, void* ws, siz
     a->heads = d->p.hk / a->pack;
     a->width = d->p.d * a->pack;
     a->group = a->own * a->pack;
+    a->by_group = fast_div(a->group);
     const int width = paged_width(a->width);
-    for (int list = 0; list < kLists; ++list) a->tile[list] = shared_tile(list, width, one_term(d->p) ? 1 : 3);
+    for (int list = 0; list < kLists; ++list) a->tile[list] = __builtin_ctz(shared_tile(list, width, one_term(d->p) ? 1 : 3));   // powers of two
     a->workers = 256 * (width <= 128 ? 2 : 1);
     a->whole_queries = aligned_rows(d->p.q, d->p.q_stride, d->p.q_dtype, 8);
     a->last = 256;
-    const size_t parts = (size_t)a->workers * 2 * (a->tile[0] + a->tile[1]) + (size_t)a->last * 2 * a->tile[2], queries = (size_t)d->p.B * d->p.hq;
+    const size_t parts = (size_t)a->workers * 2 * ((1 << a->tile[0]) + (1 << a->tile[1])) + ((size_t)a->last * 2 << a->tile[2]), queries = (size_t)d->p.B * d->p.hq;
     Carve c{static_cast<char*>(ws)};
     c.take(a->head, 1);
     c.take(a->ent, (size_t)d->G + d->p.B);
@@ -1014,7 +1033,7 @@ int32_t nm_shared_attention(const nm_shared_desc* desc, void* ws, size_t ws_byte
     else if (d.q_dtype == NM_DT_F16) launch_shared<int8_t, f16>(a, s);
     else launch_shared<int8_t, bf16>(a, s);
     if ((rc = check_hip(hipGetLastError(), "nm_shared_attention launch"))) return rc;
-    queue_kernel(shared_join_kernel, dim3(d.B * d.hq), dim3(kPagedThreads), 0, s, a);
+    queue_kernel(shared_join_kernel, dim3(d.hq, d.B), dim3(kPagedThreads), 0, s, a);
     return check_hip(hipGetLastError(), "nm_shared_attention launch");
 }
 
