@@ -3,11 +3,19 @@
 // Each row's own positions are nm_paged_attention's work: every key and value once, bound by memory.  A group's prefix is read once for all its
 // rows: for one key head the queries of all of them, rows times heads, are as many columns of the same matrix products.  Softmax over both: each piece
 // of work, a range of positions, leaves its maximum, sum and output, and a last kernel joins what a query has.
-//   A first kernel of one workgroup makes two lists.  Ranges of up to 16 queries, which the rows' own are, are taken as nm_paged_attention takes them: each of
-// a workgroup's four wavefronts has tiles of 32 positions of its own.  Ranges of more have their 128 positions at a time in LDS for all four: each has 32
-// queries, or 16 where they are three terms, of up to four times as many, and the positions that are left to it (few queries: a half or a quarter of them).
-// A fixed number of workgroups is divided among the lists by their cost, and shares each evenly, whatever the lengths are; a run's first and
-// last piece may be parts of a range.  Tiles, operand layouts and precision are nm_paged_attention's.
+//   A first kernel of one workgroup makes three lists, by a range's queries.  Up to 16, which the rows' own are: as nm_paged_attention takes them, each of
+// a workgroup's four wavefronts has tiles of 32 positions of its own.  More: 128 positions at a time are in LDS for all wavefronts, each of which has 32
+// queries in registers (16 where they are three terms), and, where there are fewer queries than that, only some of the positions.  Up to 64 queries (32),
+// in the first list's launch, four wavefronts; more, in a launch of their own, eight wavefronts and 256 queries (64 to 256) to a CU, which has registers for
+// the operands of one product while another runs, and LDS for the next positions beside these.  (With four wavefronts of 64 queries each, one to a
+// SIMD, nothing ran under a wavefront's own waits: 18 us for 128 positions, 7 so.)  A fixed number of workgroups shares each list evenly, whatever the lengths
+// are (the first two lists' by their cost); a run's first and last piece may be parts of a range.  Tiles, operand layouts and precision are nm_paged_attention's, but that a
+// running maximum is only moved when it is passed by a factor of 32.
+//   bf16, 32 query and 8 key heads of 128, GPU time: 64 rows behind 32768 common positions (190 MB, 35 GFLOP) 107 us: 7 the lists, 23 the rows' own, 66 the
+// prefix (39 % of the cycles in matrix instructions, 44 % in vector instructions, which one after the other would fill them: the weights' two terms are both
+// double the second product and half of the vector instructions), 11 the joining of 34 pieces a query.  96 rows behind 4096, each with up to 4096 of its own (671 MB) 183: 130 the own
+// positions, at a copy's rate.  int8, 16 heads of 64, two as one, 16 groups of 8 rows behind up to 8192 (134 MB) 63: 45 for 3500 units of 128 positions and a thousand ranges of one
+// or two, whose beginning and end cost as much as two more.
 #include "nm_paged_parts.h"
 
 namespace nm {
@@ -15,6 +23,8 @@ namespace nm {
 constexpr int kSharedMost = NM_PLAN_MAX_REQUESTS;     // rows, groups
 constexpr int kSharePrefix = kUnit;                   // shorter prefixes are every row's own
 constexpr int kPlanners = 1024;
+// Units of all rows up to which nm_paged_attention takes them, two to each of its workgroups or fewer: 4 rows of 640 positions, 12 heads of 64, 13.9 us,
+// 20.8 by the lists.
 constexpr long kFewUnits = 1024;
 constexpr int kLists = 3;
 
@@ -833,7 +843,7 @@ __global__ __launch_bounds__(kPagedThreads, DP <= 128 ? 2 : 1) void shared_atten
     }
 }
 
-// The third: a workgroup of eight wavefronts to a CU.
+// The third: a workgroup of eight wavefronts to a CU.  (Launched wherever a group could be that large: 4.5 us where none is.)
 template <typename C, typename T, int DP, int kQ, int kP>
 __global__ __launch_bounds__(64 * shared_waves(2), 2) void shared_prefix_kernel(SharedArgs a)
 {
@@ -951,8 +961,7 @@ static int32_t plan_shared(const nm_shared_desc* d, SharedArgs* a, void* ws, siz
     if (d->G < 0) return fail(NM_ERR_INVALID_ARG, "%s: G is negative", what);
     if (d->p.window) return fail(NM_ERR_UNSUPPORTED, "%s: a window", what);
     if (d->p.B > kSharedMost || d->G > kSharedMost) return fail(NM_ERR_UNSUPPORTED, "%s: B %d or G %d > %d", what, d->p.B, d->G, kSharedMost);
-    // rows that are not divided, and few units in all, which every workgroup then has one or two of whether or not they are shared (the first kernel and the
-    // third take longer than what sharing saves)
+    // rows that are not divided, no groups, or few units in all
     const long most = (long)d->p.B * d->p.hk * ((((long)d->p.max_pages << page_shift(d->p.page_size)) + kUnit - 1) / kUnit);
     *alone = !divided || d->G == 0 || most <= kFewUnits;
     *a = SharedArgs{};
@@ -962,7 +971,8 @@ static int32_t plan_shared(const nm_shared_desc* d, SharedArgs* a, void* ws, siz
     a->shared = d->shared;
     a->shift = page_shift(d->p.page_size);
     a->own = d->p.hq / d->p.hk;
-    // Heads of int8 as one, whole lines of 128 bytes, where their queries, of a group's rows (of so many as the groups have among them), are still few.
+    // Heads of int8 as one, whole lines of 128 bytes, where their queries, of a group's rows (of so many as the groups have among them), are still few
+    // (16 groups of 8 rows, 16 heads of 64: 67 us, 78.6 apart); more would double the products.
     a->pack = 1;
     if (d->p.cache_dtype == NM_DT_I8 && d->p.head_stride == d->p.d)
         while (2 * a->pack * d->p.d <= 128 && d->p.hk % (2 * a->pack) == 0 && (d->G ? (d->p.B + d->G - 1) / d->G : 1) * a->own * 2 * a->pack <= shared_tile(0, 128, 1)) a->pack *= 2;
