@@ -670,7 +670,7 @@ int32_t nm_gemv_w4(const nm_w4_desc* desc, void* stream);
  * logits: device [R W, V], rows logits_stride elements apart, logits_dtype F32, BF16 or F16.  scores, weight: device fp32 [R, W]; done: device int32 [R, W] or
  * NULL.  parents, tokens, done_out (or NULL): device int32 [R, K]; scores_out: device fp32 [R, K].  history, history_out: device int32, rows
  * history_stride and history_out_stride apart; history_lens, history_lens_out: device int32 [R W], [R K].  No output may be an input or another output.
- * Limits: 1 <= W, K <= NM_BEAM_MAX; R W <= 2^20; 1 <= V <= 2^26; 1 <= max_history.  -1 <= end_token < V (-1: none; then done is NULL).
+ * Limits: 1 <= W, K <= NM_BEAM_MAX; R W <= 2^20; R K <= 2^23; 1 <= V <= 2^26; 1 <= max_history <= 2^30.  -1 <= end_token < V (-1: none; then done is NULL).
  */
 #define NM_BEAM_MAX 64
 typedef struct {
@@ -716,7 +716,8 @@ int32_t nm_beam_select(const nm_beam_desc* desc, void* ws, size_t ws_bytes, void
  * lens: device int32 [B_in].  parents: [B_out].  block_table, table_out: int32, rows of max_pages entries, table_stride and table_out_stride
  * apart.  keep: int32 [num_pages] or NULL.  free_pages, free_out: [n_free].  lens_out, copy_src, copy_dst, copy_slots: [B_out].  Apart from free_out no output may be an
  * input, and none another output.
- * Limits: B_in, B_out <= NM_PLAN_MAX_REQUESTS; page_size a power of two up to 65536; num_pages * page_size and max_pages * page_size < 2^31; n_free <= 2^30.
+ * Limits: B_in, B_out <= NM_PLAN_MAX_REQUESTS; page_size a power of two up to 65536; num_pages * page_size and max_pages * page_size < 2^31; num_pages, max_pages,
+ * n_free <= 2^30.
  */
 enum { NM_FORK_NO_PAGES = 1,      /* the free list is too short */
        NM_FORK_BAD_LENGTH = 8,    /* a length that is negative or longer than max_pages, or *free_begin outside [0, n_free] */
@@ -750,9 +751,9 @@ int32_t nm_page_fork(const nm_fork_desc* desc, void* ws, size_t ws_bytes, void* 
  * that are one page, is left out.  No page may be the destination of two copies, or the source of one and the destination of another: what those
  * hold is not said then.
  * caches: HOST array of n_caches device pointers, read during the call.  dtype: F32, BF16, F16 or I8; elements are moved as they are.  src, dst,
- * slots: device int32 [n].  Strides as above, in elements.  Where addresses, strides and rows are multiples of 16 bytes, whole groups move at once.
+ * slots: device int32 [n].  Strides as above, in elements.  Where addresses, strides and rows are multiples of 16 bytes, whole groups of 16 bytes move at once (else as wide ones as they allow).
  * Limits: n <= 2^20; n_caches <= NM_COPY_MAX_CACHES; page_size a power of two up to 65536; hk, d >= 1; num_pages * page_size, and
- * page_size * hk * d, < 2^31.
+ * page_size * hk * d, < 2^31; each of the n pages in pieces of 1024 such groups, fewer than 2^24 pieces in all.
  */
 #define NM_COPY_MAX_CACHES 256
 typedef struct {

@@ -9,6 +9,10 @@
 // equal logits, or all large ones in a few lanes), they are put one by one into lists, sorted, an entry to a lane.
 //   A second kernel has a workgroup to a request: it joins the chunks' sums, forms the candidates' log-probabilities in 64 bits, and chooses among
 // them in the same way; short histories it copies itself.
+//   Bound by latency at few rows: one request of 4 hypotheses, 32000 fp32 logits, 5.5 + 4.2 us, chains of loads, a sort of 21 steps, barriers.  32 of 8, 131072
+// bf16 (67 MB, 13 us at a copy's rate): 20.6 + 5.7, 3.3 TB/s in the first: two workgroups to a CU, vector instructions 42 % of
+// the cycles, and 4 us of the same chain behind the last logits.  (More chunks, or more loads ahead, take longer: 512 workgroups 26.1 us, 1024 27.8; lists of K
+// kept by every wavefront as it goes 83.)
 #include <algorithm>
 
 #include "nm_decode.h"
@@ -484,9 +488,10 @@ __global__ __launch_bounds__(kBeamThreads) void beam_history_kernel(nm_beam_desc
 }
 
 constexpr long kBeamGroups = 512;                             // workgroups of the first kernel, about
-// Tokens of a history, and of a request's, that its workgroup of the second kernel copies, a wavefront to a history; more go to a kernel of their own.
-constexpr int kHistory = 1024;
-constexpr long kHistories = 8192;
+// Tokens that a history, and a request's histories, have room for up to which its workgroup of the second kernel copies them, a wavefront to a history; more go to a
+// kernel of their own.  (There and by a kernel: 4 of 1000 12.1 and 13.2 us, of 4000 14.3 and 13.3; 16 requests of 8 of 2000 16.0 and 16.2; 300 of 2 of 4000 24.4 and 23.4.)
+constexpr int kHistory = 2048;
+constexpr long kHistories = 16384;
 
 static int32_t plan_beam(const nm_beam_desc* d, BeamArgs* a, size_t* bytes, const char* what)
 {
@@ -494,7 +499,9 @@ static int32_t plan_beam(const nm_beam_desc* d, BeamArgs* a, size_t* bytes, cons
     if (d->R < 0 || d->W < 1 || d->K < 1 || d->V < 1) return fail(NM_ERR_INVALID_ARG, "%s: bad shape", what);
     if (!float_dtype(d->logits_dtype)) return fail(NM_ERR_INVALID_ARG, "%s: bad logits_dtype", what);
     if (d->W > NM_BEAM_MAX || d->K > NM_BEAM_MAX) return fail(NM_ERR_UNSUPPORTED, "%s: W %d or K %d > %d", what, d->W, d->K, NM_BEAM_MAX);
-    if ((int64_t)d->R * d->W > 1 << 20 || d->V > 1 << 26) return fail(NM_ERR_UNSUPPORTED, "%s: R * W > 2^20 or V > 2^26", what);
+    if ((int64_t)d->R * d->W > 1 << 20 || (int64_t)d->R * d->K > 1 << 23 || d->V > 1 << 26)   // 2^24 workgroups of 256 are more than a launch takes
+        return fail(NM_ERR_UNSUPPORTED, "%s: R * W > 2^20, R * K > 2^23 or V > 2^26", what);
+    if (d->history && d->max_history > 1 << 30) return fail(NM_ERR_UNSUPPORTED, "%s: max_history > 2^30", what);
     *a = BeamArgs{};
     a->d = *d;
     // chunks of one tile where there are few rows, and as many as give every CU four workgroups

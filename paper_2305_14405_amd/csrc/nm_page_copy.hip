@@ -100,7 +100,7 @@ extern "C" int32_t nm_page_copy(const nm_copy_desc* d, void* stream)
     a.head_stride = d->head_stride * bytes / unit;
     const long units = (long)a.unit_row.d * d->hk * d->page_size, piece = kCopyThreads * kCopyEach;
     a.pieces = (int)((units + piece - 1) / piece);
-    if ((double)a.pieces * d->n >= 2147483648.0) return fail(NM_ERR_UNSUPPORTED, "nm_page_copy: n pages of this size are too many for one call");
+    if ((double)a.pieces * d->n * kCopyThreads >= 4294967296.0) return fail(NM_ERR_UNSUPPORTED, "nm_page_copy: n pages of this size are too many for one call");
     const dim3 grid(a.pieces * d->n, d->n_caches);
     const hipStream_t s = (hipStream_t)stream;
     if (unit == 16) queue_kernel(page_copy_kernel<v4i>, grid, dim3(kCopyThreads), 0, s, a);

@@ -1,11 +1,14 @@
 // Block tables of a new batch whose rows go on from rows of the old one (nm_page_fork).
 //
 // Nothing is counted from call to call: who refers to a page is found from the tables.  Each page has marks: that an old row refers to it; that one with
-// children does so in front of its partial last page; and how many rows with children have it as that.  From them follow which rows take a page
-// of their own (a scan over the rows) and which pages become free (a scan over the pages).  The marks are set by integer atomics, whose order does not change their result.
-//   Small batches: one workgroup, marks in LDS, a chain of dependent steps.  Others: four kernels, marks in the workspace.  Clear them
-// and find every old row's first child; mark (a row leaves out what the row in front of it marks as well: hypotheses of a request share most of their
-// pages, and atomics on one word wait for one another); decide for the rows, and count the freed pages of every block; write the tables and the list.
+// children does so in front of its partial last page; how many rows with children have it as that.  From them follow which rows take a page
+// of their own (a scan over the rows) and which pages become free (a scan over the pages).  Marks are set by stores of one value, and counted by integer
+// atomics, whose order does not change their result.
+//   Small batches: one workgroup, marks in LDS, a chain of dependent steps: 16 rows of up to 135 entries 7.2 us.  Others: four kernels, marks in the workspace.  Clear them
+// and find every old row's first child; mark (a row leaves out what the row in front of it marks as well: hypotheses of a request share most of their pages,
+// and 4096 rows that all marked theirs by atomics took 53 us, 13 so); decide for the rows, and count the freed pages of every block; write the tables and the
+// list.  4096 rows, 860000 entries, a pool of 332000 pages (6.9 MB that the call cannot do without): 3.2 + 13.2 + 4.7 + 4.6 us, each a chain of three
+// or four dependent loads; marks are bytes at scattered places.  (The decisions for all rows in one workgroup took 12 to 17: 8192 lines through one CU.)
 #include <algorithm>
 
 #include "nm_decode.h"
@@ -17,8 +20,9 @@ constexpr int kForkBlocks = 1024;                  // of pages at most
 constexpr int kForkBlock = 4096;                   // pages of one at least
 constexpr int kRowThreads = 1024, kRows = NM_PLAN_MAX_REQUESTS / kRowThreads;
 constexpr int kRowBlocks = NM_PLAN_MAX_REQUESTS / kForkThreads;   // of rows at most
-// What one workgroup does alone: rows, entries of either table, pages, the list.
-constexpr int kSmallRows = 1024, kSmallEntries = 16384, kSmallPages = 65536, kSmallList = 65536;
+// What one workgroup does alone: rows, entries of either table, pages, the list.  (GPU time there and by four kernels: 16 rows of 135 entries 7.2 and 10.1 us, 64 10.0 and
+// 10.7, 128 13.8 and 11.5, 256 23.6 and 11.6, of 38 18.1 and 11.1; but it is one launch, and they are four.)
+constexpr int kSmallRows = 128, kSmallEntries = 16384, kSmallPages = 65536, kSmallList = 65536;
 
 struct ForkArgs {
     nm_fork_desc d;
@@ -276,7 +280,7 @@ __global__ __launch_bounds__(kForkThreads) void fork_write_kernel(ForkArgs a)
 __global__ __launch_bounds__(kRowThreads) void fork_small_kernel(ForkArgs a)
 {
     extern __shared__ unsigned s_marks[];          // eight pages to a word
-    __shared__ int s_first[kSmallRows], s_n[kSmallRows], s_src[kSmallRows], s_dst[kSmallRows], s[kRowThreads / 64];
+    __shared__ int s_first[kRowThreads], s_n[kRowThreads], s_src[kRowThreads], s_dst[kRowThreads], s[kRowThreads / 64];
     const nm_fork_desc& d = a.d;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, words = (d.num_pages + 7) / 8;
     const int begin = *d.free_begin;
@@ -356,6 +360,7 @@ static int32_t plan_fork(const nm_fork_desc* d, ForkArgs* a, size_t* bytes, cons
     if (d->n_free > 1 << 30) return fail(NM_ERR_UNSUPPORTED, "%s: n_free > 2^30", what);
     const int shift = page_shift(d->page_size);
     if (shift < 0) return fail(NM_ERR_UNSUPPORTED, "%s: page_size %d is no power of two up to 65536", what, d->page_size);
+    if (d->num_pages > 1 << 30 || d->max_pages > 1 << 30) return fail(NM_ERR_UNSUPPORTED, "%s: num_pages or max_pages > 2^30", what);
     if ((int64_t)d->num_pages << shift > 0x7fffffffLL || (int64_t)d->max_pages << shift > 0x7fffffffLL)
         return fail(NM_ERR_UNSUPPORTED, "%s: num_pages * page_size or max_pages * page_size >= 2^31", what);
     *a = ForkArgs{};

@@ -55,7 +55,8 @@ def test_beam_select_refuses(lib, changes):
     refused(with_workspace(lib.nm_beam_select), beam(), nm.NM_ERR_INVALID_ARG, **changes)
 
 
-@pytest.mark.parametrize("changes", [dict(W=65), dict(K=65), dict(R=1 << 19), dict(V=(1 << 26) + 1, logits_stride=1 << 27), dict(logits=P + 1)])
+@pytest.mark.parametrize("changes", [dict(W=65), dict(K=65), dict(R=1 << 19), dict(R=(1 << 17) + 1, K=64, W=1), dict(max_history=(1 << 30) + 1, history_stride=1 << 31, history_out_stride=1 << 31),
+                                     dict(V=(1 << 26) + 1, logits_stride=1 << 27), dict(logits=P + 1)])
 def test_beam_select_does_not_cover(lib, changes):
     refused(with_workspace(lib.nm_beam_select), beam(), nm.NM_ERR_UNSUPPORTED, **changes)
 
@@ -102,7 +103,8 @@ def test_page_fork_refuses(lib, changes):
 
 
 @pytest.mark.parametrize("changes", [dict(B_in=nm.NM_PLAN_MAX_REQUESTS + 1), dict(B_out=nm.NM_PLAN_MAX_REQUESTS + 1), dict(page_size=0), dict(page_size=24), dict(page_size=1 << 17),
-                                     dict(num_pages=1 << 27), dict(max_pages=1 << 27, table_stride=1 << 27, table_out_stride=1 << 27), dict(n_free=(1 << 30) + 1)])
+                                     dict(num_pages=1 << 27), dict(max_pages=1 << 27, table_stride=1 << 27, table_out_stride=1 << 27), dict(n_free=(1 << 30) + 1),
+                                     dict(num_pages=(1 << 30) + 1, page_size=1), dict(max_pages=(1 << 30) + 1, page_size=1, table_stride=1 << 31, table_out_stride=1 << 31)])
 def test_page_fork_does_not_cover(lib, changes):
     refused(with_workspace(lib.nm_page_fork), fork(), nm.NM_ERR_UNSUPPORTED, **changes)
 
@@ -138,7 +140,7 @@ def test_page_copy_refuses_caches(lib, caches):
 
 
 @pytest.mark.parametrize("changes", [dict(n=(1 << 20) + 1), dict(n_caches=nm.NM_COPY_MAX_CACHES + 1), dict(page_size=12), dict(num_pages=1 << 27),
-                                     dict(hk=1 << 14, d=1 << 14), dict(n=1 << 20, hk=1 << 12, d=1 << 14)])
+                                     dict(hk=1 << 14, d=1 << 14), dict(n=1 << 20, hk=1 << 12, d=1 << 14), dict(n=1 << 20, hk=128, d=128)])
 def test_page_copy_does_not_cover(lib, changes):
     refused(do_copy(lib), copy(), nm.NM_ERR_UNSUPPORTED, **changes)
 
