@@ -13,7 +13,7 @@
 // running maximum is only moved when it is passed by a factor of 32.
 //   bf16, 32 query and 8 key heads of 128, GPU time: 64 rows behind 32768 common positions (190 MB, 35 GFLOP) 107 us: 7 the lists, 23 the rows' own, 66 the
 // prefix (39 % of the cycles in matrix instructions, 44 % in vector instructions, which one after the other would fill them: the weights' two terms are both
-// double the second product and half of the vector instructions), 11 the joining of 34 pieces a query.  96 rows behind 4096, each with up to 4096 of its own (671 MB) 183: 130 the own
+// double the second product and half of the vector instructions), 11 the joining of 36 pieces a query.  96 rows behind 4096, each with up to 4096 of its own (671 MB) 183: 130 the own
 // positions, at a copy's rate.  int8, 16 heads of 64, two as one, 16 groups of 8 rows behind up to 8192 (134 MB) 63: 45 for 3500 units of 128 positions and a thousand ranges of one
 // or two, whose beginning and end cost as much as two more.
 #include "nm_paged_parts.h"
@@ -853,12 +853,15 @@ __global__ __launch_bounds__(64 * shared_waves(2), 2) void shared_prefix_kernel(
     if ((int)(blockIdx.x / 8) < each && worker < head.workers[2]) run_many<C, T, DP, kQ, kP, shared_sets(2, DP, kQ), shared_waves(2)>(a, Run(a, head, 2, worker), s);
 }
 
-// Joins what a query has: its group's prefix and its row's own positions, each whole or in pieces.  A workgroup to a query; lanes of four elements read every
-// so-manieth piece's output and join them as they come; their results are joined through LDS.
+// Joins what a query has: its group's prefix and its row's own positions, each whole or in pieces.  A workgroup to a query: a thread to a piece finds the piece's
+// place and weight, then lanes of four elements add every so-manieth piece's output, whose first loads are under way before the weights are there.  2048 queries
+// of 128 of 36 pieces (47 MB fetched, at 4.4 TB/s) 10.7 us, 3072 of 8 11.0; where threads found the weights of their pieces as they added them 10.7 and 12.6.
 __global__ __launch_bounds__(kPagedThreads) void shared_join_kernel(SharedArgs a)
 {
+    constexpr int kAhead = 4;
     __shared__ __attribute__((aligned(16))) float s_o[kPagedThreads * 4];
-    __shared__ float s_m[kPagedThreads / 4], s_l[kPagedThreads / 4];
+    __shared__ const float* s_from[kPagedThreads];
+    __shared__ float s_by[kPagedThreads], s_top[kPagedWaves], s_sum[kPagedWaves];
     const nm_paged_desc& d = a.d;
     const int tid = threadIdx.x, b = blockIdx.y, h = blockIdx.x, g = (int)quotient(h, a.by_group), in_group = h - g * a.group;
     const int lead = a.lead[b];
@@ -878,34 +881,57 @@ __global__ __launch_bounds__(kPagedThreads) void shared_join_kernel(SharedArgs a
     const int lanes = d.d / 4, at_once = kPagedThreads / lanes, mine = tid / lanes, c = tid % lanes * 4;
     float m = -INFINITY, l = 0.0f;
     v4f x{0, 0, 0, 0};
-    if (mine < at_once) {
-#pragma unroll 4
-        for (int k = mine; k < used; k += at_once) {
-            const int own = k >= info[0].x, i = own ? k - info[0].x : k;
-            const int4 of = info[own];
+    for (int k0 = 0; k0 < used; k0 += kPagedThreads) {
+        const int n = min(used - k0, kPagedThreads), k = k0 + tid;
+        float2 ml{-INFINITY, 0.0f};
+        if (tid < n) {
+            const bool own = k >= info[0].x;
+            const int4 of = own ? info[1] : info[0];
+            const int i = own ? k - info[0].x : k;
             const bool whole = of.y < 0;
-            const long part = whole ? own * all + bh : (i ? of.z + (long)(i - 1) * of.w : of.y) + nth[own];
-            const float2 ml = (whole ? a.whole_ml : a.part_ml)[part];
-            const v4f y = *reinterpret_cast<const v4f*>((whole ? a.whole_o : a.part_o) + part * d.d + c);
-            const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.0f : top;
-            const float shrink = __builtin_amdgcn_exp2f(m - base), by = __builtin_amdgcn_exp2f(ml.x - base);
-            l = l * shrink + ml.y * by;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = x[k] * shrink + y[k] * by;
-            m = top;
+            const long part = whole ? own * all + bh : (i ? of.z + (long)(i - 1) * of.w : of.y) + (own ? nth[1] : nth[0]);
+            ml = (whole ? a.whole_ml : a.part_ml)[part];
+            s_from[tid] = (whole ? a.whole_o : a.part_o) + part * d.d;
         }
-        *reinterpret_cast<v4f*>(&s_o[mine * d.d + c]) = x;
-        if (c == 0) { s_m[mine] = m; s_l[mine] = l; }
+        const float most = __int_as_float(group_reduce<64>(__float_as_int(ml.x), MaxF32{}));
+        if (tid % 64 == 0) s_top[tid / 64] = most;
+        __syncthreads();
+        v4f y[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e)
+            if (mine < at_once && mine + e * at_once < n) y[e] = *reinterpret_cast<const v4f*>(s_from[mine + e * at_once] + c);
+        float top = m;
+        for (int i = 0; i < kPagedWaves; ++i) top = fmaxf(top, s_top[i]);
+        const float base = top == -INFINITY ? 0.0f : top, shrink = __builtin_amdgcn_exp2f(m - base), by = __builtin_amdgcn_exp2f(ml.x - base);
+        l = l * shrink + ml.y * by;
+        s_by[tid] = by;
+        m = top;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] *= shrink;
+        if (mine < at_once)
+            for (int j = mine;;) {
+#pragma unroll
+                for (int e = 0; e < kAhead; ++e)
+                    if (j + e * at_once < n)
+                        for (int i = 0; i < 4; ++i) x[i] += y[e][i] * s_by[j + e * at_once];
+                j += kAhead * at_once;
+                if (j >= n) break;
+#pragma unroll
+                for (int e = 0; e < kAhead; ++e)
+                    if (j + e * at_once < n) y[e] = *reinterpret_cast<const v4f*>(s_from[j + e * at_once] + c);
+            }
+        if (k0 + kPagedThreads < used) __syncthreads();
     }
+    const float part_sum = group_sum<64>(l);
+    if (tid % 64 == 0) s_sum[tid / 64] = part_sum;
+    if (mine < at_once) *reinterpret_cast<v4f*>(&s_o[mine * d.d + c]) = x;
     __syncthreads();
-    float top = -INFINITY, sum = 0.0f, v = 0.0f;
-    for (int i = 0; i < at_once; ++i) top = fmaxf(top, s_m[i]);
-    const float base = top == -INFINITY ? 0.0f : top;
-    for (int i = 0; i < at_once; ++i) {
-        const float by = __builtin_amdgcn_exp2f(s_m[i] - base);
-        sum += s_l[i] * by;
-        if (tid < d.d) v += s_o[i * d.d + tid] * by;
-    }
+    const float top = m;
+    float sum = 0.0f, v = 0.0f;
+    for (int i = 0; i < kPagedWaves; ++i) sum += s_sum[i];
+    if (tid < d.d)
+        for (int i = 0; i < at_once; ++i) v += s_o[i * d.d + tid];
     const float by = (sum == 0.0f ? 0.0f : 1.0f / sum) * (d.cache_dtype == NM_DT_I8 ? d.v_scale[h / a.own] : 1.0f);
     if (tid < d.d) store1(d.out, d.out_dtype, b * d.out_stride + (long)h * d.d + tid, v * by, d.out_inv_scale);
     if (tid == 0 && d.lse) d.lse[bh] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
