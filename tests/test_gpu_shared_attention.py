@@ -229,6 +229,23 @@ def test_shared_attention_is_what_paged_attention_gives():
     assert bool(((out - o2).abs() <= 2 * e_out + 2.0 ** -22 * out.abs()).all()) and bool(((lse - l2).abs() <= 2 * e_lse + 2.0 ** -22 * lse.abs()).all())
 
 
+@pytest.mark.parametrize("groups,hq,hk,d,dtype", [([(700, [720 + i for i in range(12)]), (None, [900])], 8, 4, 64, torch.int8),
+                                                  ([(1500, [1510 + i % 7 for i in range(160)]), (400, [450] * 40)], 4, 2, 128, torch.bfloat16)])
+def test_shared_attention_beyond_2_32_elements(groups, hq, hk, d, dtype):
+    """The bits of a cache whose pages are neighbours, with pages so far apart that offsets need more than 32 bits."""
+    c = shared_case(13, groups, hq, hk, d, torch.bfloat16, dtype)
+    want, wl = check(c, torch.bfloat16)
+    _, pages, page, _, _ = c["cache"].shape
+    apart = (3 << 31) // pages // 128 * 128
+    assert (pages - 1) * apart > 1 << 32
+    far = torch.empty(2 * pages * apart, dtype=dtype, device=DEV).as_strided((2, pages, page, hk, d), (pages * apart, apart, hk * d, d, 1))
+    for i in range(2):
+        for j in range(pages):
+            far[i, j].copy_(c["cache"][i, j])
+    out, lse = attend({**c, "cache": far}, torch.bfloat16, d ** -0.5)
+    assert torch.equal(out, want) and torch.equal(lse, wl)
+
+
 def test_shared_attention_twice_at_once_and_replayed():
     """Two calls on two streams with workspaces of their own; a captured call, replayed while lengths, groups and tables change, its workspace filled anew."""
     a = shared_case(11, [(600, [650] * 6), (300, [400] * 5)], 8, 2, 64, torch.bfloat16, torch.bfloat16, columns=900)
