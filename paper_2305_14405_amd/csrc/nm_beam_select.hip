@@ -3,16 +3,16 @@
 // One pass over the logits makes both of what is needed of a row: its sum of exponentials, and its K best logits.  (Within a row the order of
 // candidates is that of the logits, so nothing but K of a row can be among the request's K.)  A workgroup goes over a chunk of a row, every lane with a
 // maximum and a sum of its own.  Each wavefront sorts its lanes' maxima; the K-th of one wavefront, and the least of the wavefronts' K/4-th, are values that at least
-// K logits of the chunk reach.  The lanes that hold such logits, K and a few more, are few: what they went over is read again, the logits that
-// reach the value are collected in LDS, and each counts how many are better: that is its place.  A candidate is one 64-bit number, the logit's bits in the order
+// K logits of the chunk reach.  The lanes that hold such logits, K and a few more, are few: of what they went over, the tiles whose
+// largest logit (kept in LDS) reaches the value are read again, the logits that reach the value are collected in LDS, and each counts how many are better: that is its place.  A candidate is one 64-bit number, the logit's bits in the order
 // of their values above the complement of the token, so that comparing it settles ties too.  Where more than LDS takes reach the value (many
 // equal logits, or all large ones in a few lanes), they are put one by one into lists, sorted, an entry to a lane.
 //   A second kernel has a workgroup to a request: it joins the chunks' sums, forms the candidates' log-probabilities in 64 bits, and chooses among
 // them in the same way; short histories it copies itself.
-//   Bound by latency at few rows: one request of 4 hypotheses, 32000 fp32 logits, 5.5 + 4.2 us, chains of loads, a sort of 21 steps, barriers.  32 of 8, 131072
-// bf16 (67 MB, 13 us at a copy's rate): 20.6 + 5.7, 3.3 TB/s in the first: two workgroups to a CU, vector instructions 42 % of
-// the cycles, and 4 us of the same chain behind the last logits.  (More chunks, or more loads ahead, take longer: 512 workgroups 26.1 us, 1024 27.8; lists of K
-// kept by every wavefront as it goes 83.)
+//   Bound by latency at few rows: one request of 4 hypotheses, 32000 fp32 logits, 5.8 + 4.2 us, chains of loads, a sort of 21 steps, barriers.  32 of 8, 131072
+// bf16 (67 MB, 13 us at a copy's rate): 17.0 + 5.4, 4.0 TB/s in the first: two workgroups to a CU, vector instructions 46 % of the cycles, and 3 us of the
+// same chain behind the last logits.  (All of a lane's logits read again, where only some of its tiles are wanted: 20.6, 5.5 and 4 us for the one request.  Lists of
+// K kept by every wavefront as it goes: 83 in all.)
 #include <algorithm>
 
 #include "nm_decode.h"
@@ -23,6 +23,7 @@ constexpr int kBeamWaves = 4, kBeamThreads = 64 * kBeamWaves;   // of the first 
 constexpr int kJoinWaves = 8, kJoinThreads = 64 * kJoinWaves;   // of the second
 constexpr int kBeamStep = 4;                                    // groups of 16 bytes that a lane asks for at a time
 constexpr int kBeamMost = 512;                                 // candidates that are ranked at once
+constexpr int kRecords = 32;                                   // maxima that a lane of the first kernel keeps of its logits
 
 struct BeamArgs {
     nm_beam_desc d;
@@ -186,7 +187,8 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a)
     __shared__ Key s_key[kBeamMost];
     __shared__ float s_max[kBeamWaves], s_reached[2][kBeamWaves];
     __shared__ double s_sum[kBeamWaves];
-    __shared__ int s_count, s_lanes, s_lane[kBeamThreads];
+    __shared__ float s_record[kRecords][kBeamThreads];        // largest logits of a lane's tiles, `span` tiles to a number
+    __shared__ unsigned s_count, s_hits, s_hit[kBeamMost];
     const nm_beam_desc& d = a.d;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = d.K;
     const long row = blockIdx.y;
@@ -222,7 +224,9 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a)
     Vec w[kBeamStep];
     ask(begin, w);
     if (!offers(d, row) || (d.done && d.done[row])) return;    // uniform
-    if (tid == 0) s_count = s_lanes = 0;
+    if (tid == 0) s_count = s_hits = 0;
+    const int span = (a.chunk / kTile + kRecords - 1) / kRecords;
+    int records;
 
     // Logits as they are; where an infinity or a NaN turns up in the maximum or the sum, once more with what they count as.
     float top, least, mine;
@@ -230,16 +234,24 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a)
     auto sweep = [&](auto special) {
         mine = -INFINITY;
         sum = 0;
-        float off = 0.0f;                                      // what is subtracted from x log2(e)
+        records = 0;
+        int left = span;
+        float record = -INFINITY, off = 0.0f;                  // off: what is subtracted from x log2(e)
         for (int t = begin; t < end; t += kTile) {
             float y[kEach];
 #pragma unroll
             for (int i = 0; i < kEach; ++i) y[i] = special ? logit((float)w[i / kGroup][i % kGroup]) : (float)w[i / kGroup][i % kGroup];
             if (t + kTile < end) ask(t + kTile, w);
-            float now = fmaxf(mine, y[0]);
+            float tile = y[0];
 #pragma unroll
-            for (int i = 1; i + 1 < kEach; i += 2) now = max3(now, y[i], y[i + 1]);
-            now = fmaxf(now, y[kEach - 1]);
+            for (int i = 1; i + 1 < kEach; i += 2) tile = max3(tile, y[i], y[i + 1]);
+            record = max3(record, tile, y[kEach - 1]);
+            const float now = fmaxf(mine, record);
+            if (--left == 0) {                                 // uniform
+                s_record[records++][tid] = record;
+                record = -INFINITY;
+                left = span;
+            }
             float part[4] = {0, 0, 0, 0};
             if (!special) {
                 // exp(x - m) as a power of two of x log2(e) - m log2(e), rounded once (what the second product's rounding leaves is made up for behind)
@@ -257,6 +269,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a)
             sum += (double)((part[0] + part[1]) + (part[2] + part[3]));
             mine = now;
         }
+        if (left < span) s_record[records++][tid] = record;
         top = wave_max(mine);
         if (lane == 0) s_max[wave] = top;
         least = reached(mine, K, s_reached);                   // synchronises
@@ -284,25 +297,37 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a)
         a.part_sum[out] = sum;
     }
 
-    // The lanes that hold any of those: their groups are read once more, by all lanes.  (Code for what few lanes come to is fetched for all.)
-    if (mine >= least && mine > -INFINITY) s_lane[atomicAdd(&s_lanes, 1)] = tid;
+    // The tiles of lanes that hold any of those are read once more, by all lanes.  (Code for what few lanes come to is fetched for all.)
+    if (mine >= least && mine > -INFINITY)
+#pragma unroll 1
+        for (int i = tid; i < records * kBeamThreads; i += kBeamThreads) {
+            const float record = s_record[i / kBeamThreads][i % kBeamThreads];
+            if (record >= least && record > -INFINITY) {
+                const unsigned at = atomicAdd(&s_hits, 1u);
+                if (at < kBeamMost) s_hit[at] = i;
+            }
+        }
     __syncthreads();
-    const int lanes = s_lanes, groups = lanes * (a.chunk / kApart);
-    auto number = [&](int i) { return begin + i / lanes * kApart + s_lane[i % lanes] * kGroup; };
-    for (int i = tid; i < groups; i += kBeamThreads) {
+    const unsigned hits = s_hits, all = a.chunk / kGroup, each = span * kBeamStep, groups = hits <= kBeamMost ? hits * each : 0;
+    auto number = [&](unsigned i) {
+        const unsigned hit = s_hit[i % hits];
+        return begin + (int)((hit / kBeamThreads * each + i / hits) * kApart + hit % kBeamThreads * kGroup);
+    };
+    for (unsigned i = tid; i < groups; i += kBeamThreads) {
         const int v = number(i);
+        if (v >= begin + a.chunk) continue;                    // the last number's tiles may be fewer
         const Vec y = group(v);
 #pragma unroll
         for (int e = 0; e < kGroup; ++e) {
             const float z = logit((float)y[e]);
             if (z >= least && z > -INFINITY) {
-                const int at = atomicAdd(&s_count, 1);
+                const unsigned at = atomicAdd(&s_count, 1u);
                 if (at < kBeamMost) s_key[at] = key_of(z, v + e);
             }
         }
     }
     __syncthreads();
-    const int n = s_count;
+    const int n = (int)(hits <= kBeamMost ? s_count : hits);          // each of them has a logit of those
     Key* best = a.part_key + out * K;
     if (n <= kBeamMost) {
         if (tid >= n && tid < K) best[tid] = 0;
@@ -313,11 +338,11 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a)
     }
     __syncthreads();
     Key list = 0;
-    for (int i0 = 0; i0 < groups; i0 += kBeamThreads) {        // every lane of a wavefront comes along
-        const int i = i0 + tid;
+    for (unsigned i0 = 0; i0 < all; i0 += kBeamThreads) {      // every lane of a wavefront comes along
+        const unsigned i = i0 + tid;
 #pragma unroll 1
         for (int e = 0; e < kGroup; ++e) {
-            const int v = i < groups ? number(i) + e : -1;
+            const int v = i < all ? begin + (int)(i * kGroup) + e : -1;
             const float z = v >= 0 && v < d.V ? logit((float)x[v]) : -INFINITY;
             list = insert_all(list, z >= least && z > -INFINITY ? key_of(z, v) : 0, K, lane);
         }

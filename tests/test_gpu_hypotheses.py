@@ -213,6 +213,34 @@ def test_beam_select_ascending_and_descending_rows():
         check_select(c, 64)
 
 
+@pytest.mark.parametrize("V", [140001, 300000])
+def test_beam_select_long_rows_of_one_workgroup(V):
+    """So many rows that a workgroup has a whole one; the best ones at a row's ends and in one lane, equal logits everywhere, and all but a few masked."""
+    R, W, K = 130, 4, 6
+    g = torch.Generator(device=DEV)
+    g.manual_seed(V)
+    x, scores = torch.randn((R * W, V), generator=g, device=DEV), -4 * torch.rand((R, W), generator=g, device=DEV)
+    x[::3, 0], x[::4, V - 1], x[1::5, V - 4097] = 7.0, 7.5, 8.0
+    x[7, 16:4096 * 30:4096] = 9.0                                             # a lane's, in every tile
+    x[9] = -INF
+    x[9, [5, V - 1]] = torch.tensor([1.0, 2.0], device=DEV)
+    out = [torch.full((R, K), -77, dtype=t, device=DEV) for t in (torch.int32, torch.int32, torch.float32)]
+    ws = scratch(nm.nm_beam_select_workspace(x, scores, *out))
+    for equal in (False, True):
+        if equal:
+            x.fill_(0.5), scores.fill_(-1.0)
+        nm.nm_beam_select(x, scores, *out, ws=ws)
+        if equal:
+            assert torch.equal(out[1], torch.arange(K, dtype=torch.int32, device=DEV).expand(R, K)) and torch.equal(out[0], (torch.arange(R, dtype=torch.int32, device=DEV) * W)[:, None].expand(R, K))
+            continue
+        total = (torch.log_softmax(x.double(), -1) + scores.double().view(-1, 1)).view(R, W * V)
+        best = torch.topk(total, K + 1).values
+        at = (out[0].long() - torch.arange(R, device=DEV)[:, None] * W) * V + out[1]
+        mine = torch.gather(total, 1, at)
+        assert bool(((mine - best[:, :K]).abs() <= NEAR).all()) and bool((torch.sort(at).values.diff() > 0).all())
+        assert bool(((out[2].double() - mine).abs() <= NEAR + 2.0 ** -24 * (mine.abs() + NEAR)).all())
+
+
 def test_beam_select_large_differences():
     """Sums over logits that lie hundreds apart, and far from zero."""
     c = beam_case(4, 3, 4, 20000, torch.float32, spread=300.0)
