@@ -9,10 +9,10 @@
 // equal logits, or all large ones in a few lanes), they are put one by one into lists, sorted, an entry to a lane.
 //   A second kernel has a workgroup to a request: it joins the chunks' sums, forms the candidates' log-probabilities in 64 bits, and chooses among
 // them in the same way; short histories it copies itself.
-//   Bound by latency at few rows: one request of 4 hypotheses, 32000 fp32 logits, 5.8 + 4.2 us, chains of loads, a sort of 21 steps, barriers.  32 of 8, 131072
-// bf16 (67 MB, 13 us at a copy's rate): 17.0 + 5.4, 4.0 TB/s in the first: two workgroups to a CU, vector instructions 46 % of the cycles, and 3 us of the
-// same chain behind the last logits.  (All of a lane's logits read again, where only some of its tiles are wanted: 20.6, 5.5 and 4 us for the one request.  Lists of
-// K kept by every wavefront as it goes: 83 in all.)
+//   Bound by latency at few rows: one request of 4 hypotheses, 32000 fp32 logits, 5.3 + 4.4 us, chains of loads, a sort of 21 steps, barriers.  32 of 8, 131072
+// bf16 (67 MB, 13 us at a copy's rate): 17.9 + 5.4, 3.8 TB/s in the first: two workgroups to a CU, vector instructions 47 % of the cycles, and 3 us of the
+// same chain behind the last logits.  (All of a lane's logits read again, where only some of its tiles are wanted: 20.6.  Lists of K kept by every wavefront as it goes:
+// 83 in all.)
 #include <algorithm>
 
 #include "nm_decode.h"
@@ -21,7 +21,9 @@ namespace nm {
 
 constexpr int kBeamWaves = 4, kBeamThreads = 64 * kBeamWaves;   // of the first kernel
 constexpr int kJoinWaves = 8, kJoinThreads = 64 * kJoinWaves;   // of the second
-constexpr int kBeamStep = 4;                                    // groups of 16 bytes that a lane asks for at a time
+// Groups of 16 bytes that a lane asks for at a time: with 4 the code, which is fetched as it first runs, is longer (one request of 4 over 32000 9.6 us, 9.1 with
+// 2; 24 of 6 over 50001 16.9 and 15.9; 32 of 8 over 131072 22.8 either way), with 1 too little is under way (16.5, 25.3).
+constexpr int kBeamStep = 2;
 constexpr int kBeamMost = 512;                                 // candidates that are ranked at once
 constexpr int kRecords = 32;                                   // maxima that a lane of the first kernel keeps of its logits
 
@@ -512,7 +514,8 @@ __global__ __launch_bounds__(kBeamThreads) void beam_history_kernel(nm_beam_desc
     follow(d, row, d.parents[row], d.tokens[row], blockIdx.y * kBeamThreads + threadIdx.x, gridDim.y * kBeamThreads);
 }
 
-constexpr long kBeamGroups = 512;                             // workgroups of the first kernel, about
+// Workgroups of the first kernel, about: 512 22.8 us for 32 requests of 8 over 131072, 768 23.2; 24 of 6 over 50001 with twice as many 2 us longer.
+constexpr long kBeamGroups = 512;
 // Tokens that a history, and a request's histories, have room for up to which its workgroup of the second kernel copies them, a wavefront to a history; more go to a
 // kernel of their own.  (There and by a kernel: 4 of 1000 12.1 and 13.2 us, of 4000 14.3 and 13.3; 16 requests of 8 of 2000 16.0 and 16.2; 300 of 2 of 4000 24.4 and 23.4.)
 constexpr int kHistory = 2048;
@@ -529,7 +532,7 @@ static int32_t plan_beam(const nm_beam_desc* d, BeamArgs* a, size_t* bytes, cons
     if (d->history && d->max_history > 1 << 30) return fail(NM_ERR_UNSUPPORTED, "%s: max_history > 2^30", what);
     *a = BeamArgs{};
     a->d = *d;
-    // chunks of one tile where there are few rows, and as many as give every CU four workgroups
+    // chunks of one tile where there are few rows, and as many as give every CU two workgroups
     const long rows = (long)d->R * d->W, tile = kBeamStep * kBeamThreads * 16 / dtype_bytes(d->logits_dtype);
     const long tiles = ((long)d->V + 15 + tile - 1) / tile;    // a row's first group of 16 bytes may begin in front of it
     const long wanted = rows ? std::min(std::max(1l, kBeamGroups / rows), tiles) : 1;
