@@ -668,11 +668,11 @@ def _type(t, dev, name):
 
 
 def _vector(t, dtype, n, dev, name):
-    """Address of a contiguous tensor of n elements of one type; 0 for None."""
+    """Address of a contiguous tensor of n elements (None: they have been counted) of one type; 0 for None."""
     if t is None:
         return 0
-    if t.dtype is not dtype or t.get_device() != dev or t.numel() != n or not t.is_contiguous():
-        _refuse(f"{name}: a contiguous tensor of {n} elements of {dtype} on the current device is wanted, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or (n is not None and t.numel() != n):
+        _refuse(f"{name}: a contiguous tensor of {t.numel() if n is None else n} elements of {dtype} on the current device is wanted, got {tuple(t.shape)} of {t.dtype} on {t.device}")
     return t.data_ptr()
 
 
@@ -864,7 +864,7 @@ def _work_space(ws, ws_bytes):
     try:
         if ws.get_device() != _here() or not ws.is_contiguous():
             _refuse("ws: contiguous memory on the current device is wanted")
-        return ws.data_ptr(), ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+        return ws.data_ptr(), ws.nbytes if ws_bytes is None else ws_bytes
     except _MISFITS as e:
         _misfit("ws", e)
 
@@ -882,9 +882,10 @@ def _workspace_of(call, packed, make, tensors, more):
 
 def _rows(t, n, dev, name):
     """Row stride and columns of an int32 matrix of n rows, whose columns are neighbours."""
-    if t.dtype is not _i32 or t.get_device() != dev or t.dim() != 2 or t.shape[0] != n or (n and t.shape[1] > 1 and t.stride(1) != 1):
+    shape, strides = t.shape, t.stride()
+    if t.dtype is not _i32 or t.get_device() != dev or len(shape) != 2 or shape[0] != n or (n and shape[1] > 1 and strides[1] != 1):
         _refuse(f"{name}: int32 [{n}, ...] with neighbouring columns on the current device is wanted")
-    return (t.stride(0) if n > 1 else t.shape[1]), t.shape[1]
+    return (strides[0] if n > 1 else shape[1]), shape[1]
 
 
 def make_beam_desc(logits, scores, parents, tokens, scores_out, done=None, weight=None, end_token=-1, done_out=None, history=None, history_lens=None,
@@ -894,14 +895,15 @@ def make_beam_desc(logits, scores, parents, tokens, scores_out, done=None, weigh
     try:
         dev = _here()
         (R, W), K = scores.shape, parents.shape[1]
-        if logits.dim() != 2 or logits.shape[0] != R * W or (logits.shape[1] > 1 and logits.stride(1) != 1):
-            _refuse(f"logits: [{R * W}, V] with neighbouring elements is wanted, got {tuple(logits.shape)}")
+        shape, strides = logits.shape, logits.stride()
+        if len(shape) != 2 or shape[0] != R * W or (shape[1] > 1 and strides[1] != 1):
+            _refuse(f"logits: [{R * W}, V] with neighbouring elements is wanted, got {tuple(shape)}")
         for t, n in ((parents, "parents"), (tokens, "tokens"), (scores_out, "scores_out"), (done_out, "done_out")):
             if t is not None and t.shape != (R, K):
                 _refuse(f"{n}: shape {tuple(t.shape)}, wanted {(R, K)}")
         if end_token is None:
             _refuse("end_token: -1 for none")
-        V, most, at = logits.shape[1], 0, (0, 0, 0, 0, 0, 0)
+        V, most, at = shape[1], 0, (0, 0, 0, 0, 0, 0)
         if history is not None or history_lens is not None or history_out is not None or history_lens_out is not None:
             if history is None or history_lens is None or history_out is None or history_lens_out is None:
                 _refuse("history, history_lens, history_out and history_lens_out belong together")
@@ -911,10 +913,10 @@ def make_beam_desc(logits, scores, parents, tokens, scores_out, done=None, weigh
                 _refuse(f"history and history_out have rows of {most} and {out_most}")
             at = (history.data_ptr(), stride, _vector(history_lens, _i32, R * W, dev, "history_lens"), history_out.data_ptr(), out_stride,
                   _vector(history_lens_out, _i32, R * K, dev, "history_lens_out"))
-        return _BEAM.pack(R, W, K, V, _type(logits, dev, "logits"), end_token, most, logits.data_ptr(), logits.stride(0) if R * W > 1 else V,
-                          _vector(scores, _f32, R * W, dev, "scores"), _vector(weight, _f32, R * W, dev, "weight"), _vector(done, _i32, R * W, dev, "done"),
-                          _vector(parents, _i32, R * K, dev, "parents"), _vector(tokens, _i32, R * K, dev, "tokens"),
-                          _vector(scores_out, _f32, R * K, dev, "scores_out"), _vector(done_out, _i32, R * K, dev, "done_out"), *at)
+        return _BEAM.pack(R, W, K, V, _type(logits, dev, "logits"), end_token, most, logits.data_ptr(), strides[0] if R * W > 1 else V,
+                          _vector(scores, _f32, None, dev, "scores"), _vector(weight, _f32, R * W, dev, "weight"), _vector(done, _i32, R * W, dev, "done"),
+                          _vector(parents, _i32, None, dev, "parents"), _vector(tokens, _i32, None, dev, "tokens"),
+                          _vector(scores_out, _f32, None, dev, "scores_out"), _vector(done_out, _i32, None, dev, "done_out"), *at)
     except _MISFITS as e:
         _misfit("nm_beam_select", e)
 
@@ -945,9 +947,9 @@ def make_fork_desc(block_table, lens, parents, free_pages, free_begin, table_out
         out_stride, out_columns = _rows(table_out, B_out, dev, "table_out")
         if out_columns != columns:
             _refuse(f"block_table and table_out have {columns} and {out_columns} columns")
-        return _FORK.pack(B_in, B_out, page_size, num_pages, columns, n_free, block_table.data_ptr(), stride, _vector(lens, _i32, B_in, dev, "lens"),
-                          _vector(parents, _i32, B_out, dev, "parents"), _vector(keep, _i32, num_pages, dev, "keep"),
-                          _vector(free_pages, _i32, n_free, dev, "free_pages"), _vector(free_begin, _i32, 1, dev, "free_begin"), table_out.data_ptr(), out_stride,
+        return _FORK.pack(B_in, B_out, page_size, num_pages, columns, n_free, block_table.data_ptr(), stride, _vector(lens, _i32, None, dev, "lens"),
+                          _vector(parents, _i32, None, dev, "parents"), _vector(keep, _i32, num_pages, dev, "keep"),
+                          _vector(free_pages, _i32, None, dev, "free_pages"), _vector(free_begin, _i32, 1, dev, "free_begin"), table_out.data_ptr(), out_stride,
                           _vector(lens_out, _i32, B_out, dev, "lens_out"), _vector(free_out, _i32, n_free, dev, "free_out"),
                           _vector(free_end, _i32, 1, dev, "free_end"), _vector(copy_src, _i32, B_out, dev, "copy_src"),
                           _vector(copy_dst, _i32, B_out, dev, "copy_dst"), _vector(copy_slots, _i32, B_out, dev, "copy_slots"),
@@ -999,7 +1001,7 @@ def make_copy_desc(caches, src, dst, slots=None) -> bytes:
             _refuse("the elements of a head have to be neighbours in the caches")
         copies = src.numel()
         array = (C.c_void_p * max(n, 1))(*at)
-        desc = _CopyBytes(_COPY.pack(copies, n, hk, e, dtype, pages, page, C.addressof(array), *strides[:3], _vector(src, _i32, copies, dev, "src"),
+        desc = _CopyBytes(_COPY.pack(copies, n, hk, e, dtype, pages, page, C.addressof(array), *strides[:3], _vector(src, _i32, None, dev, "src"),
                                      _vector(dst, _i32, copies, dev, "dst"), _vector(slots, _i32, copies, dev, "slots")))
         desc.addresses = array
         return desc
@@ -1021,7 +1023,7 @@ def make_shared_desc(q, k_cache, v_cache, block_table, lens, group_start, shared
         dev = _here()
         G = shared.numel()
         return make_paged_desc(q, k_cache, v_cache, block_table, lens, out, scale, 0, k_scale, v_scale, out_inv_scale, lse) + _GROUPS.pack(
-            G, _vector(group_start, _i32, G + 1, dev, "group_start"), _vector(shared, _i32, G, dev, "shared"))
+            G, _vector(group_start, _i32, G + 1, dev, "group_start"), _vector(shared, _i32, None, dev, "shared"))
     except _MISFITS as e:
         _misfit("nm_shared_attention", e)
 
