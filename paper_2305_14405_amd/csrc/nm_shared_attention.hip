@@ -13,7 +13,7 @@
 // running maximum is only moved when it is passed by a factor of 32.
 //   bf16, 32 query and 8 key heads of 128, GPU time: 64 rows behind 32768 common positions (190 MB, 35 GFLOP) 107 us: 7 the lists, 23 the rows' own, 66 the
 // prefix (39 % of the cycles in matrix instructions, 44 % in vector instructions, which one after the other would fill them: the weights' two terms are both
-// double the second product and half of the vector instructions), 11 the joining of 36 pieces a query.  96 rows behind 4096, each with up to 4096 of its own (671 MB) 183: 130 the own
+// double the second product and half of the vector instructions), 11 the joining of 36 pieces a query.  96 rows behind 4096, each with up to 4096 of its own (671 MB) 182: 130 the own
 // positions, at a copy's rate.  int8, 16 heads of 64, two as one, 16 groups of 8 rows behind up to 8192 (134 MB) 63: 45 for 3500 units of 128 positions and a thousand ranges of one
 // or two, whose beginning and end cost as much as two more.
 #include "nm_paged_parts.h"
@@ -21,7 +21,9 @@
 namespace nm {
 
 constexpr int kSharedMost = NM_PLAN_MAX_REQUESTS;     // rows, groups
-constexpr int kSharePrefix = kUnit;                   // shorter prefixes are every row's own
+// Shorter prefixes are every row's own.  (256 rows of 32 heads of 128 in groups of 2 to 64 behind up to 512, 1024 and 2048 positions: 128, 256 and 512 within 3 % of one
+// another, 768 up to 12 % longer; all of them their own, 16 rows to a group: 70, 102 and 143 us, shared 70, 106 and 112.)
+constexpr int kSharePrefix = kUnit;
 constexpr int kPlanners = 1024;
 // Units of all rows up to which nm_paged_attention takes them, two to each of its workgroups or fewer: 4 rows of 640 positions, 12 heads of 64, 13.9 us,
 // 20.8 by the lists.
@@ -855,7 +857,7 @@ __global__ __launch_bounds__(64 * shared_waves(2), 2) void shared_prefix_kernel(
 
 // Joins what a query has: its group's prefix and its row's own positions, each whole or in pieces.  A workgroup to a query: a thread to a piece finds the piece's
 // place and weight, then lanes of four elements add every so-manieth piece's output, whose first loads are under way before the weights are there.  2048 queries
-// of 128 of 36 pieces (47 MB fetched, at 4.4 TB/s) 10.7 us, 3072 of 8 11.0; where threads found the weights of their pieces as they added them 10.7 and 12.6.
+// of 128 of 36 pieces (47 MB fetched, at 4.4 TB/s) 10.7 us, 96 rows of 32 heads, of 8 pieces, 11.0; where threads found the weights of their pieces as they added them 10.7 and 12.6.
 __global__ __launch_bounds__(kPagedThreads) void shared_join_kernel(SharedArgs a)
 {
     constexpr int kAhead = 4;
