@@ -147,6 +147,9 @@ __device__ __forceinline__ float reached(float top, int K, float (&s)[2][W])
 }
 
 constexpr float kLog2e = 1.44269504088896340736f;
+// Largest logits of a row, of either sign, whose products with log2(e) a rounding moves by 64 at most, half a step of numbers below 2^31: powers of two of what it leaves, and
+// of its opposite, are far from exp2's ends.  (Of 2092843776 it leaves -127.3: the power is flushed to 0, its inverse is no infinity, and the sum would be 0.)
+constexpr float kFarLogit = 1073741824.0f;
 
 // NaN: -inf, +inf: the largest number.  (A median of three with -inf as a bound is folded into a minimum, which passes the number in place of a NaN.)
 __device__ __forceinline__ float logit(float x) { return x == x ? fminf(x, 3.40282346638528859812e38f) : -INFINITY; }
@@ -230,7 +233,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a)
     const int span = (a.chunk / kTile + kRecords - 1) / kRecords;
     int records;
 
-    // Logits as they are; where an infinity or a NaN turns up in the maximum or the sum, once more with what they count as.
+    // Logits as they are; where an infinity or a NaN turns up in the maximum or the sum, or the maximum is far from 0, once more with what they count as, by differences.
     float top, least, mine;
     double sum;
     auto sweep = [&](auto special) {
@@ -288,7 +291,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a)
         for (int i = 0; i < kBeamWaves; ++i) sum += s_sum[i];
     };
     sweep(std::false_type{});
-    if (!(top < 1e30f && sum < INFINITY)) {                    // uniform; NaNs too
+    if (!((__builtin_fabsf(top) <= kFarLogit || top == -INFINITY) && sum < INFINITY)) {   // uniform; NaNs too
         __syncthreads();
         ask(begin, w);
         sweep(std::true_type{});

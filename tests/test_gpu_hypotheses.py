@@ -249,6 +249,44 @@ def test_beam_select_large_differences():
     check_select(c, 12)
 
 
+# As NEAR, of rows whose logits are summed by differences from the largest: a difference's rounding and its product's, of up to 2^5, by half a step of 2^-19 each (16 half
+# steps of 2^-24 and 11), the constant's and the power's (4 and 2), ten additions and two rescalings (4 and 4).
+NEAR_FAR = 48 * 2.0 ** -24
+
+
+def check_far(x, scores, K, got):
+    """A selection over logits of any size: what is compared is formed by differences from a row's largest."""
+    (R, W), V = scores.shape, x.shape[1]
+    x = x.double()
+    y = x - x.max(-1, keepdim=True).values
+    total = (y - torch.log(torch.exp(y).sum(-1, keepdim=True)) + scores.double().view(-1, 1)).view(R, W * V)
+    at = (got["parents"].long() - torch.arange(R)[:, None] * W) * V + got["tokens"].long()
+    assert bool(((at >= 0) & (at < W * V)).all()) and all(len(set(row)) == K for row in at.tolist())
+    mine, best = torch.gather(total, 1, at), torch.topk(total, K).values
+    assert bool(((mine - best).abs() <= 2 * NEAR_FAR + 1e-12 * best.abs()).all()), (mine, best)
+    assert bool(got["totals"].isfinite().all())
+    assert bool(((got["totals"].double() - mine).abs() <= NEAR_FAR + 2.0 ** -24 * (mine.abs() + NEAR_FAR)).all()), (got["totals"], mine)
+
+
+@pytest.mark.parametrize("whole", [False, True])
+@pytest.mark.parametrize("far", [65504.0, 1e9, -1e9, 2092843776.0, 2183619840.0, -4259921152.0, 5802540032.0, -7489040384.0, -1e10, 15939420160.0, 98973351936.0, -1430329884672.0, 1e29, -1e29,
+                                 3.4e38, -3.4e38])
+def test_beam_select_far_logits(far, whole):
+    """A logit, or a row of them, so large that the rounding of its product with log2(e) is many powers of two (127 of them below it, for some)."""
+    c = beam_case(17, 2, 3, 9001, torch.float32)
+    if whole:
+        c["x"][1] = c["x"][5] = far
+        c["x"][5, 4000:] = far * (1 + 2.0 ** -20 * (1 if far < 0 else -1))    # the lower of two
+        c["scores"][1, 2] = 0.0
+    else:
+        c["x"][1, 4000] = c["x"][5, 8999] = c["x"][5, 3] = far
+    got = select(c, 7)
+    check_far(c["x"], c["scores"], 7, got)
+    for row in (1, 5) if whole else ():                                       # of equal ones the lowest tokens
+        mine = got["tokens"][got["parents"] == row].tolist()
+        assert mine == list(range(len(mine)))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_beam_select_repeats_bits_on_a_stream_and_in_a_graph(dtype):
     c = beam_case(8, 5, 4, 12345, dtype, done=0.2, weight=True, history=50)
