@@ -11,7 +11,9 @@
 // them in the same way; short histories it copies itself.
 //   Bound by latency at few rows: one request of 4 hypotheses, 32000 fp32 logits, 5.3 + 4.4 us, chains of loads, a sort of 21 steps, barriers.  32 of 8, 131072
 // bf16 (67 MB, 13 us at a copy's rate): 17.9 + 5.4, 3.8 TB/s in the first: two workgroups to a CU, vector instructions 47 % of the cycles, and 3 us of the
-// same chain behind the last logits.  (All of a lane's logits read again, where only some of its tiles are wanted: 20.6.  Lists of K kept by every wavefront as it goes:
+// same chain behind the last logits.  Half of the tokens masked, by -inf or a finite number: the same (22.9, 35.5 where a lane's sum began from a logit of 0, so that low first
+// ones had the chunk read twice).  Chunks of nothing but one finite number, three quarters of a row: 97, for all of their logits are equal, and go through the lists, one
+// by one; of -inf: 22.5.  (All of a lane's logits read again, where only some of its tiles are wanted: 20.6.  Lists of K kept by every wavefront as it goes:
 // 83 in all.)
 #include <algorithm>
 
@@ -233,7 +235,8 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a)
     const int span = (a.chunk / kTile + kRecords - 1) / kRecords;
     int records;
 
-    // Logits as they are; where an infinity or a NaN turns up in the maximum or the sum, or the maximum is far from 0, once more with what they count as, by differences.
+    // Logits as they are (of numbers that mask tokens, such as -1e9 or a type's lowest, the powers are 0); where +inf or a NaN turns up in the maximum or the sum, or the maximum of the
+    // chunk is far from 0, once more with what they count as, by differences.
     float top, least, mine;
     double sum;
     auto sweep = [&](auto special) {
@@ -241,7 +244,8 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a)
         sum = 0;
         records = 0;
         int left = span;
-        float record = -INFINITY, off = 0.0f;                  // off: what is subtracted from x log2(e)
+        // off: what is subtracted from x log2(e); from the lowest on, so that a sum of nothing is never multiplied by an infinity
+        float record = -INFINITY, off = -kFarLogit * kLog2e;
         for (int t = begin; t < end; t += kTile) {
             float y[kEach];
 #pragma unroll
@@ -260,7 +264,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a)
             float part[4] = {0, 0, 0, 0};
             if (!special) {
                 // exp(x - m) as a power of two of x log2(e) - m log2(e), rounded once (what the second product's rounding leaves is made up for behind)
-                const float next = now == -INFINITY ? 0.0f : now * kLog2e;
+                const float next = fmaxf(now, -kFarLogit) * kLog2e;
 #pragma unroll
                 for (int i = 0; i < kEach; ++i) part[i % 4] += __builtin_amdgcn_exp2f(__builtin_fmaf(y[i], kLog2e, -next));
                 sum *= (double)__builtin_amdgcn_exp2f(off - next);
@@ -281,8 +285,9 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a)
 #pragma unroll
         for (int i = 0; i < kBeamWaves; ++i) top = fmaxf(top, s_max[i]);
         const float base = top == -INFINITY ? 0.0f : top;
-        float by = __builtin_amdgcn_exp2f((mine - base) * kLog2e);
-        if (!special && mine > -INFINITY) by *= __builtin_amdgcn_exp2f(-__builtin_fmaf(mine, kLog2e, -off));
+        const float from = special ? mine : fmaxf(mine, -kFarLogit);
+        float by = __builtin_amdgcn_exp2f((from - base) * kLog2e);
+        if (!special) by *= __builtin_amdgcn_exp2f(-__builtin_fmaf(from, kLog2e, -off));
         sum = wave_sum(sum * (double)by);
         if (lane == 0) s_sum[wave] = sum;
         __syncthreads();

@@ -287,6 +287,35 @@ def test_beam_select_far_logits(far, whole):
         assert mine == list(range(len(mine)))
 
 
+@pytest.mark.parametrize("dtype,low", [(t, v) for t in TYPES for v in (-1e3, -1e4, -1e9, -1e10, None) if t is not torch.float16 or v is None or v > -65504])
+@pytest.mark.parametrize("R,W,V", [(2, 3, 30011), (70, 2, 50001)])
+def test_beam_select_tokens_masked_by_low_numbers(dtype, low, R, W, V):
+    """Exponentials of such logits are 0, as those of minus infinity are: the same bits come out, for the same sweep takes both."""
+    low = float(torch.finfo(dtype).min) if low is None else low
+    c = beam_case(23, R, W, V, dtype)
+    masked = torch.rand((R * W, V), generator=gen(29)) < 0.5
+    masked[1, :V // 2] = True                                                 # whole chunks
+    masked[2, :9000] = True                                                   # the beginning of every lane
+    c["x"][masked] = low
+    got = select(c, 4)
+    c["x"][masked] = -INF
+    want = check_select(c, 4)
+    assert all(torch.equal(got[n], want[n]) for n in ("parents", "tokens", "totals"))
+
+
+def test_beam_select_rows_of_low_numbers():
+    """Logits that all lie far below 0 give what the same ones near 0 give (multiples of 1/64, which the difference leaves as they are)."""
+    c = beam_case(31, 3, 4, 20001, torch.float32)
+    c["x"][:] = (c["x"] * 64).round() / 64
+    want = check_select(c, 5)
+    for by in (512.0, 8192.0):
+        n = dict(c, wide=c["wide"] - by)
+        n["x"] = n["wide"]
+        got = check_select(n, 5)
+        assert all(torch.equal(got[k], want[k]) for k in ("parents", "tokens"))
+        assert bool(((got["totals"] - want["totals"]).abs() <= 2 * NEAR + 2.0 ** -23 * want["totals"].abs()).all())
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_beam_select_repeats_bits_on_a_stream_and_in_a_graph(dtype):
     c = beam_case(8, 5, 4, 12345, dtype, done=0.2, weight=True, history=50)
