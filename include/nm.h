@@ -663,7 +663,8 @@ int32_t nm_gemv_w4(const nm_w4_desc* desc, void* stream);
  * done_out[r,k] = done[r,w] != 0 or v == end_token.  Fewer than K candidates: parents and tokens -1, scores_out -inf, done_out 0.
  * No candidates: tokens whose logit is -inf or NaN (masked), and hypotheses whose score or weight is not finite, or whose weight is not above 0.
  * A logit of +inf counts as the largest binary32 number.  Logits are compared as they are; t and weight * t are formed in 64 bits from a sum of exponentials
- * in 32 (partial sums of up to 16 terms, joined in 64), so that of two hypotheses' candidates whose t are closer than 2^-20 either may come first, but always the same.
+ * in 32 (partial sums of up to 16 terms, joined in 64), whose logarithm is right to 2^-18, so that of two hypotheses' candidates whose weight * t are closer than 2^-17 times the larger
+ * weight either may come first, but always the same.
  * history (NULL: none): row r W + w holds the history_lens[r W + w] tokens of that hypothesis, in rows of max_history.  Row r K + k of history_out receives
  * its parent's tokens and, unless the parent was done or the row is full, the new one; history_lens_out how many these are (no parent: 0).  What is behind
  * them is left as it was.  Lengths outside [0, max_history] count as the nearest.

@@ -316,6 +316,50 @@ def test_beam_select_rows_of_low_numbers():
         assert bool(((got["totals"] - want["totals"]).abs() <= 2 * NEAR + 2.0 ** -23 * want["totals"].abs()).all())
 
 
+@pytest.mark.parametrize("differences", [False, True])
+def test_beam_select_order_of_hypotheses_that_are_2_to_minus_17_apart(differences):
+    """Rows of one logit and 2^20 - 1 equal ones below it, which most of the sum is, so chosen that their exponent is rounded by half a step, up in one row, down in the other.
+    differences: a NaN among them, so that the sum is formed by differences."""
+    V, R = 1 << 20, 24
+    c = np.float32(1.44269504088896340736)
+    r = np.random.default_rng(5)
+    top = r.uniform(4, 20, 400000).astype(np.float32)
+    low = (top - r.uniform(11.1, 12.0, top.size).astype(np.float32)).astype(np.float32)
+    if differences:                                                           # two roundings: of the difference, of its product
+        d = (low - top).astype(np.float32)
+        power = (d * c).astype(np.float32)
+        off = power.astype(np.float64) - (low.astype(np.float64) - top) / math.log(2)
+    else:
+        product, next = low.astype(np.float64) * float(c), (top * c).astype(np.float32).astype(np.float64)
+        power = (product - next).astype(np.float32)
+        off = power.astype(np.float64) - (product - next)
+    order = np.argsort(off)
+    pairs = [(order[i], order[-1 - i]) for i in range(R // 2)] + [(order[-1 - i], order[i]) for i in range(R // 2)]
+    assert off[order[0]] < -2.0 ** -21 and off[order[-1]] > 2.0 ** -21
+    x = torch.empty((2 * R, V))
+    scores = torch.zeros((R, 2))
+    at = r.integers(1, V, 2 * R)
+    totals = []
+    for k, pair in enumerate(pairs):
+        t = []
+        for w, i in enumerate(pair):
+            x[2 * k + w] = float(low[i])
+            x[2 * k + w, at[2 * k + w]] = float(top[i])
+            others = V - 1
+            if differences:
+                x[2 * k + w, 0] = NAN
+                others -= 1
+            t.append(-math.log1p(others * math.exp(float(low[i]) - float(top[i]))))
+        scores[k, 1] = t[0] - t[1] - 1.01 * 2.0 ** -17
+        t[1] += float(scores[k, 1])
+        assert t[0] - t[1] > 2.0 ** -17
+        totals.append(t)
+    got = select(dict(x=x, wide=x, scores=scores, done=None, weight=None, history=None), 2)
+    want = torch.tensor(totals, dtype=torch.float64)
+    assert torch.equal(got["parents"], torch.arange(2 * R, dtype=torch.int32).view(R, 2)) and torch.equal(got["tokens"], torch.as_tensor(at, dtype=torch.int32).view(R, 2))
+    assert bool(((got["totals"].double() - want).abs() <= 2.0 ** -18 + 2.0 ** -24 * want.abs()).all())
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_beam_select_repeats_bits_on_a_stream_and_in_a_graph(dtype):
     c = beam_case(8, 5, 4, 12345, dtype, done=0.2, weight=True, history=50)
