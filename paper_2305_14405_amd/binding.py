@@ -891,7 +891,7 @@ def _rows(t, n, dev, name):
 def make_beam_desc(logits, scores, parents, tokens, scores_out, done=None, weight=None, end_token=-1, done_out=None, history=None, history_lens=None,
                    history_out=None, history_lens_out=None) -> bytes:
     """logits: [R * W, V], rows may be apart; scores, done, weight: [R, W]; parents, tokens, scores_out, done_out: [R, K]; history: [R * W, max_history],
-    history_out: [R * K, max_history], rows may be apart.  The description refers to the tensors' memory: keep them."""
+    history_out: [R * K, max_history], rows may be apart; history_lens, history_lens_out: [R * W], [R * K], or as scores and parents.  The description refers to the tensors' memory: keep them."""
     try:
         dev = _here()
         (R, W), K = scores.shape, parents.shape[1]
@@ -901,6 +901,9 @@ def make_beam_desc(logits, scores, parents, tokens, scores_out, done=None, weigh
         for t, n in ((parents, "parents"), (tokens, "tokens"), (scores_out, "scores_out"), (done_out, "done_out")):
             if t is not None and t.shape != (R, K):
                 _refuse(f"{n}: shape {tuple(t.shape)}, wanted {(R, K)}")
+        for t, n in ((done, "done"), (weight, "weight")):
+            if t is not None and t.shape != (R, W):
+                _refuse(f"{n}: shape {tuple(t.shape)}, wanted {(R, W)}")
         if end_token is None:
             _refuse("end_token: -1 for none")
         V, most, at = shape[1], 0, (0, 0, 0, 0, 0, 0)
@@ -911,10 +914,13 @@ def make_beam_desc(logits, scores, parents, tokens, scores_out, done=None, weigh
             out_stride, out_most = _rows(history_out, R * K, dev, "history_out")
             if out_most != most:
                 _refuse(f"history and history_out have rows of {most} and {out_most}")
-            at = (history.data_ptr(), stride, _vector(history_lens, _i32, R * W, dev, "history_lens"), history_out.data_ptr(), out_stride,
-                  _vector(history_lens_out, _i32, R * K, dev, "history_lens_out"))
+            for t, n, k in ((history_lens, "history_lens", W), (history_lens_out, "history_lens_out", K)):
+                if t.shape != (R, k) and t.shape != (R * k,):
+                    _refuse(f"{n}: shape {tuple(t.shape)}, wanted {(R * k,)} or {(R, k)}")
+            at = (history.data_ptr(), stride, _vector(history_lens, _i32, None, dev, "history_lens"), history_out.data_ptr(), out_stride,
+                  _vector(history_lens_out, _i32, None, dev, "history_lens_out"))
         return _BEAM.pack(R, W, K, V, _type(logits, dev, "logits"), end_token, most, logits.data_ptr(), strides[0] if R * W > 1 else V,
-                          _vector(scores, _f32, None, dev, "scores"), _vector(weight, _f32, R * W, dev, "weight"), _vector(done, _i32, R * W, dev, "done"),
+                          _vector(scores, _f32, None, dev, "scores"), _vector(weight, _f32, None, dev, "weight"), _vector(done, _i32, None, dev, "done"),
                           _vector(parents, _i32, None, dev, "parents"), _vector(tokens, _i32, None, dev, "tokens"),
                           _vector(scores_out, _f32, None, dev, "scores_out"), _vector(done_out, _i32, None, dev, "done_out"), *at)
     except _MISFITS as e:

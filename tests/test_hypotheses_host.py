@@ -298,3 +298,20 @@ def test_copies_of_a_list_of_caches_and_of_one_tensor_are_described_alike(host_t
     for bad in ([], [x[0], x[1].float()], [x[0], x[1][:4]], [x[0], x[1].contiguous()], x[0], x[..., ::2]):
         with pytest.raises(nm.NmError):
             nm.make_copy_desc(bad, i, i)
+
+
+def test_beam_select_refuses_hypotheses_numbers_of_another_shape(host_tensors):
+    """done and weight are [R, W], as scores are: their transposes, which have as many elements, and their elements in a row are refused."""
+    import torch
+    good = {**host_tensors[nm.make_beam_desc], "weight": torch.ones((2, 3))}
+    assert len(nm.make_beam_desc(**good)) > 0
+    for name in ("done", "weight"):
+        for bad in (good[name].t().contiguous(), good[name].view(-1), good[name][None], good[name][:, :2].contiguous()):
+            with pytest.raises(nm.NmError) as e:
+                nm.make_beam_desc(**{**good, name: bad})
+            assert e.value.status == nm.NM_ERR_INVALID_ARG and name in str(e.value)
+    for name, fits in (("history_lens", (2, 3)), ("history_lens_out", (2, 4))):
+        assert len(nm.make_beam_desc(**{**good, name: good[name].view(fits)})) > 0
+        with pytest.raises(nm.NmError) as e:
+            nm.make_beam_desc(**{**good, name: good[name].view(fits[::-1])})
+        assert e.value.status == nm.NM_ERR_INVALID_ARG and name in str(e.value)
