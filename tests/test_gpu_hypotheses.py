@@ -678,3 +678,99 @@ def test_page_copy_kept_description_on_a_stream_and_in_a_graph():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(cache, want)
+
+
+# ---- order, special values, and calls at once -----------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_beam_select_order_of_equal_candidates_whole(dtype):
+    """Three equal rows of two values: the larger one's tokens row by row, then the other's of the first row."""
+    c = beam_case(1, 1, 3, 70000, dtype)
+    c["x"][:] = 1.5
+    c["x"][:, 69990:] = 2.0
+    c["scores"][:] = -2
+    got = check_select(c, 64)
+    assert got["tokens"][0].tolist() == [*range(69990, 70000)] * 3 + [*range(34)]
+    assert got["parents"][0].tolist() == [0] * 10 + [1] * 10 + [2] * 10 + [0] * 34
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_beam_select_infinite_logits_count_as_the_largest_number(dtype):
+    """One +inf has all of its row's probability, two have half of it each, and next to the largest number itself it is that."""
+    c = beam_case(3, 1, 4, 5000, torch.float32)
+    c["x"] = c["wide"] = c["x"].to(dtype)
+    c["x"][0, 17] = INF
+    c["x"][1, [4001, 30]] = INF
+    c["x"][2, :] = NAN
+    c["x"][2, 8] = INF
+    c["scores"][0] = torch.tensor([-1.0, -1.0, -2.0, -3000.0])
+    c["x"][3] = -INF
+    c["x"][3, 4999] = INF
+    got = select(c, 5)
+    half = float(torch.tensor(-1.0 + math.log(0.5), dtype=torch.float64).float())
+    assert got["parents"][0].tolist() == [0, 1, 1, 2, 3] and got["tokens"][0].tolist() == [17, 30, 4001, 8, 4999]
+    assert got["totals"][0].tolist() == [-1.0, half, half, -2.0, -3000.0]
+
+
+def both_at_once(calls):
+    """Calls of (entry point, arguments, keywords), prepared before any runs, on streams of their own with nothing between them."""
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for (call, args, more), s in zip(calls, streams):
+            call(*args, stream=s, **more)
+    torch.cuda.synchronize()
+
+
+def test_beam_select_two_calls_at_once():
+    cases = [beam_case(51, 40, 4, 30001, torch.bfloat16, done=0.1, history=40), beam_case(52, 60, 3, 20011, torch.bfloat16, weight=True, history=3000)]
+    calls, outs = [], []
+    for c in cases:
+        (R, W), K, n = c["scores"].shape, 5, c["history"].shape[1]
+        d = {k: None if c[k] is None else c[k].to(DEV) for k in ("x", "scores", "done", "weight", "history", "held")}
+        o = {k: torch.full((R, K), -7, dtype=torch.int32, device=DEV) for k in ("parents", "tokens", "done_out")}
+        o.update(totals=torch.zeros((R, K), device=DEV), history=torch.full((R * K, n + 3), -77, dtype=torch.int32, device=DEV), held=torch.zeros(R * K, dtype=torch.int32, device=DEV))
+        args = (d["x"], d["scores"], o["parents"], o["tokens"], o["totals"])
+        more = dict(done=d["done"], weight=d["weight"], end_token=3, done_out=o["done_out"], history=d["history"], history_lens=d["held"], history_out=o["history"][:, :n],
+                    history_lens_out=o["held"])
+        calls.append((nm.nm_beam_select, args, dict(more, ws=scratch(nm.nm_beam_select_workspace(*args, **more)))))
+        outs.append(o)
+    both_at_once(calls)
+    for c, o in zip(cases, outs):
+        check_select(c, 5, 3, got={n: t.cpu() for n, t in o.items()})
+
+
+def test_page_fork_two_calls_at_once():
+    """A large batch and one of another, and a small one's single workgroup beside them: each has the tables that the rules give."""
+    cases = [random_fork(31, 700, 800, 8, 200), random_fork(32, 300, 350, 8, 300, keep=0.1), random_fork(33, 16, 16, 16, 600)]
+    calls, outs = [], []
+    for table, lens, parents, keep, free, begin, page, num_pages in cases:
+        n_rows = len(parents)
+        o = {n: torch.full((n_rows,), -5, dtype=torch.int32, device=DEV) for n in ("lens_out", "src", "dst", "slots")}
+        o.update(table_out=torch.full((n_rows, table.shape[1]), -66, dtype=torch.int32, device=DEV), free_out=torch.full((len(free),), -88, dtype=torch.int32, device=DEV),
+                 end=torch.full((1,), -5, dtype=torch.int32, device=DEV), status=torch.full((4,), -5, dtype=torch.int32, device=DEV))
+        args = (i32(table), i32(lens), i32(parents), i32(np.asarray(free, np.int32)), i32([begin]), o["table_out"])
+        more = dict(page_size=page, num_pages=num_pages, keep=None if keep is None else i32(keep), lens_out=o["lens_out"], free_out=o["free_out"], free_end=o["end"], copy_src=o["src"],
+                    copy_dst=o["dst"], copy_slots=o["slots"], status=o["status"])
+        calls.append((nm.nm_page_fork, args, dict(more, ws=scratch(nm.nm_page_fork_workspace(*args, **more)))))
+        outs.append(o)
+    both_at_once(calls)
+    for c, o in zip(cases, outs):
+        want = fork_in_python(*c, np.full((len(c[2]), c[0].shape[1]), -66, np.int32), np.full(len(c[4]), -88, np.int32))
+        assert want["status"][0] == 0 and o["end"].tolist() == [want["end"]]
+        assert np.array_equal(o["table_out"].cpu().numpy(), want["table_out"]) and np.array_equal(o["free_out"].cpu().numpy(), want["free_out"])
+        assert [o[n].tolist() for n in ("lens_out", "src", "dst", "slots", "status")] == [want[n] for n in ("lens_out", "src", "dst", "slots", "status")]
+
+
+def test_page_copy_two_calls_at_once():
+    caches = [torch.randn((24, 40, 32, 4, 128), generator=gen(s)).to(torch.bfloat16).to(DEV) for s in (1, 2)]
+    calls, wants = [], []
+    for cache, m in zip(caches, (20, 13)):
+        src, dst, slots = torch.arange(m), torch.arange(m) + 20, torch.arange(m) % 33
+        want = cache.clone()
+        for a, b, k in zip(src.tolist(), dst.tolist(), slots.tolist()):
+            want[:, b, :k] = want[:, a, :k]
+        calls.append((nm.nm_page_copy, (cache, i32(src), i32(dst), i32(slots)), {}))
+        wants.append(want)
+    both_at_once(calls)
+    assert all(torch.equal(c, w) for c, w in zip(caches, wants))

@@ -280,6 +280,24 @@ def test_shared_attention_twice_at_once_and_replayed():
         assert_rounded(out, want, e_out, "replay")
 
 
+@pytest.mark.parametrize("groups,hq,hk,d,dtype", [([(5000, [5010 + 9 * i for i in range(64)])], 32, 8, 128, torch.bfloat16), ([(3000, [3000 + i for i in range(96)])], 16, 4, 64, torch.float32),
+                                                  ([(2000, [2001 + i for i in range(8)]), (900, [950 + 30 * i for i in range(8)])], 16, 16, 64, torch.int8)])
+def test_shared_attention_gives_the_same_bits_every_time(groups, hq, hk, d, dtype):
+    """Prefixes of few and of many queries: in new workspaces, in old ones, and behind calls that leave other numbers there."""
+    q = torch.float16 if dtype == torch.int8 else dtype
+    c = shared_case(41, groups, hq, hk, d, q, torch.int8 if dtype == torch.int8 else torch.bfloat16, page=32)
+    other = {**c, "q": c["q"] * 1.7, "lens": torch.clamp(c["lens"] - 40, min=0)}
+    want, lse = check(c, q)
+    args = (c["q"], c["cache"][0], c["cache"][1], c["table"], c["lens"], c["start"], c["shared"], torch.empty_like(c["q"]))
+    s = (None, None) if c["scales"] is None else c["scales"]
+    ws = torch.full((nm.nm_shared_attention_workspace(*args, scale=1.0, k_scale=s[0], v_scale=s[1]),), 0xff, dtype=torch.uint8, device=DEV)
+    for i in range(12):
+        if i % 3 == 2:
+            attend(other, q, d ** -0.5, ws=ws)
+        got, l = attend(c, q, d ** -0.5, ws=ws if i % 2 else None)
+        assert torch.equal(got, want) and torch.equal(l, lse), i
+
+
 def test_shared_attention_as_many_rows_as_it_takes():
     """4096 rows in 1024 groups of four."""
     B, hk, d, page = 4096, 1, 16, 32
