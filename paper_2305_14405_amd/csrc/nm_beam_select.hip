@@ -10,7 +10,7 @@
 //   A second kernel has a workgroup to a request: it joins the chunks' sums, forms the candidates' log-probabilities in 64 bits, and chooses among
 // them in the same way; short histories it copies itself.
 //   Bound by latency at few rows: one request of 4 hypotheses, 32000 fp32 logits, 5.3 + 4.4 us, chains of loads, a sort of 21 steps, barriers.  32 of 8, 131072
-// bf16 (67 MB, 13 us at a copy's rate): 17.9 + 5.4, 3.8 TB/s in the first: two workgroups to a CU, vector instructions 47 % of the cycles, and 3 us of the
+// bf16 (67 MB, 13 us at a copy's rate): 18.1 + 5.2, 3.7 TB/s in the first: two workgroups to a CU, vector instructions 47 % of the cycles, and 3 us of the
 // same chain behind the last logits.  Half of the tokens masked, by -inf or a finite number: the same (22.9, 35.5 where a lane's sum began from a logit of 0, so that low first
 // ones had the chunk read twice).  Chunks of nothing but one finite number, three quarters of a row: 97, for all of their logits are equal, and go through the lists, one
 // by one; of -inf: 22.5.  (All of a lane's logits read again, where only some of its tiles are wanted: 20.6.  Lists of K kept by every wavefront as it goes:

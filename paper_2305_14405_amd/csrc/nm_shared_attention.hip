@@ -6,16 +6,19 @@
 //   A first kernel of one workgroup makes three lists, by a range's queries.  Up to 16, which the rows' own are: as nm_paged_attention takes them, each of
 // a workgroup's four wavefronts has tiles of 32 positions of its own.  More: 128 positions at a time are in LDS for all wavefronts, each of which has 32
 // queries in registers (16 where they are three terms), and, where there are fewer queries than that, only some of the positions.  Up to 64 queries (32),
-// in the first list's launch, four wavefronts; more, in a launch of their own, eight wavefronts and 256 queries (64 to 256) to a CU, which has registers for
-// the operands of one product while another runs, and LDS for the next positions beside these.  (With four wavefronts of 64 queries each, one to a
+// in the first list's launch, four wavefronts; more, in a launch of their own, eight wavefronts and 256 queries (128 of heads of more than 128 elements, and of
+// heads of more than 64 where queries are three terms) to a CU, which has registers for the operands of one product while another runs, and LDS for the next positions beside these.  (With four wavefronts of 64 queries each, one to a
 // SIMD, nothing ran under a wavefront's own waits: 18 us for 128 positions, 7 so.)  A fixed number of workgroups shares each list evenly, whatever the lengths
-// are (the first two lists' by their cost); a run's first and last piece may be parts of a range.  Tiles, operand layouts and precision are nm_paged_attention's, but that a
+// are (the first two lists' by their cost; a range costs its units of 128 positions and two, however many queries its tile has, so that tiles of the third list that
+// are not full, 128 of 256 queries for one, take less time than they count for); a run's first and last piece may be parts of a range.  Tiles, operand layouts and precision are nm_paged_attention's, but that a
 // running maximum is only moved when it is passed by a factor of 32.
 //   bf16, 32 query and 8 key heads of 128, GPU time: 64 rows behind 32768 common positions (190 MB, 35 GFLOP) 107 us: 7 the lists, 23 the rows' own, 66 the
 // prefix (39 % of the cycles in matrix instructions, 44 % in vector instructions, which one after the other would fill them: the weights' two terms are both
-// double the second product and half of the vector instructions), 11 the joining of 36 pieces a query.  96 rows behind 4096, each with up to 4096 of its own (671 MB) 182: 130 the own
-// positions, at a copy's rate.  int8, 16 heads of 64, two as one, 16 groups of 8 rows behind up to 8192 (134 MB) 63: 45 for 3500 units of 128 positions and a thousand ranges of one
+// double the second product and half of the vector instructions), 11 the joining of 36 pieces a query.  96 rows behind 4096, each with up to 4096 of its own (671 MB) 180: 130 the own
+// positions, at a copy's rate.  int8, 16 heads of 64, two as one, 16 groups of 8 rows behind up to 8192 (134 MB) 64: 45 for 3500 units of 128 positions and a thousand ranges of one
 // or two, whose beginning and end cost as much as two more.
+//   Registers: the first two lists' kernel has those that the second list's code takes, for the rows' own positions too: heads of 128 of 16-bit caches 256, and 28 to 36 bytes of scratch
+// a lane; of 64 about 180, two workgroups to a CU where nm_paged_attention has three.  Heads of 256 with queries of three terms spill 90 registers in the third list's kernel (270 to 290 bytes).
 #include "nm_paged_parts.h"
 
 namespace nm {
@@ -1000,7 +1003,7 @@ static int32_t plan_shared(const nm_shared_desc* d, SharedArgs* a, void* ws, siz
     a->shift = page_shift(d->p.page_size);
     a->own = d->p.hq / d->p.hk;
     // Heads of int8 as one, whole lines of 128 bytes, where their queries, of a group's rows (of so many as the groups have among them), are still few
-    // (16 groups of 8 rows, 16 heads of 64: 67 us, 78.6 apart); more would double the products.
+    // (16 groups of 8 rows, 16 heads of 64: 64 us, 78.6 apart); more would double the products.
     a->pack = 1;
     if (d->p.cache_dtype == NM_DT_I8 && d->p.head_stride == d->p.d)
         while (2 * a->pack * d->p.d <= 128 && d->p.hk % (2 * a->pack) == 0 && (d->G ? (d->p.B + d->G - 1) / d->G : 1) * a->own * 2 * a->pack <= shared_tile(0, 128, 1)) a->pack *= 2;
